@@ -40,7 +40,8 @@ enum {
     CODEC_ERR_WORKSPACE_TOO_SMALL = -4,
     CODEC_ERR_HIP = -5,                 /* a HIP runtime call failed                           */
     CODEC_ERR_NOT_UPLOADED = -6,        /* decode called before codec_plan_upload              */
-    CODEC_ERR_OUT_OF_MEMORY = -7        /* host allocation failed                              */
+    CODEC_ERR_OUT_OF_MEMORY = -7,       /* host allocation failed                              */
+    CODEC_ERR_NO_PAGES = -8             /* fewer free pages than the call needs                */
 };
 
 enum { CODEC_DTYPE_FP16 = 0, CODEC_DTYPE_BF16 = 1 };
@@ -395,6 +396,105 @@ size_t codec_static_scratch_bytes(void);       /* CODEC_STATIC_SCRATCH_BYTES of 
  */
 int codec_stream_read_probe(const void *buffer, size_t bytes, int32_t pattern, int32_t nontemporal,
                             int32_t workgroups, void *sink, void *stream);
+
+/*
+ * New tokens: rotary positions, keys and values into their pages
+ * --------------------------------------------------------------
+ *
+ * Between the projections of a step's tokens and codec_decode_attention: queries and keys get their
+ * positions, keys and values go to the slots of the page pools where the plan will look for them.
+ */
+
+/*
+ * Which channels of a head form the pairs that turn, of the first `rotary_dim`: HALF pairs channel i
+ * with i + rotary_dim / 2, INTERLEAVED channel 2i with 2i + 1.  The other channels pass unchanged.
+ */
+enum { CODEC_ROTARY_HALF = 0, CODEC_ROTARY_INTERLEAVED = 1 };
+
+/* How the frequencies f_i = theta^(-2i / rotary_dim) are scaled for contexts longer than those of training. */
+enum {
+    CODEC_ROTARY_UNSCALED = 0,
+    CODEC_ROTARY_LINEAR = 1,        /* f_i / factor (positions interpolated)                               */
+    CODEC_ROTARY_NTK = 2,           /* theta * factor^(rotary_dim / (rotary_dim - 2)) in the place of theta:
+                                       the slowest pair as LINEAR, the fastest unchanged                   */
+    CODEC_ROTARY_WAVELENGTH = 3,    /* by n_i = original_length * f_i / (2 pi), the turns of pair i over the
+                                       original context: f_i from `high` turns on, f_i / factor up to `low`,
+                                       in between blended in n_i                                           */
+    CODEC_ROTARY_YARN = 4           /* YaRN (arXiv 2309.00071): f_i up to the pair that turns `fast` times
+                                       over the original context (rounded down), f_i / factor from the one
+                                       that turns `slow` times (rounded up), in between blended in i; the
+                                       turned channels grow by 0.1 ln(factor) + 1                          */
+};
+
+typedef struct {
+    int32_t kind;               /* CODEC_ROTARY_UNSCALED ..                                     */
+    int32_t original_length;    /* WAVELENGTH, YARN: context length of training, >= 1           */
+    double  factor;             /* all but UNSCALED: > 0                                        */
+    double  low, high;          /* WAVELENGTH: low < high                                       */
+    double  fast, slow;         /* YARN: fast > slow > 0                                        */
+} codec_rotary_scaling;
+
+/*
+ * Host only: turns[i] = f_i / (2 pi), the turns pair i makes from one position to the next, for
+ * i < rotary_dim / 2 (`turns`: host memory; the caller keeps a device copy, see codec_rotary_config),
+ * and the factor on the turned channels that belongs to the scaling.  rotary_dim is even, 2..256;
+ * theta > 1; scaling NULL = unscaled.
+ */
+int codec_rotary_turns(int32_t rotary_dim, double theta, const codec_rotary_scaling *scaling,
+                       double *turns, float *magnitude);
+
+typedef struct {
+    int32_t rotary_dim;         /* channels that turn: even, 2..head_dim                        */
+    int32_t layout;             /* CODEC_ROTARY_HALF or CODEC_ROTARY_INTERLEAVED                */
+    int32_t inverse;            /* nonzero: turn the other way (the gradient of the turn, whose
+                                   transpose it is; with magnitude 1 what undoes it)            */
+    float   magnitude;          /* factor on the turned channels, e.g. from codec_rotary_turns  */
+    const double *turns;        /* device [rotary_dim / 2]: turns of a pair from one position to
+                                   the next                                                     */
+} codec_rotary_config;
+
+/*
+ * Rows of a batch of tokens: element (token, head, c) lives at token * token_stride + head *
+ * head_stride + c, as in a projection's output or in a part of it.  16-byte aligned; strides
+ * are multiples of 8 elements, >= 0.  Rows that are written must not overlap one another.
+ */
+typedef struct {
+    void   *data;
+    int64_t token_stride;
+    int64_t head_stride;
+} codec_rows;
+
+/*
+ * Turns `num_heads` heads of `head_dim` (64, 128 or 256) channels of every token to its position:
+ * pair i of token t by positions[t] * turns[i] turns, (a, b) -> magnitude * (a cos - b sin,
+ * b cos + a sin).  The angle is taken in 64 bits, whatever the position; products and sums are
+ * 32-bit, rounded once to `dtype` (CODEC_DTYPE_FP16 or _BF16).
+ *   x, out      device rows; out may be x itself, otherwise the two must not overlap
+ *   positions   device [num_tokens], any values
+ * Enqueued on `stream` without synchronising; num_tokens == 0 does nothing.
+ */
+int codec_rotary(const codec_rotary_config *rotary, int32_t num_heads, int32_t head_dim, int32_t dtype,
+                 const codec_rows *x, const codec_rows *out, const int64_t *positions,
+                 int32_t num_tokens, void *stream);
+
+/*
+ * The step's tokens into the cache: queries and keys turned as by codec_rotary (rotary NULL: passed as
+ * they are, positions is then not read), key t and value t stored at token slots[t] % page_size of
+ * page slots[t] / page_size of the pools.
+ *   head        head_dim, page_size and dtype as for a plan; num_q_heads and num_kv_heads >= 1 (scale is
+ *               not used)
+ *   q, q_out    device rows [num_tokens][num_q_heads]; q_out may be q itself.  Both NULL: no queries
+ *   k, v        device rows [num_tokens][num_kv_heads]
+ *   slots       device [num_tokens]; a token whose slot is negative or beyond the pools' last page (padding
+ *               of a batch) is not stored, its queries are turned all the same.  The slots of a call
+ *               are distinct: what two tokens store in one slot is undefined
+ *   k_pages, v_pages, layout    as for codec_decode_attention; no element of a pool may coincide with
+ *               another one or with the rows.  Slots that are not named keep their contents
+ */
+int codec_append(const codec_head_config *head, const codec_rotary_config *rotary,
+                 const codec_rows *q, const codec_rows *q_out, const codec_rows *k, const codec_rows *v,
+                 const int64_t *positions, const int64_t *slots, int32_t num_tokens,
+                 void *k_pages, void *v_pages, const codec_kv_layout *layout, void *stream);
 
 /* Static, human-readable name of a status code. */
 const char *codec_status_string(int status);

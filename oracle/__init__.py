@@ -8,6 +8,8 @@ and the benchmark's ``cpu_baseline`` leg do.  Contents:
 * ``method``     - the paper's partial-attention / partial-reduction steps
   (Alg. 2-4) in fp64 numpy, to check that tree-merged results equal the
   definition and to replay a task list on the CPU.
+* ``operators``  - rotary positions, page lists, beam selection: what surrounds a
+  decode step, in fp64 numpy.
 * ``planner``    - integer re-derivation of cost estimation, division and
   scheduling, to check the library's plan bit for bit.
 """

@@ -8,7 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import (POINTER, Structure, c_char_p, c_float, c_int, c_int32, c_int64, c_size_t,
+from ctypes import (POINTER, Structure, c_char_p, c_double, c_float, c_int, c_int32, c_int64, c_size_t,
                     c_void_p, byref)
 
 import numpy as np
@@ -24,8 +24,16 @@ CODEC_ERR_WORKSPACE_TOO_SMALL = -4
 CODEC_ERR_HIP = -5
 CODEC_ERR_NOT_UPLOADED = -6
 CODEC_ERR_OUT_OF_MEMORY = -7
+CODEC_ERR_NO_PAGES = -8
 CODEC_DTYPE_FP16 = 0
 CODEC_DTYPE_BF16 = 1
+CODEC_ROTARY_HALF = 0
+CODEC_ROTARY_INTERLEAVED = 1
+CODEC_ROTARY_UNSCALED = 0
+CODEC_ROTARY_LINEAR = 1
+CODEC_ROTARY_NTK = 2
+CODEC_ROTARY_WAVELENGTH = 3
+CODEC_ROTARY_YARN = 4
 CODEC_PLAN_EXT_SLACK = 1
 CODEC_PLAN_EXT_DIAGONAL = 2
 
@@ -36,7 +44,7 @@ EXPORTED_SYMBOLS = [
     "codec_plan_workspace_bytes", "codec_decode_attention", "codec_partial_attention",
     "codec_partial_reduction", "codec_status_string", "codec_last_error_message",
     "codec_plan_refresh_lengths", "codec_decode_attention_static", "codec_static_scratch_bytes",
-    "codec_stream_read_probe",
+    "codec_stream_read_probe", "codec_rotary_turns", "codec_rotary", "codec_append",
 ]
 
 _i32p = POINTER(c_int32)
@@ -94,6 +102,20 @@ class codec_kv_layout(Structure):
                 ("head_stride", c_int64)]
 
 
+class codec_rotary_scaling(Structure):
+    _fields_ = [("kind", c_int32), ("original_length", c_int32), ("factor", c_double),
+                ("low", c_double), ("high", c_double), ("fast", c_double), ("slow", c_double)]
+
+
+class codec_rotary_config(Structure):
+    _fields_ = [("rotary_dim", c_int32), ("layout", c_int32), ("inverse", c_int32), ("magnitude", c_float),
+                ("turns", c_void_p)]
+
+
+class codec_rows(Structure):
+    _fields_ = [("data", c_void_p), ("token_stride", c_int64), ("head_stride", c_int64)]
+
+
 # PyTorch wheels carry their own copy of the HIP runtime.  Device pointers and streams handed to the
 # library come from PyTorch, so both must use the same runtime instance: load PyTorch's first, and
 # libcodec.so's dependency on libamdhip64 then resolves to the copy already in the process.
@@ -142,6 +164,14 @@ _lib.codec_static_scratch_bytes.restype = c_size_t
 _lib.codec_static_scratch_bytes.argtypes = []
 _lib.codec_stream_read_probe.restype = c_int
 _lib.codec_stream_read_probe.argtypes = [c_void_p, c_size_t, c_int32, c_int32, c_int32, c_void_p, c_void_p]
+_lib.codec_rotary_turns.restype = c_int
+_lib.codec_rotary_turns.argtypes = [c_int32, c_double, POINTER(codec_rotary_scaling), POINTER(c_double), POINTER(c_float)]
+_lib.codec_rotary.restype = c_int
+_lib.codec_rotary.argtypes = [POINTER(codec_rotary_config), c_int32, c_int32, c_int32, POINTER(codec_rows), POINTER(codec_rows),
+                              c_void_p, c_int32, c_void_p]
+_lib.codec_append.restype = c_int
+_lib.codec_append.argtypes = [POINTER(codec_head_config), POINTER(codec_rotary_config)] + [POINTER(codec_rows)] * 4 + [
+    c_void_p, c_void_p, c_int32, c_void_p, c_void_p, POINTER(codec_kv_layout), c_void_p]
 _lib.codec_status_string.restype = c_char_p
 _lib.codec_status_string.argtypes = [c_int]
 _lib.codec_last_error_message.restype = c_char_p
@@ -318,3 +348,25 @@ def codec_stream_read_probe(buffer_ptr: int, nbytes: int, pattern: int, nontempo
                             sink_ptr: int, stream: int = 0) -> int:
     return _lib.codec_stream_read_probe(c_void_p(buffer_ptr), nbytes, pattern, nontemporal, workgroups,
                                         c_void_p(sink_ptr), c_void_p(stream))
+
+
+def codec_rotary_turns(rotary_dim: int, theta: float, scaling=None):
+    """Returns (status, turns of the pairs as float64 array or None, magnitude).  ``scaling``: codec_rotary_scaling or None."""
+    turns = np.zeros(max(1, rotary_dim // 2), np.float64)
+    magnitude = c_float(0.0)
+    st = _lib.codec_rotary_turns(rotary_dim, theta, byref(scaling) if scaling is not None else None, _ptr(turns, c_double),
+                                 byref(magnitude))
+    return st, (turns if st == CODEC_OK else None), magnitude.value
+
+
+def codec_rotary(rotary, num_heads: int, head_dim: int, dtype: int, x, out, positions_ptr: int, num_tokens: int,
+                 stream: int = 0) -> int:
+    """``rotary``: codec_rotary_config; ``x`` and ``out``: codec_rows."""
+    return _lib.codec_rotary(rotary, num_heads, head_dim, dtype, x, out, positions_ptr, num_tokens, stream)
+
+
+def codec_append(head, rotary, q, q_out, k, v, positions_ptr: int, slots_ptr: int, num_tokens: int, k_ptr: int, v_ptr: int,
+                 layout, stream: int = 0) -> int:
+    """``head``: codec_head_config; ``rotary``: codec_rotary_config or None; ``q``, ``q_out``: codec_rows or None; ``k``,
+    ``v``: codec_rows; ``layout``: codec_kv_layout."""
+    return _lib.codec_append(head, rotary, q, q_out, k, v, positions_ptr, slots_ptr, num_tokens, k_ptr, v_ptr, layout, stream)

@@ -1,0 +1,195 @@
+"""Page pools of a K/V cache with what fills them, and rotary positions (marshalling only)."""
+from __future__ import annotations
+
+import contextlib
+from types import SimpleNamespace
+
+import torch
+
+from . import binding as B
+from .runtime import _current_stream
+
+_TORCH_DTYPE = {B.CODEC_DTYPE_FP16: torch.float16, B.CODEC_DTYPE_BF16: torch.bfloat16}
+_CODE = {t: c for c, t in _TORCH_DTYPE.items()}
+_SCALINGS = {"linear": B.CODEC_ROTARY_LINEAR, "ntk": B.CODEC_ROTARY_NTK, "wavelength": B.CODEC_ROTARY_WAVELENGTH,
+             "yarn": B.CODEC_ROTARY_YARN}
+
+
+def _device(device) -> torch.device:
+    d = torch.device(device)
+    if d.type == "cuda" and d.index is None:
+        d = torch.device("cuda", torch.cuda.current_device())
+    return d
+
+
+@contextlib.contextmanager
+def _on(device: torch.device, stream):
+    """Makes `device` and `stream` the current ones; the handle of the stream.  What is allocated meanwhile belongs to the
+    stream that uses it."""
+    with torch.cuda.device(device), torch.cuda.stream(stream):
+        yield _current_stream(device)
+
+
+def _enter(device: torch.device, stream):
+    """The stream's handle if the call can go ahead as things are, else None: another device or stream has to be made current."""
+    if stream is None and torch.cuda.current_device() == device.index:
+        return _current_stream(device)
+    return None
+
+
+def _rows(t: torch.Tensor, what: str, tokens: int, heads: int, head_dim: int, dtype: torch.dtype, device: torch.device):
+    """`t` as codec_rows: [tokens, heads, head_dim] with contiguous channels, in storage that is there."""
+    if t.shape != (tokens, heads, head_dim) or t.dtype != dtype or t.device != device or t.stride(2) != 1:
+        raise ValueError(f"{what}: need a {dtype} tensor of shape {(tokens, heads, head_dim)} with contiguous channels on "
+                         f"{device}, got {t.dtype} {tuple(t.shape)} on {t.device}, strides {t.stride()}")
+    last = (tokens - 1) * t.stride(0) + (heads - 1) * t.stride(1) + head_dim
+    if tokens and t.untyped_storage().nbytes() // 2 - t.storage_offset() < last:
+        raise ValueError(f"{what}: the tensor's storage ends before its last element")
+    # the stride of a single token or head says nothing
+    return B.codec_rows(t.data_ptr(), t.stride(0) if tokens > 1 else 0, t.stride(1) if heads > 1 else 0)
+
+
+def _index(t: torch.Tensor, what: str, tokens: int, device: torch.device) -> int:
+    if t.shape != (tokens,) or t.dtype != torch.int64 or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{what}: need a contiguous int64 tensor of shape {(tokens,)} on {device}, "
+                         f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+    if tokens and t.untyped_storage().nbytes() // 8 - t.storage_offset() < tokens:
+        raise ValueError(f"{what}: the tensor's storage ends before its last element")
+    return t.data_ptr()
+
+
+class Rotary:
+    """Rotary positions: which channels turn and how fast (codec_rotary_config), with the device table behind them.
+
+    ``rotary_dim`` channels of a head turn, in pairs (i, i + rotary_dim / 2) or, with ``interleaved``, (2i, 2i + 1).
+    ``scaling``: None or a dict with ``kind`` ("linear", "ntk", "wavelength", "yarn"), ``factor`` and, for the last two,
+    ``original_length`` and ``low``, ``high`` (wavelength; 1 and 4 unless given) or ``fast``, ``slow`` (yarn; 32 and 1).
+    ``magnitude`` overrides the factor on turned channels that belongs to the scaling.
+    """
+
+    def __init__(self, rotary_dim, theta=10000.0, interleaved=False, scaling=None, device="cuda:0", magnitude=None):
+        s = None
+        if scaling is not None:
+            known = {"kind", "factor", "original_length", "low", "high", "fast", "slow"}
+            if scaling.get("kind") not in _SCALINGS or set(scaling) - known:
+                raise ValueError(f"scaling: kind is one of {sorted(_SCALINGS)}, beside {sorted(known - {'kind'})}; got {scaling}")
+            s = B.codec_rotary_scaling(_SCALINGS[scaling["kind"]], scaling.get("original_length", 0), scaling.get("factor", 0.0),
+                                       scaling.get("low", 1.0), scaling.get("high", 4.0), scaling.get("fast", 32.0),
+                                       scaling.get("slow", 1.0))
+        st, turns, factor = B.codec_rotary_turns(rotary_dim, theta, s)
+        if st != B.CODEC_OK:
+            raise B.CodecError(st, "codec_rotary_turns")
+        self.device = _device(device)
+        self.rotary_dim = rotary_dim
+        self.magnitude = factor if magnitude is None else magnitude
+        self.turns = torch.from_numpy(turns).to(self.device)        # turns a position, 64 bits
+        layout = B.CODEC_ROTARY_INTERLEAVED if interleaved else B.CODEC_ROTARY_HALF
+        self._config = [B.codec_rotary_config(rotary_dim, layout, inverse, self.magnitude, self.turns.data_ptr())
+                        for inverse in (0, 1)]
+
+    def apply(self, x: torch.Tensor, positions: torch.Tensor, inverse=False, out: torch.Tensor = None, stream=None) -> torch.Tensor:
+        """x [tokens, heads, head_dim] turned to its positions, or back (the gradient); ``out`` may be x itself."""
+        if x.dim() != 3 or x.dtype not in _CODE or self.device.type != "cuda":
+            raise ValueError(f"x: need a 16-bit tensor [tokens, heads, head_dim] and a GPU, got {x.dtype} {tuple(x.shape)} on {x.device}")
+        s = _enter(self.device, stream)
+        if s is None:
+            with _on(self.device, stream) as s:
+                return self._apply(x, positions, inverse, out, s)
+        return self._apply(x, positions, inverse, out, s)
+
+    def _apply(self, x, positions, inverse, out, s):
+        tokens, heads, d = x.shape
+        rows = _rows(x, "x", tokens, heads, d, x.dtype, self.device)
+        at = _index(positions, "positions", tokens, self.device)
+        if out is None:
+            out = torch.empty((tokens, heads, d), dtype=x.dtype, device=self.device)
+        into = _rows(out, "out", tokens, heads, d, x.dtype, self.device)
+        st = B.codec_rotary(self._config[bool(inverse)], heads, d, _CODE[x.dtype], rows, into, at, tokens, s)
+        if st != B.CODEC_OK:
+            raise B.CodecError(st, "codec_rotary")
+        return out
+
+
+class KVCache:
+    """The page pools of a cache, one K and one V pool per layer, with the operations that fill them.
+
+    ``head`` is the attribute bag a plan is built from (num_q_heads, num_kv_heads, head_dim, dtype, page_size).  ``layout``
+    "thd": pools [num_pages, page_size, num_kv_heads, head_dim]; "htd": [num_pages, num_kv_heads, page_size, head_dim].
+    ``pools``: the (k, v) tensors of the layers if the program has them already (views with other strides too, the same
+    in every layer); otherwise they are allocated.
+    """
+
+    def __init__(self, head, num_pages, layers=1, layout="htd", device="cuda:0", pools=None):
+        if layout not in ("thd", "htd"):
+            raise ValueError(f"layout: thd or htd, got {layout!r}")
+        if head.dtype not in _TORCH_DTYPE:
+            raise ValueError(f"head.dtype: {head.dtype}")
+        self.head, self.layout, self.num_pages, self.device = head, layout, int(num_pages), _device(device)
+        self.dtype = _TORCH_DTYPE[head.dtype]
+        ps, h, d = head.page_size, head.num_kv_heads, head.head_dim
+        shape = (self.num_pages, ps, h, d) if layout == "thd" else (self.num_pages, h, ps, d)
+        if pools is None:
+            pools = [tuple(torch.empty(shape, dtype=self.dtype, device=self.device) for _ in "kv") for _ in range(layers)]
+        self.pools = [tuple(kv) for kv in pools]
+        flat = [p for kv in self.pools for p in kv]
+        if not flat or any(len(kv) != 2 for kv in self.pools):
+            raise ValueError("pools: need a (k, v) pair for every layer")
+        strides = flat[0].stride()
+        for p in flat:
+            if p.shape != shape or p.dtype != self.dtype or p.device != self.device or p.stride() != strides or p.stride(3) != 1:
+                raise ValueError(f"pools: need {self.dtype} tensors of shape {shape} on {self.device} with the same strides and "
+                                 f"contiguous channels, got {p.dtype} {tuple(p.shape)} on {p.device}, strides {p.stride()}")
+        page, token, kv_head = (strides[0], strides[1], strides[2]) if layout == "thd" else (strides[0], strides[2], strides[1])
+        self.page_stride, self.token_stride, self.head_stride = page, token, kv_head
+        self._layout = B.codec_kv_layout(self.num_pages, page, token, kv_head)
+        self._head = B.codec_head_config(head.num_q_heads, h, d, head.dtype, ps, 0.0)
+        self._reach = (self.num_pages - 1) * page + (ps - 1) * token + (h - 1) * kv_head + d
+        self._storages = [tuple(p.untyped_storage() for p in kv) for kv in self.pools]
+
+    def paged(self, node_page_off, page_ids):
+        """These pools with a forest's page lists: the ``paged`` of a PlannedAttention."""
+        return SimpleNamespace(node_page_off=node_page_off, page_ids=page_ids, num_pages=self.num_pages,
+                               page_stride=self.page_stride, token_stride=self.token_stride, head_stride=self.head_stride)
+
+    def _check_storage(self, layer: int) -> None:
+        """A tensor keeps its shape when its storage is given back: the memory behind it is what counts."""
+        for pool, storage in zip(self.pools[layer], self._storages[layer]):
+            if storage.nbytes() // 2 - pool.storage_offset() < self._reach:
+                raise ValueError(f"pools of layer {layer}: the storage ends before the last page")
+
+    def append(self, layer, q, k, v, positions, slots, rotary: Rotary = None, q_out: torch.Tensor = None, stream=None):
+        """The step's tokens into ``layer``: queries and keys turned to ``positions``, keys and values stored at ``slots``
+        (page * page_size + token; negative: not stored).  Returns the turned queries (``q_out``, which may be q itself);
+        q None: keys and values only.  Without ``rotary`` rows pass as they are and ``positions`` may be None."""
+        if self.device.type != "cuda":
+            raise ValueError(f"append needs pools on a GPU, these are on {self.device}")
+        s = _enter(self.device, stream)
+        if s is None:
+            with _on(self.device, stream) as s:
+                return self._append(layer, q, k, v, positions, slots, rotary, q_out, s)
+        return self._append(layer, q, k, v, positions, slots, rotary, q_out, s)
+
+    def _append(self, layer, q, k, v, positions, slots, rotary, q_out, s):
+        h, device, dtype = self.head, self.device, self.dtype
+        self._check_storage(layer)
+        tokens = k.shape[0]
+        k_rows = _rows(k, "k", tokens, h.num_kv_heads, h.head_dim, dtype, device)
+        v_rows = _rows(v, "v", tokens, h.num_kv_heads, h.head_dim, dtype, device)
+        q_rows = out_rows = config = at = None
+        if q is not None:
+            q_rows = _rows(q, "q", tokens, h.num_q_heads, h.head_dim, dtype, device)
+            if q_out is None:
+                q_out = torch.empty((tokens, h.num_q_heads, h.head_dim), dtype=dtype, device=device)
+            out_rows = _rows(q_out, "q_out", tokens, h.num_q_heads, h.head_dim, dtype, device)
+        elif q_out is not None:
+            raise ValueError("q_out without q")
+        if rotary is not None:
+            if rotary.device != device:
+                raise ValueError(f"rotary is on {rotary.device}, the pools are on {device}")
+            config, at = rotary._config[0], _index(positions, "positions", tokens, device)
+        kp, vp = self.pools[layer]
+        st = B.codec_append(self._head, config, q_rows, out_rows, k_rows, v_rows, at,
+                            _index(slots, "slots", tokens, device), tokens, kp.data_ptr(), vp.data_ptr(), self._layout, s)
+        if st != B.CODEC_OK:
+            raise B.CodecError(st, "codec_append")
+        return q_out

@@ -9,6 +9,7 @@
 #include "codec.h"
 #include "kernels.hpp"
 #include "planner.hpp"
+#include "status.hpp"
 
 struct codec_plan {
     codec::PlanData d;
@@ -22,14 +23,19 @@ namespace {
 
 thread_local char g_last_error[256] = "";
 
-// Records which HIP call failed and why; returns CODEC_ERR_HIP.
-int hip_failure(const char *what, int code)
+}  // namespace
+
+int codec::hip_failure(const char *what, int code)
 {
     std::snprintf(g_last_error, sizeof g_last_error, "%s: %s (%d)", what,
                   hipGetErrorString(static_cast<hipError_t>(code)), code);
     (void)hipGetLastError();        // do not leave the error for the caller's next HIP call
     return CODEC_ERR_HIP;
 }
+
+namespace {
+
+using codec::hip_failure;
 
 size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
@@ -378,6 +384,7 @@ const char *codec_status_string(int status)
     case CODEC_ERR_HIP: return "HIP runtime error";
     case CODEC_ERR_NOT_UPLOADED: return "plan metadata not uploaded";
     case CODEC_ERR_OUT_OF_MEMORY: return "out of host memory";
+    case CODEC_ERR_NO_PAGES: return "not enough free pages";
     default: return "unknown status";
     }
 }

@@ -1,0 +1,3 @@
+// Every kernel of the library, in one translation unit: the library carries one device image.
+#include "kernels.hip"
+#include "rotary.hip"

@@ -1,0 +1,235 @@
+// C ABI of the operators around a decode step: argument checks and launches.
+#include "operators.hpp"
+
+#include <algorithm>
+#include <cmath>
+
+#include "status.hpp"
+
+namespace {
+
+using codec::hip_failure;
+
+constexpr double kTwoPi = 6.283185307179586476925;
+constexpr int64_t kMaxSpan = int64_t(1) << 58;          // elements: byte offsets, and sums of a few, stay in 64 bits
+
+bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+// What the pools of this library hold; the codes codec_plan_create returns.
+int check_rows_of(int32_t head_dim, int32_t dtype)
+{
+    if (head_dim != 64 && head_dim != 128 && head_dim != 256) return CODEC_ERR_UNSUPPORTED;
+    if (dtype != CODEC_DTYPE_FP16 && dtype != CODEC_DTYPE_BF16) return CODEC_ERR_UNSUPPORTED;
+    return CODEC_OK;
+}
+
+int check_head(const codec_head_config &h)
+{
+    if (h.num_kv_heads < 1 || h.num_q_heads < 1 || h.num_kv_heads > (1 << 16) || h.num_q_heads > (1 << 16)) return CODEC_ERR_INVALID_ARGUMENT;
+    if (int st = check_rows_of(h.head_dim, h.dtype)) return st;
+    if (h.page_size < 16 || h.page_size > 4096 || (h.page_size & (h.page_size - 1)) != 0) return CODEC_ERR_UNSUPPORTED;
+    return CODEC_OK;
+}
+
+struct Extent { int64_t count, stride; };
+
+// Elements from the first to behind the last of `inner` contiguous ones repeated along `dims`; -1 where two coincide.
+template <size_t N>
+int64_t separate_span(int64_t inner, Extent (&dims)[N])
+{
+    std::sort(dims, dims + N, [](const Extent &a, const Extent &b) { return a.stride < b.stride; });
+    int64_t span = inner;
+    for (const Extent &d : dims) {
+        if (d.count <= 1) continue;
+        if (d.stride < span || d.stride > kMaxSpan / d.count) return -1;
+        span += (d.count - 1) * d.stride;
+        if (span > kMaxSpan) return -1;
+    }
+    return span;
+}
+
+// Elements of a pool behind its first one that `layout` reaches; -1 for a layout a cache cannot be written by.
+int64_t pool_span(const codec_head_config &h, const codec_kv_layout &l)
+{
+    if (l.num_pages < 1 || l.num_pages > (int64_t(1) << 31) || l.page_stride < 1 || l.token_stride < h.head_dim || l.head_stride < h.head_dim) return -1;
+    if (l.page_stride % 8 || l.token_stride % 8 || l.head_stride % 8) return -1;
+    Extent dims[] = {{l.num_pages, l.page_stride}, {h.page_size, l.token_stride}, {h.num_kv_heads, l.head_stride}};
+    return separate_span(h.head_dim, dims);
+}
+
+struct Range { const char *begin, *end; };
+bool overlap(const Range &a, const Range &b) { return a.begin < b.end && b.begin < a.end; }
+
+bool rows_ok(const codec_rows *r, int64_t tokens, int64_t heads)
+{
+    return r && r->data && aligned16(r->data) && r->token_stride >= 0 && r->head_stride >= 0 && r->token_stride % 8 == 0 &&
+           r->head_stride % 8 == 0 && r->token_stride <= kMaxSpan / tokens && r->head_stride <= kMaxSpan / heads;
+}
+
+int64_t rows_span(const codec_rows &r, int64_t tokens, int64_t heads, int64_t d)
+{
+    return (tokens - 1) * r.token_stride + (heads - 1) * r.head_stride + d;
+}
+
+Range range_of(const codec_rows &r, int64_t tokens, int64_t heads, int64_t d)
+{
+    const char *p = static_cast<const char *>(r.data);
+    return {p, p + 2 * rows_span(r, tokens, heads, d)};
+}
+
+// Rows that may be written: none overlaps another.
+bool separate(const codec_rows &r, int64_t tokens, int64_t heads, int64_t d)
+{
+    Extent dims[] = {{tokens, r.token_stride}, {heads, r.head_stride}};
+    return separate_span(d, dims) >= 0;
+}
+
+bool same_rows(const codec_rows &a, const codec_rows &b, int64_t tokens, int64_t heads)
+{
+    return a.data == b.data && (tokens == 1 || a.token_stride == b.token_stride) && (heads == 1 || a.head_stride == b.head_stride);
+}
+
+// No element of a is one of b: apart in memory, or other heads of the same tokens' tensor.
+bool apart(const codec_rows &a, int64_t heads_a, const codec_rows &b, int64_t heads_b, int64_t tokens, int64_t d)
+{
+    if (!overlap(range_of(a, tokens, heads_a, d), range_of(b, tokens, heads_b, d))) return true;
+    if (a.token_stride != b.token_stride) return false;
+    const bool a_first = a.data < b.data;
+    const codec_rows &lo = a_first ? a : b, &hi = a_first ? b : a;
+    const int64_t offset = (static_cast<const char *>(hi.data) - static_cast<const char *>(lo.data)) / 2;
+    return offset >= rows_span(lo, 1, a_first ? heads_a : heads_b, d) &&
+           offset + rows_span(hi, 1, a_first ? heads_b : heads_a, d) <= a.token_stride;
+}
+
+int check_rotary(const codec_rotary_config &r, int32_t head_dim, const int64_t *positions)
+{
+    if (r.rotary_dim < 2 || r.rotary_dim > head_dim || r.rotary_dim % 2 || !r.turns || !positions) return CODEC_ERR_INVALID_ARGUMENT;
+    if (r.layout != CODEC_ROTARY_HALF && r.layout != CODEC_ROTARY_INTERLEAVED) return CODEC_ERR_INVALID_ARGUMENT;
+    if (!std::isfinite(r.magnitude)) return CODEC_ERR_INVALID_ARGUMENT;
+    return CODEC_OK;
+}
+
+codec::RowsView view_of(const codec_rows &r) { return {static_cast<char *>(r.data), 2 * r.token_stride, 2 * r.head_stride}; }
+
+void set_rotary(codec::RotaryParams &p, const codec_rotary_config &r, const int64_t *positions)
+{
+    p.positions = positions;
+    p.turns = r.turns;
+    p.rotary_dim = r.rotary_dim;
+    p.magnitude = r.magnitude;
+    p.sign = r.inverse ? -1.f : 1.f;
+}
+
+}  // namespace
+
+extern "C" {
+
+int codec_rotary_turns(int32_t rotary_dim, double theta, const codec_rotary_scaling *scaling, double *turns, float *magnitude)
+{
+    if (!turns || !magnitude || rotary_dim < 2 || rotary_dim > 256 || rotary_dim % 2) return CODEC_ERR_INVALID_ARGUMENT;
+    if (!(theta > 1.0) || !std::isfinite(theta)) return CODEC_ERR_INVALID_ARGUMENT;
+    codec_rotary_scaling s{};
+    if (scaling) s = *scaling;
+    if (s.kind < CODEC_ROTARY_UNSCALED || s.kind > CODEC_ROTARY_YARN) return CODEC_ERR_INVALID_ARGUMENT;
+    if (s.kind != CODEC_ROTARY_UNSCALED && (!(s.factor > 0.0) || !std::isfinite(s.factor))) return CODEC_ERR_INVALID_ARGUMENT;
+    const bool long_context = s.kind == CODEC_ROTARY_WAVELENGTH || s.kind == CODEC_ROTARY_YARN;
+    if (long_context && s.original_length < 1) return CODEC_ERR_INVALID_ARGUMENT;
+    if (s.kind == CODEC_ROTARY_WAVELENGTH && (!(s.low < s.high) || !std::isfinite(s.low) || !std::isfinite(s.high))) return CODEC_ERR_INVALID_ARGUMENT;
+    if (s.kind == CODEC_ROTARY_YARN && (!(s.slow > 0.0) || !(s.fast > s.slow) || !std::isfinite(s.fast))) return CODEC_ERR_INVALID_ARGUMENT;
+
+    const int32_t pairs = rotary_dim / 2;
+    if (s.kind == CODEC_ROTARY_NTK && rotary_dim > 2) theta *= std::pow(s.factor, double(rotary_dim) / (rotary_dim - 2));
+    if (!(theta > 0.0) || !std::isfinite(theta)) return CODEC_ERR_INVALID_ARGUMENT;
+    double from = 0.0, to = 0.0;                // YARN: the pairs between which the two frequencies are blended
+    if (s.kind == CODEC_ROTARY_YARN) {
+        auto pair_of = [&](double n) { return rotary_dim * std::log(s.original_length / (n * kTwoPi)) / (2.0 * std::log(theta)); };
+        from = std::max(std::floor(pair_of(s.fast)), 0.0);
+        to = std::min(std::ceil(pair_of(s.slow)), double(rotary_dim - 1));
+    }
+    for (int32_t i = 0; i < pairs; ++i) {
+        double f = std::pow(theta, -2.0 * i / rotary_dim);
+        if (s.kind == CODEC_ROTARY_LINEAR) {
+            f /= s.factor;
+        } else if (long_context) {
+            const double scaled = s.kind == CODEC_ROTARY_WAVELENGTH ? 1.0 - (s.original_length * f / kTwoPi - s.low) / (s.high - s.low)
+                                                                    : (i - from) / std::max(to - from, 0.001);
+            const double w = std::min(std::max(scaled, 0.0), 1.0);
+            f = (1.0 - w) * f + w * (f / s.factor);
+        }
+        turns[i] = f / kTwoPi;
+    }
+    *magnitude = s.kind == CODEC_ROTARY_YARN && s.factor > 1.0 ? float(0.1 * std::log(s.factor) + 1.0) : 1.f;
+    return CODEC_OK;
+}
+
+int codec_rotary(const codec_rotary_config *rotary, int32_t num_heads, int32_t head_dim, int32_t dtype, const codec_rows *x,
+                 const codec_rows *out, const int64_t *positions, int32_t num_tokens, void *stream)
+{
+    if (!rotary || num_heads < 1 || num_heads > (1 << 16) || num_tokens < 0) return CODEC_ERR_INVALID_ARGUMENT;
+    if (int st = check_rows_of(head_dim, dtype)) return st;
+    if (num_tokens == 0) return CODEC_OK;
+    if (int st = check_rotary(*rotary, head_dim, positions)) return st;
+    if (!rows_ok(x, num_tokens, num_heads) || !rows_ok(out, num_tokens, num_heads) || !separate(*out, num_tokens, num_heads, head_dim)) return CODEC_ERR_INVALID_ARGUMENT;
+    if (!same_rows(*x, *out, num_tokens, num_heads) && !apart(*x, num_heads, *out, num_heads, num_tokens, head_dim)) return CODEC_ERR_INVALID_ARGUMENT;
+
+    codec::RotaryParams p{};
+    p.q = view_of(*x);
+    p.q_out = view_of(*out);
+    p.q_heads = num_heads;
+    p.head_dim = head_dim;
+    p.num_tokens = num_tokens;
+    set_rotary(p, *rotary, positions);
+    if (int e = codec::launch_rotary(p, dtype, rotary->layout == CODEC_ROTARY_INTERLEAVED, stream)) return hip_failure("rotary launch", e);
+    return CODEC_OK;
+}
+
+int codec_append(const codec_head_config *head, const codec_rotary_config *rotary, const codec_rows *q, const codec_rows *q_out,
+                 const codec_rows *k, const codec_rows *v, const int64_t *positions, const int64_t *slots, int32_t num_tokens,
+                 void *k_pages, void *v_pages, const codec_kv_layout *layout, void *stream)
+{
+    if (!head || !layout || num_tokens < 0 || !q != !q_out) return CODEC_ERR_INVALID_ARGUMENT;
+    if (int st = check_head(*head)) return st;
+    const int64_t pool = pool_span(*head, *layout);
+    if (pool < 0) return CODEC_ERR_INVALID_ARGUMENT;
+    if (num_tokens == 0) return CODEC_OK;
+    if (rotary)
+        if (int st = check_rotary(*rotary, head->head_dim, positions)) return st;
+    if (!slots || !k_pages || !v_pages || !aligned16(k_pages) || !aligned16(v_pages) || k_pages == v_pages) return CODEC_ERR_INVALID_ARGUMENT;
+    const int64_t t = num_tokens, d = head->head_dim, hq = head->num_q_heads, h = head->num_kv_heads;
+    if (!rows_ok(k, t, h) || !rows_ok(v, t, h) || (q && (!rows_ok(q, t, hq) || !rows_ok(q_out, t, hq)))) return CODEC_ERR_INVALID_ARGUMENT;
+    for (const void *pages : {k_pages, v_pages}) {
+        const Range r{static_cast<const char *>(pages), static_cast<const char *>(pages) + 2 * pool};
+        if (overlap(r, range_of(*k, t, h, d)) || overlap(r, range_of(*v, t, h, d))) return CODEC_ERR_INVALID_ARGUMENT;
+        if (q && (overlap(r, range_of(*q, t, hq, d)) || overlap(r, range_of(*q_out, t, hq, d)))) return CODEC_ERR_INVALID_ARGUMENT;
+    }
+    if (q) {
+        if (!separate(*q_out, t, hq, d)) return CODEC_ERR_INVALID_ARGUMENT;
+        if (!same_rows(*q, *q_out, t, hq) && !apart(*q, hq, *q_out, hq, t, d)) return CODEC_ERR_INVALID_ARGUMENT;
+        if (!apart(*q_out, hq, *k, h, t, d) || !apart(*q_out, hq, *v, h, t, d)) return CODEC_ERR_INVALID_ARGUMENT;
+    }
+
+    codec::RotaryParams p{};
+    if (q) {
+        p.q = view_of(*q);
+        p.q_out = view_of(*q_out);
+        p.q_heads = head->num_q_heads;
+    }
+    p.k = view_of(*k);
+    p.v = view_of(*v);
+    p.kv_heads = head->num_kv_heads;
+    p.k_pages = static_cast<char *>(k_pages);
+    p.v_pages = static_cast<char *>(v_pages);
+    p.page_stride = 2 * layout->page_stride;
+    p.slot_stride = 2 * layout->token_stride;
+    p.head_stride = 2 * layout->head_stride;
+    p.slots = slots;
+    p.num_slots = layout->num_pages * head->page_size;
+    while ((1 << p.page_shift) < head->page_size) ++p.page_shift;
+    p.head_dim = head->head_dim;
+    p.num_tokens = num_tokens;
+    if (rotary) set_rotary(p, *rotary, positions);
+    if (int e = codec::launch_rotary(p, head->dtype, rotary && rotary->layout == CODEC_ROTARY_INTERLEAVED, stream)) return hip_failure("append launch", e);
+    return CODEC_OK;
+}
+
+}  // extern "C"

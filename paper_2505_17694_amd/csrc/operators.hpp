@@ -1,0 +1,32 @@
+// Launch interface of the kernels around a decode step, and checks their entry points share.
+#pragma once
+
+#include <cstddef>
+#include <cstdint>
+
+#include "codec.h"
+
+namespace codec {
+
+// Rows of one kind (queries, keys, values) of the tokens: strides in bytes.
+struct RowsView {
+    char *data;
+    int64_t token_stride, head_stride;
+};
+
+struct RotaryParams {
+    RowsView q, q_out, k, v;        // q.data == nullptr: no queries; k.data == nullptr: no keys and values
+    char *k_pages, *v_pages;
+    int64_t page_stride, slot_stride, head_stride;      // bytes
+    const int64_t *positions;
+    const int64_t *slots;
+    const double *turns;            // [rotary_dim / 2]; not read where rotary_dim == 0
+    int64_t num_tokens, num_slots;  // slots of the pools: slot s is token s % page size of page s / page size
+    int32_t q_heads, kv_heads, head_dim, rotary_dim, page_shift;
+    float magnitude, sign;          // factors on the turned channels and on the sine
+};
+
+// All return a hipError_t value (0 = success) without synchronising.
+int launch_rotary(const RotaryParams &p, int dtype, bool interleaved, void *stream);
+
+}  // namespace codec

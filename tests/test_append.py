@@ -1,0 +1,374 @@
+"""Rotary positions and appending to the cache: frequencies and refusals on the CPU, results on the GPU."""
+import ctypes
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2505_17694_amd as C
+from oracle import operators as O
+from workloads import HeadConfig, DTYPE_BF16, DTYPE_FP16
+
+DEV = "cuda:0"
+TORCH = {DTYPE_FP16: torch.float16, DTYPE_BF16: torch.bfloat16}
+SCALINGS = [None, dict(kind="linear", factor=4.0), dict(kind="ntk", factor=8.0),
+            dict(kind="wavelength", factor=8.0, original_length=8192, low=1.0, high=4.0),
+            dict(kind="yarn", factor=4.0, original_length=4096, fast=32.0, slow=1.0),
+            dict(kind="yarn", factor=0.5, original_length=64, fast=32.0, slow=1.0)]
+
+
+def frequencies(r, theta, scaling):
+    return O.rotary_frequencies(r, theta, **(scaling or {}))
+
+
+# ---- on the CPU ------------------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("r", [2, 4, 20, 64, 128, 256])
+@pytest.mark.parametrize("theta", [10000.0, 500000.0])
+@pytest.mark.parametrize("scaling", SCALINGS)
+def test_turns_of_a_position(r, theta, scaling):
+    rot = C.Rotary(r, theta=theta, scaling=scaling, device="cpu")
+    want, magnitude = frequencies(r, theta, scaling)
+    # a handful of 64-bit operations, among them a power with an exponent of up to log(theta) = 13
+    assert np.all(np.abs(rot.turns.numpy() * 2 * math.pi - want) <= 2.0 ** -47 * np.abs(want))
+    assert abs(rot.magnitude - magnitude) <= 2.0 ** -24 * magnitude
+
+
+def test_turns_refusals():
+    def status(r=64, theta=1e4, **s):
+        kind = s.pop("kind", 0)
+        v = dict(original_length=4096, factor=2.0, low=1.0, high=4.0, fast=32.0, slow=1.0)
+        v.update(s)
+        return C.codec_rotary_turns(r, theta, C.codec_rotary_scaling(kind, v["original_length"], v["factor"], v["low"], v["high"],
+                                                                    v["fast"], v["slow"]))[0]
+    assert all(status(kind=k) == C.CODEC_OK for k in range(5))
+    nan, inf = float("nan"), float("inf")
+    bad = [dict(r=r) for r in (0, -2, 1, 63, 258)] + [dict(theta=t) for t in (1.0, 0.0, -5.0, nan, inf)] + [dict(kind=k) for k in (-1, 5)]
+    bad += [dict(kind=k, factor=f) for k in (1, 2, 3, 4) for f in (0.0, -1.0, nan, inf)]
+    bad += [dict(kind=k, original_length=n) for k in (3, 4) for n in (0, -1)]
+    bad += [dict(kind=3, low=4.0), dict(kind=3, low=nan), dict(kind=3, high=inf)]
+    bad += [dict(kind=4, slow=0.0), dict(kind=4, slow=32.0), dict(kind=4, fast=nan), dict(kind=4, fast=inf)]
+    for b in bad:
+        assert status(**b) == C.CODEC_ERR_INVALID_ARGUMENT, b
+    assert C.codec_rotary_turns(64, 1e4, None)[0] == C.CODEC_OK
+    lib = ctypes.CDLL(C.LIB_PATH)
+    assert lib.codec_rotary_turns(64, ctypes.c_double(1e4), None, None, None) == C.CODEC_ERR_INVALID_ARGUMENT
+    for s in (dict(kind="other", factor=2.0), dict(factor=2.0), dict(kind="linear", factor=2.0, length=3)):
+        with pytest.raises(ValueError):
+            C.Rotary(64, scaling=s, device="cpu")
+    with pytest.raises(C.CodecError):
+        C.Rotary(64, scaling=dict(kind="linear"), device="cpu")
+
+
+def test_rotary_refusals():
+    """Argument errors that are caught before any HIP call."""
+    def status(tokens=4, heads=2, d=64, dtype=1, positions=4096, x=(1 << 20, 128, 64), out=(1 << 21, 128, 64), r=64, layout=0,
+               magnitude=1.0, turns=4096, config=True):
+        cfg = C.codec_rotary_config(r, layout, 0, magnitude, turns) if config else None
+        return C.codec_rotary(cfg, heads, d, dtype, C.codec_rows(*x) if x else None, C.codec_rows(*out) if out else None,
+                              positions, tokens)
+    assert status(tokens=0) == C.CODEC_OK                              # nothing to do, nothing launched
+    assert status(tokens=0, x=None, out=None, positions=0) == C.CODEC_OK
+    at = 1 << 20
+    for bad in (dict(config=False), dict(tokens=-1), dict(heads=0), dict(heads=1 << 17), dict(positions=0), dict(x=None), dict(out=None),
+                dict(x=(0, 128, 64)), dict(x=(at + 8, 128, 64)), dict(x=(at, 132, 64)), dict(x=(at, 128, 68)), dict(x=(at, -128, 64)),
+                dict(x=(at, 1 << 57, 64)), dict(out=(1 << 21, 64, 64)), dict(out=(1 << 21, 128, 0)), dict(out=(1 << 21, 0, 64)),
+                dict(out=(at + 256, 128, 64)), dict(out=(at, 256, 64)), dict(out=(at + 128, 128, 64)),
+                dict(r=0), dict(r=3), dict(r=66), dict(r=-2), dict(layout=2), dict(layout=-1), dict(magnitude=float("nan")),
+                dict(magnitude=float("inf")), dict(turns=0)):
+        assert status(**bad) == C.CODEC_ERR_INVALID_ARGUMENT, bad
+    for bad in (dict(d=96), dict(d=32), dict(dtype=2), dict(dtype=-1)):
+        assert status(**bad) == C.CODEC_ERR_UNSUPPORTED, bad
+
+
+def test_append_refusals():
+    base = 1 << 30
+    good = dict(head=(8, 2, 128, 1, 16), q=(base, 1024, 128), q_out=(base, 1024, 128), k=(base + (1 << 20), 256, 128),
+                v=(base + (1 << 21), 256, 128), positions=4096, slots=4096, tokens=3, kp=base * 2, vp=base * 3,
+                layout=(8, 4096, 128, 2048), rotary=(128, 0, 0, 1.0, 4096))
+
+    def status(**kw):
+        a = dict(good, **kw)
+        row = lambda r: C.codec_rows(*r) if r else None
+        head = C.codec_head_config(*a["head"], 0.0) if a["head"] else None
+        return C.codec_append(head, C.codec_rotary_config(*a["rotary"]) if a["rotary"] else None, row(a["q"]), row(a["q_out"]),
+                              row(a["k"]), row(a["v"]), a["positions"], a["slots"], a["tokens"], a["kp"], a["vp"],
+                              C.codec_kv_layout(*a["layout"]) if a["layout"] else None)
+    assert status(tokens=0) == C.CODEC_OK
+    at = base + (1 << 20)
+    for bad in (dict(head=None), dict(layout=None), dict(tokens=-1), dict(q=None), dict(q_out=None), dict(k=None), dict(v=None),
+                dict(slots=0), dict(positions=0), dict(kp=0), dict(vp=0), dict(kp=base * 2 + 8), dict(vp=base * 2),
+                dict(head=(8, 0, 128, 1, 16)), dict(head=(0, 2, 128, 1, 16)), dict(head=(8, 2, 128, 1, 16), rotary=(130, 0, 0, 1.0, 4096)),
+                dict(layout=(0, 4096, 128, 2048)), dict(layout=(8, 4096, 64, 2048)), dict(layout=(8, 4096, 132, 2048)),
+                dict(layout=(8, 2048, 128, 2048)), dict(layout=(8, 4096, 128, 128)), dict(layout=(1 << 32, 4096, 128, 2048)),
+                dict(k=(at + 2, 256, 128)), dict(k=(at, 256, 100)), dict(k=(base * 2 + 4096, 256, 128)), dict(v=(base * 3, 256, 128)),
+                dict(q=(base * 3, 1024, 128), q_out=(base * 3, 1024, 128)), dict(q_out=(at, 1024, 128)),
+                dict(q_out=(base + 1024, 1024, 128))):
+        assert status(**bad) == C.CODEC_ERR_INVALID_ARGUMENT, bad
+    for bad in (dict(head=(8, 2, 96, 1, 16)), dict(head=(8, 2, 128, 2, 16)), dict(head=(8, 2, 128, 1, 24)), dict(head=(8, 2, 128, 1, 8))):
+        assert status(**bad) == C.CODEC_ERR_UNSUPPORTED, bad
+
+
+def test_cache_refusals():
+    head = HeadConfig(8, 2, 128, DTYPE_BF16)
+    cache = C.KVCache(head, 4, layers=2, device="cpu")
+    assert cache.pools[0][0].shape == (4, 2, 16, 128) and C.KVCache(head, 4, layout="thd", device="cpu").pools[0][0].shape == (4, 16, 2, 128)
+    z = torch.zeros(1, 2, 128, dtype=torch.bfloat16)
+    i = torch.zeros(1, dtype=torch.int64)
+    with pytest.raises(ValueError):                      # no CPU path
+        cache.append(0, None, z, z, None, i)
+    with pytest.raises(ValueError):
+        C.Rotary(128, device="cpu").apply(z, i)
+    for pools in ([], [(cache.pools[0][0],)], [(cache.pools[0][0], cache.pools[0][1][:3])], [(cache.pools[0][0], cache.pools[0][1].half())],
+                  [(cache.pools[0][0], torch.zeros(4, 2, 16, 256, dtype=torch.bfloat16)[..., :128])],
+                  [(cache.pools[0][0].transpose(2, 3).contiguous().transpose(2, 3),) * 2]):
+        with pytest.raises(ValueError):
+            C.KVCache(head, 4, pools=pools, device="cpu")
+    with pytest.raises(ValueError):
+        C.KVCache(head, 4, layout="dht", device="cpu")
+    with pytest.raises(ValueError):
+        C.KVCache(HeadConfig(8, 2, 128, 2), 4, device="cpu")
+
+
+# ---- on the GPU ------------------------------------------------------------------------------------------
+
+
+def half_step(dtype):
+    """A rounding's relative error, and its absolute one where the type's steps no longer shrink."""
+    f = torch.finfo(TORCH[dtype])
+    return f.eps / 2, f.tiny * f.eps / 2
+
+
+def close(got, want, size, dtype, what=""):
+    """One rounding to 16 bits, behind 32-bit products: cosine and sine are off by at most 3 half steps of a 32-bit one (the
+    reduced angle, the series, the magnitude), a product and a sum round once each: 5 half steps of the pair's |a| + |b|;
+    6 are allowed."""
+    rel, least = half_step(dtype)
+    got = got.double().cpu().numpy()
+    same = (got == want) | (np.isnan(got) & np.isnan(want))
+    with np.errstate(invalid="ignore"):
+        ok = np.abs(got - want) <= rel * np.abs(want) + (1 + rel) * 6 * 2.0 ** -24 * size + least
+    assert np.all(same | ok), f"{what}: {np.count_nonzero(~(same | ok))} values, worst {np.nanmax(np.abs(got - want))}"
+
+
+def rows(gen, dtype, *shape):
+    return torch.randn(shape, generator=gen).to(TORCH[dtype])
+
+
+def flat_pool(pool, layout):
+    """[pages * page_size, heads, d]"""
+    return (pool if layout == "thd" else pool.transpose(1, 2)).flatten(0, 1)
+
+
+def run_append(tokens, hq, hkv, d, dtype, page, layout, r, interleaved=False, scaling=None, fused=False, seed=0, positions=None, slots=None,
+               pool=None, in_place=False, theta=10000.0, queries=True, rotate=True, spare=5):
+    """One call against the oracle, pools checked whole: slots that are not named keep their bits."""
+    print(f"[case] append tokens={tokens} heads={hq}/{hkv} d={d} dtype={dtype} page={page} {layout} r={r} interleaved={interleaved} "
+          f"scaling={scaling} fused={fused} in_place={in_place} queries={queries} rotate={rotate}", flush=True)
+    gen = torch.Generator().manual_seed(seed + 17)
+    rng = np.random.default_rng(seed)
+    head = HeadConfig(hq, hkv, d, dtype, page)
+    pages = -(-tokens // page) + spare
+    x = rows(gen, dtype, tokens, hq + 2 * hkv, d)
+    x_dev = x.to(DEV)
+    q, k, v = x_dev.split([hq, hkv, hkv], 1) if fused else (p.contiguous() for p in x_dev.split([hq, hkv, hkv], 1))
+    if pool is None:
+        shape = (pages, page, hkv, d) if layout == "thd" else (pages, hkv, page, d)
+        pool = tuple(rows(gen, dtype, *shape).to(DEV) for _ in "kv")
+    before = [p.cpu().clone() for p in pool]
+    cache = C.KVCache(head, pages, layout=layout, device=DEV, pools=[pool])
+    if positions is None:
+        positions = rng.integers(-1000, 200000, tokens)
+    if slots is None:
+        slots = rng.permutation(pages * page)[:tokens]
+        slots[rng.random(tokens) < 0.2] = -1
+    positions, slots = np.asarray(positions, np.int64), np.asarray(slots, np.int64)
+    rot = C.Rotary(r, theta=theta, interleaved=interleaved, scaling=scaling, device=DEV) if rotate else None
+    out = cache.append(0, q if queries else None, k, v, torch.from_numpy(positions).to(DEV) if rotate else None,
+                       torch.from_numpy(slots).to(DEV), rot, q_out=q if in_place else None)
+    torch.cuda.synchronize()
+    turns, magnitude = (rot.turns.cpu().numpy(), rot.magnitude) if rotate else (np.zeros(0), 1.0)
+    x64 = x.double().numpy()
+    turn = lambda a: O.rotary(a, positions, turns, magnitude, interleaved)
+    if queries:
+        close(out, *turn(x64[:, :hq]), dtype, "queries")
+        if in_place:
+            assert out.data_ptr() == q.data_ptr()
+        elif fused:
+            assert torch.equal(x_dev[:, :hq].cpu().view(torch.int16), x[:, :hq].view(torch.int16))
+    else:
+        assert out is None
+    kept = (slots >= 0) & (slots < pages * page)
+    want_k, size = turn(x64[:, hq:hq + hkv])
+    k_now, v_now = (flat_pool(p.cpu(), layout) for p in pool)
+    close(k_now[slots[kept]], want_k[kept], size[kept], dtype, "keys")
+    v_want = flat_pool(before[1], layout).clone()
+    v_want[slots[kept]] = x[:, hq + hkv:][kept]
+    assert torch.equal(v_now.contiguous().view(torch.int16), v_want.contiguous().view(torch.int16))
+    others = np.setdiff1d(np.arange(pages * page), slots)
+    assert torch.equal(k_now[others].contiguous().view(torch.int16), flat_pool(before[0], layout)[others].contiguous().view(torch.int16))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("d,r", [(64, 64), (64, 32), (64, 2), (64, 20), (64, 62), (64, 48), (128, 128), (128, 64), (128, 16), (128, 24),
+                                 (128, 126), (256, 256), (256, 64), (256, 144), (256, 250)])
+@pytest.mark.parametrize("dtype", [DTYPE_FP16, DTYPE_BF16])
+def test_append_channels(d, r, interleaved, dtype):
+    run_append(37, 6, 3, d, dtype, 16, "htd", r, interleaved, seed=d + r)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("tokens", [1, 2, 3, 7, 16, 33, 64, 129, 500, 1023, 2048, 4099])
+@pytest.mark.parametrize("hq,hkv,d,layout,fused", [(8, 8, 128, "htd", False), (32, 8, 128, "thd", True), (28, 4, 64, "htd", True), (16, 1, 256, "thd", False),
+                                                   (1, 1, 64, "thd", True)])
+def test_append_sizes(tokens, hq, hkv, d, layout, fused):
+    run_append(tokens, hq, hkv, d, DTYPE_BF16, 32, layout, d, fused=fused, seed=tokens)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("scaling", SCALINGS)
+@pytest.mark.parametrize("positions", [[0, 1, -1], [131071, 1 << 20, (1 << 31) + 5], [-(1 << 33) - 7, 12345678901, 3]])
+def test_append_positions(scaling, positions):
+    """Near and far positions: the angle keeps its fraction of a turn."""
+    for r, interleaved in ((128, False), (128, True), (36, False)):
+        run_append(3, 4, 2, 128, DTYPE_FP16, 16, "htd", r, interleaved, scaling=scaling, positions=positions, theta=500000.0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("variant", [dict(in_place=True), dict(in_place=True, fused=True), dict(queries=False), dict(rotate=False),
+                                     dict(rotate=False, queries=False), dict(slots=[-1] * 21), dict(fused=True, rotate=False)])
+def test_append_variants(variant):
+    run_append(21, 10, 2, 128, DTYPE_BF16, 16, "thd", 96, **variant)
+
+
+@pytest.mark.gpu
+def test_append_slots_out_of_range_are_not_stored():
+    last = 6 * 16
+    run_append(9, 4, 2, 64, DTYPE_FP16, 16, "htd", 64, slots=[last, last - 1, -1, 0, last + 5, 1 << 40, -(1 << 62), (1 << 63) - 1, 17], spare=5)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["side by side", "padded tokens", "pages last"])
+def test_append_pools_with_other_strides(kind):
+    pages, page, hkv, d = 7, 16, 3, 64
+    gen = torch.Generator().manual_seed(5)
+    if kind == "side by side":                          # K and V of a page and head in one pool
+        big = rows(gen, DTYPE_BF16, pages, hkv, 2, page, d).to(DEV)
+        pool = (big[:, :, 0], big[:, :, 1])
+    elif kind == "padded tokens":
+        pool = tuple(rows(gen, DTYPE_BF16, pages, hkv, page, d + 24).to(DEV)[..., 8:8 + d] for _ in "kv")
+    else:                                               # all pages of a head together
+        pool = tuple(rows(gen, DTYPE_BF16, hkv, pages, page, d).to(DEV).transpose(0, 1) for _ in "kv")
+    run_append(20, 6, hkv, d, DTYPE_BF16, page, "htd", 64, pool=pool, spare=5)
+
+
+@pytest.mark.gpu
+def test_append_values_that_are_not_numbers():
+    """Infinities and NaN stay in their pairs; channels that pass keep their bits."""
+    for r, interleaved in ((32, False), (32, True), (20, False), (22, True)):
+        x = torch.randn(5, 4, 64, generator=torch.Generator().manual_seed(1)).half()
+        x[0, 0, 3], x[1, 1, 40], x[2, 2, 63], x[3, 3, r], x[4, 0, r - 1] = math.inf, math.nan, -math.inf, math.nan, math.nan
+        rot = C.Rotary(r, interleaved=interleaved, device=DEV)
+        positions = np.array([5, 0, 9, 100, 7])
+        got = rot.apply(x.to(DEV), torch.from_numpy(positions).to(DEV))
+        want, size = O.rotary(x.double().numpy(), positions, rot.turns.cpu().numpy(), 1.0, interleaved)
+        size[~np.isfinite(size)] = 0.0
+        close(got, want, size, DTYPE_FP16)
+        assert torch.equal(got[..., r:].cpu().view(torch.int16), x[..., r:].contiguous().view(torch.int16))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("tokens,heads,d,r", [(1, 1, 64, 64), (5, 3, 128, 128), (100, 16, 256, 64), (3001, 32, 128, 128), (64, 7, 64, 30)])
+def test_rotary_back(tokens, heads, d, r, interleaved):
+    """The inverse is the transpose: the gradient of the turn.  In place and not, from a strided view too."""
+    print(f"[case] rotary back {tokens} {heads} {d} {r} {interleaved}", flush=True)
+    gen = torch.Generator().manual_seed(tokens)
+    rng = np.random.default_rng(3)
+    scaling = dict(kind="yarn", factor=4.0, original_length=4096)
+    g = rows(gen, DTYPE_BF16, tokens, heads + 2, d)
+    positions = rng.integers(0, 1 << 17, tokens)
+    rot = C.Rotary(r, interleaved=interleaved, scaling=scaling, device=DEV)
+    at = torch.from_numpy(positions).to(DEV)
+    turns, magnitude = rot.turns.cpu().numpy(), rot.magnitude
+    want, size = O.rotary(g[:, 1:-1].double().numpy(), positions, turns, magnitude, interleaved, inverse=True)
+    big = g.to(DEV)
+    got = rot.apply(big[:, 1:-1], at, inverse=True)
+    close(got, want, size, DTYPE_BF16)
+    assert torch.equal(rot.apply(big[:, 1:-1], at, inverse=True, out=big[:, 1:-1]), got)
+    assert torch.equal(big[:, 1:-1], got) and torch.equal(big[:, 0].cpu(), g[:, 0]) and torch.equal(big[:, -1].cpu(), g[:, -1])
+    # against differences: the turn is linear, so a step of any size gives the derivative along it
+    x, dx = (rng.standard_normal((1, 1, d)) for _ in range(2))
+    ahead, behind = (O.rotary(x + h * dx, positions[:1], turns, magnitude, interleaved)[0] for h in (0.5, -0.5))
+    w = g[:1, 1:2].double().numpy()
+    assert abs(np.sum(w * (ahead - behind)) - np.sum(dx * want[:1, :1])) <= 1e-9 * d
+
+
+@pytest.mark.gpu
+def test_append_on_another_stream_and_captured():
+    """The call's stream is the one it is given; a captured call replays on what its tensors then hold."""
+    head = HeadConfig(8, 2, 128, DTYPE_BF16)
+    cache = C.KVCache(head, 8, device=DEV)
+    for p in cache.pools[0]:
+        p.zero_()
+    rot = C.Rotary(128, device=DEV)
+    gen = torch.Generator().manual_seed(2)
+    batches = [[rows(gen, DTYPE_BF16, 5, n, 128).to(DEV) for n in (8, 2, 2)] for _ in range(4)]
+    positions = [torch.arange(5, device=DEV) * (i + 1) for i in range(4)]
+    slots = [torch.arange(5, device=DEV) * 3 + 20 * i for i in range(4)]
+    want = [cache.append(0, *b, p, s, rot) for b, p, s in zip(batches, positions, slots)]
+    pools = [p.clone() for p in cache.pools[0]]
+    for p in cache.pools[0]:
+        p.zero_()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    got = cache.append(0, *batches[0], positions[0], slots[0], rot, stream=side)
+    side.synchronize()
+    assert torch.equal(got, want[0])
+    held, at, where = [t.clone() for t in batches[0]], positions[0].clone(), slots[0].clone()
+    out = torch.empty_like(held[0])
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        cache.append(0, *held, at, where, rot, q_out=out)
+    for i in (1, 2, 3, 1, 2):
+        for t, new in zip(held, batches[i]):
+            t.copy_(new)
+        at.copy_(positions[i])
+        where.copy_(slots[i])
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[i])
+    for p, q in zip(cache.pools[0], pools):
+        assert torch.equal(p, q)
+
+
+@pytest.mark.gpu
+def test_append_tensor_refusals():
+    head = HeadConfig(8, 2, 128, DTYPE_BF16)
+    cache = C.KVCache(head, 8, device=DEV)
+    rot = C.Rotary(128, device=DEV)
+    q, k = (torch.zeros(3, n, 128, dtype=torch.bfloat16, device=DEV) for n in (8, 2))
+    i = torch.zeros(3, dtype=torch.int64, device=DEV)
+    for bad in (dict(q=q[:2]), dict(q=q.half()), dict(q=q.cpu()), dict(k=k[:, :1]), dict(v=k[:2]), dict(v=torch.zeros(3, 2, 256, dtype=torch.bfloat16, device=DEV)[..., ::2]),
+                dict(positions=i[:2]), dict(positions=i.int()), dict(slots=i.int()), dict(slots=i.cpu()), dict(q=None, q_out=q), dict(q_out=q[:2]),
+                dict(slots=torch.zeros(6, dtype=torch.int64, device=DEV)[::2])):
+        a = dict(dict(q=q, k=k, v=k.clone(), positions=i, slots=i, rotary=rot, q_out=None), **bad)
+        with pytest.raises(ValueError):
+            cache.append(0, a["q"], a["k"], a["v"], a["positions"], a["slots"], a["rotary"], q_out=a["q_out"])
+    odd = torch.zeros(3, 2, 132, dtype=torch.bfloat16, device=DEV)[..., 4:]                # not 16-byte aligned
+    with pytest.raises(C.CodecError):
+        cache.append(0, q, odd, k, i, i, rot)
+    with pytest.raises(ValueError):                                                        # a table on the CPU
+        cache.append(0, q, k, k.clone(), i, i, C.Rotary(128, device="cpu"))
+    gone = torch.zeros(3, 2, 128, dtype=torch.bfloat16, device=DEV)
+    gone.untyped_storage().resize_(16)
+    with pytest.raises(ValueError):
+        cache.append(0, q, gone, k, i, i, rot)
+    assert cache.append(0, q[:0], k[:0], k[:0], i[:0], i[:0], rot).shape == (0, 8, 128)
+    cache.pools[0][1].untyped_storage().resize_(16)
+    with pytest.raises(ValueError):
+        cache.append(0, q, k, k.clone(), i, i, rot)
