@@ -496,6 +496,85 @@ int codec_append(const codec_head_config *head, const codec_rotary_config *rotar
                  const int64_t *positions, const int64_t *slots, int32_t num_tokens,
                  void *k_pages, void *v_pages, const codec_kv_layout *layout, void *stream);
 
+/*
+ * Pages of a cache: who holds them, branches, moves
+ * -------------------------------------------------
+ *
+ * A codec_pages_t keeps, in host memory, how many page lists hold each page of a pool.  Branches of a
+ * context (parallel samples, beams) share its whole pages and need only what is partly filled of
+ * their own; codec_pages_fork says which tokens that takes, codec_cache_copy moves them, in all layers at
+ * once.  Like a plan, a codec_pages_t is for one thread at a time.  Calls that fail change nothing.
+ */
+typedef struct codec_pages codec_pages_t;       /* opaque, library-owned */
+
+/* Tokens src_token .. src_token + tokens - 1 of page src_page, to be copied to dst_token .. of page dst_page. */
+typedef struct {
+    int32_t src_page;
+    int32_t src_token;
+    int32_t dst_page;
+    int32_t dst_token;
+    int32_t tokens;
+} codec_run;
+
+/* Pages 0 .. num_pages - 1 (>= 1), all free. */
+int codec_pages_create(int32_t num_pages, codec_pages_t **out);
+
+/* NULL is accepted. */
+int codec_pages_destroy(codec_pages_t *pages);
+
+/* Number of free pages; a negative status for NULL. */
+int32_t codec_pages_free(const codec_pages_t *pages);
+
+/* The n lowest free pages, ascending, now with one holder each; CODEC_ERR_NO_PAGES if there are fewer. */
+int codec_pages_take(codec_pages_t *pages, int32_t n, int32_t *ids);
+
+/* One more holder for every entry of ids[n] (free pages get their first one); a page may be listed several times. */
+int codec_pages_hold(codec_pages_t *pages, const int32_t *ids, int32_t n);
+
+/*
+ * One holder less for every entry of ids[n]; pages without holders are free.  CODEC_ERR_INVALID_ARGUMENT
+ * if a page is listed more often than it has holders.
+ */
+int codec_pages_release(codec_pages_t *pages, const int32_t *ids, int32_t n);
+
+/*
+ * Sequence s holds pages page_ids[page_off[s] .. page_off[s+1]), filled in order with tokens[s] tokens.
+ * num_out sequences go on in their place, sequence j from sequence parents[j]: any sequence may go on
+ * once (it keeps its pages), several times (a fork) or not at all (it lets go of its pages), as the
+ * beams of a search do.  Whole pages are shared.  The pages that are not full (the partly filled one
+ * and empty ones behind it) stay with the first that goes on, if the sequence alone holds them; the others
+ * get the lowest free pages in their place, in the order of j, and one run that copies the partly filled page.
+ *   out_off [num_out + 1], out_ids [out_capacity]   the new page lists; the old ones' holders are let go
+ *   runs [num_out], *num_runs                       what to copy (codec_cache_copy) before anything writes to
+ *                                                   the new lists' pages or takes pages again
+ * Errors: CODEC_ERR_INVALID_ARGUMENT for an index out of range, a page that its lists do not hold, fewer
+ * pages than tokens; CODEC_ERR_WORKSPACE_TOO_SMALL if the new lists are longer than out_capacity;
+ * CODEC_ERR_NO_PAGES (pages that this call lets go of do not count as free).
+ */
+int codec_pages_fork(codec_pages_t *pages, int32_t page_size, int32_t num_seq, const int32_t *page_off,
+                     const int32_t *page_ids, const int32_t *tokens, int32_t num_out, const int32_t *parents,
+                     int32_t *out_off, int32_t *out_ids, int32_t out_capacity, codec_run *runs, int32_t *num_runs);
+
+/*
+ * Moves the held pages to the lowest ids: the i-th held page that is not below the number of held pages
+ * goes to the i-th free one that is.  runs [capacity], *num_runs: whole pages to copy, one run a
+ * page; num_pages / 2 always suffice (CODEC_ERR_WORKSPACE_TOO_SMALL otherwise).  The caller copies them
+ * and puts the new ids into its page lists.
+ */
+int codec_pages_compact(codec_pages_t *pages, int32_t page_size, codec_run *runs, int32_t capacity, int32_t *num_runs);
+
+/*
+ * Copies runs of tokens between pages of the K pool and of the V pool of every layer.
+ *   head, layout    as for codec_append (num_q_heads is not used beyond its check)
+ *   k_pages, v_pages   host arrays [num_layers] of device pointers, 16-byte aligned, every pool laid out by `layout`
+ *   runs            host array [num_runs], borrowed for the call only: the list travels in the launches' arguments,
+ *                   so that the call needs no device memory and can be captured
+ * No token may be written twice or be both read and written (CODEC_ERR_INVALID_ARGUMENT), and no two pools may
+ * share memory: the order of the copies is undefined.  Enqueued on `stream` without synchronising.
+ */
+int codec_cache_copy(const codec_head_config *head, const codec_kv_layout *layout, int32_t num_layers,
+                     void *const *k_pages, void *const *v_pages, const codec_run *runs, int32_t num_runs, void *stream);
+
 /* Static, human-readable name of a status code. */
 const char *codec_status_string(int status);
 

@@ -47,3 +47,51 @@ def rotary(x, positions, turns, magnitude, interleaved, inverse=False):
             out[t][:, second] = x[t][:, second] * turn.real + x[t][:, first] * turn.imag
             size[t][:, first] = size[t][:, second] = np.abs(x[t][:, first]) + np.abs(x[t][:, second])
     return out, size
+
+
+class Pages:
+    """Who holds which page: lists of holders, nothing clever."""
+
+    def __init__(self, n):
+        self.holders = [0] * n
+
+    def free(self):
+        return [p for p, h in enumerate(self.holders) if h == 0]
+
+    def take(self, n):
+        ids = self.free()[:n]
+        assert len(ids) == n
+        for p in ids:
+            self.holders[p] = 1
+        return ids
+
+    def fork(self, page_size, lists, tokens, parents):
+        """New lists of the sequences that go on from `parents`, and the runs to copy."""
+        free, out, runs = self.free(), [], []
+        gone_on = set()
+        for s in parents:
+            whole = tokens[s] // page_size
+            mine = list(lists[s])
+            alone = all(self.holders[p] == 1 for p in mine[whole:])
+            if not alone or s in gone_on:
+                for i in range(whole, len(mine)):
+                    page = free.pop(0)
+                    if i == whole and tokens[s] % page_size:
+                        runs.append((mine[i], 0, page, 0, tokens[s] % page_size))
+                    mine[i] = page
+            gone_on.add(s)
+            out.append(mine)
+        for p in (p for pages in out for p in pages):
+            self.holders[p] += 1
+        for p in (p for pages in lists for p in pages):
+            self.holders[p] -= 1
+        assert min(self.holders) >= 0
+        return out, runs
+
+    def compact(self, page_size):
+        n = sum(h != 0 for h in self.holders)
+        high = [p for p, h in enumerate(self.holders) if h and p >= n]
+        low = [p for p in self.free() if p < n]
+        for a, b in zip(high, low):
+            self.holders[b], self.holders[a] = self.holders[a], 0
+        return [(a, 0, b, 0, page_size) for a, b in zip(high, low)]

@@ -45,6 +45,8 @@ EXPORTED_SYMBOLS = [
     "codec_partial_reduction", "codec_status_string", "codec_last_error_message",
     "codec_plan_refresh_lengths", "codec_decode_attention_static", "codec_static_scratch_bytes",
     "codec_stream_read_probe", "codec_rotary_turns", "codec_rotary", "codec_append",
+    "codec_pages_create", "codec_pages_destroy", "codec_pages_free", "codec_pages_take", "codec_pages_hold",
+    "codec_pages_release", "codec_pages_fork", "codec_pages_compact", "codec_cache_copy",
 ]
 
 _i32p = POINTER(c_int32)
@@ -116,6 +118,11 @@ class codec_rows(Structure):
     _fields_ = [("data", c_void_p), ("token_stride", c_int64), ("head_stride", c_int64)]
 
 
+class codec_run(Structure):
+    _fields_ = [("src_page", c_int32), ("src_token", c_int32), ("dst_page", c_int32), ("dst_token", c_int32),
+                ("tokens", c_int32)]
+
+
 # PyTorch wheels carry their own copy of the HIP runtime.  Device pointers and streams handed to the
 # library come from PyTorch, so both must use the same runtime instance: load PyTorch's first, and
 # libcodec.so's dependency on libamdhip64 then resolves to the copy already in the process.
@@ -172,6 +179,26 @@ _lib.codec_rotary.argtypes = [POINTER(codec_rotary_config), c_int32, c_int32, c_
 _lib.codec_append.restype = c_int
 _lib.codec_append.argtypes = [POINTER(codec_head_config), POINTER(codec_rotary_config)] + [POINTER(codec_rows)] * 4 + [
     c_void_p, c_void_p, c_int32, c_void_p, c_void_p, POINTER(codec_kv_layout), c_void_p]
+_lib.codec_pages_create.restype = c_int
+_lib.codec_pages_create.argtypes = [c_int32, POINTER(c_void_p)]
+_lib.codec_pages_destroy.restype = c_int
+_lib.codec_pages_destroy.argtypes = [c_void_p]
+_lib.codec_pages_free.restype = c_int32
+_lib.codec_pages_free.argtypes = [c_void_p]
+_lib.codec_pages_take.restype = c_int
+_lib.codec_pages_take.argtypes = [c_void_p, c_int32, c_void_p]
+_lib.codec_pages_hold.restype = c_int
+_lib.codec_pages_hold.argtypes = [c_void_p, c_void_p, c_int32]
+_lib.codec_pages_release.restype = c_int
+_lib.codec_pages_release.argtypes = [c_void_p, c_void_p, c_int32]
+_lib.codec_pages_fork.restype = c_int
+_lib.codec_pages_fork.argtypes = [c_void_p, c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_int32, c_void_p, c_void_p, c_void_p,
+                                  c_int32, c_void_p, _i32p]
+_lib.codec_pages_compact.restype = c_int
+_lib.codec_pages_compact.argtypes = [c_void_p, c_int32, c_void_p, c_int32, _i32p]
+_lib.codec_cache_copy.restype = c_int
+_lib.codec_cache_copy.argtypes = [POINTER(codec_head_config), POINTER(codec_kv_layout), c_int32, POINTER(c_void_p), POINTER(c_void_p),
+                                  c_void_p, c_int32, c_void_p]
 _lib.codec_status_string.restype = c_char_p
 _lib.codec_status_string.argtypes = [c_int]
 _lib.codec_last_error_message.restype = c_char_p
@@ -370,3 +397,68 @@ def codec_append(head, rotary, q, q_out, k, v, positions_ptr: int, slots_ptr: in
     """``head``: codec_head_config; ``rotary``: codec_rotary_config or None; ``q``, ``q_out``: codec_rows or None; ``k``,
     ``v``: codec_rows; ``layout``: codec_kv_layout."""
     return _lib.codec_append(head, rotary, q, q_out, k, v, positions_ptr, slots_ptr, num_tokens, k_ptr, v_ptr, layout, stream)
+
+
+def codec_pages_create(num_pages: int):
+    """Returns (status, handle or None)."""
+    handle = c_void_p()
+    st = _lib.codec_pages_create(num_pages, byref(handle))
+    return st, (handle if st == CODEC_OK else None)
+
+
+def codec_pages_destroy(pages) -> int:
+    return _lib.codec_pages_destroy(pages)
+
+
+def codec_pages_free(pages) -> int:
+    return int(_lib.codec_pages_free(pages))
+
+
+def codec_pages_take(pages, n: int):
+    """Returns (status, ids or None)."""
+    ids = np.empty(max(0, n), np.int32)
+    st = _lib.codec_pages_take(pages, n, ids.ctypes.data)
+    return st, (ids if st == CODEC_OK else None)
+
+
+def codec_pages_hold(pages, ids) -> int:
+    ids = _i32(ids)
+    return _lib.codec_pages_hold(pages, ids.ctypes.data, ids.size)
+
+
+def codec_pages_release(pages, ids) -> int:
+    ids = _i32(ids)
+    return _lib.codec_pages_release(pages, ids.ctypes.data, ids.size)
+
+
+def codec_pages_fork(pages, page_size: int, page_off, page_ids, tokens, parents):
+    """Returns (status, page_off, page_ids, runs [n, 5]) of the sequences that go on, or (status, None, None, None)."""
+    off, ids, tokens, parents = _i32(page_off), _i32(page_ids), _i32(tokens), _i32(parents)
+    if off.ndim != 1 or off.size != tokens.size + 1 or off[0] != 0 or off[-1] != ids.size:      # the C call reads by these lengths
+        return CODEC_ERR_INVALID_ARGUMENT, None, None, None
+    lens = np.diff(off)
+    within = parents[(parents >= 0) & (parents < tokens.size)]
+    capacity = int(np.maximum(lens, 0)[within].sum(dtype=np.int64))
+    if capacity > 0x7fffffff:
+        return CODEC_ERR_INVALID_ARGUMENT, None, None, None
+    out_off, out_ids = np.empty(parents.size + 1, np.int32), np.empty(capacity, np.int32)
+    runs, n = np.empty((parents.size, 5), np.int32), c_int32(0)
+    st = _lib.codec_pages_fork(pages, page_size, tokens.size, off.ctypes.data, ids.ctypes.data, tokens.ctypes.data, parents.size,
+                               parents.ctypes.data, out_off.ctypes.data, out_ids.ctypes.data, capacity, runs.ctypes.data, byref(n))
+    return (st, out_off, out_ids, runs[:n.value]) if st == CODEC_OK else (st, None, None, None)
+
+
+def codec_pages_compact(pages, page_size: int, capacity: int):
+    """Returns (status, runs [n, 5] or None)."""
+    runs, n = np.empty((max(0, capacity), 5), np.int32), c_int32(0)
+    st = _lib.codec_pages_compact(pages, page_size, runs.ctypes.data, capacity, byref(n))
+    return st, (runs[:n.value] if st == CODEC_OK else None)
+
+
+def codec_cache_copy(head, layout, k_ptrs, v_ptrs, runs, stream: int = 0) -> int:
+    """``head``: codec_head_config; ``layout``: codec_kv_layout; ``k_ptrs``, ``v_ptrs``: the layers' pools; ``runs``: [n, 5]."""
+    runs = _i32(runs)
+    if len(k_ptrs) != len(v_ptrs) or runs.ndim != 2 or runs.shape[1] != 5:
+        return CODEC_ERR_INVALID_ARGUMENT
+    pools = c_void_p * len(k_ptrs)
+    return _lib.codec_cache_copy(head, layout, len(k_ptrs), pools(*k_ptrs), pools(*v_ptrs), runs.ctypes.data, len(runs), stream)

@@ -10,7 +10,7 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libcodec.so")
-SOURCES = ["planner.cpp", "api.cpp", "operators.cpp", "device.hip"]     # device.hip includes every kernel
+SOURCES = ["planner.cpp", "api.cpp", "operators.cpp", "pages.cpp", "device.hip"]     # device.hip includes every kernel
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
          # scalar fp32 code must not be fused into packed-fp32 instructions on this target
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

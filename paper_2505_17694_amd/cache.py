@@ -4,6 +4,7 @@ from __future__ import annotations
 import contextlib
 from types import SimpleNamespace
 
+import numpy as np
 import torch
 
 from . import binding as B
@@ -111,13 +112,16 @@ class Rotary:
 
 
 class KVCache:
-    """The page pools of a cache, one K and one V pool per layer, with the operations that fill them.
+    """The page pools of a cache, one K and one V pool per layer, with the operations that fill them, and who holds which page.
 
     ``head`` is the attribute bag a plan is built from (num_q_heads, num_kv_heads, head_dim, dtype, page_size).  ``layout``
     "thd": pools [num_pages, page_size, num_kv_heads, head_dim]; "htd": [num_pages, num_kv_heads, page_size, head_dim].
     ``pools``: the (k, v) tensors of the layers if the program has them already (views with other strides too, the same
-    in every layer); otherwise they are allocated.
+    in every layer); otherwise they are allocated.  All pages are free at first: page lists that are in use already
+    are made known by ``hold``.
     """
+
+    _pages = None
 
     def __init__(self, head, num_pages, layers=1, layout="htd", device="cuda:0", pools=None):
         if layout not in ("thd", "htd"):
@@ -145,6 +149,15 @@ class KVCache:
         self._head = B.codec_head_config(head.num_q_heads, h, d, head.dtype, ps, 0.0)
         self._reach = (self.num_pages - 1) * page + (ps - 1) * token + (h - 1) * kv_head + d
         self._storages = [tuple(p.untyped_storage() for p in kv) for kv in self.pools]
+        st, self._pages = B.codec_pages_create(self.num_pages)
+        if st != B.CODEC_OK:
+            raise B.CodecError(st, "codec_pages_create")
+
+    def __del__(self):
+        try:
+            B.codec_pages_destroy(self._pages)
+        except Exception:
+            pass
 
     def paged(self, node_page_off, page_ids):
         """These pools with a forest's page lists: the ``paged`` of a PlannedAttention."""
@@ -193,3 +206,77 @@ class KVCache:
         if st != B.CODEC_OK:
             raise B.CodecError(st, "codec_append")
         return q_out
+
+    @property
+    def free_pages(self) -> int:
+        return B.codec_pages_free(self._pages)
+
+    def take(self, n: int) -> np.ndarray:
+        """The n lowest free pages, now held."""
+        st, ids = B.codec_pages_take(self._pages, n)
+        if st != B.CODEC_OK:
+            raise B.CodecError(st, "codec_pages_take")
+        return ids
+
+    def hold(self, page_ids) -> None:
+        """One more holder for every page of the list."""
+        st = B.codec_pages_hold(self._pages, page_ids)
+        if st != B.CODEC_OK:
+            raise B.CodecError(st, "codec_pages_hold")
+
+    def release(self, page_ids) -> None:
+        """One holder less for every page of the list; those without are free."""
+        st = B.codec_pages_release(self._pages, page_ids)
+        if st != B.CODEC_OK:
+            raise B.CodecError(st, "codec_pages_release")
+
+    def copy(self, runs, stream=None) -> None:
+        """Copies runs of tokens, rows (source page, source token, destination page, destination token, tokens), in the
+        pools of every layer.  No token may be written twice, or read and written."""
+        if self.device.type != "cuda":
+            raise ValueError(f"copy needs pools on a GPU, these are on {self.device}")
+        for layer in range(len(self.pools)):
+            self._check_storage(layer)
+        s = _enter(self.device, stream)
+        if s is None:
+            with _on(self.device, stream) as s:
+                return self._copy(runs, s)
+        self._copy(runs, s)
+
+    def _copy(self, runs, s):
+        st = B.codec_cache_copy(self._head, self._layout, [k.data_ptr() for k, _ in self.pools],
+                                [v.data_ptr() for _, v in self.pools], runs, s)
+        if st != B.CODEC_OK:
+            raise B.CodecError(st, "codec_cache_copy")
+
+    def fork(self, page_off, page_ids, tokens, parents, stream=None):
+        """Sequence s holds the pages page_ids[page_off[s]:page_off[s + 1]] with tokens[s] tokens.  In the place of these
+        sequences others go on, sequence j from sequence parents[j]: a sequence may go on once, several times or not at
+        all.  Returns the page lists (page_off, page_ids) of those that go on.  They share whole pages; what is partly
+        filled is copied on `stream` for all but the first (see codec_pages_fork)."""
+        if self.device.type != "cuda":
+            raise ValueError(f"fork needs pools on a GPU, these are on {self.device}")
+        for layer in range(len(self.pools)):
+            self._check_storage(layer)
+        st, off, ids, runs = B.codec_pages_fork(self._pages, self.head.page_size, page_off, page_ids, tokens, parents)
+        if st != B.CODEC_OK:
+            raise B.CodecError(st, "codec_pages_fork")
+        if len(runs):
+            self.copy(runs, stream)
+        return off, ids
+
+    def compact(self, stream=None) -> np.ndarray:
+        """Moves the held pages to the lowest ids, copying them on `stream`.  Returns the new id of every page: page
+        lists go on as ``moved[page_ids]``."""
+        if self.device.type != "cuda":
+            raise ValueError(f"compact needs pools on a GPU, these are on {self.device}")
+        for layer in range(len(self.pools)):
+            self._check_storage(layer)
+        st, runs = B.codec_pages_compact(self._pages, self.head.page_size, self.num_pages // 2)
+        if st != B.CODEC_OK:
+            raise B.CodecError(st, "codec_pages_compact")
+        moved = np.arange(self.num_pages, dtype=np.int32)
+        moved[runs[:, 0]] = runs[:, 2]
+        if len(runs):
+            self.copy(runs, stream)
+        return moved

@@ -1,3 +1,4 @@
 // Every kernel of the library, in one translation unit: the library carries one device image.
 #include "kernels.hip"
+#include "pagecopy.hip"
 #include "rotary.hip"

@@ -3,6 +3,8 @@
 
 #include <algorithm>
 #include <cmath>
+#include <new>
+#include <vector>
 
 #include "status.hpp"
 
@@ -107,6 +109,73 @@ int check_rotary(const codec_rotary_config &r, int32_t head_dim, const int64_t *
     if (r.layout != CODEC_ROTARY_HALF && r.layout != CODEC_ROTARY_INTERLEAVED) return CODEC_ERR_INVALID_ARGUMENT;
     if (!std::isfinite(r.magnitude)) return CODEC_ERR_INVALID_ARGUMENT;
     return CODEC_OK;
+}
+
+// Tokens of the pages that a list of copies writes, as bits: an open-addressing table of pages.
+class WrittenTokens {
+public:
+    WrittenTokens(int32_t runs, int32_t page_size)
+    {
+        while ((page_size >> shift_) > 64) ++shift_;
+        size_t n = 16;
+        while (n < 2 * size_t(runs)) n *= 2;
+        slots_.resize(n);
+    }
+    // Marks tokens [at, at + n) of the page; whether one of them may be marked already.
+    bool mark(int32_t page, int32_t at, int32_t n)
+    {
+        Slot &s = slot(page);
+        s.page = page;
+        const uint64_t b = bits(at, n);
+        const bool met = s.bits & b;
+        s.bits |= b;
+        return met;
+    }
+    // Whether one of these tokens may be marked.
+    bool holds(int32_t page, int32_t at, int32_t n) { return slot(page).bits & bits(at, n); }
+    bool exact() const { return shift_ == 0; }          // a bit is a token
+
+private:
+    struct Slot { int32_t page = -1; uint64_t bits = 0; };
+    Slot &slot(int32_t page)
+    {
+        size_t i = (uint32_t(page) * 2654435769u >> 8) & (slots_.size() - 1);
+        while (slots_[i].page >= 0 && slots_[i].page != page) i = (i + 1) & (slots_.size() - 1);
+        return slots_[i];
+    }
+    uint64_t bits(int32_t at, int32_t n) const
+    {
+        const int first = at >> shift_, last = (at + n - 1) >> shift_;
+        return (~uint64_t(0) >> (63 - last)) & (~uint64_t(0) << first);
+    }
+    int shift_ = 0;
+    std::vector<Slot> slots_;
+};
+
+// Whether a token is written twice or both read and written.
+bool runs_collide(const codec_run *runs, int32_t n, int32_t page_size)
+{
+    WrittenTokens written(n, page_size);
+    bool met = false;
+    for (int32_t i = 0; i < n; ++i) met |= written.mark(runs[i].dst_page, runs[i].dst_token, runs[i].tokens);
+    for (int32_t i = 0; i < n && !met; ++i) met = written.holds(runs[i].src_page, runs[i].src_token, runs[i].tokens);
+    if (!met || written.exact()) return met;
+    // pages of more than 64 tokens share bits: compare the token ranges themselves
+    struct Span { int64_t begin, end; };
+    std::vector<Span> spans(n);
+    for (int32_t i = 0; i < n; ++i) {
+        const int64_t at = int64_t(runs[i].dst_page) * page_size + runs[i].dst_token;
+        spans[i] = {at, at + runs[i].tokens};
+    }
+    std::sort(spans.begin(), spans.end(), [](const Span &a, const Span &b) { return a.begin < b.begin; });
+    for (int32_t i = 1; i < n; ++i)
+        if (spans[i].begin < spans[i - 1].end) return true;
+    for (int32_t i = 0; i < n; ++i) {
+        const int64_t at = int64_t(runs[i].src_page) * page_size + runs[i].src_token, end = at + runs[i].tokens;
+        const auto next = std::lower_bound(spans.begin(), spans.end(), end, [](const Span &a, int64_t e) { return a.begin < e; });
+        if (next != spans.begin() && std::prev(next)->end > at) return true;
+    }
+    return false;
 }
 
 codec::RowsView view_of(const codec_rows &r) { return {static_cast<char *>(r.data), 2 * r.token_stride, 2 * r.head_stride}; }
@@ -229,6 +298,51 @@ int codec_append(const codec_head_config *head, const codec_rotary_config *rotar
     p.num_tokens = num_tokens;
     if (rotary) set_rotary(p, *rotary, positions);
     if (int e = codec::launch_rotary(p, head->dtype, rotary && rotary->layout == CODEC_ROTARY_INTERLEAVED, stream)) return hip_failure("append launch", e);
+    return CODEC_OK;
+}
+
+int codec_cache_copy(const codec_head_config *head, const codec_kv_layout *layout, int32_t num_layers, void *const *k_pages,
+                     void *const *v_pages, const codec_run *runs, int32_t num_runs, void *stream)
+{
+    if (!head || !layout || num_layers < 1 || num_runs < 0) return CODEC_ERR_INVALID_ARGUMENT;
+    if (int st = check_head(*head)) return st;
+    if (pool_span(*head, *layout) < 0) return CODEC_ERR_INVALID_ARGUMENT;
+    if (num_runs == 0) return CODEC_OK;
+    if (!k_pages || !v_pages || !runs) return CODEC_ERR_INVALID_ARGUMENT;
+    for (int32_t l = 0; l < num_layers; ++l)
+        if (!k_pages[l] || !v_pages[l] || !aligned16(k_pages[l]) || !aligned16(v_pages[l]) || k_pages[l] == v_pages[l]) return CODEC_ERR_INVALID_ARGUMENT;
+    const int32_t ps = head->page_size;
+    for (int32_t i = 0; i < num_runs; ++i) {
+        const codec_run &r = runs[i];
+        if (r.src_page < 0 || r.src_page >= layout->num_pages || r.dst_page < 0 || r.dst_page >= layout->num_pages) return CODEC_ERR_INVALID_ARGUMENT;
+        if (r.tokens < 1 || r.tokens > ps || r.src_token < 0 || r.src_token > ps - r.tokens || r.dst_token < 0 || r.dst_token > ps - r.tokens) return CODEC_ERR_INVALID_ARGUMENT;
+    }
+    try {
+        if (runs_collide(runs, num_runs, ps)) return CODEC_ERR_INVALID_ARGUMENT;
+    } catch (const std::bad_alloc &) {
+        return CODEC_ERR_OUT_OF_MEMORY;
+    }
+
+    codec::CopyParams p{};
+    p.page_stride = 2 * layout->page_stride;
+    p.slot_stride = 2 * layout->token_stride;
+    p.head_stride = 2 * layout->head_stride;
+    p.heads = head->num_kv_heads;
+    p.head_bytes = 2 * head->head_dim;
+    for (int64_t first = 0; first < 2 * int64_t(num_layers); first += codec::kCopyPools) {
+        p.num_pools = int32_t(std::min<int64_t>(codec::kCopyPools, 2 * int64_t(num_layers) - first));
+        for (int32_t i = 0; i < p.num_pools; ++i) p.pools[i] = static_cast<char *>(((first + i) & 1 ? v_pages : k_pages)[(first + i) / 2]);
+        for (int32_t at = 0; at < num_runs; at += codec::kCopyRuns) {
+            p.num_runs = std::min(codec::kCopyRuns, num_runs - at);
+            p.most_tokens = 0;
+            for (int32_t i = 0; i < p.num_runs; ++i) {
+                const codec_run &r = runs[at + i];
+                p.runs[i] = {r.src_page, r.dst_page, uint16_t(r.src_token), uint16_t(r.dst_token), uint16_t(r.tokens), 0};
+                p.most_tokens = std::max(p.most_tokens, r.tokens);
+            }
+            if (int e = codec::launch_copy(p, stream)) return hip_failure("page copy launch", e);
+        }
+    }
     return CODEC_OK;
 }
 

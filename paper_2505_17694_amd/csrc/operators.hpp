@@ -26,7 +26,25 @@ struct RotaryParams {
     float magnitude, sign;          // factors on the turned channels and on the sine
 };
 
+// A launch's worth of codec_cache_copy: pools and runs travel in the kernel's arguments, which hold 4 KB.
+constexpr int kCopyPools = 64;
+constexpr int kCopyRuns = 200;
+
+struct CopyRun {
+    int32_t src_page, dst_page;
+    uint16_t src_token, dst_token, tokens, unused;
+};
+
+struct CopyParams {
+    int64_t page_stride, slot_stride, head_stride;      // bytes
+    int32_t heads, head_bytes, num_pools, num_runs, most_tokens;
+    char *pools[kCopyPools];
+    CopyRun runs[kCopyRuns];
+};
+static_assert(sizeof(CopyParams) <= 4096, "kernel arguments");
+
 // All return a hipError_t value (0 = success) without synchronising.
 int launch_rotary(const RotaryParams &p, int dtype, bool interleaved, void *stream);
+int launch_copy(const CopyParams &p, void *stream);
 
 }  // namespace codec

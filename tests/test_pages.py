@@ -1,0 +1,377 @@
+"""Pages of a cache: who holds them, branches, moves (on the CPU), and the copies that belong to them (on the GPU)."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2505_17694_amd as C
+from oracle import operators as O
+from workloads import HeadConfig, DTYPE_BF16, DTYPE_FP16
+
+DEV = "cuda:0"
+TORCH = {DTYPE_FP16: torch.float16, DTYPE_BF16: torch.bfloat16}
+
+
+class Held:
+    """A codec_pages_t beside its model."""
+
+    def __init__(self, n):
+        st, self.h = C.codec_pages_create(n)
+        assert st == C.CODEC_OK
+        self.model = O.Pages(n)
+
+    def same(self):
+        assert C.codec_pages_free(self.h) == len(self.model.free())
+
+    def csr(self, lists):
+        return np.cumsum([0] + [len(x) for x in lists]), [p for x in lists for p in x]
+
+    def __del__(self):
+        C.codec_pages_destroy(self.h)
+
+
+# ---- on the CPU ------------------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("n", [1, 2, 63, 64, 65, 1000])
+def test_take_hold_release(n):
+    x = Held(n)
+    assert C.codec_pages_free(x.h) == n
+    st, ids = C.codec_pages_take(x.h, (n + 1) // 2)
+    assert st == C.CODEC_OK and ids.tolist() == list(range((n + 1) // 2))
+    assert C.codec_pages_take(x.h, n // 2 + 1)[0] == C.CODEC_ERR_NO_PAGES and C.codec_pages_free(x.h) == n // 2
+    assert C.codec_pages_take(x.h, 0)[0] == C.CODEC_OK
+    assert C.codec_pages_hold(x.h, [0, 0, n - 1, n - 1]) == C.CODEC_OK                  # three holders; the last page gets two
+    held = (n + 1) // 2 + (n > 1)
+    assert C.codec_pages_free(x.h) == n - held
+    for bad in ([0] * 6, [-1], [n], [0, n]):
+        assert C.codec_pages_release(x.h, bad) == C.CODEC_ERR_INVALID_ARGUMENT and C.codec_pages_free(x.h) == n - held
+        if bad != [0] * 6:
+            assert C.codec_pages_hold(x.h, bad) == C.CODEC_ERR_INVALID_ARGUMENT and C.codec_pages_free(x.h) == n - held
+    assert C.codec_pages_release(x.h, [0, 0]) == C.CODEC_OK and C.codec_pages_free(x.h) == n - held
+    assert C.codec_pages_release(x.h, [0] if n > 1 else [0, 0, 0]) == C.CODEC_OK
+    assert C.codec_pages_free(x.h) == n - held + 1
+    st, ids = C.codec_pages_take(x.h, 1)                                                # the lowest free one
+    assert st == C.CODEC_OK and ids.tolist() == [0]
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_pages_go_as_in_the_model(seed):
+    """Random forks, new sequences, ends and compactions against a model with lists."""
+    rng = np.random.default_rng(seed)
+    page_size, n = int(rng.choice([1, 4, 16, 64])), int(rng.integers(20, 400))
+    x = Held(n)
+    lists, tokens = [], []
+    for step in range(150):
+        what = rng.integers(0, 4)
+        if what == 0:                                   # a prompt arrives, perhaps with a page to spare
+            t = int(rng.integers(0, 6 * page_size))
+            want = -(-t // page_size) + int(rng.integers(0, 2))
+            st, ids = C.codec_pages_take(x.h, want)
+            if want > len(x.model.free()):
+                assert st == C.CODEC_ERR_NO_PAGES
+                continue
+            assert ids.tolist() == x.model.take(want)
+            lists.append(ids.tolist())
+            tokens.append(t)
+        elif what == 1 and lists:                       # tokens fill what is there
+            for i, pages in enumerate(lists):
+                tokens[i] = int(rng.integers(tokens[i], len(pages) * page_size + 1))
+        elif what == 2 and lists:                       # beams: some go on several times, some not
+            parents = rng.integers(0, len(lists), int(rng.integers(0, 2 * len(lists) + 1)))
+            if rng.random() < 0.3:
+                parents = np.arange(len(lists))         # all go on once
+            free_before = C.codec_pages_free(x.h)
+            st, off, ids, runs = C.codec_pages_fork(x.h, page_size, *x.csr(lists), tokens, parents)
+            if st == C.CODEC_ERR_NO_PAGES:
+                held = list(x.model.holders)
+                with pytest.raises(IndexError):
+                    x.model.fork(page_size, lists, tokens, parents.tolist())
+                x.model.holders = held
+                assert C.codec_pages_free(x.h) == free_before
+                continue
+            assert st == C.CODEC_OK
+            new, copies = x.model.fork(page_size, lists, tokens, parents.tolist())
+            assert [ids[a:b].tolist() for a, b in zip(off, off[1:])] == new
+            assert [tuple(r) for r in runs.tolist()] == copies
+            tokens = [tokens[s] for s in parents]
+            lists = new
+        elif what == 3 and rng.random() < 0.3:
+            st, runs = C.codec_pages_compact(x.h, page_size, n // 2)
+            assert st == C.CODEC_OK and [tuple(r) for r in runs.tolist()] == x.model.compact(page_size)
+            moved = {a: b for a, _, b, _, _ in runs.tolist()}
+            lists = [[moved.get(p, p) for p in pages] for pages in lists]
+            held = n - C.codec_pages_free(x.h)
+            assert all(p < held for pages in lists for p in pages)
+        x.same()
+    for pages in lists:
+        assert C.codec_pages_release(x.h, pages) == C.CODEC_OK
+    assert C.codec_pages_free(x.h) == n
+
+
+def test_fork_shares_whole_pages_and_copies_the_last():
+    x = Held(10)
+    assert C.codec_pages_take(x.h, 5)[0] == C.CODEC_OK
+    # 40 tokens on pages 0 1 2, 16 on page 3, none on page 4
+    st, off, ids, runs = C.codec_pages_fork(x.h, 16, [0, 3, 4, 5], [0, 1, 2, 3, 4], [40, 16, 0], [0, 0, 1, 1, 2, 2, 0])
+    assert st == C.CODEC_OK and off.tolist() == [0, 3, 6, 7, 8, 9, 10, 13]
+    assert ids.tolist() == [0, 1, 2, 0, 1, 5, 3, 3, 4, 6, 0, 1, 7]
+    assert runs.tolist() == [[2, 0, 5, 0, 8], [2, 0, 7, 0, 8]] and C.codec_pages_free(x.h) == 2
+    # a page that others hold too stays as it is: also who goes on alone copies
+    st, off2, ids2, runs = C.codec_pages_fork(x.h, 16, [0, 1], [3], [15], [0])
+    assert st == C.CODEC_OK and ids2.tolist() == [8] and runs.tolist() == [[3, 0, 8, 0, 15]] and C.codec_pages_free(x.h) == 1
+    # nobody goes on
+    st, off, ids, runs = C.codec_pages_fork(x.h, 16, off[:4], ids[:7], [40, 40, 16], [])
+    assert st == C.CODEC_OK and off.tolist() == [0] and len(ids) == len(runs) == 0
+    assert C.codec_pages_free(x.h) == 10 - len({4, 6, 0, 1, 7, 8})
+
+
+def test_pages_refusals():
+    assert C.codec_pages_create(0) == (C.CODEC_ERR_INVALID_ARGUMENT, None) and C.codec_pages_create(-3)[0] == C.CODEC_ERR_INVALID_ARGUMENT
+    assert C.codec_pages_destroy(None) == C.CODEC_OK and C.codec_pages_free(None) == C.CODEC_ERR_INVALID_ARGUMENT
+    assert C.codec_status_string(C.CODEC_ERR_NO_PAGES) == "not enough free pages"
+    x = Held(6)
+    assert C.codec_pages_take(x.h, 4)[0] == C.CODEC_OK and C.codec_pages_take(x.h, -1)[0] == C.CODEC_ERR_INVALID_ARGUMENT
+    good = dict(page_size=16, off=[0, 2, 4], ids=[0, 1, 2, 3], tokens=[20, 32], parents=[0, 0, 1])
+    for bad in (dict(page_size=0), dict(off=[0, 3, 2]), dict(off=[1, 2, 4]), dict(off=[0, 2]), dict(off=[0, 2, 3]), dict(ids=[0, 1, 2, 6]),
+                dict(ids=[0, -1, 2, 3]), dict(ids=[0, 1, 2, 5]), dict(ids=[0, 1, 2, 2]), dict(tokens=[33, 32]), dict(tokens=[20, -1]),
+                dict(tokens=[20, 32, 3]), dict(parents=[0, 2]), dict(parents=[-1])):
+        a = dict(good, **bad)
+        assert C.codec_pages_fork(x.h, a["page_size"], a["off"], a["ids"], a["tokens"], a["parents"])[0] == C.CODEC_ERR_INVALID_ARGUMENT, bad
+        assert C.codec_pages_free(x.h) == 2
+    assert C.codec_pages_fork(x.h, 16, good["off"], good["ids"], good["tokens"], [0] * 4)[0] == C.CODEC_ERR_NO_PAGES
+    assert C.codec_pages_free(x.h) == 2
+    lib = C.binding._lib
+    a = [np.array(v, np.int32) for v in ([0, 2, 4], [0, 1, 2, 3], [20, 32], [0, 0, 1])]
+    out, runs, n = np.zeros(8, np.int32), np.zeros((3, 5), np.int32), ctypes.c_int32(77)
+    p = [v.ctypes.data for v in a]
+
+    def fork(capacity=8, runs_ptr=runs.ctypes.data, ids=p[1], handle=x.h):
+        return lib.codec_pages_fork(handle, 16, 2, p[0], ids, p[2], 3, p[3], out.ctypes.data, out.ctypes.data, capacity, runs_ptr, ctypes.byref(n))
+    assert fork(capacity=5) == C.CODEC_ERR_WORKSPACE_TOO_SMALL and n.value == 77
+    assert fork(runs_ptr=None) == fork(ids=None) == fork(handle=None) == C.CODEC_ERR_INVALID_ARGUMENT
+    assert C.codec_pages_release(x.h, [0, 1]) == C.CODEC_OK
+    assert C.codec_pages_compact(x.h, 16, 1)[0] == C.CODEC_ERR_WORKSPACE_TOO_SMALL
+    assert C.codec_pages_compact(x.h, 0, 3)[0] == C.CODEC_ERR_INVALID_ARGUMENT
+    assert C.codec_pages_compact(x.h, 16, 3)[1].tolist() == [[2, 0, 0, 0, 16], [3, 0, 1, 0, 16]]
+    assert C.codec_pages_compact(x.h, 16, 0)[1].tolist() == []                          # nothing left to move
+
+
+@pytest.mark.parametrize("page_size", [16, 64, 256, 4096])
+def test_copy_refusals(page_size):
+    """Lists that would write a token twice, or read and write it, and everything else that is caught on the host."""
+    head = C.codec_head_config(8, 2, 128, 1, page_size, 0.0)
+    token, kv_head, page = 128, page_size * 128, 2 * page_size * 128
+    lay = C.codec_kv_layout(9, page, token, kv_head)
+    a, b = 1 << 32, 1 << 33
+
+    def status(runs, head=head, lay=lay, k=(a, a * 3), v=(b, b * 3)):
+        return C.codec_cache_copy(head, lay, k, v, np.array(runs, np.int32).reshape(-1, 5))
+    assert status([]) == C.CODEC_OK
+    ps = page_size
+    for bad in ([[9, 0, 0, 0, 1]], [[-1, 0, 0, 0, 1]], [[1, 0, 9, 0, 1]], [[1, 0, -1, 0, 1]], [[1, 0, 2, 0, 0]], [[1, 0, 2, 0, -1]], [[1, 0, 2, 0, ps + 1]],
+                [[1, 1, 2, 0, ps]], [[1, 0, 2, ps, 1]], [[1, -1, 2, 0, 1]], [[1, 0, 2, -1, 1]], [[1, ps - 1, 2, 0, 2]], [[1, 0, 2, (1 << 31) - 1, 1]],
+                [[1, 0, 1, 0, 1]], [[1, 0, 1, ps // 2, ps // 2 + 1]],                                   # onto itself, off the page
+                [[1, 0, 2, 0, ps], [3, 0, 2, ps - 1, 1]], [[1, 0, 2, 3, 4], [3, 0, 2, 6, 1]],          # written twice
+                [[1, 0, 2, 0, ps], [2, 0, 3, 0, 1]], [[2, ps - 1, 3, 0, 1], [1, 0, 2, 0, ps]],         # read and written
+                [[1, 0, 2, 5, 1], [2, 4, 3, 0, 3]], [[1, 0, 1, 1, 2]]):
+        assert status(bad) == C.CODEC_ERR_INVALID_ARGUMENT, bad
+    one = [[1, 0, 2, 0, 1]]
+    for bad in (dict(k=(a,)), dict(k=(), v=()), dict(k=(0, a)), dict(v=(b + 8, b)), dict(k=(b, a)),
+                dict(lay=C.codec_kv_layout(9, page, token, 128)), dict(lay=C.codec_kv_layout(9, page - 8, token, kv_head)),
+                dict(head=C.codec_head_config(8, 0, 128, 1, page_size, 0.0)), dict(head=None), dict(lay=None)):
+        assert status(one, **bad) == C.CODEC_ERR_INVALID_ARGUMENT, bad
+    for bad in (C.codec_head_config(8, 2, 100, 1, page_size, 0.0), C.codec_head_config(8, 2, 128, 3, page_size, 0.0), C.codec_head_config(8, 2, 128, 1, 17, 0.0)):
+        assert status(one, head=bad) == C.CODEC_ERR_UNSUPPORTED
+    assert C.codec_cache_copy(head, lay, (a,), (b,), np.zeros((2, 4), np.int32)) == C.CODEC_ERR_INVALID_ARGUMENT
+
+
+def test_cache_without_a_gpu_refuses():
+    cache = C.KVCache(HeadConfig(8, 2, 128, DTYPE_BF16), 8, device="cpu")
+    assert cache.free_pages == 8 and cache.take(3).tolist() == [0, 1, 2]
+    for call in (lambda: cache.copy([[0, 0, 1, 0, 1]]), lambda: cache.fork([0, 1], [0], [3], [0, 0]), cache.compact):
+        with pytest.raises(ValueError):
+            call()
+    assert cache.free_pages == 5
+    with pytest.raises(C.CodecError):
+        cache.take(6)
+    with pytest.raises(C.CodecError):
+        cache.release([7])
+    cache.hold([7])
+    cache.release([7, 0, 1, 2])
+    assert cache.free_pages == 8
+
+
+# ---- on the GPU ------------------------------------------------------------------------------------------
+
+
+def pools_of(head, pages, layers, layout, seed=3):
+    gen = torch.Generator().manual_seed(seed)
+    ps, h, d = head.page_size, head.num_kv_heads, head.head_dim
+    shape = (pages, ps, h, d) if layout == "thd" else (pages, h, ps, d)
+    return [tuple(torch.randint(-30000, 30000, shape, dtype=torch.int16, generator=gen).view(TORCH[head.dtype]).to(DEV) for _ in "kv") for _ in range(layers)]
+
+
+def copied(pools, runs, layout):
+    """What the pools hold afterwards, on the host."""
+    out = []
+    for kv in pools:
+        for p in kv:
+            old = p.cpu().view(torch.int16)
+            new = old.clone()
+            for a, at, b, to, n in np.asarray(runs).tolist():
+                if layout == "thd":
+                    new[b, to:to + n] = old[a, at:at + n]
+                else:
+                    new[b, :, to:to + n] = old[a, :, at:at + n]
+            out.append(new)
+    return out
+
+
+def same_bits(pools, want):
+    torch.cuda.synchronize()
+    for p, w in zip((p for kv in pools for p in kv), want):
+        assert torch.equal(p.cpu().view(torch.int16), w)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("layout", ["thd", "htd"])
+@pytest.mark.parametrize("hkv,d,page", [(8, 128, 16), (1, 64, 16), (3, 64, 32), (4, 256, 16), (2, 128, 64), (2, 64, 1024)])
+@pytest.mark.parametrize("layers", [1, 3])
+def test_copy_runs(hkv, d, page, layout, layers):
+    """Runs of every length at every place, whole pages, many runs from one source and into one page."""
+    head = HeadConfig(hkv, hkv, d, DTYPE_BF16, page)
+    pages = 24 if page < 1024 else 6
+    rng = np.random.default_rng(page + d)
+    half = pages // 2
+    runs = []
+    for dst in range(half):
+        at = 0
+        while at < page and (dst or at == 0):
+            n = page if dst == 0 else int(rng.integers(1, min(page - at, 1 + page // 3) + 1))
+            runs.append((int(rng.integers(half, pages)), int(rng.integers(0, page - n + 1)), dst, at, n))
+            at += n + int(rng.integers(0, 3))
+    rng.shuffle(runs)
+    print(f"[case] copy {hkv} {d} {page} {layout} layers={layers} runs={len(runs)}", flush=True)
+    pools = pools_of(head, pages, layers, layout)
+    want = copied(pools, runs, layout)
+    C.KVCache(head, pages, layout=layout, device=DEV, pools=pools).copy(np.array(runs))
+    same_bits(pools, want)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,layers", [(1, 1), (199, 2), (200, 1), (201, 33), (1000, 1)])
+def test_copy_lists_longer_than_a_launch(n, layers):
+    """More runs and more pools than one launch's arguments hold."""
+    head = HeadConfig(2, 1, 64, DTYPE_FP16)
+    pools = pools_of(head, 2 * n, layers, "htd")
+    order = np.random.default_rng(n).permutation(2 * n)
+    runs = np.array([(order[i], i % 16, order[n + i], (3 * i) % 16, 1 + min(15 - i % 16, 15 - (3 * i) % 16)) for i in range(n)], np.int32)
+    want = copied(pools, runs, "htd")
+    print(f"[case] long copy {n} {layers}", flush=True)
+    C.KVCache(head, 2 * n, device=DEV, pools=pools).copy(runs)
+    same_bits(pools, want)
+
+
+@pytest.mark.gpu
+def test_copy_in_pools_side_by_side():
+    """K and V of a page and head in one pool: the strides are the view's, the other half keeps its bits."""
+    head = HeadConfig(4, 2, 64, DTYPE_BF16)
+    big = torch.randint(-30000, 30000, (10, 2, 2, 16, 64), dtype=torch.int16).view(torch.bfloat16).to(DEV)
+    pools = [(big[:, :, 0], big[:, :, 1])]
+    runs = [(1, 0, 5, 0, 16), (2, 3, 6, 1, 7)]
+    want = copied(pools, runs, "htd")
+    C.KVCache(head, 10, device=DEV, pools=pools).copy(runs)
+    same_bits(pools, want)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("layout", ["thd", "htd"])
+def test_fork_and_compact_move_what_the_lists_say(layout):
+    """Contents follow their page lists through forks, writes to the branches and a compaction."""
+    head = HeadConfig(4, 2, 64, DTYPE_BF16)
+    rng = np.random.default_rng(11)
+    cache = C.KVCache(head, 60, layers=2, layout=layout, device=DEV)
+    for kv in cache.pools:
+        for p in kv:
+            p.copy_(torch.randint(-30000, 30000, p.shape, dtype=torch.int16).view(torch.bfloat16))
+    cache.take(7)                                       # somebody else's pages
+    tokens = np.array([40, 16, 3, 0], np.int32)
+    off = np.array([0, 3, 4, 5, 5], np.int32)
+    ids = cache.take(5)
+
+    def contents(off, ids, tokens):
+        out = []
+        for s in range(len(tokens)):
+            t = np.arange(tokens[s])
+            pages = torch.from_numpy(ids[off[s]:off[s + 1]][t // 16].astype(np.int64))
+            out.append([p.cpu().view(torch.int16)[pages, t % 16] if layout == "thd" else p.cpu().view(torch.int16)[pages, :, t % 16] for kv in cache.pools for p in kv])
+        return out
+    for step in range(6):
+        before = contents(off, ids, tokens)
+        parents = rng.integers(0, len(tokens), 5)
+        off, ids = cache.fork(off, ids, tokens, parents)
+        tokens = tokens[parents]
+        if step % 2:
+            moved = cache.compact()
+            ids = moved[ids]
+            assert ids.max(initial=0) < 60 - cache.free_pages
+        torch.cuda.synchronize()
+        for got, s in zip(contents(off, ids, tokens), parents):
+            for a, b in zip(got, before[s]):
+                assert torch.equal(a, b)
+        # every branch writes to its own last page; the others do not see it
+        for s in range(len(tokens)):
+            if tokens[s] % 16:
+                other = contents(off, ids, tokens)
+                page, t = int(ids[off[s + 1] - 1]), int(tokens[s]) - 1
+                for kv in cache.pools:
+                    for p in kv:
+                        (p[page, t % 16] if layout == "thd" else p[page, :, t % 16]).fill_(float(step * 10 + s))
+                now = contents(off, ids, tokens)
+                for r in range(len(tokens)):
+                    if r != s:
+                        assert all(torch.equal(a, b) for a, b in zip(now[r], other[r]))
+
+
+@pytest.mark.gpu
+def test_copy_on_another_stream_and_captured():
+    head = HeadConfig(4, 2, 128, DTYPE_BF16)
+    pools = pools_of(head, 12, 2, "htd")
+    cache = C.KVCache(head, 12, device=DEV, pools=pools)
+    side = torch.cuda.Stream()
+    runs = [(1, 0, 5, 0, 16), (2, 3, 6, 1, 7)]
+    want = copied(pools, runs, "htd")
+    cache.copy(runs, stream=side)
+    same_bits(pools, want)
+    graph = torch.cuda.CUDAGraph()
+    more = [(3, 0, 7, 0, 16), (4, 1, 8, 2, 5)]
+    with torch.cuda.graph(graph):
+        cache.copy(more)
+    same_bits(pools, want)                              # recorded, not run
+    for i in range(4):
+        pools[0][0][3].fill_(float(i))
+        want = copied(pools, more, "htd")
+        graph.replay()
+        same_bits(pools, want)
+
+
+@pytest.mark.gpu
+def test_refused_calls_change_nothing():
+    head = HeadConfig(4, 2, 128, DTYPE_BF16)
+    pools = pools_of(head, 4, 1, "htd")
+    cache = C.KVCache(head, 4, device=DEV, pools=pools)
+    want = copied(pools, [], "htd")
+    ids = cache.take(3)
+    with pytest.raises(C.CodecError):
+        cache.copy([(0, 0, 0, 0, 16)])
+    with pytest.raises(C.CodecError):
+        cache.fork([0, 3], ids, [40], [0, 0, 0])        # two pages needed, one free
+    same_bits(pools, want)
+    assert cache.free_pages == 1
+    pools[0][1].untyped_storage().resize_(64)
+    for call in (lambda: cache.copy([(0, 0, 1, 0, 16)]), lambda: cache.fork([0, 3], ids, [40], [0, 0]), cache.compact):
+        with pytest.raises(ValueError):
+            call()
+    assert cache.free_pages == 1
