@@ -44,7 +44,7 @@ enum {
     CODEC_ERR_NO_PAGES = -8             /* fewer free pages than the call needs                */
 };
 
-enum { CODEC_DTYPE_FP16 = 0, CODEC_DTYPE_BF16 = 1 };
+enum { CODEC_DTYPE_FP16 = 0, CODEC_DTYPE_BF16 = 1, CODEC_DTYPE_FP32 = 2 /* logits only */ };
 
 typedef struct codec_plan codec_plan_t;         /* opaque, library-owned, immutable after create */
 
@@ -574,6 +574,63 @@ int codec_pages_compact(codec_pages_t *pages, int32_t page_size, codec_run *runs
  */
 int codec_cache_copy(const codec_head_config *head, const codec_kv_layout *layout, int32_t num_layers,
                      void *const *k_pages, void *const *v_pages, const codec_run *runs, int32_t num_runs, void *stream);
+
+/*
+ * Beam search: which continuations go on, and their states
+ * --------------------------------------------------------
+ */
+
+typedef struct {
+    int32_t batch;              /* searches, >= 0                                               */
+    int32_t beams;              /* beams of a search, 1..64                                     */
+    int32_t vocab;              /* 1..2^24                                                      */
+    int32_t k;                  /* continuations wanted, 1..64, at most beams * vocab           */
+    int32_t dtype;              /* of the logits: CODEC_DTYPE_FP16, _BF16 or _FP32              */
+    int32_t eos;                /* the token finished beams go on with, 0..vocab - 1            */
+} codec_beam_config;
+
+/* Bytes of scratch codec_beam_select needs; 0 for a configuration it refuses. */
+size_t codec_beam_workspace_bytes(const codec_beam_config *config);
+
+/*
+ * The k best continuations of every search over beams and vocabulary.  Continuing beam b with token t
+ * scores scores[b] + logit[b][t] - log sum_u exp(logit[b][u]); a finished beam goes on with `eos` alone,
+ * at its own score (every other token scores -inf, and its logits are not read).
+ *   logits      device: element (search, beam, token) at search * batch_stride + beam * beam_stride + token (elements,
+ *               strides >= 0; no alignment beyond the type's)
+ *   scores      device [batch][beams], 32-bit; -inf for a beam that is not in use
+ *   finished    device [batch][beams], bytes, nonzero = finished; NULL: none is
+ *   out_scores, out_beams, out_tokens   device [batch][k], best first
+ *   workspace   device scratch, >= codec_beam_workspace_bytes, 256-byte aligned; calls that share one must not overlap
+ * Equal scores go by the lowest beam, then the lowest token: in one beam equal logits, between beams scores equal in
+ * 64 bits (32-bit exponentials, their sum in 64).  A logit of -inf is a token that is ruled out; NaN counts
+ * as -inf, +inf as the largest 32-bit number; a score of NaN or +inf counts as -inf.  Candidates that score
+ * -inf come last, lowest beam and token first.  The result does not depend on strides or alignment.
+ * Enqueued on `stream` without synchronising.
+ */
+int codec_beam_select(const codec_beam_config *config, const void *logits, int64_t batch_stride, int64_t beam_stride,
+                      const float *scores, const uint8_t *finished, float *out_scores, int32_t *out_beams,
+                      int32_t *out_tokens, void *workspace, size_t workspace_bytes, void *stream);
+
+/* A state that a beam carries along: row (search, beam) starts search * batch_stride + beam * beam_stride bytes in. */
+typedef struct {
+    const void *src;
+    void       *dst;
+    int64_t     row_bytes;                              /* >= 0                                 */
+    int64_t     src_batch_stride, src_beam_stride;      /* bytes, >= 0                          */
+    int64_t     dst_batch_stride, dst_beam_stride;      /* bytes; rows must not overlap         */
+} codec_state;
+
+/*
+ * The states of the beams that go on: row (s, j) of every dst becomes row (s, beams[s][j]) of its src.
+ *   states      host array [num_states], borrowed for the call only; any types, row sizes and alignments (a
+ *               call moves them in the largest unit that divides them all).  From its first row to its last, no dst
+ *               may overlap a src
+ *   beams       device [batch][beams_out]; a row whose entry is not in 0..beams_in - 1 is left as it was
+ * Enqueued on `stream` without synchronising.
+ */
+int codec_beam_reorder(const codec_state *states, int32_t num_states, const int32_t *beams, int32_t batch,
+                       int32_t beams_in, int32_t beams_out, void *stream);
 
 /* Static, human-readable name of a status code. */
 const char *codec_status_string(int status);

@@ -95,3 +95,29 @@ class Pages:
         for a, b in zip(high, low):
             self.holders[b], self.holders[a] = self.holders[a], 0
         return [(a, 0, b, 0, page_size) for a, b in zip(high, low)]
+
+
+def beam_scores(logits, scores, finished=None, eos=0):
+    """Score of every continuation [batch, beams, vocab], float64."""
+    x = np.array(logits, np.float64)
+    x[np.isnan(x)] = -np.inf
+    x[x == np.inf] = float(np.finfo(np.float32).max)
+    c = np.array(scores, np.float64)
+    c[np.isnan(c) | (c == np.inf)] = -np.inf
+    top = x.max(-1, keepdims=True)
+    with np.errstate(divide="ignore", invalid="ignore"):
+        y = (x - top) - np.log(np.exp(x - top).sum(-1, keepdims=True))
+    y[np.isnan(y)] = -np.inf
+    if finished is not None:
+        done = np.asarray(finished) != 0
+        y[done] = -np.inf
+        y[done, eos] = 0.0
+    return c[..., None] + y
+
+
+def beam_select(logits, scores, k, finished=None, eos=0):
+    """(scores, beams, tokens), each [batch, k]: the best continuations, equal ones by the lowest beam and token."""
+    s = beam_scores(logits, scores, finished, eos)
+    flat = s.reshape(len(s), -1)
+    order = np.argsort(-flat, axis=1, kind="stable")[:, :k]
+    return np.take_along_axis(flat, order, 1), order // s.shape[2], order % s.shape[2]

@@ -27,6 +27,7 @@ CODEC_ERR_OUT_OF_MEMORY = -7
 CODEC_ERR_NO_PAGES = -8
 CODEC_DTYPE_FP16 = 0
 CODEC_DTYPE_BF16 = 1
+CODEC_DTYPE_FP32 = 2
 CODEC_ROTARY_HALF = 0
 CODEC_ROTARY_INTERLEAVED = 1
 CODEC_ROTARY_UNSCALED = 0
@@ -47,6 +48,7 @@ EXPORTED_SYMBOLS = [
     "codec_stream_read_probe", "codec_rotary_turns", "codec_rotary", "codec_append",
     "codec_pages_create", "codec_pages_destroy", "codec_pages_free", "codec_pages_take", "codec_pages_hold",
     "codec_pages_release", "codec_pages_fork", "codec_pages_compact", "codec_cache_copy",
+    "codec_beam_workspace_bytes", "codec_beam_select", "codec_beam_reorder",
 ]
 
 _i32p = POINTER(c_int32)
@@ -121,6 +123,17 @@ class codec_rows(Structure):
 class codec_run(Structure):
     _fields_ = [("src_page", c_int32), ("src_token", c_int32), ("dst_page", c_int32), ("dst_token", c_int32),
                 ("tokens", c_int32)]
+
+
+class codec_beam_config(Structure):
+    _fields_ = [("batch", c_int32), ("beams", c_int32), ("vocab", c_int32), ("k", c_int32), ("dtype", c_int32),
+                ("eos", c_int32)]
+
+
+class codec_state(Structure):
+    _fields_ = [("src", c_void_p), ("dst", c_void_p), ("row_bytes", c_int64),
+                ("src_batch_stride", c_int64), ("src_beam_stride", c_int64),
+                ("dst_batch_stride", c_int64), ("dst_beam_stride", c_int64)]
 
 
 # PyTorch wheels carry their own copy of the HIP runtime.  Device pointers and streams handed to the
@@ -199,6 +212,13 @@ _lib.codec_pages_compact.argtypes = [c_void_p, c_int32, c_void_p, c_int32, _i32p
 _lib.codec_cache_copy.restype = c_int
 _lib.codec_cache_copy.argtypes = [POINTER(codec_head_config), POINTER(codec_kv_layout), c_int32, POINTER(c_void_p), POINTER(c_void_p),
                                   c_void_p, c_int32, c_void_p]
+_lib.codec_beam_workspace_bytes.restype = c_size_t
+_lib.codec_beam_workspace_bytes.argtypes = [POINTER(codec_beam_config)]
+_lib.codec_beam_select.restype = c_int
+_lib.codec_beam_select.argtypes = [POINTER(codec_beam_config), c_void_p, c_int64, c_int64, c_void_p, c_void_p, c_void_p, c_void_p,
+                                   c_void_p, c_void_p, c_size_t, c_void_p]
+_lib.codec_beam_reorder.restype = c_int
+_lib.codec_beam_reorder.argtypes = [POINTER(codec_state), c_int32, c_void_p, c_int32, c_int32, c_int32, c_void_p]
 _lib.codec_status_string.restype = c_char_p
 _lib.codec_status_string.argtypes = [c_int]
 _lib.codec_last_error_message.restype = c_char_p
@@ -462,3 +482,20 @@ def codec_cache_copy(head, layout, k_ptrs, v_ptrs, runs, stream: int = 0) -> int
         return CODEC_ERR_INVALID_ARGUMENT
     pools = c_void_p * len(k_ptrs)
     return _lib.codec_cache_copy(head, layout, len(k_ptrs), pools(*k_ptrs), pools(*v_ptrs), runs.ctypes.data, len(runs), stream)
+
+
+def codec_beam_workspace_bytes(config) -> int:
+    return int(_lib.codec_beam_workspace_bytes(config))
+
+
+def codec_beam_select(config, logits_ptr: int, batch_stride: int, beam_stride: int, scores_ptr: int, finished_ptr: int,
+                      out_scores_ptr: int, out_beams_ptr: int, out_tokens_ptr: int, workspace_ptr: int, workspace_bytes: int,
+                      stream: int = 0) -> int:
+    """``config``: codec_beam_config."""
+    return _lib.codec_beam_select(config, logits_ptr, batch_stride, beam_stride, scores_ptr, finished_ptr, out_scores_ptr,
+                                  out_beams_ptr, out_tokens_ptr, workspace_ptr, workspace_bytes, stream)
+
+
+def codec_beam_reorder(states, beams_ptr: int, batch: int, beams_in: int, beams_out: int, stream: int = 0) -> int:
+    """``states``: a sequence of codec_state."""
+    return _lib.codec_beam_reorder((codec_state * len(states))(*states), len(states), beams_ptr, batch, beams_in, beams_out, stream)

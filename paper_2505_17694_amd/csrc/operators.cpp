@@ -2,6 +2,7 @@
 #include "operators.hpp"
 
 #include <algorithm>
+#include <climits>
 #include <cmath>
 #include <new>
 #include <vector>
@@ -178,6 +179,36 @@ bool runs_collide(const codec_run *runs, int32_t n, int32_t page_size)
     return false;
 }
 
+int check_beams(const codec_beam_config &c)
+{
+    if (c.batch < 0 || c.beams < 1 || c.beams > 64 || c.vocab < 1 || c.vocab > (1 << 24) || c.k < 1 || c.k > 64 ||
+        c.k > int64_t(c.beams) * c.vocab || int64_t(c.batch) * c.beams > INT32_MAX)
+        return CODEC_ERR_INVALID_ARGUMENT;
+    if (c.dtype != CODEC_DTYPE_FP16 && c.dtype != CODEC_DTYPE_BF16 && c.dtype != CODEC_DTYPE_FP32) return CODEC_ERR_UNSUPPORTED;
+    return CODEC_OK;
+}
+
+size_t align_up(size_t n) { return (n + 255) / 256 * 256; }
+
+// Scratch of a selection behind one another: best tokens, sums, largest logits.
+struct BeamScratch { size_t sums, tops, total; };
+BeamScratch beam_scratch(const codec_beam_config &c)
+{
+    const size_t rows = size_t(c.batch) * c.beams, kept = std::min(c.k, c.vocab);
+    BeamScratch s;
+    s.sums = align_up(rows * kept * sizeof(uint64_t));
+    s.tops = s.sums + align_up(rows * sizeof(double));
+    s.total = std::max<size_t>(s.tops + align_up(rows * sizeof(float)), 256);
+    return s;
+}
+
+// Bytes from the first to behind the last of a state's rows; -1 for strides that are out of range.
+int64_t state_span(int64_t row_bytes, int64_t batch, int64_t batch_stride, int64_t beams, int64_t beam_stride)
+{
+    if (row_bytes > kMaxSpan || batch_stride < 0 || beam_stride < 0 || batch_stride > kMaxSpan / batch || beam_stride > kMaxSpan / beams) return -1;
+    return (batch - 1) * batch_stride + (beams - 1) * beam_stride + row_bytes;
+}
+
 codec::RowsView view_of(const codec_rows &r) { return {static_cast<char *>(r.data), 2 * r.token_stride, 2 * r.head_stride}; }
 
 void set_rotary(codec::RotaryParams &p, const codec_rotary_config &r, const int64_t *positions)
@@ -341,6 +372,113 @@ int codec_cache_copy(const codec_head_config *head, const codec_kv_layout *layou
                 p.most_tokens = std::max(p.most_tokens, r.tokens);
             }
             if (int e = codec::launch_copy(p, stream)) return hip_failure("page copy launch", e);
+        }
+    }
+    return CODEC_OK;
+}
+
+size_t codec_beam_workspace_bytes(const codec_beam_config *config)
+{
+    if (!config || check_beams(*config)) return 0;
+    return beam_scratch(*config).total;
+}
+
+int codec_beam_select(const codec_beam_config *config, const void *logits, int64_t batch_stride, int64_t beam_stride, const float *scores,
+                      const uint8_t *finished, float *out_scores, int32_t *out_beams, int32_t *out_tokens, void *workspace,
+                      size_t workspace_bytes, void *stream)
+{
+    if (!config) return CODEC_ERR_INVALID_ARGUMENT;
+    const codec_beam_config &c = *config;
+    if (int st = check_beams(c)) return st;
+    if (c.batch == 0) return CODEC_OK;
+    if (!logits || !scores || !out_scores || !out_beams || !out_tokens || !workspace) return CODEC_ERR_INVALID_ARGUMENT;
+    const int size = c.dtype == CODEC_DTYPE_FP32 ? 4 : 2;
+    if (reinterpret_cast<uintptr_t>(logits) % size || reinterpret_cast<uintptr_t>(workspace) % 256) return CODEC_ERR_INVALID_ARGUMENT;
+    if (batch_stride < 0 || beam_stride < 0 || batch_stride > kMaxSpan / c.batch || beam_stride > kMaxSpan / c.beams) return CODEC_ERR_INVALID_ARGUMENT;
+    if (finished && (c.eos < 0 || c.eos >= c.vocab)) return CODEC_ERR_INVALID_ARGUMENT;
+    const BeamScratch s = beam_scratch(c);
+    if (workspace_bytes < s.total) return CODEC_ERR_WORKSPACE_TOO_SMALL;
+
+    char *ws = static_cast<char *>(workspace);
+    codec::BeamParams p{};
+    p.logits = static_cast<const char *>(logits);
+    p.batch_stride = batch_stride;
+    p.beam_stride = beam_stride;
+    p.scores = scores;
+    p.finished = finished;
+    p.out_scores = out_scores;
+    p.out_beams = out_beams;
+    p.out_tokens = out_tokens;
+    p.best = reinterpret_cast<uint64_t *>(ws);
+    p.sums = reinterpret_cast<double *>(ws + s.sums);
+    p.tops = reinterpret_cast<float *>(ws + s.tops);
+    p.batch = c.batch;
+    p.beams = c.beams;
+    p.vocab = c.vocab;
+    p.k = c.k;
+    p.kept = std::min(c.k, c.vocab);
+    p.eos = c.eos;
+    if (int e = codec::launch_beam_select(p, c.dtype, stream)) return hip_failure("beam selection launch", e);
+    return CODEC_OK;
+}
+
+int codec_beam_reorder(const codec_state *states, int32_t num_states, const int32_t *beams, int32_t batch, int32_t beams_in,
+                       int32_t beams_out, void *stream)
+{
+    if (num_states < 0 || batch < 0 || beams_in < 1 || beams_out < 1 || int64_t(batch) * beams_out > INT32_MAX) return CODEC_ERR_INVALID_ARGUMENT;
+    if (num_states == 0 || batch == 0) return CODEC_OK;
+    if (!states || !beams) return CODEC_ERR_INVALID_ARGUMENT;
+    struct Touched { Range range; bool written; };
+    std::vector<Touched> touched;
+    try {
+        touched.reserve(2 * size_t(num_states));
+    } catch (const std::bad_alloc &) {
+        return CODEC_ERR_OUT_OF_MEMORY;
+    }
+    uint64_t bits = 0;                      // of every address, stride and size: their common factor of two
+    for (int32_t i = 0; i < num_states; ++i) {
+        const codec_state &s = states[i];
+        if (s.row_bytes < 0) return CODEC_ERR_INVALID_ARGUMENT;
+        if (s.row_bytes == 0) continue;
+        if (!s.src || !s.dst) return CODEC_ERR_INVALID_ARGUMENT;
+        const int64_t src_span = state_span(s.row_bytes, batch, s.src_batch_stride, beams_in, s.src_beam_stride);
+        Extent dims[] = {{batch, s.dst_batch_stride}, {beams_out, s.dst_beam_stride}};
+        const int64_t dst_span = state_span(s.row_bytes, batch, s.dst_batch_stride, beams_out, s.dst_beam_stride);
+        if (src_span < 0 || dst_span < 0 || separate_span(s.row_bytes, dims) < 0) return CODEC_ERR_INVALID_ARGUMENT;
+        const char *src = static_cast<const char *>(s.src), *dst = static_cast<const char *>(s.dst);
+        touched.push_back({{src, src + src_span}, false});
+        touched.push_back({{dst, dst + dst_span}, true});
+        bits |= reinterpret_cast<uintptr_t>(src) | reinterpret_cast<uintptr_t>(dst) | uint64_t(s.row_bytes);
+        if (batch > 1) bits |= uint64_t(s.src_batch_stride) | uint64_t(s.dst_batch_stride);
+        if (beams_in > 1) bits |= uint64_t(s.src_beam_stride);
+        if (beams_out > 1) bits |= uint64_t(s.dst_beam_stride);
+    }
+    // a sweep over the ranges by their begin: what is read must end before what is written begins, and the other way round
+    std::sort(touched.begin(), touched.end(), [](const Touched &a, const Touched &b) { return a.range.begin < b.range.begin; });
+    const char *read_end = nullptr, *written_end = nullptr;
+    for (const Touched &t : touched) {
+        if (t.range.begin < (t.written ? read_end : written_end)) return CODEC_ERR_INVALID_ARGUMENT;
+        const char *&end = t.written ? written_end : read_end;
+        end = std::max(end, t.range.end);
+    }
+    const int unit = bits & 1 ? 1 : bits & 2 ? 2 : bits & 4 ? 4 : bits & 8 ? 8 : 16;
+
+    codec::ReorderParams p{};
+    p.beams = beams;
+    p.batch = batch;
+    p.beams_in = beams_in;
+    p.beams_out = beams_out;
+    for (int32_t i = 0; i < num_states; ++i) {
+        const codec_state &s = states[i];
+        if (s.row_bytes) {
+            p.states[p.num_states++] = {static_cast<const char *>(s.src), static_cast<char *>(s.dst), s.src_batch_stride, s.src_beam_stride,
+                                        s.dst_batch_stride, s.dst_beam_stride, s.row_bytes / unit};
+            p.most_units = std::max(p.most_units, s.row_bytes / unit);
+        }
+        if (p.num_states == codec::kReorderStates || (i == num_states - 1 && p.num_states)) {
+            if (int e = codec::launch_reorder(p, unit, stream)) return hip_failure("beam reorder launch", e);
+            p.num_states = 0;
+            p.most_units = 0;
         }
     }
     return CODEC_OK;

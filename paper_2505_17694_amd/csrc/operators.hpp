@@ -43,8 +43,42 @@ struct CopyParams {
 };
 static_assert(sizeof(CopyParams) <= 4096, "kernel arguments");
 
+struct BeamParams {
+    const char *logits;
+    int64_t batch_stride, beam_stride;      // elements
+    const float *scores;
+    const uint8_t *finished;                // or nullptr
+    float *out_scores;
+    int32_t *out_beams, *out_tokens;
+    // Of every beam (search * beams + beam): its best tokens, and its largest logit with the sum of exp(logit - largest)
+    uint64_t *best;
+    double *sums;
+    float *tops;
+    int32_t batch, beams, vocab, k, kept, eos;      // kept = min(k, vocab): tokens a beam can bring
+};
+
+constexpr int kReorderStates = 64;
+
+struct ReorderState {
+    const char *src;
+    char *dst;
+    int64_t src_batch, src_beam, dst_batch, dst_beam;   // bytes
+    int64_t row_units;
+};
+
+struct ReorderParams {
+    const int32_t *beams;
+    int32_t batch, beams_in, beams_out, num_states;
+    int64_t most_units;
+    ReorderState states[kReorderStates];
+};
+static_assert(sizeof(ReorderParams) <= 4096, "kernel arguments");
+
 // All return a hipError_t value (0 = success) without synchronising.
 int launch_rotary(const RotaryParams &p, int dtype, bool interleaved, void *stream);
 int launch_copy(const CopyParams &p, void *stream);
+int launch_beam_select(const BeamParams &p, int dtype, void *stream);
+// `unit`: bytes moved at a time, 1, 2, 4, 8 or 16
+int launch_reorder(const ReorderParams &p, int unit, void *stream);
 
 }  // namespace codec
