@@ -36,15 +36,6 @@ __device__ __forceinline__ float logit_of(uint64_t key)
     return __uint_as_float(b >> 31 ? b ^ 0x80000000u : ~b);
 }
 
-// exp(d) for d <= 0 (or d = -inf).  2^y alone would be off by half a step of y = d log2 e, 3e-7 at d = -10, and equally so for
-// every logit of that value: y's whole part is split off first, its fraction taken with 1 / ln 2 in two pieces.
-__device__ __forceinline__ float exp_below(float d)
-{
-    const float whole = __builtin_rintf(d * 1.44269504f);
-    const float part = __builtin_fmaf(d, 1.92596303e-8f, __builtin_fmaf(d, 1.44269502f, -whole));
-    return d < -200.f ? 0.f : __builtin_ldexpf(__builtin_amdgcn_exp2f(part), int(whole));
-}
-
 // A beam whose logits do not count: finished, or of score -inf (NaN and +inf are taken for that).
 __device__ __forceinline__ bool score_counts(float s) { return s > kMinusInf && s < __builtin_inff(); }
 __device__ __forceinline__ bool reads_logits(const BeamParams &P, int row)
@@ -52,97 +43,343 @@ __device__ __forceinline__ bool reads_logits(const BeamParams &P, int row)
     return score_counts(P.scores[row]) && !(P.finished && P.finished[row]);
 }
 
-template <class T, class Combine>
-__device__ __forceinline__ T block_reduce(T v, T *lds, Combine combine)
+// ---- the 64 best of many, one in a lane ------------------------------------------------------------------
+//
+// A wave keeps a list of keys in decreasing order, the i-th best in lane i, 0 where there is none; keys are distinct.
+
+__device__ __forceinline__ uint64_t lane_value(uint64_t v, int lane)
 {
-    __syncthreads();
-    lds[threadIdx.x] = v;
-    for (int n = blockDim.x / 2; n; n /= 2) {
-        __syncthreads();
-        if (int(threadIdx.x) < n) lds[threadIdx.x] = combine(lds[threadIdx.x], lds[threadIdx.x + n]);
-    }
-    __syncthreads();
-    return lds[0];
+    const uint32_t lo = __builtin_amdgcn_readlane(uint32_t(v), lane), hi = __builtin_amdgcn_readlane(uint32_t(v >> 32), lane);
+    return uint64_t(hi) << 32 | lo;
 }
 
-// A workgroup per beam: largest logit, sum, then one best token after the other.
-template <int DT>
-__global__ __launch_bounds__(256) void beam_rows_kernel(BeamParams P)
+__device__ __forceinline__ uint64_t from_lane_xor(uint64_t v, int n) { return __shfl_xor(v, n); }
+
+// A bitonic list (over runs of 2 * FROM lanes) into decreasing order, or increasing where `up`.
+template <int FROM>
+__device__ __forceinline__ uint64_t bitonic_steps(uint64_t v, int lane, bool up)
 {
-    __shared__ uint64_t keys[256];
-    __shared__ double sums[256];
-    const int row = blockIdx.x;
-    if (!reads_logits(P, row)) return;
-    constexpr int kSize = DT == CODEC_DTYPE_FP32 ? 4 : 2;
-    const char *x = P.logits + (row / P.beams * P.batch_stride + row % P.beams * P.beam_stride) * kSize;
-    uint64_t last = ~uint64_t(0);
-    for (int i = 0; i < P.kept; ++i) {
-        uint64_t best = 0;
-        for (int t = threadIdx.x; t < P.vocab; t += 256) {
-            const uint64_t key = key_of(logit_at<DT>(x, t), t);
-            if (key < last && key > best) best = key;
+#pragma unroll
+    for (int n = FROM; n; n /= 2) {
+        const uint64_t other = from_lane_xor(v, n);
+        const bool first = (lane & n) == 0;             // the lower lane of the two takes the larger key
+        v = (other > v) == (first != up) ? other : v;
+    }
+    return v;
+}
+
+__device__ __forceinline__ uint64_t sort_lanes(uint64_t v, int lane)
+{
+    v = bitonic_steps<1>(v, lane, lane & 2);
+    v = bitonic_steps<2>(v, lane, lane & 4);
+    v = bitonic_steps<4>(v, lane, lane & 8);
+    v = bitonic_steps<8>(v, lane, lane & 16);
+    v = bitonic_steps<16>(v, lane, lane & 32);
+    return bitonic_steps<32>(v, lane, false);
+}
+
+struct BestList {
+    uint64_t key = 0;       // this lane's entry
+    uint64_t least = 0;     // the entry a newcomer has to beat: number `wanted`, 0 while there are fewer
+    int lane, wanted;
+
+    __device__ BestList(int lane_, int wanted_) : lane(lane_), wanted(wanted_) {}
+
+    // One newcomer a lane (0: none).  A few are put in their places one by one; many are sorted and merged: the larger of
+    // entry i of one list and entry 63 - i of the other are the 64 best of both, and bitonic.
+    __device__ void absorb(uint64_t newcomer)
+    {
+        uint64_t hits = __ballot(newcomer > least);
+        if (__popcll(hits) > 10) {
+            const uint64_t sorted = sort_lanes(newcomer > least ? newcomer : 0, lane);
+            const uint64_t other = from_lane_xor(sorted, 63);
+            key = bitonic_steps<32>(other > key ? other : key, lane, false);
+            least = lane_value(key, wanted - 1);
+            return;
         }
-        last = block_reduce(best, keys, [](uint64_t a, uint64_t b) { return a > b ? a : b; });
-        if (threadIdx.x == 0) P.best[int64_t(row) * P.kept + i] = last;
-        if (i == 0) {
-            const float top = logit_of(last);
-            double sum = 0.0;
-            for (int t = threadIdx.x; t < P.vocab && top > kMinusInf; t += 256) sum += double(exp_below(logit_at<DT>(x, t) - top));
-            sum = block_reduce(sum, sums, [](double a, double b) { return a + b; });
-            if (threadIdx.x == 0) {
-                P.sums[row] = sum;
-                P.tops[row] = top;
+        for (; hits; hits &= hits - 1) {
+            const uint64_t k = lane_value(newcomer, __builtin_ctzll(hits));
+            if (k <= least) continue;
+            const int at = __popcll(__ballot(key > k));
+            const uint32_t lo = __builtin_amdgcn_update_dpp(0, uint32_t(key), 0x138 /* wave_shr:1 */, 0xf, 0xf, false);
+            const uint32_t hi = __builtin_amdgcn_update_dpp(0, uint32_t(key >> 32), 0x138, 0xf, 0xf, false);
+            key = lane < at ? key : lane == at ? k : uint64_t(hi) << 32 | lo;
+            least = lane_value(key, wanted - 1);
+        }
+    }
+};
+
+__device__ __forceinline__ float wave_max(float x)
+{
+#pragma unroll
+    for (int n = 1; n < 64; n *= 2) x = fmaxf(x, __shfl_xor(x, n));
+    return x;
+}
+__device__ __forceinline__ double wave_sum(double x)
+{
+#pragma unroll
+    for (int n = 1; n < 64; n *= 2) x += __shfl_xor(x, n);
+    return x;
+}
+
+// ---- the sum of exponentials -----------------------------------------------------------------------------
+//
+// Kept as sum * 2^ref, in 64 bits, with whole references; log2(e) stands for its 32-bit value throughout: what it is off by (1.3e-8 of x - m)
+// weighs on the distance from the largest logit only, because that is brought to the same scale at the end.
+
+constexpr float kLog2e = 1.44269502f;
+constexpr double kNoRef = -1e300;
+
+__device__ __forceinline__ PartialSum joined(PartialSum a, PartialSum b)
+{
+    const double ref = a.ref > b.ref ? a.ref : b.ref;
+    return {ref, (a.sum ? a.sum * exp2(a.ref - ref) : 0.0) + (b.sum ? b.sum * exp2(b.ref - ref) : 0.0)};
+}
+
+constexpr int kPieces = 32;                 // tokens of a lane in a chunk
+constexpr int kChunk = 64 * kPieces;
+
+template <int DT>
+struct Logits {
+    static constexpr int kSize = DT == CODEC_DTYPE_FP32 ? 4 : 2;
+    static constexpr int kPerLoad = 16 / kSize;
+    static constexpr int kLoads = kPieces / kPerLoad;
+    typedef uint32_t __attribute__((ext_vector_type(4))) Vec;
+    struct __attribute__((packed, aligned(kSize))) Unaligned { Vec v; };
+
+    // Tokens of a lane: kPerLoad consecutive ones of each of kLoads consecutive pieces of 64 lanes.
+    __device__ static __forceinline__ int token(int chunk, int lane, int e)
+    {
+        return chunk * kChunk + (e / kPerLoad * 64 + lane) * kPerLoad + e % kPerLoad;
+    }
+    __device__ static __forceinline__ float widen(Vec v, int e)
+    {
+        if constexpr (DT == CODEC_DTYPE_FP32) return __uint_as_float(v[e]);
+        else if constexpr (DT == CODEC_DTYPE_FP16) return float(__builtin_bit_cast(_Float16, uint16_t(e & 1 ? v[e / 2] >> 16 : v[e / 2])));
+        else return __uint_as_float(e & 1 ? v[e / 2] & 0xffff0000u : v[e / 2] << 16);
+    }
+    __device__ static __forceinline__ void load(const char *row, int chunk, int lane, Vec (&raw)[kLoads])
+    {
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j)
+            raw[j] = reinterpret_cast<const Unaligned *>(row + int64_t(token(chunk, lane, j * kPerLoad)) * kSize)->v;
+    }
+    // The row's last chunk: tokens behind the last one are -inf.
+    __device__ static __forceinline__ void load_last(const char *row, int chunk, int lane, int vocab, Vec (&raw)[kLoads])
+    {
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) {
+            const int t = token(chunk, lane, j * kPerLoad);
+            const char *at = row + int64_t(t) * kSize;
+            if (t + kPerLoad <= vocab) {
+                raw[j] = reinterpret_cast<const Unaligned *>(at)->v;
+                continue;
+            }
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                if constexpr (kSize == 4) {
+                    raw[j][w] = t + w < vocab ? reinterpret_cast<const uint32_t *>(at)[w] : 0xff800000u;
+                } else {
+                    constexpr uint32_t kInf = DT == CODEC_DTYPE_FP16 ? 0xfc00u : 0xff80u;
+                    const uint16_t *p = reinterpret_cast<const uint16_t *>(at);
+                    const uint32_t lo = t + 2 * w < vocab ? p[2 * w] : kInf, hi = t + 2 * w + 1 < vocab ? p[2 * w + 1] : kInf;
+                    raw[j][w] = hi << 16 | lo;
+                }
             }
         }
     }
-}
+};
 
-struct Candidate { double score; int32_t beam, token; };
+constexpr int kRowWaves = 8;                // most waves of a workgroup that share a beam's tokens
 
-__device__ __forceinline__ bool before(const Candidate &a, const Candidate &b)
+// The best tokens and the sum of a beam's part of the vocabulary.  A wave goes over its chunks once, 32 tokens of a chunk in
+// a lane: the largest of them, the sum of 2^(x log2 e - ref), and, where the largest beats the wave's list, the tokens
+// that do.  Every chunk's tokens follow those of the wave's chunks before it, so that an equal logit does not beat the list.
+// Bound by the loads: an element takes eight lane operations (four of them the exponential).
+template <int DT>
+__global__ __launch_bounds__(kRowWaves * 64) void beam_rows_kernel(BeamParams P)
 {
-    return a.score != b.score ? a.score > b.score : a.beam != b.beam ? a.beam < b.beam : a.token < b.token;
-}
+    typedef Logits<DT> L;
+    __shared__ uint64_t lists[kRowWaves * 64];
+    __shared__ PartialSum sums[kRowWaves];
+    const int row = blockIdx.x, part = blockIdx.y;
+    if (!reads_logits(P, row)) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+    const char *x = P.logits + (row / P.beams * P.batch_stride + row % P.beams * P.beam_stride) * L::kSize;
+    const int chunks = (P.vocab + kChunk - 1) / kChunk, whole = P.vocab / kChunk;
+    const int64_t share = part * waves + wave, shares = int64_t(gridDim.y) * waves;
+    const int first = int(share * chunks / shares), end = int((share + 1) * chunks / shares);
 
-// The i-th best continuation of a beam, i < kept.
-__device__ __forceinline__ Candidate candidate(const BeamParams &P, int search, int beam, int i)
-{
-    const int row = search * P.beams + beam;
-    const double ruled_out = -__builtin_inf();
-    const float score = P.scores[row];
-    if (!score_counts(score)) return {ruled_out, beam, i};
-    if (P.finished && P.finished[row]) {
-        if (i == 0) return {double(score), beam, P.eos};
-        return {ruled_out, beam, i - 1 < P.eos ? i - 1 : i};
+    BestList best(lane, P.kept);
+    double ref = kNoRef, sum = 0.0;
+    auto load = [&](int chunk, typename L::Vec (&raw)[L::kLoads]) {
+        if (chunk < whole) L::load(x, chunk, lane, raw);
+        else L::load_last(x, chunk, lane, P.vocab, raw);
+    };
+    typename L::Vec raw[L::kLoads];
+    if (first < end) load(first, raw);
+    for (int chunk = first; chunk < end; ++chunk) {
+        float v[kPieces];
+#pragma unroll
+        for (int e = 0; e < kPieces; ++e) v[e] = L::widen(raw[e / L::kPerLoad], e % L::kPerLoad);
+        if (chunk + 1 < end) load(chunk + 1, raw);
+
+        auto largest = [&] {
+            float m[4] = {v[0], v[1], v[2], v[3]};
+#pragma unroll
+            for (int e = 4; e < kPieces; ++e) m[e % 4] = fmaxf(m[e % 4], v[e]);
+            return fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
+        };
+        auto total = [&](auto term) {
+            float t[4] = {term(v[0]), term(v[1]), term(v[2]), term(v[3])};
+#pragma unroll
+            for (int e = 4; e < kPieces; ++e) t[e % 4] += term(v[e]);
+            return (t[0] + t[1]) + (t[2] + t[3]);
+        };
+        auto refer_to = [&](double r) {
+            sum = sum ? sum * exp2(ref - r) : 0.0;
+            ref = r;
+        };
+        float mine = largest();
+        float top = wave_max(mine);
+        float chunk_sum = 0.f;
+        bool plain = __builtin_fabsf(top) < 0x1p20f;
+        if (plain) {
+            // a reference stays while nothing outgrows it by more than 2^60
+            if (double(top * kLog2e) > ref + 60.0 || ref == kNoRef) refer_to(__builtin_ceilf(top * kLog2e));
+            const float r = float(ref);
+            chunk_sum = total([r](float a) { return __builtin_amdgcn_exp2f(__builtin_fmaf(a, kLog2e, -r)); });
+            plain = __all(chunk_sum < 3e38f);           // false for NaN, too
+        }
+        if (!plain) {
+            // +inf, NaN, no token at all, or logits whose size leaves the reference no fraction: differences instead
+#pragma unroll
+            for (int e = 0; e < kPieces; ++e) v[e] = v[e] != v[e] ? kMinusInf : fminf(v[e], 3.402823466e38f);
+            mine = largest();
+            top = wave_max(mine);
+            chunk_sum = 0.f;
+            if (top > kMinusInf) {
+                const double at = double(top) * double(kLog2e);
+                if (at > ref) refer_to(__builtin_ceil(at));
+                chunk_sum = total([top](float a) { return __builtin_amdgcn_exp2f((a - top) * kLog2e); });
+                sum += double(chunk_sum) * exp2(at - ref);
+            }
+        } else {
+            sum += double(chunk_sum);
+        }
+
+        // which of them beat the list; before there is one, those that reach the `kept`-th largest of the lanes' largest
+        const bool filling = best.least == 0;
+        float bar;
+        if (filling) {
+            const uint64_t order = sort_lanes(key_of(mine, lane), lane);
+            bar = logit_of(lane_value(order, P.kept - 1));
+        } else {
+            bar = logit_of(best.least);
+            if (!__any(mine > bar)) continue;
+        }
+        uint32_t reach = 0;
+#pragma unroll
+        for (int e = 0; e < kPieces; ++e) reach |= (filling ? v[e] >= bar : v[e] > bar) ? 1u << e : 0u;
+        if (chunk >= whole) {
+#pragma unroll
+            for (int e = 0; e < kPieces; ++e) reach &= L::token(chunk, lane, e) < P.vocab ? ~0u : ~(1u << e);
+        }
+        while (__any(reach != 0)) {
+            uint64_t key = 0;
+            if (reach) {
+                const int t = L::token(chunk, lane, __builtin_ctz(reach));
+                reach &= reach - 1;
+                key = key_of(logit_at<DT>(x, t), t);
+            }
+            best.absorb(key);
+        }
     }
-    const uint64_t key = P.best[int64_t(row) * P.kept + i];
-    const float x = logit_of(key);
-    const int32_t token = int32_t(token_of(key));
-    if (x == kMinusInf) return {ruled_out, beam, token};
-    return {double(score) + ((double(x) - double(P.tops[row])) - log(P.sums[row])), beam, token};
+
+    const PartialSum mine{ref, wave_sum(sum)};
+    PartialSum *out_sum = P.sums + (int64_t(row) * P.parts + part);
+    uint64_t *out_best = P.best + (int64_t(row) * P.parts + part) * P.kept;
+    if (waves > 1) {
+        lists[threadIdx.x] = best.key;
+        if (lane == 0) sums[wave] = mine;
+        __syncthreads();
+        if (wave) return;
+        // the waves' lists, 64 entries at a time
+        const int others = (waves - 1) * P.kept;
+        for (int i = lane; i - lane < others; i += 64) best.absorb(i < others ? lists[64 + i / P.kept * 64 + i % P.kept] : 0);
+        PartialSum all = mine;
+        for (int w = 1; w < waves; ++w) all = joined(all, sums[w]);
+        if (lane == 0) *out_sum = all;
+    } else if (lane == 0) {
+        *out_sum = mine;
+    }
+    if (lane < P.kept) out_best[lane] = best.key;
 }
 
-// A wave per search: k times the best of what is left.
-__global__ __launch_bounds__(64) void beam_merge_kernel(BeamParams P)
+// Order of (score, beam, place in the beam's list) as an integer: the higher score, then the lower beam and place, is the
+// larger key.  The score keeps 52 of its 64 bits, 2^-40 of itself: what is nearer counts as equal.
+__device__ __forceinline__ uint64_t score_key(double score, int place)
 {
+    const uint64_t b = __builtin_bit_cast(uint64_t, score + 0.0);
+    return ((b ^ (b >> 63 ? ~uint64_t(0) : uint64_t(1) << 63)) & ~uint64_t(0xfff)) | uint64_t(0xfff - place);
+}
+
+constexpr int kMergeBeams = 8;              // most waves of a workgroup, a beam at a time each
+
+// A workgroup per search: every beam's parts are joined by a wave, which scores the beam's best tokens; then one wave
+// finds the best of all.
+__global__ __launch_bounds__(kMergeBeams * 64) void beam_merge_kernel(BeamParams P)
+{
+    extern __shared__ uint64_t keys[];      // per beam and place: the score's key, the score, the token; 64 KB at most
+    float *scores = reinterpret_cast<float *>(keys + P.beams * P.kept);
+    int32_t *tokens = reinterpret_cast<int32_t *>(scores + P.beams * P.kept);
     const int search = blockIdx.x;
-    Candidate last{__builtin_inf(), -1, -1};
-    for (int i = 0; i < P.k; ++i) {
-        Candidate best{-__builtin_inf(), 1 << 30, 0};
-        for (int at = threadIdx.x; at < P.beams * P.kept; at += 64) {
-            const Candidate c = candidate(P, search, at / P.kept, at % P.kept);
-            if (before(last, c) && before(c, best)) best = c;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+    for (int beam = wave; beam < P.beams; beam += waves) {
+        const int row = search * P.beams + beam;
+        const float before = P.scores[row];
+        double score = -__builtin_inf();
+        int token = lane;
+        if (!score_counts(before)) {
+            // every token of it scores -inf
+        } else if (P.finished && P.finished[row]) {
+            if (lane == 0) score = before;
+            token = lane == 0 ? P.eos : lane - 1 < P.eos ? lane - 1 : lane;
+        } else {
+            BestList best(lane, P.kept);
+            const uint64_t *from = P.best + int64_t(row) * P.parts * P.kept;
+            const int entries = P.parts * P.kept;
+            if (P.parts == 1) best.key = lane < P.kept ? from[lane] : 0;
+            else
+                for (int i = lane; i - lane < entries; i += 64) best.absorb(i < entries ? from[i] : 0);
+            PartialSum all{kNoRef, 0.0};
+            for (int i = lane; i < P.parts; i += 64) all = joined(all, P.sums[int64_t(row) * P.parts + i]);
+            for (int n = 1; n < 64 && n < P.parts; n *= 2) all = joined(all, {__shfl_xor(all.ref, n), __shfl_xor(all.sum, n)});
+            all = {__shfl(all.ref, 0), __shfl(all.sum, 0)};
+            const float top = logit_of(lane_value(best.key, 0)), x = logit_of(best.key);
+            // log of the sum of exp(x - top)
+            const double log_sum = log(all.sum) + (all.ref - double(top) * double(kLog2e)) * 0.6931471805599453;
+            if (x > kMinusInf) score = double(before) + ((double(x) - double(top)) - log_sum);
+            token = int(token_of(best.key));
         }
-        for (int n = 32; n; n /= 2) {
-            const Candidate c{__shfl_xor(best.score, n), __shfl_xor(best.beam, n), __shfl_xor(best.token, n)};
-            if (before(c, best)) best = c;
+        if (lane < P.kept) {
+            const int at = beam * P.kept + lane;
+            scores[at] = float(score);
+            keys[at] = score_key(score, beam * 64 + lane);
+            tokens[at] = token;
         }
-        last = best;
-        if (threadIdx.x == 0) {
-            P.out_scores[int64_t(search) * P.k + i] = float(best.score);
-            P.out_beams[int64_t(search) * P.k + i] = best.beam;
-            P.out_tokens[int64_t(search) * P.k + i] = best.token;
-        }
+    }
+    __syncthreads();
+    if (wave) return;
+    BestList best(lane, P.k);
+    const int entries = P.beams * P.kept;
+    for (int i = lane; i - lane < entries; i += 64) best.absorb(i < entries ? keys[i] : 0);
+    if (lane < P.k) {
+        const int place = 0xfff - int(best.key & 0xfff), beam = place / 64, at = beam * P.kept + place % 64;
+        const int64_t to = int64_t(search) * P.k + lane;
+        P.out_scores[to] = scores[at];
+        P.out_beams[to] = beam;
+        P.out_tokens[to] = tokens[at];
     }
 }
 
@@ -162,17 +399,31 @@ __global__ __launch_bounds__(256) void reorder_kernel(ReorderParams P)
 
 }  // namespace
 
+// Waves that share a beam: enough for 16 on every CU, each with a chunk at least.
+BeamSplit beam_split(int64_t rows, int vocab)
+{
+    const int64_t chunks = (int64_t(vocab) + kChunk - 1) / kChunk;
+    int64_t waves = (4096 + rows - 1) / rows;
+    if (waves > chunks) waves = chunks;
+    const int64_t parts = (waves + kRowWaves - 1) / kRowWaves;
+    return {int((waves + parts - 1) / parts), int(parts)};
+}
+
 int launch_beam_select(const BeamParams &p, int dtype, void *stream)
 {
     hipStream_t s = static_cast<hipStream_t>(stream);
-    const dim3 rows(unsigned(p.batch) * unsigned(p.beams));
+    const int64_t rows = int64_t(p.batch) * p.beams;
+    const BeamSplit split = beam_split(rows, p.vocab);
+    if (split.parts != p.parts) return int(hipErrorInvalidValue);
+    const dim3 grid(unsigned(rows), unsigned(split.parts)), block(unsigned(split.waves) * 64);
     switch (dtype) {
-    case CODEC_DTYPE_FP16: hipLaunchKernelGGL(beam_rows_kernel<CODEC_DTYPE_FP16>, rows, dim3(256), 0, s, p); break;
-    case CODEC_DTYPE_BF16: hipLaunchKernelGGL(beam_rows_kernel<CODEC_DTYPE_BF16>, rows, dim3(256), 0, s, p); break;
-    default: hipLaunchKernelGGL(beam_rows_kernel<CODEC_DTYPE_FP32>, rows, dim3(256), 0, s, p); break;
+    case CODEC_DTYPE_FP16: hipLaunchKernelGGL(beam_rows_kernel<CODEC_DTYPE_FP16>, grid, block, 0, s, p); break;
+    case CODEC_DTYPE_BF16: hipLaunchKernelGGL(beam_rows_kernel<CODEC_DTYPE_BF16>, grid, block, 0, s, p); break;
+    default: hipLaunchKernelGGL(beam_rows_kernel<CODEC_DTYPE_FP32>, grid, block, 0, s, p); break;
     }
     if (hipError_t e = hipGetLastError()) return int(e);
-    hipLaunchKernelGGL(beam_merge_kernel, dim3(unsigned(p.batch)), dim3(64), 0, s, p);
+    const unsigned waves = unsigned(p.beams < kMergeBeams ? p.beams : kMergeBeams);
+    hipLaunchKernelGGL(beam_merge_kernel, dim3(unsigned(p.batch)), dim3(waves * 64), size_t(16) * p.beams * p.kept, s, p);
     return int(hipGetLastError());
 }
 

@@ -190,15 +190,16 @@ int check_beams(const codec_beam_config &c)
 
 size_t align_up(size_t n) { return (n + 255) / 256 * 256; }
 
-// Scratch of a selection behind one another: best tokens, sums, largest logits.
-struct BeamScratch { size_t sums, tops, total; };
+// Scratch of a selection: best tokens, then sums.
+struct BeamScratch { int parts; size_t sums, total; };
 BeamScratch beam_scratch(const codec_beam_config &c)
 {
-    const size_t rows = size_t(c.batch) * c.beams, kept = std::min(c.k, c.vocab);
-    BeamScratch s;
-    s.sums = align_up(rows * kept * sizeof(uint64_t));
-    s.tops = s.sums + align_up(rows * sizeof(double));
-    s.total = std::max<size_t>(s.tops + align_up(rows * sizeof(float)), 256);
+    BeamScratch s{};
+    if (c.batch == 0) return s;
+    s.parts = codec::beam_split(int64_t(c.batch) * c.beams, c.vocab).parts;
+    const size_t lists = size_t(c.batch) * c.beams * s.parts;
+    s.sums = align_up(lists * std::min(c.k, c.vocab) * sizeof(uint64_t));
+    s.total = s.sums + align_up(lists * sizeof(codec::PartialSum));
     return s;
 }
 
@@ -380,7 +381,7 @@ int codec_cache_copy(const codec_head_config *head, const codec_kv_layout *layou
 size_t codec_beam_workspace_bytes(const codec_beam_config *config)
 {
     if (!config || check_beams(*config)) return 0;
-    return beam_scratch(*config).total;
+    return std::max<size_t>(beam_scratch(*config).total, 256);
 }
 
 int codec_beam_select(const codec_beam_config *config, const void *logits, int64_t batch_stride, int64_t beam_stride, const float *scores,
@@ -410,8 +411,8 @@ int codec_beam_select(const codec_beam_config *config, const void *logits, int64
     p.out_beams = out_beams;
     p.out_tokens = out_tokens;
     p.best = reinterpret_cast<uint64_t *>(ws);
-    p.sums = reinterpret_cast<double *>(ws + s.sums);
-    p.tops = reinterpret_cast<float *>(ws + s.tops);
+    p.sums = reinterpret_cast<codec::PartialSum *>(ws + s.sums);
+    p.parts = s.parts;
     p.batch = c.batch;
     p.beams = c.beams;
     p.vocab = c.vocab;

@@ -43,6 +43,9 @@ struct CopyParams {
 };
 static_assert(sizeof(CopyParams) <= 4096, "kernel arguments");
 
+// A sum of exponentials: sum * 2^ref
+struct PartialSum { double ref, sum; };
+
 struct BeamParams {
     const char *logits;
     int64_t batch_stride, beam_stride;      // elements
@@ -50,12 +53,15 @@ struct BeamParams {
     const uint8_t *finished;                // or nullptr
     float *out_scores;
     int32_t *out_beams, *out_tokens;
-    // Of every beam (search * beams + beam): its best tokens, and its largest logit with the sum of exp(logit - largest)
+    // Of every part of a beam's vocabulary ([batch * beams][parts]): its best tokens, its sum of exponentials
     uint64_t *best;
-    double *sums;
-    float *tops;
-    int32_t batch, beams, vocab, k, kept, eos;      // kept = min(k, vocab): tokens a beam can bring
+    PartialSum *sums;
+    int32_t batch, beams, vocab, k, kept, eos, parts;   // kept = min(k, vocab): tokens a beam can bring
 };
+
+// How many workgroups share a beam's vocabulary, and how many waves each has.
+struct BeamSplit { int waves, parts; };
+BeamSplit beam_split(int64_t rows, int vocab);
 
 constexpr int kReorderStates = 64;
 
