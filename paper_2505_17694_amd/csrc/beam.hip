@@ -5,6 +5,8 @@
 // of those the search keeps is decided between the beams, on scores in 64 bits.
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "operators.hpp"
 
 namespace codec {
@@ -24,11 +26,12 @@ __device__ __forceinline__ float logit_at(const char *row, int64_t i)
 }
 
 // Order of (logit, token) as an integer: the higher logit, then the lower token, is the larger key.  -0 is 0.
-__device__ __forceinline__ uint64_t key_of(float x, uint32_t token)
+__device__ __forceinline__ uint32_t order_of(float x)
 {
     const uint32_t b = __float_as_uint(x + 0.f);
-    return uint64_t(b ^ (b >> 31 ? 0xffffffffu : 0x80000000u)) << 32 | (0xffffffffu - token);
+    return b ^ (b >> 31 ? 0xffffffffu : 0x80000000u);
 }
+__device__ __forceinline__ uint64_t key_of(float x, uint32_t token) { return uint64_t(order_of(x)) << 32 | (0xffffffffu - token); }
 __device__ __forceinline__ uint32_t token_of(uint64_t key) { return 0xffffffffu - uint32_t(key); }
 __device__ __forceinline__ float logit_of(uint64_t key)
 {
@@ -53,22 +56,45 @@ __device__ __forceinline__ uint64_t lane_value(uint64_t v, int lane)
     return uint64_t(hi) << 32 | lo;
 }
 
-__device__ __forceinline__ uint64_t from_lane_xor(uint64_t v, int n) { return __shfl_xor(v, n); }
-
-// A bitonic list (over runs of 2 * FROM lanes) into decreasing order, or increasing where `up`.
-template <int FROM>
-__device__ __forceinline__ uint64_t bitonic_steps(uint64_t v, int lane, bool up)
+// The value of lane ^ N, without the LDS unit: row operations up to 15, swaps of rows and halves above.
+template <int N>
+__device__ __forceinline__ uint32_t from_lane_xor(uint32_t v)
 {
-#pragma unroll
-    for (int n = FROM; n; n /= 2) {
-        const uint64_t other = from_lane_xor(v, n);
-        const bool first = (lane & n) == 0;             // the lower lane of the two takes the larger key
-        v = (other > v) == (first != up) ? other : v;
+    auto moved = [](uint32_t x, auto control) { return uint32_t(__builtin_amdgcn_update_dpp(0, x, decltype(control)::value, 0xf, 0xf, true)); };
+    if constexpr (N == 1) return moved(v, std::integral_constant<int, 0xb1>{});             // quad_perm 1 0 3 2
+    else if constexpr (N == 2) return moved(v, std::integral_constant<int, 0x4e>{});        // quad_perm 2 3 0 1
+    else if constexpr (N == 4) return moved(moved(v, std::integral_constant<int, 0x141>{}), std::integral_constant<int, 0x1b>{});   // ^ 7 ^ 3
+    else if constexpr (N == 8) return moved(v, std::integral_constant<int, 0x128>{});       // row_ror 8
+    else if constexpr (N == 16) {
+        const auto rows = __builtin_amdgcn_permlane16_swap(v, v, false, false);             // even rows twice, odd rows twice
+        return threadIdx.x & 16 ? rows[0] : rows[1];
+    } else if constexpr (N == 32) {
+        const auto halves = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+        return threadIdx.x & 32 ? halves[0] : halves[1];
+    } else {
+        static_assert(N == 63);
+        return from_lane_xor<32>(from_lane_xor<16>(moved(v, std::integral_constant<int, 0x140>{})));    // row_mirror
     }
-    return v;
+}
+template <int N>
+__device__ __forceinline__ uint64_t from_lane_xor(uint64_t v)
+{
+    return uint64_t(from_lane_xor<N>(uint32_t(v >> 32))) << 32 | from_lane_xor<N>(uint32_t(v));
 }
 
-__device__ __forceinline__ uint64_t sort_lanes(uint64_t v, int lane)
+// A bitonic list (over runs of 2 * N lanes) into decreasing order, or increasing where `up`.
+template <int N, class T>
+__device__ __forceinline__ T bitonic_steps(T v, int lane, bool up)
+{
+    const T other = from_lane_xor<N>(v);
+    const bool first = (lane & N) == 0;                 // the lower lane of the two takes the larger key
+    v = (other > v) == (first != up) ? other : v;
+    if constexpr (N > 1) return bitonic_steps<N / 2>(v, lane, up);
+    else return v;
+}
+
+template <class T>
+__device__ __forceinline__ T sort_lanes(T v, int lane)
 {
     v = bitonic_steps<1>(v, lane, lane & 2);
     v = bitonic_steps<2>(v, lane, lane & 4);
@@ -78,6 +104,14 @@ __device__ __forceinline__ uint64_t sort_lanes(uint64_t v, int lane)
     return bitonic_steps<32>(v, lane, false);
 }
 
+// The 64 best of two decreasing lists: the larger of entry i of one and entry 63 - i of the other, which is bitonic.
+template <class T>
+__device__ __forceinline__ T merge_lanes(T a, T b, int lane)
+{
+    const T other = from_lane_xor<63>(b);
+    return bitonic_steps<32>(other > a ? other : a, lane, false);
+}
+
 struct BestList {
     uint64_t key = 0;       // this lane's entry
     uint64_t least = 0;     // the entry a newcomer has to beat: number `wanted`, 0 while there are fewer
@@ -85,15 +119,12 @@ struct BestList {
 
     __device__ BestList(int lane_, int wanted_) : lane(lane_), wanted(wanted_) {}
 
-    // One newcomer a lane (0: none).  A few are put in their places one by one; many are sorted and merged: the larger of
-    // entry i of one list and entry 63 - i of the other are the 64 best of both, and bitonic.
+    // One newcomer a lane (0: none).  A few are put in their places one by one; many are sorted and merged.
     __device__ void absorb(uint64_t newcomer)
     {
         uint64_t hits = __ballot(newcomer > least);
         if (__popcll(hits) > 10) {
-            const uint64_t sorted = sort_lanes(newcomer > least ? newcomer : 0, lane);
-            const uint64_t other = from_lane_xor(sorted, 63);
-            key = bitonic_steps<32>(other > key ? other : key, lane, false);
+            key = merge_lanes(key, sort_lanes(newcomer > least ? newcomer : uint64_t(0), lane), lane);
             least = lane_value(key, wanted - 1);
             return;
         }
@@ -192,16 +223,19 @@ struct Logits {
 
 constexpr int kRowWaves = 8;                // most waves of a workgroup that share a beam's tokens
 
-// The best tokens and the sum of a beam's part of the vocabulary.  A wave goes over its chunks once, 32 tokens of a chunk in
-// a lane: the largest of them, the sum of 2^(x log2 e - ref), and, where the largest beats the wave's list, the tokens
-// that do.  Every chunk's tokens follow those of the wave's chunks before it, so that an equal logit does not beat the list.
-// Bound by the loads: an element takes eight lane operations (four of them the exponential).
+// The best tokens and the sum of a beam's part of the vocabulary, read once: 32 tokens of a chunk in a lane, of which it keeps
+// the largest and the sum of 2^(x log2 e - ref).  Tokens are found afterwards: the `kept`-th largest of the lanes' largest
+// is a bar that at least `kept` tokens reach, all of them in the lanes whose largest does, `kept` lanes where no two are
+// equal; only their tokens are read again.  Bound by the loads: a token takes eight lane operations, four of
+// them the exponential.
 template <int DT>
 __global__ __launch_bounds__(kRowWaves * 64) void beam_rows_kernel(BeamParams P)
 {
     typedef Logits<DT> L;
     __shared__ uint64_t lists[kRowWaves * 64];
+    __shared__ uint32_t tops[kRowWaves * 64];
     __shared__ PartialSum sums[kRowWaves];
+    __shared__ int counts[kRowWaves];
     const int row = blockIdx.x, part = blockIdx.y;
     if (!reads_logits(P, row)) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
@@ -210,8 +244,8 @@ __global__ __launch_bounds__(kRowWaves * 64) void beam_rows_kernel(BeamParams P)
     const int64_t share = part * waves + wave, shares = int64_t(gridDim.y) * waves;
     const int first = int(share * chunks / shares), end = int((share + 1) * chunks / shares);
 
-    BestList best(lane, P.kept);
     double ref = kNoRef, sum = 0.0;
+    float mine = kMinusInf;
     auto load = [&](int chunk, typename L::Vec (&raw)[L::kLoads]) {
         if (chunk < whole) L::load(x, chunk, lane, raw);
         else L::load_last(x, chunk, lane, P.vocab, raw);
@@ -225,10 +259,10 @@ __global__ __launch_bounds__(kRowWaves * 64) void beam_rows_kernel(BeamParams P)
         if (chunk + 1 < end) load(chunk + 1, raw);
 
         auto largest = [&] {
-            float m[4] = {v[0], v[1], v[2], v[3]};
+            float m = fmaxf(v[0], v[1]);
 #pragma unroll
-            for (int e = 4; e < kPieces; ++e) m[e % 4] = fmaxf(m[e % 4], v[e]);
-            return fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
+            for (int e = 2; e < kPieces; e += 2) m = fmaxf(m, fmaxf(v[e], v[e + 1]));
+            return m;
         };
         auto total = [&](auto term) {
             float t[4] = {term(v[0]), term(v[1]), term(v[2]), term(v[3])};
@@ -240,79 +274,104 @@ __global__ __launch_bounds__(kRowWaves * 64) void beam_rows_kernel(BeamParams P)
             sum = sum ? sum * exp2(ref - r) : 0.0;
             ref = r;
         };
-        float mine = largest();
-        float top = wave_max(mine);
-        float chunk_sum = 0.f;
-        bool plain = __builtin_fabsf(top) < 0x1p20f;
-        if (plain) {
-            // a reference stays while nothing outgrows it by more than 2^60
-            if (double(top * kLog2e) > ref + 60.0 || ref == kNoRef) refer_to(__builtin_ceilf(top * kLog2e));
-            const float r = float(ref);
-            chunk_sum = total([r](float a) { return __builtin_amdgcn_exp2f(__builtin_fmaf(a, kLog2e, -r)); });
-            plain = __all(chunk_sum < 3e38f);           // false for NaN, too
+        float top = largest();
+        if (ref == kNoRef) {
+            const float all = wave_max(top);
+            if (__builtin_fabsf(all) < 0x1p20f) ref = __builtin_ceilf(all * kLog2e);
         }
-        if (!plain) {
-            // +inf, NaN, no token at all, or logits whose size leaves the reference no fraction: differences instead
+        // 2^20: the reference is still near enough for the fraction of x log2 e - ref; false for NaN, too
+        const float r = float(ref);
+        const float chunk_sum = total([r](float a) { return __builtin_amdgcn_exp2f(__builtin_fmaf(a, kLog2e, -r)); });
+        if (ref != kNoRef && __all(chunk_sum < 0x1p20f)) {
+            sum += double(chunk_sum);
+        } else {
+            // a larger reference, +inf, NaN, no token at all, or logits of a size that leaves the reference no fraction:
+            // differences from the chunk's largest
 #pragma unroll
             for (int e = 0; e < kPieces; ++e) v[e] = v[e] != v[e] ? kMinusInf : fminf(v[e], 3.402823466e38f);
-            mine = largest();
-            top = wave_max(mine);
-            chunk_sum = 0.f;
-            if (top > kMinusInf) {
-                const double at = double(top) * double(kLog2e);
+            top = largest();
+            const float all = wave_max(top);
+            if (all > kMinusInf) {
+                const double at = double(all) * double(kLog2e);
                 if (at > ref) refer_to(__builtin_ceil(at));
-                chunk_sum = total([top](float a) { return __builtin_amdgcn_exp2f((a - top) * kLog2e); });
-                sum += double(chunk_sum) * exp2(at - ref);
+                sum += double(total([all](float a) { return __builtin_amdgcn_exp2f((a - all) * kLog2e); })) * exp2(at - ref);
             }
-        } else {
-            sum += double(chunk_sum);
         }
+        mine = fmaxf(mine, top);
+    }
 
-        // which of them beat the list; before there is one, those that reach the `kept`-th largest of the lanes' largest
-        const bool filling = best.least == 0;
-        float bar;
-        if (filling) {
-            const uint64_t order = sort_lanes(key_of(mine, lane), lane);
-            bar = logit_of(lane_value(order, P.kept - 1));
-        } else {
-            bar = logit_of(best.least);
-            if (!__any(mine > bar)) continue;
+    // the bar; 0 where fewer lanes have tokens
+    const uint32_t reach = first < end && L::token(first, lane, 0) < P.vocab ? order_of(mine) : 0;
+    uint32_t best_lanes = sort_lanes(reach, lane);
+    if (waves > 1) {
+        if (lane < P.kept) tops[wave * P.kept + lane] = best_lanes;
+        __syncthreads();
+        best_lanes = 0;
+        for (int i = lane; i - lane < waves * P.kept; i += 64) {
+            const uint32_t sorted = sort_lanes(i < waves * P.kept ? tops[i] : 0u, lane);
+            best_lanes = i == lane ? sorted : merge_lanes(best_lanes, sorted, lane);
         }
-        uint32_t reach = 0;
+    }
+    const uint32_t bar = __builtin_amdgcn_readlane(best_lanes, P.kept - 1);
+
+    // the tokens that reach it, of this wave's lanes that do: a lane's 16 bytes at a time
+    const bool reaches = reach && reach >= bar;
+    const uint64_t reaching = __ballot(reaches);
+    if (reaches) lists[wave * 64 + __popcll(reaching & ((uint64_t(1) << lane) - 1))] = lane;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");          // read by other lanes of this wave
+    __builtin_amdgcn_wave_barrier();
+    const int pieces = (end - first) * L::kLoads, items = __popcll(reaching) * pieces;
+    BestList best(lane, P.kept);
+    for (int i = lane; i - lane < items; i += 64) {
+        uint32_t hits = 0;
+        int t = 0;
+        if (i < items) {
+            const int of = int(lists[wave * 64 + i / pieces]), piece = i % pieces;
+            t = L::token(first + piece / L::kLoads, of, piece % L::kLoads * L::kPerLoad);
+            const int n = P.vocab - t < L::kPerLoad ? P.vocab - t : L::kPerLoad;
 #pragma unroll
-        for (int e = 0; e < kPieces; ++e) reach |= (filling ? v[e] >= bar : v[e] > bar) ? 1u << e : 0u;
-        if (chunk >= whole) {
-#pragma unroll
-            for (int e = 0; e < kPieces; ++e) reach &= L::token(chunk, lane, e) < P.vocab ? ~0u : ~(1u << e);
+            for (int e = 0; e < L::kPerLoad; ++e)
+                if (e < n && order_of(logit_at<DT>(x, t + e)) >= bar) hits |= 1u << e;
         }
-        while (__any(reach != 0)) {
+        while (__any(hits != 0)) {
             uint64_t key = 0;
-            if (reach) {
-                const int t = L::token(chunk, lane, __builtin_ctz(reach));
-                reach &= reach - 1;
-                key = key_of(logit_at<DT>(x, t), t);
+            if (hits) {
+                const int token = t + __builtin_ctz(hits);
+                hits &= hits - 1;
+                key = key_of(logit_at<DT>(x, token), token);
             }
             best.absorb(key);
         }
     }
 
-    const PartialSum mine{ref, wave_sum(sum)};
-    PartialSum *out_sum = P.sums + (int64_t(row) * P.parts + part);
+    PartialSum all{ref, wave_sum(sum)};
     uint64_t *out_best = P.best + (int64_t(row) * P.parts + part) * P.kept;
     if (waves > 1) {
+        const int found = __popcll(__ballot(best.key != 0 && lane < P.kept));
         lists[threadIdx.x] = best.key;
-        if (lane == 0) sums[wave] = mine;
+        if (lane == 0) {
+            sums[wave] = all;
+            counts[wave] = found;
+        }
         __syncthreads();
         if (wave) return;
-        // the waves' lists, 64 entries at a time
-        const int others = (waves - 1) * P.kept;
-        for (int i = lane; i - lane < others; i += 64) best.absorb(i < others ? lists[64 + i / P.kept * 64 + i % P.kept] : 0);
-        PartialSum all = mine;
-        for (int w = 1; w < waves; ++w) all = joined(all, sums[w]);
-        if (lane == 0) *out_sum = all;
-    } else if (lane == 0) {
-        *out_sum = mine;
+        // the other waves' entries, 64 at a time
+        int others = 0;
+        for (int w = 1; w < waves; ++w) {
+            others += counts[w];
+            all = joined(all, sums[w]);
+        }
+        for (int i = lane; i - lane < others; i += 64) {
+            uint64_t key = 0;
+            int at = i;
+            for (int w = 1; w < waves; ++w) {
+                if (at >= 0 && at < counts[w]) key = lists[w * 64 + at];
+                at -= counts[w];
+            }
+            best.absorb(key);
+        }
     }
+    if (lane == 0) P.sums[int64_t(row) * P.parts + part] = all;
     if (lane < P.kept) out_best[lane] = best.key;
 }
 
