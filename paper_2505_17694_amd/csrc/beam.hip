@@ -140,17 +140,29 @@ struct BestList {
     }
 };
 
-__device__ __forceinline__ float wave_max(float x)
+// Over all lanes, in every lane.
+template <class T, class Combine>
+__device__ __forceinline__ T wave_reduce(T x, Combine combine)
 {
-#pragma unroll
-    for (int n = 1; n < 64; n *= 2) x = fmaxf(x, __shfl_xor(x, n));
+    typedef std::conditional_t<sizeof(T) == 8, uint64_t, uint32_t> Bits;
+    auto step = [&](auto n) { x = combine(x, __builtin_bit_cast(T, from_lane_xor<decltype(n)::value>(__builtin_bit_cast(Bits, x)))); };
+    step(std::integral_constant<int, 1>{});
+    step(std::integral_constant<int, 2>{});
+    step(std::integral_constant<int, 4>{});
+    step(std::integral_constant<int, 8>{});
+    step(std::integral_constant<int, 16>{});
+    step(std::integral_constant<int, 32>{});
     return x;
 }
-__device__ __forceinline__ double wave_sum(double x)
+__device__ __forceinline__ float wave_max(float x) { return wave_reduce(x, [](float a, float b) { return fmaxf(a, b); }); }
+__device__ __forceinline__ double wave_sum(double x) { return wave_reduce(x, [](double a, double b) { return a + b; }); }
+
+// One instruction; fmaxf of values that may be signalling NaN takes another one for each.
+__device__ __forceinline__ float max3(float a, float b, float c)
 {
-#pragma unroll
-    for (int n = 1; n < 64; n *= 2) x += __shfl_xor(x, n);
-    return x;
+    float m;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(m) : "v"(a), "v"(b), "v"(c));
+    return m;
 }
 
 // ---- the sum of exponentials -----------------------------------------------------------------------------
@@ -233,7 +245,7 @@ __global__ __launch_bounds__(kRowWaves * 64) void beam_rows_kernel(BeamParams P)
 {
     typedef Logits<DT> L;
     __shared__ uint64_t lists[kRowWaves * 64];
-    __shared__ uint32_t tops[kRowWaves * 64];
+    __shared__ uint32_t tops[kRowWaves * 64], wanted[1];
     __shared__ PartialSum sums[kRowWaves];
     __shared__ int counts[kRowWaves];
     const int row = blockIdx.x, part = blockIdx.y;
@@ -259,10 +271,10 @@ __global__ __launch_bounds__(kRowWaves * 64) void beam_rows_kernel(BeamParams P)
         if (chunk + 1 < end) load(chunk + 1, raw);
 
         auto largest = [&] {
-            float m = fmaxf(v[0], v[1]);
+            float m[2] = {max3(v[0], v[1], v[2]), max3(v[3], v[4], v[5])};
 #pragma unroll
-            for (int e = 2; e < kPieces; e += 2) m = fmaxf(m, fmaxf(v[e], v[e + 1]));
-            return m;
+            for (int e = 6; e < kPieces; e += 2) m[e / 2 % 2] = max3(m[e / 2 % 2], v[e], v[e + 1]);
+            return fmaxf(m[0], m[1]);
         };
         auto total = [&](auto term) {
             float t[4] = {term(v[0]), term(v[1]), term(v[2]), term(v[3])};
@@ -306,13 +318,17 @@ __global__ __launch_bounds__(kRowWaves * 64) void beam_rows_kernel(BeamParams P)
     if (waves > 1) {
         if (lane < P.kept) tops[wave * P.kept + lane] = best_lanes;
         __syncthreads();
-        best_lanes = 0;
-        for (int i = lane; i - lane < waves * P.kept; i += 64) {
-            const uint32_t sorted = sort_lanes(i < waves * P.kept ? tops[i] : 0u, lane);
-            best_lanes = i == lane ? sorted : merge_lanes(best_lanes, sorted, lane);
+        if (wave == 0) {
+            for (int i = lane; i - lane < waves * P.kept; i += 64) {
+                const uint32_t sorted = sort_lanes(i < waves * P.kept ? tops[i] : 0u, lane);
+                best_lanes = i == lane ? sorted : merge_lanes(best_lanes, sorted, lane);
+            }
+            if (lane == P.kept - 1) *wanted = best_lanes;
         }
+        __syncthreads();
     }
-    const uint32_t bar = __builtin_amdgcn_readlane(best_lanes, P.kept - 1);
+    const uint32_t bar = waves > 1 ? *wanted : __builtin_amdgcn_readlane(best_lanes, P.kept - 1);
+    const float least = bar > order_of(kMinusInf) ? logit_of(uint64_t(bar) << 32) : kMinusInf;      // -inf: any token, NaN too
 
     // the tokens that reach it, of this wave's lanes that do: a lane's 16 bytes at a time
     const bool reaches = reach && reach >= bar;
@@ -328,10 +344,14 @@ __global__ __launch_bounds__(kRowWaves * 64) void beam_rows_kernel(BeamParams P)
         if (i < items) {
             const int of = int(lists[wave * 64 + i / pieces]), piece = i % pieces;
             t = L::token(first + piece / L::kLoads, of, piece % L::kLoads * L::kPerLoad);
-            const int n = P.vocab - t < L::kPerLoad ? P.vocab - t : L::kPerLoad;
+            const int n = P.vocab - t;
+            if (n >= L::kPerLoad) {
+                const typename L::Vec some = reinterpret_cast<const typename L::Unaligned *>(x + int64_t(t) * L::kSize)->v;
 #pragma unroll
-            for (int e = 0; e < L::kPerLoad; ++e)
-                if (e < n && order_of(logit_at<DT>(x, t + e)) >= bar) hits |= 1u << e;
+                for (int e = 0; e < L::kPerLoad; ++e) hits |= L::widen(some, e) >= least || least == kMinusInf ? 1u << e : 0u;
+            } else {
+                for (int e = 0; e < n; ++e) hits |= logit_at<DT>(x, t + e) >= least ? 1u << e : 0u;
+            }
         }
         while (__any(hits != 0)) {
             uint64_t key = 0;
