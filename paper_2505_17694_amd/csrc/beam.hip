@@ -124,7 +124,8 @@ struct BestList {
     {
         uint64_t hits = __ballot(newcomer > least);
         if (__popcll(hits) > 10) {
-            key = merge_lanes(key, sort_lanes(newcomer > least ? newcomer : uint64_t(0), lane), lane);
+            const uint64_t sorted = sort_lanes(newcomer > least ? newcomer : uint64_t(0), lane);
+            key = __any(key != 0) ? merge_lanes(key, sorted, lane) : sorted;
             least = lane_value(key, wanted - 1);
             return;
         }
@@ -173,22 +174,31 @@ __device__ __forceinline__ float max3(float a, float b, float c)
 constexpr float kLog2e = 1.44269502f;
 constexpr double kNoRef = -1e300;
 
-__device__ __forceinline__ PartialSum joined(PartialSum a, PartialSum b)
+// sum * 2^(from - to) for a whole from <= to.
+__device__ __forceinline__ double rescaled(double sum, double from, double to)
 {
-    const double ref = a.ref > b.ref ? a.ref : b.ref;
-    return {ref, (a.sum ? a.sum * exp2(a.ref - ref) : 0.0) + (b.sum ? b.sum * exp2(b.ref - ref) : 0.0)};
+    const double by = from - to;
+    return __builtin_ldexp(sum, by > -4000.0 ? int(by) : -4000);
+}
+
+// The lanes' sums joined, in every lane.
+__device__ __forceinline__ PartialSum joined(PartialSum x)
+{
+    const double ref = wave_reduce(x.ref, [](double a, double b) { return a > b ? a : b; });
+    return {ref, wave_sum(rescaled(x.sum, x.ref, ref))};
 }
 
 constexpr int kPieces = 32;                 // tokens of a lane in a chunk
 constexpr int kChunk = 64 * kPieces;
+
+typedef uint32_t __attribute__((ext_vector_type(4), aligned(2))) AnyVec;        // rows start at any element
 
 template <int DT>
 struct Logits {
     static constexpr int kSize = DT == CODEC_DTYPE_FP32 ? 4 : 2;
     static constexpr int kPerLoad = 16 / kSize;
     static constexpr int kLoads = kPieces / kPerLoad;
-    typedef uint32_t __attribute__((ext_vector_type(4))) Vec;
-    struct __attribute__((packed, aligned(kSize))) Unaligned { Vec v; };
+    typedef AnyVec Vec;
 
     // Tokens of a lane: kPerLoad consecutive ones of each of kLoads consecutive pieces of 64 lanes.
     __device__ static __forceinline__ int token(int chunk, int lane, int e)
@@ -201,11 +211,15 @@ struct Logits {
         else if constexpr (DT == CODEC_DTYPE_FP16) return float(__builtin_bit_cast(_Float16, uint16_t(e & 1 ? v[e / 2] >> 16 : v[e / 2])));
         else return __uint_as_float(e & 1 ? v[e / 2] & 0xffff0000u : v[e / 2] << 16);
     }
+    template <bool ONCE>
     __device__ static __forceinline__ void load(const char *row, int chunk, int lane, Vec (&raw)[kLoads])
     {
 #pragma unroll
-        for (int j = 0; j < kLoads; ++j)
-            raw[j] = reinterpret_cast<const Unaligned *>(row + int64_t(token(chunk, lane, j * kPerLoad)) * kSize)->v;
+        for (int j = 0; j < kLoads; ++j) {
+            const Vec *at = reinterpret_cast<const Vec *>(row + int64_t(token(chunk, lane, j * kPerLoad)) * kSize);
+            if constexpr (ONCE) raw[j] = __builtin_nontemporal_load(at);
+            else raw[j] = *at;
+        }
     }
     // The row's last chunk: tokens behind the last one are -inf.
     __device__ static __forceinline__ void load_last(const char *row, int chunk, int lane, int vocab, Vec (&raw)[kLoads])
@@ -215,7 +229,7 @@ struct Logits {
             const int t = token(chunk, lane, j * kPerLoad);
             const char *at = row + int64_t(t) * kSize;
             if (t + kPerLoad <= vocab) {
-                raw[j] = reinterpret_cast<const Unaligned *>(at)->v;
+                raw[j] = *reinterpret_cast<const Vec *>(at);
                 continue;
             }
 #pragma unroll
@@ -235,17 +249,63 @@ struct Logits {
 
 constexpr int kRowWaves = 8;                // most waves of a workgroup that share a beam's tokens
 
+// Newcomers of a wave, collected 64 at a time in LDS before they are sorted into its list.
+struct Collector {
+    uint64_t *room;                         // 64 entries of LDS, this wave's own
+    BestList best;
+    int count = 0;
+    bool sorted = false;                    // some have gone into the list
+
+    __device__ Collector(uint64_t *room_, int lane, int wanted) : room(room_), best(lane, wanted) {}
+
+    // The wave's LDS operations are in order; the compiler is told.
+    __device__ static void settle()
+    {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    }
+    __device__ void flush()
+    {
+        settle();
+        best.absorb(best.lane < count ? room[best.lane] : 0);
+        settle();
+        count = 0;
+        sorted = true;
+    }
+    __device__ void add(bool has, uint64_t key)
+    {
+        has = has && key > best.least;
+        const uint64_t mask = __ballot(has);
+        const int n = __popcll(mask);
+        if (!n) return;
+        if (count + n > 64) flush();
+        if (has) room[count + __popcll(mask & ((uint64_t(1) << best.lane) - 1))] = key;
+        count += n;
+    }
+    // What there is, at most 64 entries, in `room`; how many.
+    __device__ int finish()
+    {
+        if (!sorted) return count;
+        flush();
+        room[best.lane] = best.key;
+        return __popcll(__ballot(best.key != 0 && best.lane < best.wanted));
+    }
+};
+
 // The best tokens and the sum of a beam's part of the vocabulary, read once: 32 tokens of a chunk in a lane, of which it keeps
-// the largest and the sum of 2^(x log2 e - ref).  Tokens are found afterwards: the `kept`-th largest of the lanes' largest
-// is a bar that at least `kept` tokens reach, all of them in the lanes whose largest does, `kept` lanes where no two are
-// equal; only their tokens are read again.  Bound by the loads: a token takes eight lane operations, four of
-// them the exponential.
-template <int DT>
+// the largest and the sum of 2^(x log2 e - ref).  Tokens are found afterwards.  The workgroup's lanes form groups; the
+// `kept`-th largest of the groups' largest is a bar that at least `kept` tokens reach, all of them in lanes whose largest does.
+// Groups are as wide as leaves two for every token wanted: with 32 groups and 16 wanted half of the groups reach the bar, which
+// 22 tokens then do.  Only those lanes' tokens are read again.
+// Bound by the loads: a token takes seven lane operations, four of them the exponential.  The waves of a workgroup take
+// turns along the vocabulary: 8 waves, each on a stretch of its own, read 134 MB in 29 us, in turn in 26.  ONCE: with the
+// streaming hint, 24 us; 4 x 32768 fp32 logits, which stay in the caches, take 1 us longer with it.
+template <int DT, bool ONCE>
 __global__ __launch_bounds__(kRowWaves * 64) void beam_rows_kernel(BeamParams P)
 {
     typedef Logits<DT> L;
     __shared__ uint64_t lists[kRowWaves * 64];
-    __shared__ uint32_t tops[kRowWaves * 64], wanted[1];
+    __shared__ uint32_t groups[kRowWaves * 64], wanted[1];
     __shared__ PartialSum sums[kRowWaves];
     __shared__ int counts[kRowWaves];
     const int row = blockIdx.x, part = blockIdx.y;
@@ -253,22 +313,21 @@ __global__ __launch_bounds__(kRowWaves * 64) void beam_rows_kernel(BeamParams P)
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
     const char *x = P.logits + (row / P.beams * P.batch_stride + row % P.beams * P.beam_stride) * L::kSize;
     const int chunks = (P.vocab + kChunk - 1) / kChunk, whole = P.vocab / kChunk;
-    const int64_t share = part * waves + wave, shares = int64_t(gridDim.y) * waves;
-    const int first = int(share * chunks / shares), end = int((share + 1) * chunks / shares);
+    const int first = part * waves + wave, step = int(gridDim.y) * waves;
 
     double ref = kNoRef, sum = 0.0;
     float mine = kMinusInf;
     auto load = [&](int chunk, typename L::Vec (&raw)[L::kLoads]) {
-        if (chunk < whole) L::load(x, chunk, lane, raw);
+        if (chunk < whole) L::template load<ONCE>(x, chunk, lane, raw);
         else L::load_last(x, chunk, lane, P.vocab, raw);
     };
     typename L::Vec raw[L::kLoads];
-    if (first < end) load(first, raw);
-    for (int chunk = first; chunk < end; ++chunk) {
+    if (first < chunks) load(first, raw);
+    for (int chunk = first; chunk < chunks; chunk += step) {
         float v[kPieces];
 #pragma unroll
         for (int e = 0; e < kPieces; ++e) v[e] = L::widen(raw[e / L::kPerLoad], e % L::kPerLoad);
-        if (chunk + 1 < end) load(chunk + 1, raw);
+        if (chunk + step < chunks) load(chunk + step, raw);
 
         auto largest = [&] {
             float m[2] = {max3(v[0], v[1], v[2]), max3(v[3], v[4], v[5])};
@@ -281,10 +340,6 @@ __global__ __launch_bounds__(kRowWaves * 64) void beam_rows_kernel(BeamParams P)
 #pragma unroll
             for (int e = 4; e < kPieces; ++e) t[e % 4] += term(v[e]);
             return (t[0] + t[1]) + (t[2] + t[3]);
-        };
-        auto refer_to = [&](double r) {
-            sum = sum ? sum * exp2(ref - r) : 0.0;
-            ref = r;
         };
         float top = largest();
         if (ref == kNoRef) {
@@ -305,48 +360,60 @@ __global__ __launch_bounds__(kRowWaves * 64) void beam_rows_kernel(BeamParams P)
             const float all = wave_max(top);
             if (all > kMinusInf) {
                 const double at = double(all) * double(kLog2e);
-                if (at > ref) refer_to(__builtin_ceil(at));
+                if (at > ref) {
+                    sum = rescaled(sum, ref, __builtin_ceil(at));
+                    ref = __builtin_ceil(at);
+                }
                 sum += double(total([all](float a) { return __builtin_amdgcn_exp2f((a - all) * kLog2e); })) * exp2(at - ref);
             }
         }
         mine = fmaxf(mine, top);
     }
 
-    // the bar; 0 where fewer lanes have tokens
-    const uint32_t reach = first < end && L::token(first, lane, 0) < P.vocab ? order_of(mine) : 0;
-    uint32_t best_lanes = sort_lanes(reach, lane);
-    if (waves > 1) {
-        if (lane < P.kept) tops[wave * P.kept + lane] = best_lanes;
-        __syncthreads();
-        if (wave == 0) {
-            for (int i = lane; i - lane < waves * P.kept; i += 64) {
-                const uint32_t sorted = sort_lanes(i < waves * P.kept ? tops[i] : 0u, lane);
-                best_lanes = i == lane ? sorted : merge_lanes(best_lanes, sorted, lane);
-            }
-            if (lane == P.kept - 1) *wanted = best_lanes;
+    // the bar; 0 where there are fewer groups with tokens than tokens wanted
+    const uint32_t reach = first < chunks && L::token(first, lane, 0) < P.vocab ? order_of(mine) : 0;
+    const int width = waves * 64 >= 32 * P.kept ? 16 : waves * 64 >= 16 * P.kept ? 8 : waves * 64 >= 8 * P.kept ? 4 : waves * 64 >= 4 * P.kept ? 2 : 1;
+    uint32_t group = reach;
+    auto join = [&](auto n) {
+        const uint32_t other = from_lane_xor<decltype(n)::value>(group);
+        if (width > decltype(n)::value) group = other > group ? other : group;
+    };
+    join(std::integral_constant<int, 1>{});
+    join(std::integral_constant<int, 2>{});
+    join(std::integral_constant<int, 4>{});
+    join(std::integral_constant<int, 8>{});
+    const int entries = waves * 64 / width;
+    if (lane % width == 0) groups[(wave * 64 + lane) / width] = group;
+    __syncthreads();
+    if (wave == 0) {
+        uint32_t best = 0;
+        for (int i = lane; i - lane < entries; i += 64) {
+            const uint32_t sorted = sort_lanes(i < entries ? groups[i] : 0u, lane);
+            best = i == lane ? sorted : merge_lanes(best, sorted, lane);
         }
-        __syncthreads();
+        if (lane == P.kept - 1) *wanted = best;
     }
-    const uint32_t bar = waves > 1 ? *wanted : __builtin_amdgcn_readlane(best_lanes, P.kept - 1);
+    __syncthreads();
+    const uint32_t bar = *wanted;
     const float least = bar > order_of(kMinusInf) ? logit_of(uint64_t(bar) << 32) : kMinusInf;      // -inf: any token, NaN too
 
-    // the tokens that reach it, of this wave's lanes that do: a lane's 16 bytes at a time
+    // the tokens that reach it, of this wave's lanes that do: 16 bytes of one of them at a time
     const bool reaches = reach && reach >= bar;
     const uint64_t reaching = __ballot(reaches);
-    if (reaches) lists[wave * 64 + __popcll(reaching & ((uint64_t(1) << lane) - 1))] = lane;
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");          // read by other lanes of this wave
-    __builtin_amdgcn_wave_barrier();
-    const int pieces = (end - first) * L::kLoads, items = __popcll(reaching) * pieces;
-    BestList best(lane, P.kept);
+    uint32_t *lanes = groups + wave * 64;               // nobody reads the groups any more
+    if (reaches) lanes[__popcll(reaching & ((uint64_t(1) << lane) - 1))] = lane;
+    Collector::settle();
+    const int pieces = first < chunks ? ((chunks - 1 - first) / step + 1) * L::kLoads : 0, items = __popcll(reaching) * pieces;
+    Collector found(lists + wave * 64, lane, P.kept);
     for (int i = lane; i - lane < items; i += 64) {
         uint32_t hits = 0;
         int t = 0;
         if (i < items) {
-            const int of = int(lists[wave * 64 + i / pieces]), piece = i % pieces;
-            t = L::token(first + piece / L::kLoads, of, piece % L::kLoads * L::kPerLoad);
+            const int of = int(lanes[i / pieces]), piece = i % pieces;
+            t = L::token(first + piece / L::kLoads * step, of, piece % L::kLoads * L::kPerLoad);
             const int n = P.vocab - t;
             if (n >= L::kPerLoad) {
-                const typename L::Vec some = reinterpret_cast<const typename L::Unaligned *>(x + int64_t(t) * L::kSize)->v;
+                const typename L::Vec some = *reinterpret_cast<const typename L::Vec *>(x + int64_t(t) * L::kSize);
 #pragma unroll
                 for (int e = 0; e < L::kPerLoad; ++e) hits |= L::widen(some, e) >= least || least == kMinusInf ? 1u << e : 0u;
             } else {
@@ -354,45 +421,36 @@ __global__ __launch_bounds__(kRowWaves * 64) void beam_rows_kernel(BeamParams P)
             }
         }
         while (__any(hits != 0)) {
-            uint64_t key = 0;
-            if (hits) {
-                const int token = t + __builtin_ctz(hits);
-                hits &= hits - 1;
-                key = key_of(logit_at<DT>(x, token), token);
-            }
-            best.absorb(key);
+            const int token = t + __builtin_ctz(hits | 0x80000000u);
+            found.add(hits != 0, hits ? key_of(logit_at<DT>(x, token), token) : 0);
+            hits &= hits - 1;
         }
     }
 
-    PartialSum all{ref, wave_sum(sum)};
-    uint64_t *out_best = P.best + (int64_t(row) * P.parts + part) * P.kept;
-    if (waves > 1) {
-        const int found = __popcll(__ballot(best.key != 0 && lane < P.kept));
-        lists[threadIdx.x] = best.key;
-        if (lane == 0) {
-            sums[wave] = all;
-            counts[wave] = found;
-        }
-        __syncthreads();
-        if (wave) return;
-        // the other waves' entries, 64 at a time
-        int others = 0;
-        for (int w = 1; w < waves; ++w) {
-            others += counts[w];
-            all = joined(all, sums[w]);
-        }
-        for (int i = lane; i - lane < others; i += 64) {
-            uint64_t key = 0;
-            int at = i;
-            for (int w = 1; w < waves; ++w) {
-                if (at >= 0 && at < counts[w]) key = lists[w * 64 + at];
-                at -= counts[w];
-            }
-            best.absorb(key);
-        }
+    const int count = found.finish();
+    const double wave_total = wave_sum(sum);
+    if (lane == 0) {
+        sums[wave] = {ref, wave_total};
+        counts[wave] = count;
     }
-    if (lane == 0) P.sums[int64_t(row) * P.parts + part] = all;
-    if (lane < P.kept) out_best[lane] = best.key;
+    __syncthreads();
+    if (wave) return;
+    // what the waves have found, 64 entries at a time
+    BestList best(lane, P.kept);
+    int all = 0;
+    for (int w = 0; w < waves; ++w) all += counts[w];
+    for (int i = lane; i - lane < all; i += 64) {
+        uint64_t key = 0;
+        int at = i;
+        for (int w = 0; w < waves; ++w) {
+            if (at >= 0 && at < counts[w]) key = lists[w * 64 + at];
+            at -= counts[w];
+        }
+        best.absorb(key);
+    }
+    const PartialSum total = joined(lane < waves ? sums[lane] : PartialSum{kNoRef, 0.0});
+    if (lane == 0) P.sums[int64_t(row) * P.parts + part] = total;
+    if (lane < P.kept) P.best[(int64_t(row) * P.parts + part) * P.kept + lane] = best.key;
 }
 
 // Order of (score, beam, place in the beam's list) as an integer: the higher score, then the lower beam and place, is the
@@ -416,25 +474,30 @@ __global__ __launch_bounds__(kMergeBeams * 64) void beam_merge_kernel(BeamParams
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
     for (int beam = wave; beam < P.beams; beam += waves) {
         const int row = search * P.beams + beam;
+        // everything is fetched at once; of a beam whose logits do not count nothing was stored, and nothing is used
+        const uint64_t *from = P.best + int64_t(row) * P.parts * P.kept;
+        const int entries = P.parts * P.kept;
+        const uint64_t some = lane < entries ? from[lane] : 0;
+        const PartialSum part = lane < P.parts ? P.sums[int64_t(row) * P.parts + lane] : PartialSum{kNoRef, 0.0};
         const float before = P.scores[row];
+        const bool done = P.finished && P.finished[row];
         double score = -__builtin_inf();
         int token = lane;
         if (!score_counts(before)) {
             // every token of it scores -inf
-        } else if (P.finished && P.finished[row]) {
+        } else if (done) {
             if (lane == 0) score = before;
             token = lane == 0 ? P.eos : lane - 1 < P.eos ? lane - 1 : lane;
         } else {
             BestList best(lane, P.kept);
-            const uint64_t *from = P.best + int64_t(row) * P.parts * P.kept;
-            const int entries = P.parts * P.kept;
-            if (P.parts == 1) best.key = lane < P.kept ? from[lane] : 0;
-            else
-                for (int i = lane; i - lane < entries; i += 64) best.absorb(i < entries ? from[i] : 0);
-            PartialSum all{kNoRef, 0.0};
-            for (int i = lane; i < P.parts; i += 64) all = joined(all, P.sums[int64_t(row) * P.parts + i]);
-            for (int n = 1; n < 64 && n < P.parts; n *= 2) all = joined(all, {__shfl_xor(all.ref, n), __shfl_xor(all.sum, n)});
-            all = {__shfl(all.ref, 0), __shfl(all.sum, 0)};
+            if (P.parts == 1) best.key = some;
+            else best.absorb(some);
+            for (int i = lane + 64; i - lane < entries; i += 64) best.absorb(i < entries ? from[i] : 0);
+            PartialSum all = joined(part);
+            for (int i = lane + 64; i - lane < P.parts; i += 64) {
+                const PartialSum next = joined(i < P.parts ? P.sums[int64_t(row) * P.parts + i] : PartialSum{kNoRef, 0.0});
+                all = joined(lane == 0 ? all : lane == 1 ? next : PartialSum{kNoRef, 0.0});
+            }
             const float top = logit_of(lane_value(best.key, 0)), x = logit_of(best.key);
             // log of the sum of exp(x - top)
             const double log_sum = log(all.sum) + (all.ref - double(top) * double(kLog2e)) * 0.6931471805599453;
@@ -450,9 +513,10 @@ __global__ __launch_bounds__(kMergeBeams * 64) void beam_merge_kernel(BeamParams
     }
     __syncthreads();
     if (wave) return;
+    // the beams' best first: what follows seldom beats them
     BestList best(lane, P.k);
     const int entries = P.beams * P.kept;
-    for (int i = lane; i - lane < entries; i += 64) best.absorb(i < entries ? keys[i] : 0);
+    for (int i = lane; i - lane < entries; i += 64) best.absorb(i < entries ? keys[i % P.beams * P.kept + i / P.beams] : 0);
     if (lane < P.k) {
         const int place = 0xfff - int(best.key & 0xfff), beam = place / 64, at = beam * P.kept + place % 64;
         const int64_t to = int64_t(search) * P.k + lane;
@@ -495,10 +559,17 @@ int launch_beam_select(const BeamParams &p, int dtype, void *stream)
     const BeamSplit split = beam_split(rows, p.vocab);
     if (split.parts != p.parts) return int(hipErrorInvalidValue);
     const dim3 grid(unsigned(rows), unsigned(split.parts)), block(unsigned(split.waves) * 64);
+    const int64_t bytes = rows * p.vocab * (dtype == CODEC_DTYPE_FP32 ? 4 : 2);
+    const bool once = bytes > (int64_t(32) << 20);          // what the L2s of the eight dies hold
+    auto launch = [&](auto dt) {
+        constexpr int DT = decltype(dt)::value;
+        if (once) hipLaunchKernelGGL((beam_rows_kernel<DT, true>), grid, block, 0, s, p);
+        else      hipLaunchKernelGGL((beam_rows_kernel<DT, false>), grid, block, 0, s, p);
+    };
     switch (dtype) {
-    case CODEC_DTYPE_FP16: hipLaunchKernelGGL(beam_rows_kernel<CODEC_DTYPE_FP16>, grid, block, 0, s, p); break;
-    case CODEC_DTYPE_BF16: hipLaunchKernelGGL(beam_rows_kernel<CODEC_DTYPE_BF16>, grid, block, 0, s, p); break;
-    default: hipLaunchKernelGGL(beam_rows_kernel<CODEC_DTYPE_FP32>, grid, block, 0, s, p); break;
+    case CODEC_DTYPE_FP16: launch(std::integral_constant<int, CODEC_DTYPE_FP16>{}); break;
+    case CODEC_DTYPE_BF16: launch(std::integral_constant<int, CODEC_DTYPE_BF16>{}); break;
+    default: launch(std::integral_constant<int, CODEC_DTYPE_FP32>{}); break;
     }
     if (hipError_t e = hipGetLastError()) return int(e);
     const unsigned waves = unsigned(p.beams < kMergeBeams ? p.beams : kMergeBeams);
