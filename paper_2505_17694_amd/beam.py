@@ -4,28 +4,21 @@ from __future__ import annotations
 import torch
 
 from . import binding as B
-from .cache import _enter, _on
+from .cache import _check_reach, _enter, _on
 
 _CODE = {torch.float16: B.CODEC_DTYPE_FP16, torch.bfloat16: B.CODEC_DTYPE_BF16, torch.float32: B.CODEC_DTYPE_FP32}
 
 
-def _reach(t: torch.Tensor) -> int:
-    """Elements from the first of a tensor to behind its last."""
-    return 1 + sum((n - 1) * s for n, s in zip(t.shape, t.stride())) if t.numel() else 0
-
-
-def _check_storage(t: torch.Tensor, what: str) -> None:
-    """A tensor keeps its shape when its storage is given back: the memory behind it is what counts."""
-    if t.untyped_storage().nbytes() // t.element_size() - t.storage_offset() < _reach(t):
-        raise ValueError(f"{what}: the tensor's storage ends before its last element")
-
-
-def _dense(t: torch.Tensor, what: str, shape, dtypes, device: torch.device) -> int:
-    if t.shape != shape or t.dtype not in dtypes or t.device != device or not t.is_contiguous():
-        raise ValueError(f"{what}: need a contiguous tensor of shape {tuple(shape)}, one of {dtypes}, on {device}, "
-                         f"got {t.dtype} {tuple(t.shape)} on {t.device}")
-    _check_storage(t, what)
+def _dense(t: torch.Tensor, what: str, rows: int, columns: int, dtypes, index: int) -> int:
+    shape = t.shape
+    if len(shape) != 2 or shape[0] != rows or shape[1] != columns or t.dtype not in dtypes or t.get_device() != index or not t.is_contiguous():
+        raise ValueError(f"{what}: need a contiguous tensor of shape {(rows, columns)}, one of {dtypes}, on cuda:{index}, "
+                         f"got {t.dtype} {tuple(shape)} on {t.device}")
+    _check_reach(t, what, rows * columns, t.element_size())
     return t.data_ptr()
+
+
+_SCORES, _FLAGS, _BEAMS = (torch.float32,), (torch.bool, torch.uint8), (torch.int32,)
 
 
 def beam_select(logits: torch.Tensor, scores: torch.Tensor, k: int, finished: torch.Tensor = None, eos: int = 0, stream=None):
@@ -42,24 +35,26 @@ def beam_select(logits: torch.Tensor, scores: torch.Tensor, k: int, finished: to
 
 
 def _select(logits, scores, k, finished, eos, s):
-    device, (batch, beams, vocab) = logits.device, logits.shape
-    if vocab > 1 and logits.stride(2) != 1:
-        raise ValueError(f"logits: the tokens of a beam must be contiguous, strides are {logits.stride()}")
-    _check_storage(logits, "logits")
+    batch, beams, vocab = logits.shape
+    strides, index = logits.stride(), logits.get_device()
+    if vocab > 1 and strides[2] != 1:
+        raise ValueError(f"logits: the tokens of a beam must be contiguous, strides are {strides}")
+    if batch and beams and vocab:
+        _check_reach(logits, "logits", (batch - 1) * strides[0] + (beams - 1) * strides[1] + vocab, logits.element_size())
     config = B.codec_beam_config(batch, beams, vocab, k, _CODE[logits.dtype], eos)
-    scores_at = _dense(scores, "scores", (batch, beams), (torch.float32,), device)
-    finished_at = None if finished is None else _dense(finished, "finished", (batch, beams), (torch.bool, torch.uint8), device)
+    scores_at = _dense(scores, "scores", batch, beams, _SCORES, index)
+    finished_at = None if finished is None else _dense(finished, "finished", batch, beams, _FLAGS, index)
     need = B.codec_beam_workspace_bytes(config)
-    rows = max(0, k)
-    out_scores = torch.empty((batch, rows), dtype=torch.float32, device=device)
-    picked = torch.empty((2, batch, rows), dtype=torch.int32, device=device)
-    workspace = torch.empty(need, dtype=torch.uint8, device=device)
-    at = picked.data_ptr()
-    st = B.codec_beam_select(config, logits.data_ptr(), logits.stride(0) if batch > 1 else 0, logits.stride(1) if beams > 1 else 0,
-                             scores_at, finished_at, out_scores.data_ptr(), at, at + 4 * batch * rows, workspace.data_ptr(), need, s)
+    rows = k if need else 0                 # 0: a configuration that the call refuses
+    out = logits.new_empty((3, batch, rows), dtype=torch.int32)
+    workspace = logits.new_empty((need,), dtype=torch.uint8)
+    at, size = out.data_ptr(), 4 * batch * rows
+    st = B.codec_beam_select(config, logits.data_ptr(), strides[0] if batch > 1 else 0, strides[1] if beams > 1 else 0, scores_at,
+                             finished_at, at, at + size, at + 2 * size, workspace.data_ptr(), need, s)
     if st != B.CODEC_OK:
         raise B.CodecError(st, "codec_beam_select")
-    return out_scores, picked[0], picked[1]
+    out_scores, out_beams, out_tokens = out.unbind(0)
+    return out_scores.view(torch.float32), out_beams, out_tokens
 
 
 def beam_reorder(states, beams: torch.Tensor, out=None, stream=None):
@@ -76,44 +71,48 @@ def beam_reorder(states, beams: torch.Tensor, out=None, stream=None):
     return _reorder(states, beams, out, s)
 
 
-def _state_row(t: torch.Tensor, what: str) -> None:
-    n = 1
-    for size, stride in zip(reversed(t.shape[2:]), reversed(t.stride()[2:])):
-        if size != 1 and stride != n:
-            raise ValueError(f"{what}: the row of a beam must be contiguous, strides are {t.stride()}")
-        n *= size
-    _check_storage(t, what)
+def _state(t: torch.Tensor, what: str, batch: int, beams: int, index: int):
+    """Checks [batch, beams, ...] with contiguous rows in storage that is there; (bytes of a row, strides in bytes)."""
+    shape, strides, size = t.shape, t.stride(), t.element_size()
+    if len(shape) < 2 or shape[0] != batch or shape[1] != beams or t.get_device() != index:
+        raise ValueError(f"{what}: need [{batch}, {beams}, ...] on cuda:{index}, got {tuple(shape)} on {t.device}")
+    row = 1
+    for n, stride in zip(shape[:1:-1], strides[:1:-1]):
+        if n != 1 and stride != row:
+            raise ValueError(f"{what}: the row of a beam must be contiguous, strides are {strides}")
+        row *= n
+    if row:
+        _check_reach(t, what, (batch - 1) * strides[0] + (beams - 1) * strides[1] + row, size)
+    return row * size, strides[0] * size, strides[1] * size
 
 
 def _reorder(states, beams, out, s):
     batch, n = beams.shape
-    device = beams.device
-    beams_at = _dense(beams, "beams", (batch, n), (torch.int32,), device)
-    if out is None:
-        out = [torch.empty((batch, n, *x.shape[2:]), dtype=x.dtype, device=device) for x in states]
-    if len(out) != len(states):
-        raise ValueError(f"out: {len(out)} tensors for {len(states)} states")
+    index = beams.get_device()
+    beams_at = _dense(beams, "beams", batch, n, _BEAMS, index)
     wide = states[0].shape[1] if states and states[0].dim() >= 2 else 1
-    items = []
-    for i, (x, y) in enumerate(zip(states, out)):
-        if x.dim() < 2 or x.shape[:2] != (batch, wide) or x.device != device:
-            raise ValueError(f"states[{i}]: need [{batch}, {wide}, ...] on {device}, got {tuple(x.shape)} on {x.device}")
-        if y.shape != (batch, n, *x.shape[2:]) or y.dtype != x.dtype or y.device != device:
-            raise ValueError(f"out[{i}]: need {x.dtype} [{batch}, {n}, ...] like states[{i}] on {device}, got {y.dtype} {tuple(y.shape)} on {y.device}")
-        if not x.is_contiguous():
-            _state_row(x, f"states[{i}]")
-        else:
-            _check_storage(x, f"states[{i}]")
-        if not y.is_contiguous():
-            _state_row(y, f"out[{i}]")
-        else:
-            _check_storage(y, f"out[{i}]")
-        size = x.element_size()
-        row = size * (x.numel() // (batch * wide)) if batch * wide else 0
-        items.append(B.codec_state(x.data_ptr(), y.data_ptr(), row, size * x.stride(0), size * x.stride(1), size * y.stride(0),
-                                   size * y.stride(1)))
-    if n and wide:
-        st = B.codec_beam_reorder(items, beams_at, batch, wide, n, s)
+    fresh = out is None
+    if fresh:
+        out = []
+    elif len(out) != len(states):
+        raise ValueError(f"out: {len(out)} tensors for {len(states)} states")
+    fields = []
+    if batch and n and wide:
+        for i, x in enumerate(states):
+            row, x_batch, x_beam = _state(x, f"states[{i}]", batch, wide, index)
+            if fresh:
+                y = torch.empty_like(x, memory_format=torch.contiguous_format) if n == wide else x.new_empty((batch, n, *x.shape[2:]))
+                out.append(y)
+                y_batch, y_beam = n * row, row
+            else:
+                y = out[i]
+                if y.dtype != x.dtype or y.shape[2:] != x.shape[2:]:
+                    raise ValueError(f"out[{i}]: need {x.dtype} [{batch}, {n}, ...] like states[{i}], got {y.dtype} {tuple(y.shape)}")
+                _, y_batch, y_beam = _state(y, f"out[{i}]", batch, n, index)
+            fields += (x.data_ptr(), y.data_ptr(), row, x_batch, x_beam, y_batch, y_beam)
+        st = B.codec_beam_reorder(fields, beams_at, batch, wide, n, s)
         if st != B.CODEC_OK:
             raise B.CodecError(st, "codec_beam_reorder")
+    elif fresh:
+        out = [x.new_empty((batch, n, *x.shape[2:])) for x in states]
     return out

@@ -33,29 +33,37 @@ def _on(device: torch.device, stream):
 
 def _enter(device: torch.device, stream):
     """The stream's handle if the call can go ahead as things are, else None: another device or stream has to be made current."""
-    if stream is None and torch.cuda.current_device() == device.index:
+    if stream is None and torch._C._cuda_getDevice() == device.index:
         return _current_stream(device)
     return None
 
 
-def _rows(t: torch.Tensor, what: str, tokens: int, heads: int, head_dim: int, dtype: torch.dtype, device: torch.device):
-    """`t` as codec_rows: [tokens, heads, head_dim] with contiguous channels, in storage that is there."""
-    if t.shape != (tokens, heads, head_dim) or t.dtype != dtype or t.device != device or t.stride(2) != 1:
-        raise ValueError(f"{what}: need a {dtype} tensor of shape {(tokens, heads, head_dim)} with contiguous channels on "
-                         f"{device}, got {t.dtype} {tuple(t.shape)} on {t.device}, strides {t.stride()}")
-    last = (tokens - 1) * t.stride(0) + (heads - 1) * t.stride(1) + head_dim
-    if tokens and t.untyped_storage().nbytes() // 2 - t.storage_offset() < last:
+def _check_reach(t: torch.Tensor, what: str, last: int, size: int) -> None:
+    """A tensor keeps its shape when its storage is given back: the memory behind it, `last` elements of `size` bytes from its
+    first, is what counts."""
+    if t.untyped_storage().nbytes() < (t.storage_offset() + last) * size:
         raise ValueError(f"{what}: the tensor's storage ends before its last element")
+
+
+def _rows(t: torch.Tensor, what: str, shape, dtype: torch.dtype, index: int):
+    """`t` as codec_rows: `shape` = (tokens, heads, head_dim) with contiguous channels, in storage that is there."""
+    s = t.stride()
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != index or s[2] != 1:
+        raise ValueError(f"{what}: need a {dtype} tensor of shape {tuple(shape)} with contiguous channels on cuda:{index}, "
+                         f"got {t.dtype} {tuple(t.shape)} on {t.device}, strides {s}")
+    tokens, heads, head_dim = shape
+    if tokens == 0:
+        return B.codec_rows(0, 0, 0)
+    _check_reach(t, what, (tokens - 1) * s[0] + (heads - 1) * s[1] + head_dim, 2)
     # the stride of a single token or head says nothing
-    return B.codec_rows(t.data_ptr(), t.stride(0) if tokens > 1 else 0, t.stride(1) if heads > 1 else 0)
+    return B.codec_rows(t.data_ptr(), s[0] if tokens > 1 else 0, s[1] if heads > 1 else 0)
 
 
-def _index(t: torch.Tensor, what: str, tokens: int, device: torch.device) -> int:
-    if t.shape != (tokens,) or t.dtype != torch.int64 or t.device != device or not t.is_contiguous():
-        raise ValueError(f"{what}: need a contiguous int64 tensor of shape {(tokens,)} on {device}, "
+def _index(t: torch.Tensor, what: str, tokens: int, index: int) -> int:
+    if t.dim() != 1 or t.shape[0] != tokens or t.dtype is not torch.int64 or t.get_device() != index or not t.is_contiguous():
+        raise ValueError(f"{what}: need a contiguous int64 tensor of shape {(tokens,)} on cuda:{index}, "
                          f"got {t.dtype} {tuple(t.shape)} on {t.device}")
-    if tokens and t.untyped_storage().nbytes() // 8 - t.storage_offset() < tokens:
-        raise ValueError(f"{what}: the tensor's storage ends before its last element")
+    _check_reach(t, what, tokens, 8)
     return t.data_ptr()
 
 
@@ -99,13 +107,13 @@ class Rotary:
         return self._apply(x, positions, inverse, out, s)
 
     def _apply(self, x, positions, inverse, out, s):
-        tokens, heads, d = x.shape
-        rows = _rows(x, "x", tokens, heads, d, x.dtype, self.device)
-        at = _index(positions, "positions", tokens, self.device)
+        shape, index = x.shape, self.device.index
+        rows = _rows(x, "x", shape, x.dtype, index)
+        at = _index(positions, "positions", shape[0], index)
         if out is None:
-            out = torch.empty((tokens, heads, d), dtype=x.dtype, device=self.device)
-        into = _rows(out, "out", tokens, heads, d, x.dtype, self.device)
-        st = B.codec_rotary(self._config[bool(inverse)], heads, d, _CODE[x.dtype], rows, into, at, tokens, s)
+            out = torch.empty_like(x, memory_format=torch.contiguous_format)
+        into = _rows(out, "out", shape, x.dtype, index)
+        st = B.codec_rotary(self._config[bool(inverse)], shape[1], shape[2], _CODE[x.dtype], rows, into, at, shape[0], s)
         if st != B.CODEC_OK:
             raise B.CodecError(st, "codec_rotary")
         return out
@@ -147,8 +155,10 @@ class KVCache:
         self.page_stride, self.token_stride, self.head_stride = page, token, kv_head
         self._layout = B.codec_kv_layout(self.num_pages, page, token, kv_head)
         self._head = B.codec_head_config(head.num_q_heads, h, d, head.dtype, ps, 0.0)
+        self._q_row, self._kv_row = (head.num_q_heads, d), (h, d)
         self._reach = (self.num_pages - 1) * page + (ps - 1) * token + (h - 1) * kv_head + d
-        self._storages = [tuple(p.untyped_storage() for p in kv) for kv in self.pools]
+        # per layer, what has to be there: (storage, bytes)
+        self._storages = [[(p.untyped_storage(), 2 * (p.storage_offset() + self._reach)) for p in kv] for kv in self.pools]
         st, self._pages = B.codec_pages_create(self.num_pages)
         if st != B.CODEC_OK:
             raise B.CodecError(st, "codec_pages_create")
@@ -166,8 +176,8 @@ class KVCache:
 
     def _check_storage(self, layer: int) -> None:
         """A tensor keeps its shape when its storage is given back: the memory behind it is what counts."""
-        for pool, storage in zip(self.pools[layer], self._storages[layer]):
-            if storage.nbytes() // 2 - pool.storage_offset() < self._reach:
+        for storage, need in self._storages[layer]:
+            if storage.nbytes() < need:
                 raise ValueError(f"pools of layer {layer}: the storage ends before the last page")
 
     def append(self, layer, q, k, v, positions, slots, rotary: Rotary = None, q_out: torch.Tensor = None, stream=None):
@@ -183,26 +193,27 @@ class KVCache:
         return self._append(layer, q, k, v, positions, slots, rotary, q_out, s)
 
     def _append(self, layer, q, k, v, positions, slots, rotary, q_out, s):
-        h, device, dtype = self.head, self.device, self.dtype
+        index, dtype, tokens = self.device.index, self.dtype, k.shape[0]
         self._check_storage(layer)
-        tokens = k.shape[0]
-        k_rows = _rows(k, "k", tokens, h.num_kv_heads, h.head_dim, dtype, device)
-        v_rows = _rows(v, "v", tokens, h.num_kv_heads, h.head_dim, dtype, device)
+        kv_shape = (tokens, *self._kv_row)
+        k_rows = _rows(k, "k", kv_shape, dtype, index)
+        v_rows = _rows(v, "v", kv_shape, dtype, index)
         q_rows = out_rows = config = at = None
         if q is not None:
-            q_rows = _rows(q, "q", tokens, h.num_q_heads, h.head_dim, dtype, device)
+            q_shape = (tokens, *self._q_row)
+            q_rows = _rows(q, "q", q_shape, dtype, index)
             if q_out is None:
-                q_out = torch.empty((tokens, h.num_q_heads, h.head_dim), dtype=dtype, device=device)
-            out_rows = _rows(q_out, "q_out", tokens, h.num_q_heads, h.head_dim, dtype, device)
+                q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
+            out_rows = _rows(q_out, "q_out", q_shape, dtype, index) if q_out is not q else q_rows
         elif q_out is not None:
             raise ValueError("q_out without q")
         if rotary is not None:
-            if rotary.device != device:
-                raise ValueError(f"rotary is on {rotary.device}, the pools are on {device}")
-            config, at = rotary._config[0], _index(positions, "positions", tokens, device)
+            if rotary.device != self.device:
+                raise ValueError(f"rotary is on {rotary.device}, the pools are on {self.device}")
+            config, at = rotary._config[0], _index(positions, "positions", tokens, index)
         kp, vp = self.pools[layer]
-        st = B.codec_append(self._head, config, q_rows, out_rows, k_rows, v_rows, at,
-                            _index(slots, "slots", tokens, device), tokens, kp.data_ptr(), vp.data_ptr(), self._layout, s)
+        st = B.codec_append(self._head, config, q_rows, out_rows, k_rows, v_rows, at, _index(slots, "slots", tokens, index),
+                            tokens, kp.data_ptr(), vp.data_ptr(), self._layout, s)
         if st != B.CODEC_OK:
             raise B.CodecError(st, "codec_append")
         return q_out

@@ -60,7 +60,7 @@ def test_reorder_refusals():
     a, b = 1 << 20, 1 << 21
 
     def status(states=((a, b, 64, 256, 64, 256, 64),), beams=4096, batch=2, wide=4, n=4):
-        return C.codec_beam_reorder([C.codec_state(*s) for s in states], beams, batch, wide, n)
+        return C.codec_beam_reorder([x for s in states for x in s], beams, batch, wide, n)
     assert status(states=()) == status(batch=0) == status(states=((0, 0, 0, 0, 0, 0, 0),)) == C.CODEC_OK
     for bad in (dict(beams=0), dict(batch=-1), dict(wide=0), dict(n=0), dict(batch=1 << 20, n=1 << 12),
                 dict(states=((0, b, 64, 256, 64, 256, 64),)), dict(states=((a, 0, 64, 256, 64, 256, 64),)), dict(states=((a, b, -1, 256, 64, 256, 64),)),
