@@ -6,6 +6,8 @@
 // reduced to an eighth of a turn around the next quarter before the series of sine and cosine run in 32.
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "operators.hpp"
 
 namespace codec {
@@ -44,9 +46,134 @@ __device__ __forceinline__ Turn turn_of(double turns)
     return {(q == 1 || q == 2) ? -a : a, q >= 2 ? -b : b};
 }
 
-// One thread per pair of channels of a row: the pairs that turn first, then the others two by two.  Rows of a token:
-// its queries, its keys, its values.
-template <int DT, bool INTERLEAVED>
+typedef uint32_t __attribute__((ext_vector_type(4))) Vec;      // eight channels
+
+template <int DT>
+__device__ __forceinline__ uint32_t narrow2(float lo, float hi)
+{
+    if constexpr (DT == CODEC_DTYPE_FP16) {
+        typedef _Float16 Two __attribute__((ext_vector_type(2)));
+        return __builtin_bit_cast(uint32_t, Two{_Float16(lo), _Float16(hi)});
+    } else {
+        typedef __bf16 Two __attribute__((ext_vector_type(2)));
+        return __builtin_bit_cast(uint32_t, Two{__bf16(lo), __bf16(hi)});
+    }
+}
+
+__device__ __forceinline__ int64_t in_registers(int64_t x)
+{
+    asm("" : "+s"(x));
+    return x;
+}
+
+// A copy with some arithmetic on the way, bound by HBM.  A lane takes 16 bytes of a row and 16 others that the same cosines and
+// sines serve: the other halves of its eight pairs, or, with neighbouring pairs, the same four pairs of another row, so that
+// the lanes of a wave write consecutive memory.  It keeps the cosines and sines for all rows it takes: a wave takes
+// 64 / U rows of one token at a time, U = head_dim / 16, `rounds` times in all; `splits` waves share a token.  The next
+// round's loads are under way while a round is turned (two rounds at a time: 66 registers, seven waves a SIMD in the place of
+// eight, 150 us in the place of 129 for the 671 MB below).
+// LARGE: with the streaming hint.  16384 tokens of 64 + 8 + 8 heads of 128 channels take 129 us with it (5.2 TB/s) and 143
+// without, 64 tokens of 32 + 8 + 8 heads 4.2 and 3.7, where the attention that follows finds its rows in the caches besides.
+template <int DT, bool INTERLEAVED, int U, bool LARGE>
+__global__ __launch_bounds__(256) void rotary_kernel(RotaryParams P, uint32_t splits, uint32_t rounds)
+{
+    constexpr int kRows = 64 / U;
+    constexpr int kLanes = INTERLEAVED ? 2 * U : U;     // of a row
+    constexpr int kPairs = INTERLEAVED ? 4 : 8;         // of a lane
+    constexpr int kOther = INTERLEAVED ? kRows / 2 : 0; // rows from a lane's first 16 bytes to its second
+    const int lane = threadIdx.x & 63, unit = lane % kLanes, sub = lane / kLanes;
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+    const uint32_t token = wave / splits, part = wave % splits;
+    if (token >= P.num_tokens) return;
+
+    const int turning = P.rotary_dim / 2;               // pairs
+    const int pair = unit * kPairs;                     // the lane's first
+    const bool turns = pair < turning;
+    const int first = INTERLEAVED || turns ? unit * 8 : unit * 16;                                  // channels
+    const int second = INTERLEAVED ? first : turns ? first + turning : first + 8;
+
+    const char *q = P.q.data + int64_t(token) * P.q.token_stride, *k = P.k.data + int64_t(token) * P.k.token_stride,
+               *v = P.v.data + int64_t(token) * P.v.token_stride;
+    char *q_out = P.q_out.data + int64_t(token) * P.q_out.token_stride;
+    const int rows = P.q_heads + 2 * P.kv_heads;
+    char *k_slot = nullptr, *v_slot = nullptr;
+    if (P.kv_heads) {
+        const int64_t slot = P.slots[token];
+        if (slot >= 0 && slot < P.num_slots) {
+            const int64_t at = (slot >> P.page_shift) * P.page_stride + (slot & ((int64_t(1) << P.page_shift) - 1)) * P.slot_stride;
+            k_slot = P.k_pages + at;
+            v_slot = P.v_pages + at;
+        }
+    }
+    const int stored = k_slot ? rows : P.q_heads;       // rows that go anywhere
+    // In registers: a choice between two of the kernel's arguments becomes a load of each lane's own choice otherwise.
+    const int64_t q_stride = in_registers(P.q.head_stride), k_stride = in_registers(P.k.head_stride), v_stride = in_registers(P.v.head_stride),
+                  out_stride = in_registers(P.q_out.head_stride), slot_stride = in_registers(P.head_stride);
+
+    auto row_of = [&](uint32_t round, int other) { return int(round * kRows) + sub + other * kOther; };
+    auto load_row = [&](int row, int channel) -> Vec {
+        if (row >= stored) return Vec{};
+        const int head = row - P.q_heads;
+        const char *from = row < P.q_heads ? q + row * q_stride : head < P.kv_heads ? k + head * k_stride : v + (head - P.kv_heads) * v_stride;
+        const Vec *at = reinterpret_cast<const Vec *>(from + 2 * channel);
+        if constexpr (LARGE) return __builtin_nontemporal_load(at);
+        else return *at;
+    };
+    auto store_row = [&](int row, int channel, Vec x) {
+        if (row >= stored) return;
+        const int head = row - P.q_heads;
+        char *to = row < P.q_heads ? q_out + row * out_stride : head < P.kv_heads ? k_slot + head * slot_stride : v_slot + (head - P.kv_heads) * slot_stride;
+        Vec *at = reinterpret_cast<Vec *>(to + 2 * channel);
+        if constexpr (LARGE) __builtin_nontemporal_store(x, at);
+        else *at = x;
+    };
+    Vec a = load_row(row_of(part, 0), first), b = load_row(row_of(part, 1), second);
+
+    float c[kPairs], s[kPairs];
+    if (turning) {
+        const double position = double(P.positions[token]);
+#pragma unroll
+        for (int i = 0; i < kPairs; ++i) {
+            const Turn t = turn_of(position * P.turns[INTERLEAVED ? (pair + i < turning ? pair + i : 0) : (turns ? pair : 0) + i]);
+            c[i] = t.cos * P.magnitude;
+            s[i] = t.sin * (P.magnitude * P.sign);
+        }
+    }
+    auto turn_neighbours = [&](Vec &x) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float lo = widen<DT>(uint16_t(x[i])), hi = widen<DT>(uint16_t(x[i] >> 16));
+            const uint32_t turned = narrow2<DT>(lo * c[i] - hi * s[i], hi * c[i] + lo * s[i]);
+            x[i] = pair + i < turning ? turned : x[i];
+        }
+    };
+
+    for (uint32_t round = part; round < rounds; round += splits) {
+        const Vec a_next = load_row(row_of(round + splits, 0), first), b_next = load_row(row_of(round + splits, 1), second);
+        const int row = row_of(round, 0), other = row_of(round, 1), values = P.q_heads + P.kv_heads;
+        if constexpr (INTERLEAVED) {
+            if (turns && row < values) turn_neighbours(a);
+            if (turns && other < values) turn_neighbours(b);
+        } else if (turns && row < values) {
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const int i = 2 * w;
+                const float a0 = widen<DT>(uint16_t(a[w])), a1 = widen<DT>(uint16_t(a[w] >> 16));
+                const float b0 = widen<DT>(uint16_t(b[w])), b1 = widen<DT>(uint16_t(b[w] >> 16));
+                a[w] = narrow2<DT>(a0 * c[i] - b0 * s[i], a1 * c[i + 1] - b1 * s[i + 1]);
+                b[w] = narrow2<DT>(b0 * c[i] + a0 * s[i], b1 * c[i + 1] + a1 * s[i + 1]);
+            }
+        }
+        store_row(row, first, a);
+        store_row(other, second, b);
+        a = a_next;
+        b = b_next;
+    }
+}
+
+// Halves whose pairs do not come in eights: one thread per pair of channels of a row, the pairs that turn first, then the
+// others two by two.  Rows of a token: its queries, its keys, its values.
+template <int DT>
 __global__ __launch_bounds__(256) void rotary_pair_kernel(RotaryParams P)
 {
     const int pairs = P.head_dim / 2, turning = P.rotary_dim / 2;
@@ -71,8 +198,8 @@ __global__ __launch_bounds__(256) void rotary_pair_kernel(RotaryParams P)
             to = reinterpret_cast<uint16_t *>((value ? P.v_pages : P.k_pages) + page * P.page_stride + in_page * P.slot_stride + head * P.head_stride);
         }
         const bool turns = !value && pair < turning;
-        const int first = turns ? (INTERLEAVED ? 2 * pair : pair) : value ? 2 * pair : P.rotary_dim + 2 * (pair - turning);
-        const int second = turns && !INTERLEAVED ? first + turning : first + 1;
+        const int first = turns ? pair : value ? 2 * pair : P.rotary_dim + 2 * (pair - turning);
+        const int second = turns ? first + turning : first + 1;
         uint16_t a = from[first], b = from[second];
         if (turns) {
             const Turn t = turn_of(double(P.positions[token]) * P.turns[pair]);
@@ -91,12 +218,37 @@ __global__ __launch_bounds__(256) void rotary_pair_kernel(RotaryParams P)
 int launch_rotary(const RotaryParams &p, int dtype, bool interleaved, void *stream)
 {
     hipStream_t s = static_cast<hipStream_t>(stream);
-    const int64_t pairs = p.num_tokens * (p.q_heads + 2 * p.kv_heads) * (p.head_dim / 2);
-    const int64_t blocks = (pairs + 255) / 256;
-    const dim3 grid(unsigned(blocks < (int64_t(1) << 22) ? blocks : int64_t(1) << 22));
-    auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, p); };
-    if (dtype == CODEC_DTYPE_FP16) interleaved ? launch(rotary_pair_kernel<CODEC_DTYPE_FP16, true>) : launch(rotary_pair_kernel<CODEC_DTYPE_FP16, false>);
-    else                           interleaved ? launch(rotary_pair_kernel<CODEC_DTYPE_BF16, true>) : launch(rotary_pair_kernel<CODEC_DTYPE_BF16, false>);
+    const int64_t rows = p.q_heads + 2 * p.kv_heads;
+    // pairs of halves are taken eight at a time: 16 channels that turn, or a multiple of them
+    if (!interleaved && p.rotary_dim % 16) {
+        const int64_t blocks = (p.num_tokens * rows * (p.head_dim / 2) + 255) / 256;
+        const dim3 grid(unsigned(blocks < (int64_t(1) << 22) ? blocks : int64_t(1) << 22));
+        if (dtype == CODEC_DTYPE_FP16) hipLaunchKernelGGL(rotary_pair_kernel<CODEC_DTYPE_FP16>, grid, dim3(256), 0, s, p);
+        else                           hipLaunchKernelGGL(rotary_pair_kernel<CODEC_DTYPE_BF16>, grid, dim3(256), 0, s, p);
+        return int(hipGetLastError());
+    }
+    // a wave for every token, or as many as it takes to have 32 on every CU
+    const int64_t at_once = 64 / (p.head_dim / 16), rounds = (rows + at_once - 1) / at_once;
+    int64_t splits = (8192 + p.num_tokens - 1) / p.num_tokens;
+    if (splits > rounds) splits = rounds;
+    const dim3 grid(unsigned((p.num_tokens * splits + 3) / 4));
+    const bool large = p.num_tokens * rows * p.head_dim * 4 > int64_t(32) << 20;        // in and out, beyond the L2s
+    const uint32_t n = uint32_t(splits), r = uint32_t(rounds);
+    auto launch_dim = [&](auto dt, auto layout, auto u) {
+        constexpr int DT = decltype(dt)::value, U = decltype(u)::value;
+        constexpr bool I = decltype(layout)::value;
+        if (large) hipLaunchKernelGGL((rotary_kernel<DT, I, U, true>), grid, dim3(256), 0, s, p, n, r);
+        else       hipLaunchKernelGGL((rotary_kernel<DT, I, U, false>), grid, dim3(256), 0, s, p, n, r);
+    };
+    auto launch = [&](auto dt, auto layout) {
+        if (p.head_dim == 64)       launch_dim(dt, layout, std::integral_constant<int, 4>{});
+        else if (p.head_dim == 128) launch_dim(dt, layout, std::integral_constant<int, 8>{});
+        else                        launch_dim(dt, layout, std::integral_constant<int, 16>{});
+    };
+    using f16 = std::integral_constant<int, CODEC_DTYPE_FP16>;
+    using b16 = std::integral_constant<int, CODEC_DTYPE_BF16>;
+    if (dtype == CODEC_DTYPE_FP16) interleaved ? launch(f16{}, std::true_type{}) : launch(f16{}, std::false_type{});
+    else                           interleaved ? launch(b16{}, std::true_type{}) : launch(b16{}, std::false_type{});
     return int(hipGetLastError());
 }
 
