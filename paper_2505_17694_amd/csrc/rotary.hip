@@ -60,11 +60,10 @@ __device__ __forceinline__ uint32_t narrow2(float lo, float hi)
     }
 }
 
-__device__ __forceinline__ int64_t in_registers(int64_t x)
-{
-    asm("" : "+s"(x));
-    return x;
-}
+// One of three values.  (They are arguments: written out where they are used, the choice is made between the places they are
+// kept in, and each lane loads its own.)
+template <class T>
+__device__ __forceinline__ T one_of(bool first, bool second, T a, T b, T c) { return first ? a : second ? b : c; }
 
 // A copy with some arithmetic on the way, bound by HBM.  A lane takes 16 bytes of a row and 16 others that the same cosines and
 // sines serve: the other halves of its eight pairs, or, with neighbouring pairs, the same four pairs of another row, so that
@@ -106,24 +105,27 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryParams P, uint32_t sp
         }
     }
     const int stored = k_slot ? rows : P.q_heads;       // rows that go anywhere
-    // In registers: a choice between two of the kernel's arguments becomes a load of each lane's own choice otherwise.
-    const int64_t q_stride = in_registers(P.q.head_stride), k_stride = in_registers(P.k.head_stride), v_stride = in_registers(P.v.head_stride),
-                  out_stride = in_registers(P.q_out.head_stride), slot_stride = in_registers(P.head_stride);
-
+    if (stored == 0) return;
     auto row_of = [&](uint32_t round, int other) { return int(round * kRows) + sub + other * kOther; };
+    // Loads have no branches around them, so that the wait for one round's leaves the next round's under way: a row that goes
+    // nowhere reads the last one that does.
     auto load_row = [&](int row, int channel) -> Vec {
-        if (row >= stored) return Vec{};
-        const int head = row - P.q_heads;
-        const char *from = row < P.q_heads ? q + row * q_stride : head < P.kv_heads ? k + head * k_stride : v + (head - P.kv_heads) * v_stride;
-        const Vec *at = reinterpret_cast<const Vec *>(from + 2 * channel);
+        row = row < stored ? row : stored - 1;
+        const bool query = row < P.q_heads, key = row < P.q_heads + P.kv_heads;
+        const char *base = one_of(query, key, q, k, v);
+        const int64_t stride = one_of(query, key, P.q.head_stride, P.k.head_stride, P.v.head_stride);
+        const int head = row - one_of(query, key, 0, P.q_heads, P.q_heads + P.kv_heads);
+        const Vec *at = reinterpret_cast<const Vec *>(base + head * stride + 2 * channel);
         if constexpr (LARGE) return __builtin_nontemporal_load(at);
         else return *at;
     };
     auto store_row = [&](int row, int channel, Vec x) {
+        const bool query = row < P.q_heads, key = row < P.q_heads + P.kv_heads;
+        char *base = one_of(query, key, q_out, k_slot, v_slot);
+        const int64_t stride = one_of(query, true, P.q_out.head_stride, P.head_stride, P.head_stride);
+        const int head = row - one_of(query, key, 0, P.q_heads, P.q_heads + P.kv_heads);
+        Vec *at = reinterpret_cast<Vec *>(base + head * stride + 2 * channel);
         if (row >= stored) return;
-        const int head = row - P.q_heads;
-        char *to = row < P.q_heads ? q_out + row * out_stride : head < P.kv_heads ? k_slot + head * slot_stride : v_slot + (head - P.kv_heads) * slot_stride;
-        Vec *at = reinterpret_cast<Vec *>(to + 2 * channel);
         if constexpr (LARGE) __builtin_nontemporal_store(x, at);
         else *at = x;
     };
@@ -148,26 +150,32 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryParams P, uint32_t sp
         }
     };
 
-    for (uint32_t round = part; round < rounds; round += splits) {
-        const Vec a_next = load_row(row_of(round + splits, 0), first), b_next = load_row(row_of(round + splits, 1), second);
+    auto finish = [&](uint32_t round, Vec &x, Vec &y) {
         const int row = row_of(round, 0), other = row_of(round, 1), values = P.q_heads + P.kv_heads;
         if constexpr (INTERLEAVED) {
-            if (turns && row < values) turn_neighbours(a);
-            if (turns && other < values) turn_neighbours(b);
+            if (turns && row < values) turn_neighbours(x);
+            if (turns && other < values) turn_neighbours(y);
         } else if (turns && row < values) {
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
                 const int i = 2 * w;
-                const float a0 = widen<DT>(uint16_t(a[w])), a1 = widen<DT>(uint16_t(a[w] >> 16));
-                const float b0 = widen<DT>(uint16_t(b[w])), b1 = widen<DT>(uint16_t(b[w] >> 16));
-                a[w] = narrow2<DT>(a0 * c[i] - b0 * s[i], a1 * c[i + 1] - b1 * s[i + 1]);
-                b[w] = narrow2<DT>(b0 * c[i] + a0 * s[i], b1 * c[i + 1] + a1 * s[i + 1]);
+                const float x0 = widen<DT>(uint16_t(x[w])), x1 = widen<DT>(uint16_t(x[w] >> 16));
+                const float y0 = widen<DT>(uint16_t(y[w])), y1 = widen<DT>(uint16_t(y[w] >> 16));
+                x[w] = narrow2<DT>(x0 * c[i] - y0 * s[i], x1 * c[i + 1] - y1 * s[i + 1]);
+                y[w] = narrow2<DT>(y0 * c[i] + x0 * s[i], y1 * c[i + 1] + x1 * s[i + 1]);
             }
         }
-        store_row(row, first, a);
-        store_row(other, second, b);
-        a = a_next;
-        b = b_next;
+        store_row(row, first, x);
+        store_row(other, second, y);
+    };
+    // two sets of registers in turn: a copy from one to the other would wait for the loads, and for the stores behind them
+    for (uint32_t round = part; round < rounds; round += 2 * splits) {
+        Vec a_next = load_row(row_of(round + splits, 0), first), b_next = load_row(row_of(round + splits, 1), second);
+        finish(round, a, b);
+        if (round + splits >= rounds) break;
+        a = load_row(row_of(round + 2 * splits, 0), first);
+        b = load_row(row_of(round + 2 * splits, 1), second);
+        finish(round + splits, a_next, b_next);
     }
 }
 
