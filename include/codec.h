@@ -481,8 +481,8 @@ int codec_rotary(const codec_rotary_config *rotary, int32_t num_heads, int32_t h
  * The step's tokens into the cache: queries and keys turned as by codec_rotary (rotary NULL: passed as
  * they are, positions is then not read), key t and value t stored at token slots[t] % page_size of
  * page slots[t] / page_size of the pools.
- *   head        head_dim, page_size and dtype as for a plan; num_q_heads and num_kv_heads >= 1 (scale is
- *               not used)
+ *   head        head_dim, page_size and dtype as for a plan; num_q_heads 1..65536, num_kv_heads 1..4096
+ *               (scale is not used)
  *   q, q_out    device rows [num_tokens][num_q_heads]; q_out may be q itself.  Both NULL: no queries
  *   k, v        device rows [num_tokens][num_kv_heads]
  *   slots       device [num_tokens]; a token whose slot is negative or beyond the pools' last page (padding

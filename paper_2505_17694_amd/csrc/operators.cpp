@@ -28,7 +28,7 @@ int check_rows_of(int32_t head_dim, int32_t dtype)
 
 int check_head(const codec_head_config &h)
 {
-    if (h.num_kv_heads < 1 || h.num_q_heads < 1 || h.num_kv_heads > (1 << 16) || h.num_q_heads > (1 << 16)) return CODEC_ERR_INVALID_ARGUMENT;
+    if (h.num_kv_heads < 1 || h.num_q_heads < 1 || h.num_kv_heads > (1 << 12) || h.num_q_heads > (1 << 16)) return CODEC_ERR_INVALID_ARGUMENT;
     if (int st = check_rows_of(h.head_dim, h.dtype)) return st;
     if (h.page_size < 16 || h.page_size > 4096 || (h.page_size & (h.page_size - 1)) != 0) return CODEC_ERR_UNSUPPORTED;
     return CODEC_OK;
@@ -361,6 +361,9 @@ int codec_cache_copy(const codec_head_config *head, const codec_kv_layout *layou
     p.head_stride = 2 * layout->head_stride;
     p.heads = head->num_kv_heads;
     p.head_bytes = 2 * head->head_dim;
+    double tokens = 0.0;
+    for (int32_t i = 0; i < num_runs; ++i) tokens += runs[i].tokens;
+    p.large = 4.0 * tokens * num_layers * p.heads * p.head_bytes > codec::kLargeBytes;
     for (int64_t first = 0; first < 2 * int64_t(num_layers); first += codec::kCopyPools) {
         p.num_pools = int32_t(std::min<int64_t>(codec::kCopyPools, 2 * int64_t(num_layers) - first));
         for (int32_t i = 0; i < p.num_pools; ++i) p.pools[i] = static_cast<char *>(((first + i) & 1 ? v_pages : k_pages)[(first + i) / 2]);
@@ -469,6 +472,9 @@ int codec_beam_reorder(const codec_state *states, int32_t num_states, const int3
     p.batch = batch;
     p.beams_in = beams_in;
     p.beams_out = beams_out;
+    double row_bytes = 0.0;
+    for (int32_t i = 0; i < num_states; ++i) row_bytes += double(states[i].row_bytes);
+    p.large = 2.0 * row_bytes * batch * beams_out > codec::kLargeBytes;
     for (int32_t i = 0; i < num_states; ++i) {
         const codec_state &s = states[i];
         if (s.row_bytes) {

@@ -8,6 +8,10 @@
 
 namespace codec {
 
+// What the L2s of the eight dies hold together.  Calls that read and write more use the streaming hint: what they leave would
+// not be found there.
+constexpr double kLargeBytes = 32 << 20;
+
 // Rows of one kind (queries, keys, values) of the tokens: strides in bytes.
 struct RowsView {
     char *data;
@@ -38,6 +42,8 @@ struct CopyRun {
 struct CopyParams {
     int64_t page_stride, slot_stride, head_stride;      // bytes
     int32_t heads, head_bytes, num_pools, num_runs, most_tokens;
+    uint32_t row_pieces, planes;                        // set by launch_copy
+    bool large;                                         // the call moves more than kLargeBytes
     char *pools[kCopyPools];
     CopyRun runs[kCopyRuns];
 };
@@ -63,7 +69,7 @@ struct BeamParams {
 struct BeamSplit { int waves, parts; };
 BeamSplit beam_split(int64_t rows, int vocab);
 
-constexpr int kReorderStates = 64;
+constexpr int kReorderStates = 64;      // of a launch
 
 struct ReorderState {
     const char *src;
@@ -76,13 +82,14 @@ struct ReorderParams {
     const int32_t *beams;
     int32_t batch, beams_in, beams_out, num_states;
     int64_t most_units;
+    bool large;                                         // the call moves more than kLargeBytes
     ReorderState states[kReorderStates];
 };
 static_assert(sizeof(ReorderParams) <= 4096, "kernel arguments");
 
 // All return a hipError_t value (0 = success) without synchronising.
 int launch_rotary(const RotaryParams &p, int dtype, bool interleaved, void *stream);
-int launch_copy(const CopyParams &p, void *stream);
+int launch_copy(CopyParams &p, void *stream);
 int launch_beam_select(const BeamParams &p, int dtype, void *stream);
 // `unit`: bytes moved at a time, 1, 2, 4, 8 or 16
 int launch_reorder(const ReorderParams &p, int unit, void *stream);

@@ -240,7 +240,7 @@ int launch_rotary(const RotaryParams &p, int dtype, bool interleaved, void *stre
     int64_t splits = (8192 + p.num_tokens - 1) / p.num_tokens;
     if (splits > rounds) splits = rounds;
     const dim3 grid(unsigned((p.num_tokens * splits + 3) / 4));
-    const bool large = p.num_tokens * rows * p.head_dim * 4 > int64_t(32) << 20;        // in and out, beyond the L2s
+    const bool large = 4.0 * double(p.num_tokens) * double(rows) * p.head_dim > kLargeBytes;
     const uint32_t n = uint32_t(splits), r = uint32_t(rounds);
     auto launch_dim = [&](auto dt, auto layout, auto u) {
         constexpr int DT = decltype(dt)::value, U = decltype(u)::value;
