@@ -86,33 +86,58 @@ def _state(t: torch.Tensor, what: str, batch: int, beams: int, index: int):
     return row * size, strides[0] * size, strides[1] * size
 
 
+def _states(tensors, what: str, batch: int, beams: int, index: int):
+    """_state of each; a dense tensor like the one before it is only looked at for what may differ."""
+    out, shape, dtype, dense, fields = [], None, None, False, None
+    for i, t in enumerate(tensors):
+        if dense and t.shape == shape and t.dtype is dtype and t.is_contiguous() and t.get_device() == index:
+            if fields[0]:
+                _check_reach(t, what, count, size)
+        else:
+            fields = _state(t, f"{what}[{i}]", batch, beams, index)
+            shape, dtype, dense, count, size = t.shape, t.dtype, t.is_contiguous(), t.numel(), t.element_size()
+        out.append(fields)
+    return out
+
+
+def _like(states, shapes, n: int, wide: int):
+    """New dense tensors for the states' rows.  Neighbours of one shape and type share an allocation, where each begins at a
+    multiple of 16 bytes."""
+    out, i = [], 0
+    while i < len(states):
+        x, j = states[i], i + 1
+        while j < len(states) and states[j].shape == x.shape and states[j].dtype is x.dtype:
+            j += 1
+        batch, row = x.shape[0], shapes[i][0]
+        if j - i > 1 and batch * n * row % 16 == 0:
+            out += x.new_empty((j - i, batch, n, *x.shape[2:])).unbind(0)
+        else:
+            out += [x.new_empty((batch, n, *x.shape[2:])) for x in states[i:j]]
+        i = j
+    return out
+
+
 def _reorder(states, beams, out, s):
     batch, n = beams.shape
     index = beams.get_device()
     beams_at = _dense(beams, "beams", batch, n, _BEAMS, index)
     wide = states[0].shape[1] if states and states[0].dim() >= 2 else 1
-    fresh = out is None
-    if fresh:
-        out = []
-    elif len(out) != len(states):
-        raise ValueError(f"out: {len(out)} tensors for {len(states)} states")
-    fields = []
+    src = _states(states, "states", batch, wide, index)
+    if out is None:
+        out = _like(states, src, n, wide)
+        dst = [(row, n * row, row) for row, _, _ in src]
+    else:
+        if len(out) != len(states):
+            raise ValueError(f"out: {len(out)} tensors for {len(states)} states")
+        for i, (x, y) in enumerate(zip(states, out)):
+            if y.dtype != x.dtype or y.shape[2:] != x.shape[2:]:
+                raise ValueError(f"out[{i}]: need {x.dtype} [{batch}, {n}, ...] like states[{i}], got {y.dtype} {tuple(y.shape)}")
+        dst = _states(out, "out", batch, n, index)
     if batch and n and wide:
-        for i, x in enumerate(states):
-            row, x_batch, x_beam = _state(x, f"states[{i}]", batch, wide, index)
-            if fresh:
-                y = torch.empty_like(x, memory_format=torch.contiguous_format) if n == wide else x.new_empty((batch, n, *x.shape[2:]))
-                out.append(y)
-                y_batch, y_beam = n * row, row
-            else:
-                y = out[i]
-                if y.dtype != x.dtype or y.shape[2:] != x.shape[2:]:
-                    raise ValueError(f"out[{i}]: need {x.dtype} [{batch}, {n}, ...] like states[{i}], got {y.dtype} {tuple(y.shape)}")
-                _, y_batch, y_beam = _state(y, f"out[{i}]", batch, n, index)
+        fields = []
+        for x, y, (row, x_batch, x_beam), (_, y_batch, y_beam) in zip(states, out, src, dst):
             fields += (x.data_ptr(), y.data_ptr(), row, x_batch, x_beam, y_batch, y_beam)
         st = B.codec_beam_reorder(fields, beams_at, batch, wide, n, s)
         if st != B.CODEC_OK:
             raise B.CodecError(st, "codec_beam_reorder")
-    elif fresh:
-        out = [x.new_empty((batch, n, *x.shape[2:])) for x in states]
     return out

@@ -455,15 +455,22 @@ def codec_pages_release(pages, ids) -> int:
 def codec_pages_fork(pages, page_size: int, page_off, page_ids, tokens, parents):
     """Returns (status, page_off, page_ids, runs [n, 5]) of the sequences that go on, or (status, None, None, None)."""
     off, ids, tokens, parents = _i32(page_off), _i32(page_ids), _i32(tokens), _i32(parents)
-    if off.ndim != 1 or off.size != tokens.size + 1 or off[0] != 0 or off[-1] != ids.size:      # the C call reads by these lengths
+    num_seq, num_out = tokens.size, parents.size
+    if off.ndim != 1 or off.size != num_seq + 1 or off[0] != 0 or off[-1] != ids.size:      # the C call reads by these lengths
         return CODEC_ERR_INVALID_ARGUMENT, None, None, None
-    longest = int((off[1:] - off[:-1]).max(initial=0))
-    capacity = min(max(longest, 0) * parents.size, 0x7fffffff)
-    out_off, out_ids = np.empty(parents.size + 1, np.int32), np.empty(capacity, np.int32)
-    runs, n = np.empty((parents.size, 5), np.int32), c_int32(0)
-    st = _lib.codec_pages_fork(pages, page_size, tokens.size, off.ctypes.data, ids.ctypes.data, tokens.ctypes.data, parents.size,
-                               parents.ctypes.data, out_off.ctypes.data, out_ids.ctypes.data, capacity, runs.ctypes.data, byref(n))
-    return (st, out_off, out_ids[:out_off[-1]], runs[:n.value]) if st == CODEC_OK else (st, None, None, None)
+    # room for lists of the longest of the old ones' length, and for a run each, in one array
+    longest = int(np.maximum.reduce(off[1:] - off[:-1], initial=0))
+    capacity = min(longest * num_out, 0x7fffffff)
+    room, n = np.empty(num_out + 1 + capacity + 5 * num_out, np.int32), c_int32(0)
+    at = room.ctypes.data
+    st = _lib.codec_pages_fork(pages, page_size, num_seq, off.ctypes.data, ids.ctypes.data, tokens.ctypes.data, num_out,
+                               parents.ctypes.data, at, at + 4 * (num_out + 1), capacity, at + 4 * (num_out + 1 + capacity), byref(n))
+    if st != CODEC_OK:
+        return st, None, None, None
+    out_off = room[:num_out + 1].copy()                     # (the lists that live on do not keep the room)
+    out_ids = room[num_out + 1:num_out + 1 + out_off[-1]].copy()
+    runs = room[num_out + 1 + capacity:num_out + 1 + capacity + 5 * n.value].reshape(-1, 5)
+    return st, out_off, out_ids, runs
 
 
 def codec_pages_compact(pages, page_size: int, capacity: int):

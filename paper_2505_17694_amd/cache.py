@@ -180,6 +180,10 @@ class KVCache:
             if storage.nbytes() < need:
                 raise ValueError(f"pools of layer {layer}: the storage ends before the last page")
 
+    def _check_storages(self) -> None:
+        for layer in range(len(self.pools)):
+            self._check_storage(layer)
+
     def append(self, layer, q, k, v, positions, slots, rotary: Rotary = None, q_out: torch.Tensor = None, stream=None):
         """The step's tokens into ``layer``: queries and keys turned to ``positions``, keys and values stored at ``slots``
         (page * page_size + token; negative: not stored).  Returns the turned queries (``q_out``, which may be q itself);
@@ -246,8 +250,10 @@ class KVCache:
         pools of every layer.  No token may be written twice, or read and written."""
         if self.device.type != "cuda":
             raise ValueError(f"copy needs pools on a GPU, these are on {self.device}")
-        for layer in range(len(self.pools)):
-            self._check_storage(layer)
+        self._check_storages()
+        self._copy_on(runs, stream)
+
+    def _copy_on(self, runs, stream):
         s = _enter(self.device, stream)
         if s is None:
             with _on(self.device, stream) as s:
@@ -267,13 +273,12 @@ class KVCache:
         filled is copied on `stream` for all but the first (see codec_pages_fork)."""
         if self.device.type != "cuda":
             raise ValueError(f"fork needs pools on a GPU, these are on {self.device}")
-        for layer in range(len(self.pools)):
-            self._check_storage(layer)
+        self._check_storages()
         st, off, ids, runs = B.codec_pages_fork(self._pages, self.head.page_size, page_off, page_ids, tokens, parents)
         if st != B.CODEC_OK:
             raise B.CodecError(st, "codec_pages_fork")
         if len(runs):
-            self.copy(runs, stream)
+            self._copy_on(runs, stream)
         return off, ids
 
     def compact(self, stream=None) -> np.ndarray:
@@ -281,13 +286,12 @@ class KVCache:
         lists go on as ``moved[page_ids]``."""
         if self.device.type != "cuda":
             raise ValueError(f"compact needs pools on a GPU, these are on {self.device}")
-        for layer in range(len(self.pools)):
-            self._check_storage(layer)
+        self._check_storages()
         st, runs = B.codec_pages_compact(self._pages, self.head.page_size, self.num_pages // 2)
         if st != B.CODEC_OK:
             raise B.CodecError(st, "codec_pages_compact")
         moved = np.arange(self.num_pages, dtype=np.int32)
         moved[runs[:, 0]] = runs[:, 2]
         if len(runs):
-            self.copy(runs, stream)
+            self._copy_on(runs, stream)
         return moved
