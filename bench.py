@@ -59,7 +59,8 @@ def parse_args():
     ap.add_argument("--no-stream-calibration", action="store_true",
                     help="skip the plain streaming-read kernel (roofline.frac_of_measured_stream is then null)")
     ap.add_argument("--sweep", default="", help="run one of the paper-shaped synthetic sweeps instead of the "
-                    "configurations: seqlen, batch, depth, ratio, shape, ablation, granularity")
+                    "configurations: seqlen, batch, depth, ratio, shape, ablation, granularity, draft, draft_masked, "
+                    "beam_search (whole decoding steps of beam searches)")
     ap.add_argument("--copy-calibration", action="store_true",
                     help="also run a plain 1 GiB device copy 3 times (reference for scaling FETCH_SIZE / "
                          "WRITE_SIZE counters when the run is profiled)")
@@ -366,6 +367,88 @@ def run_sweep(args):
     print(json.dumps(line))
 
 
+def run_beam_sweep(args):
+    """Decoding steps of beam searches, one layer of 32/8 heads: every call of a step on its own and all together.
+
+    A step puts the beams' new tokens into the cache (rotary positions), runs the attention over the prefix
+    forest, selects the continuations from random logits, moves the beams' token histories and forks
+    and prunes the page lists of their leaves.
+    """
+    import numpy as np
+    import torch
+    import paper_2505_17694_amd as C
+    from workloads import make_workload
+    from workloads.sweeps import sweep_points, sweep_head, SWEEP_SEED
+
+    head, vocab, history_len = sweep_head(), 32000, 8192
+    if args.layout == "hktd":
+        sys.exit("--sweep beam_search: pools of K and V apart (thd, htd)")
+    steps = max(5, min(args.steps, 20))
+    out_points = []
+    for label, forest in sweep_points("beam_search"):
+        w = make_workload(label, forest, head, SWEEP_SEED, device="cuda:0", layout=args.layout, spare_pages=4096)
+        leaves = np.asarray(forest.req_node)
+        searches, rows = 16, len(leaves)
+        beams, p, ps = rows // 16, w.paged, head.page_size
+        cache = C.KVCache(head, p.num_pages, layout=args.layout, pools=[(w.k_pool, w.v_pool)])
+        cache.hold(p.page_ids)
+        rotary = C.Rotary(head.head_dim, theta=500000.0)
+        plan = C.PlannedAttention(forest, p, head, share=2, schedule=2, fused=2, extensions=3)
+        lens = np.asarray(forest.node_len)[leaves]
+        lists = [p.page_ids[p.node_page_off[n]:p.node_page_off[n + 1]] for n in leaves]
+        off, ids = np.cumsum([0] + [len(x) for x in lists]), np.concatenate(lists)
+        gen = torch.Generator(device="cuda:0")
+        gen.manual_seed(SWEEP_SEED)
+        qkv = torch.randn((rows, head.num_q_heads + 2 * head.num_kv_heads, head.head_dim), generator=gen, device="cuda:0").to(head.torch_dtype)
+        q, k, v = qkv.split([head.num_q_heads, head.num_kv_heads, head.num_kv_heads], 1)
+        at = torch.from_numpy(2048 + 4096 + lens.astype(np.int64) - 1).cuda()
+        slots = torch.from_numpy(np.array([x[(n - 1) // ps] * ps + (n - 1) % ps for x, n in zip(lists, lens)], np.int64)).cuda()
+        logits = (3 * torch.randn((searches, beams, vocab), generator=gen, device="cuda:0")).to(head.torch_dtype)
+        scores = -10 * torch.rand((searches, beams), generator=gen, device="cuda:0")
+        history = torch.zeros((searches, beams, history_len), dtype=torch.int32, device="cuda:0")
+        out, q_out = torch.empty((rows, head.num_q_heads, head.head_dim), dtype=head.torch_dtype, device="cuda:0"), torch.empty_like(w.q)
+        twice = np.repeat(np.arange(rows), 2)               # every leaf goes on twice, and one of the two is pruned
+        state = {}
+
+        def select():
+            state["beams"] = C.beam_select(logits, scores, beams)[1]
+
+        def fork():
+            new_off, new_ids = cache.fork(off, ids, lens, twice)
+            cache.fork(new_off, new_ids, lens[twice], np.arange(rows) * 2)
+
+        calls = {"append": lambda: cache.append(0, q, k, v, at, slots, rotary, q_out=q_out),
+                 "attention": lambda: plan.decode(q_out, w.k_pool, w.v_pool, out), "select": select,
+                 "reorder": lambda: C.beam_reorder([history], state["beams"]), "fork_and_prune": fork}
+
+        def step():
+            for call in calls.values():
+                call()
+
+        def time_of(call):
+            for _ in range(args.warmup):
+                call()
+            torch.cuda.synchronize()
+            t0 = time.perf_counter()
+            for _ in range(steps):
+                call()
+            torch.cuda.synchronize()
+            return round((time.perf_counter() - t0) / steps * 1e6, 2)
+
+        step()
+        pt = {"point": label, "rows": rows, "us_per_step": time_of(step), "us_per_call": {n: time_of(c) for n, c in calls.items()}}
+        print(f"[sweep beam_search] {label}: step {pt['us_per_step']} us, " + ", ".join(f"{n} {t} us" for n, t in pt["us_per_call"].items()),
+              file=sys.stderr, flush=True)
+        out_points.append(pt)
+        plan.close()
+    print(json.dumps({"metric": "sweep_beam_search_us_per_step", "value": out_points[-1]["us_per_step"], "unit": "us",
+                      "n_gpus": 1, "steps": steps, "warmup": args.warmup, "higher_is_better": False, "scaling": "weak",
+                      "vs_baseline": None, "dtype": "bf16", "data": "synthetic",
+                      "config": {"workload": "sweep:beam_search", "q_heads": head.num_q_heads, "kv_heads": head.num_kv_heads,
+                                 "head_dim": head.head_dim, "page_size": head.page_size, "vocab": vocab, "kv_layout": args.layout},
+                      "points": out_points}))
+
+
 def cpu_baseline(w, gpu_out, seconds):
     """The fp64 oracle, as it stands, on a bounded sample of (request, head) pairs of the workload."""
     import numpy as np
@@ -420,7 +503,7 @@ def main():
         sys.exit(2)
 
     if args.sweep:
-        run_sweep(args)
+        run_beam_sweep(args) if args.sweep == "beam_search" else run_sweep(args)
         return
 
     stream = None

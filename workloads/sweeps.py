@@ -18,16 +18,19 @@ Forests only; tensors come from ``make_workload`` like every other input.  Each 
                use case
 * ``draft_masked``  the same verification steps with the drafted tokens of a sequence packed into one
                node and a visibility mask per query (Sec. 4.1) in place of the one-token nodes
+* ``beam_search``  16 searches of 2, 4 and 8 beams: a shared 2048-token prompt, 4096 tokens per search and a
+               leaf of 1 .. 127 generated tokens per beam; for a whole decoding step (new tokens into the
+               cache, attention, selection, states and pages of the beams that go on)
 """
 from __future__ import annotations
 
 from typing import List, Tuple
 
-from .trees import (Forest, two_level_forest, full_kary_forest, degenerate_forest, unshared_forest,
+from .trees import (Forest, two_level_forest, three_level_forest, full_kary_forest, degenerate_forest, unshared_forest,
                     draft_tree_forest, draft_masked_forest)
 from .tensors import HeadConfig, DTYPE_BF16
 
-SWEEP_NAMES = ["seqlen", "batch", "depth", "ratio", "shape", "ablation", "draft", "draft_masked"]
+SWEEP_NAMES = ["seqlen", "batch", "depth", "ratio", "shape", "ablation", "draft", "draft_masked", "beam_search"]
 SWEEP_SEED = 2000
 
 
@@ -70,4 +73,6 @@ def sweep_points(name: str) -> List[Tuple[str, Forest]]:
         return [(f"drafted={t}", draft_tree_forest(2048, [8192] * 16, t, SWEEP_SEED + t)) for t in (0, 4, 16, 64)]
     if name == "draft_masked":
         return [(f"drafted={t}", draft_masked_forest(2048, [8192] * 16, t, SWEEP_SEED + t)) for t in (0, 4, 16, 64)]
+    if name == "beam_search":
+        return [(f"beams={b}", three_level_forest(2048, [4096] * 16, b, [1 + (37 * i) % 127 for i in range(16 * b)])) for b in (2, 4, 8)]
     raise KeyError(name)
