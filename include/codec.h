@@ -581,7 +581,7 @@ int codec_cache_copy(const codec_head_config *head, const codec_kv_layout *layou
  */
 
 typedef struct {
-    int32_t batch;              /* searches, >= 0                                               */
+    int32_t batch;              /* searches, >= 0; with all their beams at most 2^22            */
     int32_t beams;              /* beams of a search, 1..64                                     */
     int32_t vocab;              /* 1..2^24                                                      */
     int32_t k;                  /* continuations wanted, 1..64, at most beams * vocab           */
@@ -625,8 +625,9 @@ typedef struct {
  * The states of the beams that go on: row (s, j) of every dst becomes row (s, beams[s][j]) of its src.
  *   states      host array [num_states], borrowed for the call only; any types, row sizes and alignments (a
  *               call moves them in the largest unit that divides them all).  From its first row to its last, no dst
- *               may overlap a src
- *   beams       device [batch][beams_out]; a row whose entry is not in 0..beams_in - 1 is left as it was
+ *               may overlap a src; no two rows of the dsts may
+ *               overlap
+ *   beams       device [batch][beams_out], at most 2^22 in all; a row whose entry is not in 0..beams_in - 1 is left as it was
  * Enqueued on `stream` without synchronising.
  */
 int codec_beam_reorder(const codec_state *states, int32_t num_states, const int32_t *beams, int32_t batch,

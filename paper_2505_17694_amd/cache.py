@@ -27,6 +27,8 @@ def _device(device) -> torch.device:
 def _on(device: torch.device, stream):
     """Makes `device` and `stream` the current ones; the handle of the stream.  What is allocated meanwhile belongs to the
     stream that uses it."""
+    if stream is not None and stream.device != device:
+        raise ValueError(f"stream: on {stream.device}, the tensors are on {device}")
     with torch.cuda.device(device), torch.cuda.stream(stream):
         yield _current_stream(device)
 

@@ -2,8 +2,8 @@
 #include "operators.hpp"
 
 #include <algorithm>
-#include <climits>
 #include <cmath>
+#include <cstdlib>
 #include <new>
 #include <vector>
 
@@ -58,6 +58,15 @@ int64_t pool_span(const codec_head_config &h, const codec_kv_layout &l)
     if (l.page_stride % 8 || l.token_stride % 8 || l.head_stride % 8) return -1;
     Extent dims[] = {{l.num_pages, l.page_stride}, {h.page_size, l.token_stride}, {h.num_kv_heads, l.head_stride}};
     return separate_span(h.head_dim, dims);
+}
+
+// Whether two pools of this layout have no element in common: apart in memory, or one between the parts of the other (K and V
+// side by side).
+bool pools_apart(const codec_head_config &h, const codec_kv_layout &l, const void *a, const void *b)
+{
+    const int64_t distance = std::abs(static_cast<const char *>(a) - static_cast<const char *>(b)) / 2;
+    Extent dims[] = {{l.num_pages, l.page_stride}, {h.page_size, l.token_stride}, {h.num_kv_heads, l.head_stride}, {2, distance}};
+    return separate_span(h.head_dim, dims) >= 0;
 }
 
 struct Range { const char *begin, *end; };
@@ -182,7 +191,7 @@ bool runs_collide(const codec_run *runs, int32_t n, int32_t page_size)
 int check_beams(const codec_beam_config &c)
 {
     if (c.batch < 0 || c.beams < 1 || c.beams > 64 || c.vocab < 1 || c.vocab > (1 << 24) || c.k < 1 || c.k > 64 ||
-        c.k > int64_t(c.beams) * c.vocab || int64_t(c.batch) * c.beams > INT32_MAX)
+        c.k > int64_t(c.beams) * c.vocab || int64_t(c.batch) * c.beams > (1 << 22))
         return CODEC_ERR_INVALID_ARGUMENT;
     if (c.dtype != CODEC_DTYPE_FP16 && c.dtype != CODEC_DTYPE_BF16 && c.dtype != CODEC_DTYPE_FP32) return CODEC_ERR_UNSUPPORTED;
     return CODEC_OK;
@@ -295,7 +304,7 @@ int codec_append(const codec_head_config *head, const codec_rotary_config *rotar
     if (num_tokens == 0) return CODEC_OK;
     if (rotary)
         if (int st = check_rotary(*rotary, head->head_dim, positions)) return st;
-    if (!slots || !k_pages || !v_pages || !aligned16(k_pages) || !aligned16(v_pages) || k_pages == v_pages) return CODEC_ERR_INVALID_ARGUMENT;
+    if (!slots || !k_pages || !v_pages || !aligned16(k_pages) || !aligned16(v_pages) || !pools_apart(*head, *layout, k_pages, v_pages)) return CODEC_ERR_INVALID_ARGUMENT;
     const int64_t t = num_tokens, d = head->head_dim, hq = head->num_q_heads, h = head->num_kv_heads;
     if (!rows_ok(k, t, h) || !rows_ok(v, t, h) || (q && (!rows_ok(q, t, hq) || !rows_ok(q_out, t, hq)))) return CODEC_ERR_INVALID_ARGUMENT;
     for (const void *pages : {k_pages, v_pages}) {
@@ -342,7 +351,7 @@ int codec_cache_copy(const codec_head_config *head, const codec_kv_layout *layou
     if (num_runs == 0) return CODEC_OK;
     if (!k_pages || !v_pages || !runs) return CODEC_ERR_INVALID_ARGUMENT;
     for (int32_t l = 0; l < num_layers; ++l)
-        if (!k_pages[l] || !v_pages[l] || !aligned16(k_pages[l]) || !aligned16(v_pages[l]) || k_pages[l] == v_pages[l]) return CODEC_ERR_INVALID_ARGUMENT;
+        if (!k_pages[l] || !v_pages[l] || !aligned16(k_pages[l]) || !aligned16(v_pages[l]) || !pools_apart(*head, *layout, k_pages[l], v_pages[l])) return CODEC_ERR_INVALID_ARGUMENT;
     const int32_t ps = head->page_size;
     for (int32_t i = 0; i < num_runs; ++i) {
         const codec_run &r = runs[i];
@@ -429,7 +438,7 @@ int codec_beam_select(const codec_beam_config *config, const void *logits, int64
 int codec_beam_reorder(const codec_state *states, int32_t num_states, const int32_t *beams, int32_t batch, int32_t beams_in,
                        int32_t beams_out, void *stream)
 {
-    if (num_states < 0 || batch < 0 || beams_in < 1 || beams_out < 1 || int64_t(batch) * beams_out > INT32_MAX) return CODEC_ERR_INVALID_ARGUMENT;
+    if (num_states < 0 || batch < 0 || beams_in < 1 || beams_out < 1 || int64_t(batch) * beams_out > (1 << 22)) return CODEC_ERR_INVALID_ARGUMENT;
     if (num_states == 0 || batch == 0) return CODEC_OK;
     if (!states || !beams) return CODEC_ERR_INVALID_ARGUMENT;
     struct Touched { Range range; bool written; };

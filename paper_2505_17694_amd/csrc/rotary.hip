@@ -65,6 +65,45 @@ __device__ __forceinline__ uint32_t narrow2(float lo, float hi)
 template <class T>
 __device__ __forceinline__ T one_of(bool first, bool second, T a, T b, T c) { return first ? a : second ? b : c; }
 
+// Where a token's rows come from and go to: its queries, its keys, its values.
+struct TokenRows {
+    const char *q, *k, *v;
+    char *q_out, *k_slot, *v_slot;
+    int stored;                     // rows that go anywhere: without a slot the queries only
+
+    __device__ __forceinline__ TokenRows(const RotaryParams &P, int64_t token)
+    {
+        q = P.q.data + token * P.q.token_stride;
+        k = P.k.data + token * P.k.token_stride;
+        v = P.v.data + token * P.v.token_stride;
+        q_out = P.q_out.data + token * P.q_out.token_stride;
+        k_slot = v_slot = nullptr;
+        stored = P.q_heads;
+        if (!P.kv_heads) return;
+        const int64_t slot = P.slots[token];
+        if (slot < 0 || slot >= P.num_slots) return;
+        const int64_t at = (slot >> P.page_shift) * P.page_stride + (slot & ((int64_t(1) << P.page_shift) - 1)) * P.slot_stride;
+        k_slot = P.k_pages + at;
+        v_slot = P.v_pages + at;
+        stored += 2 * P.kv_heads;
+    }
+    // Loads have no branches around them, so that the wait for one round's leaves the next round's under way: a row that goes
+    // nowhere reads the last one that does.
+    __device__ __forceinline__ const char *source(const RotaryParams &P, int row) const
+    {
+        row = row < stored ? row : stored - 1;
+        const bool query = row < P.q_heads, key = row < P.q_heads + P.kv_heads;
+        const int64_t stride = one_of(query, key, P.q.head_stride, P.k.head_stride, P.v.head_stride);
+        return one_of(query, key, q, k, v) + (row - one_of(query, key, 0, P.q_heads, P.q_heads + P.kv_heads)) * stride;
+    }
+    __device__ __forceinline__ char *target(const RotaryParams &P, int row) const
+    {
+        const bool query = row < P.q_heads, key = row < P.q_heads + P.kv_heads;
+        const int64_t stride = one_of(query, true, P.q_out.head_stride, P.head_stride, P.head_stride);
+        return one_of(query, key, q_out, k_slot, v_slot) + (row - one_of(query, key, 0, P.q_heads, P.q_heads + P.kv_heads)) * stride;
+    }
+};
+
 // A copy with some arithmetic on the way, bound by HBM.  A lane takes 16 bytes of a row and 16 others that the same cosines and
 // sines serve: the other halves of its eight pairs, or, with neighbouring pairs, the same four pairs of another row, so that
 // the lanes of a wave write consecutive memory.  It keeps the cosines and sines for all rows it takes: a wave takes
@@ -91,41 +130,17 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryParams P, uint32_t sp
     const int first = INTERLEAVED || turns ? unit * 8 : unit * 16;                                  // channels
     const int second = INTERLEAVED ? first : turns ? first + turning : first + 8;
 
-    const char *q = P.q.data + int64_t(token) * P.q.token_stride, *k = P.k.data + int64_t(token) * P.k.token_stride,
-               *v = P.v.data + int64_t(token) * P.v.token_stride;
-    char *q_out = P.q_out.data + int64_t(token) * P.q_out.token_stride;
-    const int rows = P.q_heads + 2 * P.kv_heads;
-    char *k_slot = nullptr, *v_slot = nullptr;
-    if (P.kv_heads) {
-        const int64_t slot = P.slots[token];
-        if (slot >= 0 && slot < P.num_slots) {
-            const int64_t at = (slot >> P.page_shift) * P.page_stride + (slot & ((int64_t(1) << P.page_shift) - 1)) * P.slot_stride;
-            k_slot = P.k_pages + at;
-            v_slot = P.v_pages + at;
-        }
-    }
-    const int stored = k_slot ? rows : P.q_heads;       // rows that go anywhere
-    if (stored == 0) return;
+    const TokenRows places(P, token);
+    if (places.stored == 0) return;
     auto row_of = [&](uint32_t round, int other) { return int(round * kRows) + sub + other * kOther; };
-    // Loads have no branches around them, so that the wait for one round's leaves the next round's under way: a row that goes
-    // nowhere reads the last one that does.
     auto load_row = [&](int row, int channel) -> Vec {
-        row = row < stored ? row : stored - 1;
-        const bool query = row < P.q_heads, key = row < P.q_heads + P.kv_heads;
-        const char *base = one_of(query, key, q, k, v);
-        const int64_t stride = one_of(query, key, P.q.head_stride, P.k.head_stride, P.v.head_stride);
-        const int head = row - one_of(query, key, 0, P.q_heads, P.q_heads + P.kv_heads);
-        const Vec *at = reinterpret_cast<const Vec *>(base + head * stride + 2 * channel);
+        const Vec *at = reinterpret_cast<const Vec *>(places.source(P, row) + 2 * channel);
         if constexpr (LARGE) return __builtin_nontemporal_load(at);
         else return *at;
     };
     auto store_row = [&](int row, int channel, Vec x) {
-        const bool query = row < P.q_heads, key = row < P.q_heads + P.kv_heads;
-        char *base = one_of(query, key, q_out, k_slot, v_slot);
-        const int64_t stride = one_of(query, true, P.q_out.head_stride, P.head_stride, P.head_stride);
-        const int head = row - one_of(query, key, 0, P.q_heads, P.q_heads + P.kv_heads);
-        Vec *at = reinterpret_cast<Vec *>(base + head * stride + 2 * channel);
-        if (row >= stored) return;
+        if (row >= places.stored) return;
+        Vec *at = reinterpret_cast<Vec *>(places.target(P, row) + 2 * channel);
         if constexpr (LARGE) __builtin_nontemporal_store(x, at);
         else *at = x;
     };
@@ -179,85 +194,121 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryParams P, uint32_t sp
     }
 }
 
-// Halves whose pairs do not come in eights: one thread per pair of channels of a row, the pairs that turn first, then the
-// others two by two.  Rows of a token: its queries, its keys, its values.
-template <int DT>
-__global__ __launch_bounds__(256) void rotary_pair_kernel(RotaryParams P)
+// Halves whose pairs do not come in eights (rotary_dim no multiple of 16): a lane takes the eight channels of one piece of 16 bytes,
+// as if neighbours were paired, and loads their other halves too, from before and behind, at any alignment.  All of a row's
+// loads come before its stores, in one wave, which a call in place needs.
+template <int DT, int U>
+__global__ __launch_bounds__(256) void rotary_uneven_kernel(RotaryParams P, uint32_t splits, uint32_t rounds)
 {
-    const int pairs = P.head_dim / 2, turning = P.rotary_dim / 2;
-    const int rows = P.q_heads + 2 * P.kv_heads;
-    const int64_t total = P.num_tokens * rows * pairs;
-    for (int64_t at = int64_t(blockIdx.x) * 256 + threadIdx.x; at < total; at += int64_t(gridDim.x) * 256) {
-        const int pair = int(at % pairs);
-        const int64_t token_row = at / pairs;
-        const int row = int(token_row % rows);
-        const int64_t token = token_row / rows;
-        const bool query = row < P.q_heads, value = row >= P.q_heads + P.kv_heads;
-        const int head = query ? row : value ? row - P.q_heads - P.kv_heads : row - P.q_heads;
-        const RowsView &in = query ? P.q : value ? P.v : P.k;
-        const uint16_t *from = reinterpret_cast<const uint16_t *>(in.data + token * in.token_stride + head * in.head_stride);
-        uint16_t *to;
-        if (query) {
-            to = reinterpret_cast<uint16_t *>(P.q_out.data + token * P.q_out.token_stride + head * P.q_out.head_stride);
-        } else {
-            const int64_t slot = P.slots[token];
-            if (slot < 0 || slot >= P.num_slots) continue;
-            const int64_t page = slot >> P.page_shift, in_page = slot & ((int64_t(1) << P.page_shift) - 1);
-            to = reinterpret_cast<uint16_t *>((value ? P.v_pages : P.k_pages) + page * P.page_stride + in_page * P.slot_stride + head * P.head_stride);
+    constexpr int kLanes = 2 * U, kRows = 64 / U, kOther = kRows / 2;
+    const int lane = threadIdx.x & 63, channel = lane % kLanes * 8, sub = lane / kLanes;
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+    const uint32_t token = wave / splits, part = wave % splits;
+    if (token >= P.num_tokens) return;
+    const TokenRows places(P, token);
+    if (places.stored == 0) return;
+
+    typedef uint32_t __attribute__((ext_vector_type(4), aligned(2))) AnyPiece;
+    const int half = P.rotary_dim / 2, d = P.head_dim;
+    // other halves of channels below `half`, from channel + half on; of those above, from channel - half on.  A piece that would
+    // reach over the row's end or begin starts at the nearest place that does not, and is shifted.
+    const bool low = channel < half, high = channel + 7 >= half && channel < P.rotary_dim;
+    const int behind = low ? (channel + half < d - 8 ? channel + half : d - 8) : 0, behind_by = low ? channel + half - behind : 0;
+    const int before = high && channel > half ? channel - half : 0, before_by = high && channel < half ? half - channel : 0;
+    float c[8], s[8];
+    const double position = double(P.positions[token]);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const int x = channel + e;
+        const Turn t = turn_of(position * P.turns[x < half ? x : x < P.rotary_dim ? x - half : 0]);
+        c[e] = t.cos * P.magnitude;
+        s[e] = t.sin * (x < half ? -P.magnitude * P.sign : P.magnitude * P.sign);
+    }
+    for (uint32_t round = part; round < rounds; round += splits) {
+        Vec own[2], a[2], b[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const char *from = places.source(P, int(round * kRows) + sub + i * kOther);
+            own[i] = *reinterpret_cast<const Vec *>(from + 2 * channel);
+            a[i] = *reinterpret_cast<const AnyPiece *>(from + 2 * behind);
+            b[i] = *reinterpret_cast<const AnyPiece *>(from + 2 * before);
         }
-        const bool turns = !value && pair < turning;
-        const int first = turns ? pair : value ? 2 * pair : P.rotary_dim + 2 * (pair - turning);
-        const int second = turns ? first + turning : first + 1;
-        uint16_t a = from[first], b = from[second];
-        if (turns) {
-            const Turn t = turn_of(double(P.positions[token]) * P.turns[pair]);
-            const float c = t.cos * P.magnitude, s = t.sin * (P.magnitude * P.sign);
-            const float x = widen<DT>(a), y = widen<DT>(b);
-            a = narrow<DT>(x * c - y * s);
-            b = narrow<DT>(y * c + x * s);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int row = int(round * kRows) + sub + i * kOther;
+            if (row >= places.stored) continue;
+            Vec out = own[i];
+            if (row < P.q_heads + P.kv_heads) {
+                typedef unsigned __int128 Bits;
+                const Vec lows = __builtin_bit_cast(Vec, __builtin_bit_cast(Bits, a[i]) >> (16 * behind_by));
+                const Vec highs = __builtin_bit_cast(Vec, __builtin_bit_cast(Bits, b[i]) << (16 * before_by));
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    uint32_t turned[2];
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const int e = 2 * w + j, x = channel + e;
+                        const uint16_t mine = uint16_t(own[i][w] >> (16 * j)), other = uint16_t((x < half ? lows[w] : highs[w]) >> (16 * j));
+                        const uint16_t y = narrow<DT>(widen<DT>(mine) * c[e] + widen<DT>(other) * s[e]);
+                        turned[j] = x < P.rotary_dim ? y : mine;
+                    }
+                    out[w] = turned[0] | turned[1] << 16;
+                }
+            }
+            *reinterpret_cast<Vec *>(places.target(P, row) + 2 * channel) = out;
         }
-        to[first] = a;
-        to[second] = b;
     }
 }
 
 }  // namespace
 
-int launch_rotary(const RotaryParams &p, int dtype, bool interleaved, void *stream)
+namespace {
+
+int launch_slice(const RotaryParams &p, int dtype, bool interleaved, hipStream_t s)
 {
-    hipStream_t s = static_cast<hipStream_t>(stream);
     const int64_t rows = p.q_heads + 2 * p.kv_heads;
-    // pairs of halves are taken eight at a time: 16 channels that turn, or a multiple of them
-    if (!interleaved && p.rotary_dim % 16) {
-        const int64_t blocks = (p.num_tokens * rows * (p.head_dim / 2) + 255) / 256;
-        const dim3 grid(unsigned(blocks < (int64_t(1) << 22) ? blocks : int64_t(1) << 22));
-        if (dtype == CODEC_DTYPE_FP16) hipLaunchKernelGGL(rotary_pair_kernel<CODEC_DTYPE_FP16>, grid, dim3(256), 0, s, p);
-        else                           hipLaunchKernelGGL(rotary_pair_kernel<CODEC_DTYPE_BF16>, grid, dim3(256), 0, s, p);
-        return int(hipGetLastError());
-    }
     // a wave for every token, or as many as it takes to have 32 on every CU
     const int64_t at_once = 64 / (p.head_dim / 16), rounds = (rows + at_once - 1) / at_once;
     int64_t splits = (8192 + p.num_tokens - 1) / p.num_tokens;
     if (splits > rounds) splits = rounds;
     const dim3 grid(unsigned((p.num_tokens * splits + 3) / 4));
     const bool large = 4.0 * double(p.num_tokens) * double(rows) * p.head_dim > kLargeBytes;
+    const bool uneven = !interleaved && p.rotary_dim % 16;
     const uint32_t n = uint32_t(splits), r = uint32_t(rounds);
-    auto launch_dim = [&](auto dt, auto layout, auto u) {
+    auto launch_dim = [&](auto dt, auto u) {
         constexpr int DT = decltype(dt)::value, U = decltype(u)::value;
-        constexpr bool I = decltype(layout)::value;
-        if (large) hipLaunchKernelGGL((rotary_kernel<DT, I, U, true>), grid, dim3(256), 0, s, p, n, r);
-        else       hipLaunchKernelGGL((rotary_kernel<DT, I, U, false>), grid, dim3(256), 0, s, p, n, r);
+        if (uneven)                    hipLaunchKernelGGL((rotary_uneven_kernel<DT, U>), grid, dim3(256), 0, s, p, n, r);
+        else if (interleaved && large) hipLaunchKernelGGL((rotary_kernel<DT, true, U, true>), grid, dim3(256), 0, s, p, n, r);
+        else if (interleaved)          hipLaunchKernelGGL((rotary_kernel<DT, true, U, false>), grid, dim3(256), 0, s, p, n, r);
+        else if (large)                hipLaunchKernelGGL((rotary_kernel<DT, false, U, true>), grid, dim3(256), 0, s, p, n, r);
+        else                           hipLaunchKernelGGL((rotary_kernel<DT, false, U, false>), grid, dim3(256), 0, s, p, n, r);
     };
-    auto launch = [&](auto dt, auto layout) {
-        if (p.head_dim == 64)       launch_dim(dt, layout, std::integral_constant<int, 4>{});
-        else if (p.head_dim == 128) launch_dim(dt, layout, std::integral_constant<int, 8>{});
-        else                        launch_dim(dt, layout, std::integral_constant<int, 16>{});
+    auto launch = [&](auto dt) {
+        if (p.head_dim == 64)       launch_dim(dt, std::integral_constant<int, 4>{});
+        else if (p.head_dim == 128) launch_dim(dt, std::integral_constant<int, 8>{});
+        else                        launch_dim(dt, std::integral_constant<int, 16>{});
     };
-    using f16 = std::integral_constant<int, CODEC_DTYPE_FP16>;
-    using b16 = std::integral_constant<int, CODEC_DTYPE_BF16>;
-    if (dtype == CODEC_DTYPE_FP16) interleaved ? launch(f16{}, std::true_type{}) : launch(f16{}, std::false_type{});
-    else                           interleaved ? launch(b16{}, std::true_type{}) : launch(b16{}, std::false_type{});
+    if (dtype == CODEC_DTYPE_FP16) launch(std::integral_constant<int, CODEC_DTYPE_FP16>{});
+    else                           launch(std::integral_constant<int, CODEC_DTYPE_BF16>{});
     return int(hipGetLastError());
+}
+
+}  // namespace
+
+// A launch takes 2^24 tokens: its threads are counted in 32 bits.
+int launch_rotary(const RotaryParams &p, int dtype, bool interleaved, void *stream)
+{
+    constexpr int64_t kSlice = int64_t(1) << 24;
+    for (int64_t at = 0; at < p.num_tokens; at += kSlice) {
+        RotaryParams part = p;
+        part.num_tokens = p.num_tokens - at < kSlice ? p.num_tokens - at : kSlice;
+        for (RowsView *r : {&part.q, &part.q_out, &part.k, &part.v})
+            if (r->data) r->data += at * r->token_stride;
+        if (p.positions) part.positions = p.positions + at;
+        if (p.slots) part.slots = p.slots + at;
+        if (int e = launch_slice(part, dtype, interleaved, static_cast<hipStream_t>(stream))) return e;
+    }
+    return 0;
 }
 
 }  // namespace codec

@@ -105,7 +105,8 @@ def test_append_refusals():
                 dict(layout=(8, 2048, 128, 2048)), dict(layout=(8, 4096, 128, 128)), dict(layout=(1 << 32, 4096, 128, 2048)),
                 dict(k=(at + 2, 256, 128)), dict(k=(at, 256, 100)), dict(k=(base * 2 + 4096, 256, 128)), dict(v=(base * 3, 256, 128)),
                 dict(q=(base * 3, 1024, 128), q_out=(base * 3, 1024, 128)), dict(q_out=(at, 1024, 128)),
-                dict(q_out=(base + 1024, 1024, 128))):
+                dict(q_out=(base + 1024, 1024, 128)), dict(head=(8, 4097, 128, 1, 16)),
+                dict(vp=base * 2 + 256), dict(vp=base * 2 + 16 * 128 * 2), dict(vp=base * 2 + 4096 * 2)):
         assert status(**bad) == C.CODEC_ERR_INVALID_ARGUMENT, bad
     for bad in (dict(head=(8, 2, 96, 1, 16)), dict(head=(8, 2, 128, 2, 16)), dict(head=(8, 2, 128, 1, 24)), dict(head=(8, 2, 128, 1, 8))):
         assert status(**bad) == C.CODEC_ERR_UNSUPPORTED, bad
@@ -266,6 +267,39 @@ def test_append_pools_with_other_strides(kind):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("r", [2, 6, 14, 18, 30, 34, 58, 60, 62, 122, 124, 126])
+@pytest.mark.parametrize("d", [64, 128])
+def test_append_halves_of_any_size_in_place(d, r):
+    """Other halves before and behind a lane's channels, over both ends of the row; queries onto themselves."""
+    if r > d:
+        return
+    run_append(19, 7, 2, d, DTYPE_FP16, 16, "thd", r, in_place=True, fused=True, seed=r)
+    run_append(700, 3, 1, d, DTYPE_BF16, 64, "htd", r, seed=r)
+
+
+@pytest.mark.gpu
+def test_append_beyond_four_gigabytes():
+    """Pools of 8.6 GB each: slots, pages and byte offsets pass 32 bits."""
+    head = HeadConfig(2, 1, 64, DTYPE_BF16, 16)
+    pages = 1 << 22
+    cache = C.KVCache(head, pages, device=DEV)
+    gen = torch.Generator().manual_seed(3)
+    x = rows(gen, DTYPE_BF16, 5, 4, 64).to(DEV)
+    slots = torch.tensor([pages * 16 - 1, 0, (1 << 31) // 64, pages * 8 + 3, pages * 16 - 17], device=DEV)
+    rot = C.Rotary(64, device=DEV)
+    positions = torch.arange(5, device=DEV)
+    cache.append(0, x[:, :2], x[:, 2:3], x[:, 3:], positions, slots, rot)
+    want = rot.apply(x[:, 2:3], positions)[:, 0]
+    k, v = (p[slots // 16, 0, slots % 16] for p in cache.pools[0])
+    assert torch.equal(k, want) and torch.equal(v, x[:, 3])
+    cache.copy([(pages - 1, 15, 7, 2, 1), (pages // 2, 3, pages - 2, 4, 1)])
+    k, v = cache.pools[0]
+    assert torch.equal(k[7, 0, 2], want[0]) and torch.equal(v[pages - 2, 0, 4], x[3, 3])
+    del cache, k, v
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.gpu
 def test_append_values_that_are_not_numbers():
     """Infinities and NaN stay in their pairs; channels that pass keep their bits."""
     for r, interleaved in ((32, False), (32, True), (20, False), (22, True)):
@@ -372,3 +406,14 @@ def test_append_tensor_refusals():
     cache.pools[0][1].untyped_storage().resize_(16)
     with pytest.raises(ValueError):
         cache.append(0, q, k, k.clone(), i, i, rot)
+    both = torch.zeros(8, 2, 2, 16, 128, dtype=torch.bfloat16, device=DEV)
+    for pools, apart in (((both[:, :, 0], both[:, :, 1]), True), ((both[:, :, 0], both[:, :, 0]), False), ((both[:7, :, 0], both[1:, :, 0]), False)):
+        side = C.KVCache(head, len(pools[0]), device=DEV, pools=[pools])
+        if apart:
+            side.append(0, None, k, k.clone(), i, torch.arange(3, device=DEV), rot)
+            side.copy([(0, 0, 1, 0, 3)])
+        else:
+            with pytest.raises(C.CodecError):
+                side.append(0, None, k, k.clone(), i, torch.arange(3, device=DEV), rot)
+            with pytest.raises(C.CodecError):
+                side.copy([(0, 0, 1, 0, 3)])

@@ -43,7 +43,7 @@ def test_select_refusals():
         return C.codec_beam_select(cfg, a["logits"], *a["strides"], a["scores"], a["finished"], *a["outs"], a["workspace"], a["room"])
     assert status(batch=0) == C.CODEC_OK
     for bad in (dict(batch=-1), dict(beams=0), dict(beams=65), dict(vocab=0), dict(vocab=(1 << 24) + 1), dict(k=0), dict(k=65), dict(beams=1, vocab=7),
-                dict(batch=1 << 30, beams=4), dict(eos=-1), dict(eos=1000), dict(logits=0), dict(logits=4097), dict(logits=4098, dtype=2), dict(strides=(-1, 1000)),
+                dict(batch=1 << 20, beams=5, k=5), dict(eos=-1), dict(eos=1000), dict(logits=0), dict(logits=4097), dict(logits=4098, dtype=2), dict(strides=(-1, 1000)),
                 dict(strides=(4000, -1)), dict(strides=(1 << 60, 0)), dict(scores=0), dict(outs=(0, 4096, 4096)), dict(outs=(4096, 0, 4096)),
                 dict(outs=(4096, 4096, 0)), dict(workspace=0), dict(workspace=(1 << 20) + 8)):
         assert status(**bad) == C.CODEC_ERR_INVALID_ARGUMENT, bad
@@ -218,6 +218,25 @@ def test_select_large():
     gen = torch.Generator().manual_seed(7)
     check(draw(gen, 16, 8, 131072, dtype=BF16), -torch.rand(16, 8, generator=gen) * 10, 16)
     check(draw(gen, 1, 4, 1 << 20, dtype=FP32), -torch.rand(1, 4, generator=gen) * 10, 8)
+
+
+@pytest.mark.gpu
+def test_select_beyond_four_gigabytes():
+    """64 beams of 2^24 logits: 4.3 GB; the best tokens are planted, the sum is known."""
+    beams, vocab = 64, 1 << 24
+    x = torch.zeros(1, beams, vocab, device=DEV)
+    planted = [(b, (b * 262139 + 17) % vocab) for b in range(beams)]
+    for b, t in planted:
+        x[0, b, t] = 20.0
+    x[0, 5, vocab - 1] = 20.0                           # the last token of a beam, behind an equal one
+    scores = -torch.arange(beams, device=DEV, dtype=torch.float32)[None]
+    s, b, t = (v.cpu() for v in C.beam_select(x, scores, 8))
+    log_sum = [math.log(math.exp(20.0) * (1 + (i == 5)) + vocab - 1 - (i == 5)) for i in range(beams)]
+    want = sorted([(-(-i + 20.0 - log_sum[i]), i, tok) for i, tok in planted[:12] + [(5, vocab - 1)]])[:8]
+    assert [(i, tok) for _, i, tok in want] == list(zip(b[0].tolist(), t[0].tolist()))
+    assert np.allclose([-v for v, _, _ in want], s[0].double().numpy(), rtol=0, atol=2.0 ** -18)
+    del x
+    torch.cuda.empty_cache()
 
 
 @pytest.mark.gpu
