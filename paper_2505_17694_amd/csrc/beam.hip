@@ -248,6 +248,7 @@ struct Logits {
 };
 
 constexpr int kRowWaves = 8;                // most waves of a workgroup that share a beam's tokens
+constexpr int kTops = 16;                   // of a lane's chunks it keeps the largest logit; from the 17th on two or more share one
 
 // Newcomers of a wave, collected 64 at a time in LDS before they are sorted into its list.
 struct Collector {
@@ -296,10 +297,13 @@ struct Collector {
 // the largest and the sum of 2^(x log2 e - ref).  Tokens are found afterwards.  The workgroup's lanes form groups; the
 // `kept`-th largest of the groups' largest is a bar that at least `kept` tokens reach, all of them in lanes whose largest does.
 // Groups are as wide as leaves two for every token wanted: with 32 groups and 16 wanted half of the groups reach the bar, which
-// 22 tokens then do.  Only those lanes' tokens are read again.
-// Bound by the loads: a token takes seven lane operations, four of them the exponential.  The waves of a workgroup take
-// turns along the vocabulary: 8 waves, each on a stretch of its own, read 134 MB in 29 us, in turn in 26.  ONCE: with the
-// streaming hint, 24 us; 4 x 32768 fp32 logits, which stay in the caches, take 1 us longer with it.
+// 22 tokens then do.  Only the chunks of a lane whose largest reaches it are read again: 134 MB of logits make 139 MB fetched
+// (all chunks of such a lane: 170 MB, and 28 us for the largest of the times below).
+// Bound by the loads: a token takes seven lane operations, four of them the exponential.  64 x 8 beams of 131072 bf16 logits
+// (134 MB) take 26 us, of which the search for the tokens is 3 to 4; the read alone would be 20 at 6.9 TB/s.  The waves of a
+// workgroup take turns along the vocabulary: without that search, and with the kernel that follows, 34.0 us where each has a
+// stretch of its own, 31.6 in turn, 28.7 with the streaming hint too (ONCE); 4 x 32768 fp32 logits, which stay in the caches, 6.4
+// in turn and 7.6 with the hint.
 template <int DT, bool ONCE>
 __global__ __launch_bounds__(kRowWaves * 64) void beam_rows_kernel(BeamParams P)
 {
@@ -308,6 +312,7 @@ __global__ __launch_bounds__(kRowWaves * 64) void beam_rows_kernel(BeamParams P)
     __shared__ uint32_t groups[kRowWaves * 64], wanted[1];
     __shared__ PartialSum sums[kRowWaves];
     __shared__ int counts[kRowWaves];
+    __shared__ float chunk_tops[kRowWaves][kTops][64];
     const int row = blockIdx.x, part = blockIdx.y;
     if (!reads_logits(P, row)) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
@@ -323,7 +328,8 @@ __global__ __launch_bounds__(kRowWaves * 64) void beam_rows_kernel(BeamParams P)
     };
     typename L::Vec raw[L::kLoads];
     if (first < chunks) load(first, raw);
-    for (int chunk = first; chunk < chunks; chunk += step) {
+    int turn = 0;
+    for (int chunk = first; chunk < chunks; chunk += step, ++turn) {
         float v[kPieces];
 #pragma unroll
         for (int e = 0; e < kPieces; ++e) v[e] = L::widen(raw[e / L::kPerLoad], e % L::kPerLoad);
@@ -367,6 +373,10 @@ __global__ __launch_bounds__(kRowWaves * 64) void beam_rows_kernel(BeamParams P)
                 sum += double(total([all](float a) { return __builtin_amdgcn_exp2f((a - all) * kLog2e); })) * exp2(at - ref);
             }
         }
+        if (chunks > step) {                            // else `mine` is all there is
+            float *kept_top = &chunk_tops[wave][turn % kTops][lane];
+            *kept_top = turn < kTops ? top : fmaxf(*kept_top, top);
+        }
         mine = fmaxf(mine, top);
     }
 
@@ -397,34 +407,47 @@ __global__ __launch_bounds__(kRowWaves * 64) void beam_rows_kernel(BeamParams P)
     const uint32_t bar = *wanted;
     const float least = bar > order_of(kMinusInf) ? logit_of(uint64_t(bar) << 32) : kMinusInf;      // -inf: any token, NaN too
 
-    // the tokens that reach it, of this wave's lanes that do: 16 bytes of one of them at a time
-    const bool reaches = reach && reach >= bar;
-    const uint64_t reaching = __ballot(reaches);
-    uint32_t *lanes = groups + wave * 64;               // nobody reads the groups any more
-    if (reaches) lanes[__popcll(reaching & ((uint64_t(1) << lane) - 1))] = lane;
-    Collector::settle();
-    const int pieces = first < chunks ? ((chunks - 1 - first) / step + 1) * L::kLoads : 0, items = __popcll(reaching) * pieces;
+    // the tokens that reach it, of the lanes' chunks that do: up to 64 (lane, place of the chunk's largest) at a time, 16 bytes of
+    // one of them in a lane
+    uint32_t *places = groups + wave * 64;              // nobody reads the groups any more
+    const int tops = turn < kTops ? turn : kTops;
+    const int pieces = (turn + kTops - 1) / kTops * L::kLoads;
     Collector found(lists + wave * 64, lane, P.kept);
-    for (int i = lane; i - lane < items; i += 64) {
-        uint32_t hits = 0;
-        int t = 0;
-        if (i < items) {
-            const int of = int(lanes[i / pieces]), piece = i % pieces;
-            t = L::token(first + piece / L::kLoads * step, of, piece % L::kLoads * L::kPerLoad);
-            const int n = P.vocab - t;
-            if (n >= L::kPerLoad) {
-                const typename L::Vec some = *reinterpret_cast<const typename L::Vec *>(x + int64_t(t) * L::kSize);
+    int listed = 0;
+#pragma unroll 1
+    for (int top = 0; top <= tops; ++top) {
+        const bool reaches = top < tops && reach >= bar && reach && (chunks <= step || least == kMinusInf || chunk_tops[wave][top][lane] >= least);
+        const uint64_t reaching = __ballot(reaches);
+        const int more = __popcll(reaching);
+        if (top == tops || listed + more > 64) {
+            Collector::settle();
+            for (int i = lane; i - lane < listed * pieces; i += 64) {
+                uint32_t hits = 0;
+                int t = 0;
+                if (i < listed * pieces) {
+                    const uint32_t place = places[i / pieces];
+                    const int piece = i % pieces;
+                    t = L::token(first + (int(place / 64) + piece / L::kLoads * kTops) * step, place % 64, piece % L::kLoads * L::kPerLoad);
+                    const int n = P.vocab - t;
+                    if (n >= L::kPerLoad) {
+                        const typename L::Vec some = *reinterpret_cast<const typename L::Vec *>(x + int64_t(t) * L::kSize);
 #pragma unroll
-                for (int e = 0; e < L::kPerLoad; ++e) hits |= L::widen(some, e) >= least || least == kMinusInf ? 1u << e : 0u;
-            } else {
-                for (int e = 0; e < n; ++e) hits |= logit_at<DT>(x, t + e) >= least ? 1u << e : 0u;
+                        for (int e = 0; e < L::kPerLoad; ++e) hits |= L::widen(some, e) >= least || least == kMinusInf ? 1u << e : 0u;
+                    } else {
+                        for (int e = 0; e < n; ++e) hits |= logit_at<DT>(x, t + e) >= least ? 1u << e : 0u;
+                    }
+                }
+                while (__any(hits != 0)) {
+                    const int token = t + __builtin_ctz(hits | 0x80000000u);
+                    found.add(hits != 0, hits ? key_of(logit_at<DT>(x, token), token) : 0);
+                    hits &= hits - 1;
+                }
             }
+            Collector::settle();
+            listed = 0;
         }
-        while (__any(hits != 0)) {
-            const int token = t + __builtin_ctz(hits | 0x80000000u);
-            found.add(hits != 0, hits ? key_of(logit_at<DT>(x, token), token) : 0);
-            hits &= hits - 1;
-        }
+        if (reaches) places[listed + __popcll(reaching & ((uint64_t(1) << lane) - 1))] = uint32_t(top * 64 + lane);
+        listed += more;
     }
 
     const int count = found.finish();
@@ -607,9 +630,9 @@ int launch_reorder(const ReorderParams &p, int unit, void *stream)
         else         hipLaunchKernelGGL((reorder_kernel<Unit, N, false>), grid, dim3(256), 0, s, p);
     };
     auto launch_size = [&](auto unit_value) {
-        if (p.most_units <= 256)             launch(unit_value, std::integral_constant<int, 1>{});
-        else if (sizeof(unit_value) == 16)   launch(unit_value, std::integral_constant<int, 2>{});
-        else                                 launch(unit_value, std::integral_constant<int, 8>{});
+        constexpr int kMany = sizeof(unit_value) == 16 ? 2 : 8;
+        if (p.most_units <= 256) launch(unit_value, std::integral_constant<int, 1>{});
+        else                     launch(unit_value, std::integral_constant<int, kMany>{});
     };
     switch (unit) {
     case 16: launch_size(Unit16{}); break;
