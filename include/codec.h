@@ -570,7 +570,7 @@ int codec_pages_compact(codec_pages_t *pages, int32_t page_size, codec_run *runs
  *   runs            host array [num_runs], borrowed for the call only: the list travels in the launches' arguments,
  *                   so that the call needs no device memory and can be captured
  * No token may be written twice or be both read and written (CODEC_ERR_INVALID_ARGUMENT), and no two pools may
- * share memory: the order of the copies is undefined.  Enqueued on `stream` without synchronising.
+ * share memory: the order of the copies is undefined.  A pool holds at most 2^32 tokens.  Enqueued on `stream` without synchronising.
  */
 int codec_cache_copy(const codec_head_config *head, const codec_kv_layout *layout, int32_t num_layers,
                      void *const *k_pages, void *const *v_pages, const codec_run *runs, int32_t num_runs, void *stream);

@@ -348,6 +348,7 @@ int codec_cache_copy(const codec_head_config *head, const codec_kv_layout *layou
     if (!head || !layout || num_layers < 1 || num_runs < 0) return CODEC_ERR_INVALID_ARGUMENT;
     if (int st = check_head(*head)) return st;
     if (pool_span(*head, *layout) < 0) return CODEC_ERR_INVALID_ARGUMENT;
+    if (layout->num_pages * head->page_size > int64_t(1) << 32) return CODEC_ERR_UNSUPPORTED;      // slots are 32-bit: 512 GB a pool
     if (num_runs == 0) return CODEC_OK;
     if (!k_pages || !v_pages || !runs) return CODEC_ERR_INVALID_ARGUMENT;
     for (int32_t l = 0; l < num_layers; ++l)
@@ -370,6 +371,7 @@ int codec_cache_copy(const codec_head_config *head, const codec_kv_layout *layou
     p.head_stride = 2 * layout->head_stride;
     p.heads = head->num_kv_heads;
     p.head_bytes = 2 * head->head_dim;
+    while ((1 << p.page_shift) < ps) ++p.page_shift;
     double tokens = 0.0;
     for (int32_t i = 0; i < num_runs; ++i) tokens += runs[i].tokens;
     p.large = 4.0 * tokens * num_layers * p.heads * p.head_bytes > codec::kLargeBytes;
@@ -381,7 +383,7 @@ int codec_cache_copy(const codec_head_config *head, const codec_kv_layout *layou
             p.most_tokens = 0;
             for (int32_t i = 0; i < p.num_runs; ++i) {
                 const codec_run &r = runs[at + i];
-                p.runs[i] = {r.src_page, r.dst_page, uint16_t(r.src_token), uint16_t(r.dst_token), uint16_t(r.tokens), 0};
+                p.runs[i] = {uint32_t(r.src_page) * uint32_t(ps) + uint32_t(r.src_token), uint32_t(r.dst_page) * uint32_t(ps) + uint32_t(r.dst_token), uint32_t(r.tokens)};
                 p.most_tokens = std::max(p.most_tokens, r.tokens);
             }
             if (int e = codec::launch_copy(p, stream)) return hip_failure("page copy launch", e);

@@ -32,16 +32,16 @@ struct RotaryParams {
 
 // A launch's worth of codec_cache_copy: pools and runs travel in the kernel's arguments, which hold 4 KB.
 constexpr int kCopyPools = 64;
-constexpr int kCopyRuns = 200;
+constexpr int kCopyRuns = 288;
 
 struct CopyRun {
-    int32_t src_page, dst_page;
-    uint16_t src_token, dst_token, tokens, unused;
+    uint32_t src, dst;              // first token's slot: page * page size + token
+    uint32_t tokens;
 };
 
 struct CopyParams {
     int64_t page_stride, slot_stride, head_stride;      // bytes
-    int32_t heads, head_bytes, num_pools, num_runs, most_tokens;
+    int32_t heads, head_bytes, page_shift, num_pools, num_runs, most_tokens;
     uint32_t row_pieces, planes;                        // set by launch_copy
     bool large;                                         // the call moves more than kLargeBytes
     char *pools[kCopyPools];

@@ -29,8 +29,10 @@ __global__ __launch_bounds__(256) void page_copy_kernel(CopyParams P)
     const uint32_t tile = P.planes == 1 ? blockIdx.x : blockIdx.x / P.planes, plane = blockIdx.x - tile * P.planes;
     const uint32_t begin = tile * (PIECES * 256);
     if (begin >= all) return;
-    const char *src = P.pools[blockIdx.z] + run.src_page * P.page_stride + run.src_token * P.slot_stride + plane * P.head_stride;
-    char *dst = P.pools[blockIdx.z] + run.dst_page * P.page_stride + run.dst_token * P.slot_stride + plane * P.head_stride;
+    char *pool = P.pools[blockIdx.z] + plane * P.head_stride;
+    auto token_at = [&](uint32_t slot) { return (slot >> P.page_shift) * P.page_stride + (slot & ((1u << P.page_shift) - 1)) * P.slot_stride; };
+    const char *src = pool + token_at(run.src);
+    char *dst = pool + token_at(run.dst);
     const uint32_t step_rows = 256 / row_pieces, step_pieces = 256 - step_rows * row_pieces;
     uint32_t row = (begin + threadIdx.x) / row_pieces, piece = begin + threadIdx.x - row * row_pieces;
     Piece x[PIECES];

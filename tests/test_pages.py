@@ -261,7 +261,7 @@ def test_copy_runs(hkv, d, page, layout, layers):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("n,layers", [(1, 1), (199, 2), (200, 1), (201, 33), (1000, 1)])
+@pytest.mark.parametrize("n,layers", [(1, 1), (199, 2), (200, 1), (201, 33), (1000, 1), (287, 1), (288, 2), (289, 32)])
 def test_copy_lists_longer_than_a_launch(n, layers):
     """More runs and more pools than one launch's arguments hold."""
     head = HeadConfig(2, 1, 64, DTYPE_FP16)
