@@ -16,9 +16,10 @@ typedef uint32_t __attribute__((ext_vector_type(4))) Piece;
 // A workgroup copies PIECES * 256 pieces of 16 bytes of one run in one pool, PIECES of a lane in flight.  The run is rows of
 // consecutive memory, `row_pieces` long: with tokens side by side a head's, with heads side by side a token's, else a token's in
 // one head (a plane each).  A lane finds its first piece by a division and the others by steps of 256.
-// Bound by HBM: 1000 pages of 8 x 128 channels in 8 layers (1.05 GB read and written) take 206 us, 5.1 TB/s, what a copy of
-// 1 GiB reaches.  PIECES 8 against 2: the last pages of 192 sequences in 16 layers 27 and 33 us, runs of one to five tokens of
-// 8 x 64 channels 16 and 12.  LARGE: stores with the streaming hint, 206 us against 220.
+// Bound by HBM: 1000 pages of 8 x 128 channels in 8 layers (1.05 GB read and written) take 198 us, 5.3 TB/s; a plain copy of 1 GiB
+// reaches 5.15.  LARGE: with the streaming hint; 222 us without.  PIECES 8 and 2: the last pages of 192 sequences in 16 layers
+// 50 and 49 us out of HBM, 27 and 33 where they have just been written; runs of one to five tokens of 8 x 64 channels 18.7
+// and 13.0, four pages of one layer 3.05 and 2.75.
 template <bool TOKENS_INSIDE, int PIECES, bool LARGE>
 __global__ __launch_bounds__(256) void page_copy_kernel(CopyParams P)
 {
@@ -41,7 +42,9 @@ __global__ __launch_bounds__(256) void page_copy_kernel(CopyParams P)
     for (int j = 0; j < PIECES; ++j) {
         // a lane behind the run's end reads its first piece: a load with a branch around it is waited for at once
         at[j] = begin + j * 256 + threadIdx.x < all ? row * row_stride + piece * 16 : 0;
-        x[j] = *reinterpret_cast<const Piece *>(src + at[j]);
+        const Piece *from = reinterpret_cast<const Piece *>(src + at[j]);
+        if constexpr (LARGE) x[j] = __builtin_nontemporal_load(from);
+        else x[j] = *from;
         row += step_rows;
         piece += step_pieces;
         if (piece >= row_pieces) {
@@ -76,8 +79,9 @@ int launch_copy(CopyParams &p, void *stream)
     auto launch_size = [&](auto inside) {
         using two = std::integral_constant<int, 2>;
         using eight = std::integral_constant<int, 8>;
-        if (most < 1024) p.large ? launch(inside, two{}, std::true_type{}) : launch(inside, two{}, std::false_type{});
-        else             p.large ? launch(inside, eight{}, std::true_type{}) : launch(inside, eight{}, std::false_type{});
+        if (!p.large)         launch(inside, two{}, std::false_type{});
+        else if (most < 1024) launch(inside, two{}, std::true_type{});
+        else                  launch(inside, eight{}, std::true_type{});
     };
     tokens_inside ? launch_size(std::true_type{}) : launch_size(std::false_type{});
     return int(hipGetLastError());
