@@ -374,7 +374,9 @@ int codec_cache_copy(const codec_head_config *head, const codec_kv_layout *layou
     while ((1 << p.page_shift) < ps) ++p.page_shift;
     double tokens = 0.0;
     for (int32_t i = 0; i < num_runs; ++i) tokens += runs[i].tokens;
-    p.large = 4.0 * tokens * num_layers * p.heads * p.head_bytes > codec::kLargeBytes;
+    const double read = 2.0 * tokens * num_layers * p.heads * p.head_bytes;
+    p.large = 2.0 * read > codec::kLargeBytes;
+    p.huge = read > codec::kHugeBytes;
     for (int64_t first = 0; first < 2 * int64_t(num_layers); first += codec::kCopyPools) {
         p.num_pools = int32_t(std::min<int64_t>(codec::kCopyPools, 2 * int64_t(num_layers) - first));
         for (int32_t i = 0; i < p.num_pools; ++i) p.pools[i] = static_cast<char *>(((first + i) & 1 ? v_pages : k_pages)[(first + i) / 2]);

@@ -11,6 +11,8 @@ namespace codec {
 // What the L2s of the eight dies hold together.  Calls that read and write more use the streaming hint: what they leave would
 // not be found there.
 constexpr double kLargeBytes = 32 << 20;
+// What the last-level cache holds.
+constexpr double kHugeBytes = 256 << 20;
 
 // Rows of one kind (queries, keys, values) of the tokens: strides in bytes.
 struct RowsView {
@@ -43,7 +45,7 @@ struct CopyParams {
     int64_t page_stride, slot_stride, head_stride;      // bytes
     int32_t heads, head_bytes, page_shift, num_pools, num_runs, most_tokens;
     uint32_t row_pieces, planes;                        // set by launch_copy
-    bool large;                                         // the call moves more than kLargeBytes
+    bool large, huge;                                   // the call moves more than kLargeBytes, reads more than kHugeBytes
     char *pools[kCopyPools];
     CopyRun runs[kCopyRuns];
 };

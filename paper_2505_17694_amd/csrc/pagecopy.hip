@@ -17,10 +17,11 @@ typedef uint32_t __attribute__((ext_vector_type(4))) Piece;
 // consecutive memory, `row_pieces` long: with tokens side by side a head's, with heads side by side a token's, else a token's in
 // one head (a plane each).  A lane finds its first piece by a division and the others by steps of 256.
 // Bound by HBM: 1000 pages of 8 x 128 channels in 8 layers (1.05 GB read and written) take 198 us, 5.3 TB/s; a plain copy of 1 GiB
-// reaches 5.15.  LARGE: with the streaming hint; 222 us without.  PIECES 8 and 2: the last pages of 192 sequences in 16 layers
-// 50 and 49 us out of HBM, 27 and 33 where they have just been written; runs of one to five tokens of 8 x 64 channels 18.7
-// and 13.0, four pages of one layer 3.05 and 2.75.
-template <bool TOKENS_INSIDE, int PIECES, bool LARGE>
+// reaches 5.15.  STORES_ONCE, LOADS_ONCE: with the streaming hint; without either 222 us, with that on the stores 206.  What
+// may lie in the last-level cache is loaded without: the last pages of 192 sequences in 16 layers take 27 us where they are there and
+// 47 with the hint, out of HBM 51 and 50.  PIECES 8 and 2: those pages 27 and 33 us; runs of one to five tokens of 8 x 64
+// channels 18.7 and 13.0, four pages of one layer 3.05 and 2.75.
+template <bool TOKENS_INSIDE, int PIECES, bool STORES_ONCE, bool LOADS_ONCE>
 __global__ __launch_bounds__(256) void page_copy_kernel(CopyParams P)
 {
     const CopyRun run = P.runs[blockIdx.y];
@@ -43,7 +44,7 @@ __global__ __launch_bounds__(256) void page_copy_kernel(CopyParams P)
         // a lane behind the run's end reads its first piece: a load with a branch around it is waited for at once
         at[j] = begin + j * 256 + threadIdx.x < all ? row * row_stride + piece * 16 : 0;
         const Piece *from = reinterpret_cast<const Piece *>(src + at[j]);
-        if constexpr (LARGE) x[j] = __builtin_nontemporal_load(from);
+        if constexpr (LOADS_ONCE) x[j] = __builtin_nontemporal_load(from);
         else x[j] = *from;
         row += step_rows;
         piece += step_pieces;
@@ -56,7 +57,7 @@ __global__ __launch_bounds__(256) void page_copy_kernel(CopyParams P)
     for (int j = 0; j < PIECES; ++j) {
         if (begin + j * 256 + threadIdx.x >= all) break;
         Piece *to = reinterpret_cast<Piece *>(dst + at[j]);
-        if constexpr (LARGE) __builtin_nontemporal_store(x[j], to);
+        if constexpr (STORES_ONCE) __builtin_nontemporal_store(x[j], to);
         else *to = x[j];
     }
 }
@@ -71,19 +72,23 @@ int launch_copy(CopyParams &p, void *stream)
     p.row_pieces = heads_inside ? head_pieces * p.heads : head_pieces;
     p.planes = tokens_inside || heads_inside ? 1 : p.heads;
     const int64_t most = int64_t(head_pieces) * p.most_tokens * (p.heads / p.planes);       // pieces of a run in a plane
-    auto launch = [&](auto inside, auto pieces, auto once) {
+    using no = std::false_type;
+    using yes = std::true_type;
+    auto launch = [&](auto inside, auto pieces, auto stores_once, auto loads_once) {
         constexpr int N = decltype(pieces)::value;
         const dim3 grid(unsigned((most + N * 256 - 1) / (N * 256) * p.planes), unsigned(p.num_runs), unsigned(p.num_pools));
-        hipLaunchKernelGGL((page_copy_kernel<decltype(inside)::value, N, decltype(once)::value>), grid, dim3(256), 0, s, p);
+        hipLaunchKernelGGL((page_copy_kernel<decltype(inside)::value, N, decltype(stores_once)::value, decltype(loads_once)::value>), grid,
+                           dim3(256), 0, s, p);
     };
     auto launch_size = [&](auto inside) {
         using two = std::integral_constant<int, 2>;
         using eight = std::integral_constant<int, 8>;
-        if (!p.large)         launch(inside, two{}, std::false_type{});
-        else if (most < 1024) launch(inside, two{}, std::true_type{});
-        else                  launch(inside, eight{}, std::true_type{});
+        if (!p.large)         launch(inside, two{}, no{}, no{});
+        else if (most < 1024) launch(inside, two{}, yes{}, no{});
+        else if (!p.huge)     launch(inside, eight{}, yes{}, no{});
+        else                  launch(inside, eight{}, yes{}, yes{});
     };
-    tokens_inside ? launch_size(std::true_type{}) : launch_size(std::false_type{});
+    tokens_inside ? launch_size(yes{}) : launch_size(no{});
     return int(hipGetLastError());
 }
 

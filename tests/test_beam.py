@@ -218,6 +218,8 @@ def test_select_large():
     gen = torch.Generator().manual_seed(7)
     check(draw(gen, 16, 8, 131072, dtype=BF16), -torch.rand(16, 8, generator=gen) * 10, 16)
     check(draw(gen, 1, 4, 1 << 20, dtype=FP32), -torch.rand(1, 4, generator=gen) * 10, 8)
+    check(draw(gen, 25, 6, 131073, dtype=FP16), -torch.rand(25, 6, generator=gen) * 10, 12)     # more than the L2s hold, odd rows
+    check(draw(gen, 24, 6, 131072, dtype=BF16), -torch.rand(24, 6, generator=gen) * 10, 64)
 
 
 @pytest.mark.gpu
@@ -281,6 +283,16 @@ def test_reorder(dtype, shape, batch, wide, n):
     want = x[torch.arange(batch)[:, None], beams.long()]
     (got,) = C.beam_reorder([x.to(DEV)], beams.to(DEV))
     assert got.shape == want.shape and torch.equal(got.cpu().contiguous().view(torch.uint8), want.contiguous().view(torch.uint8))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,width", [(torch.int64, 40000), (FP16, 150001), (torch.uint8, 300007)])
+def test_reorder_more_than_the_caches_hold(dtype, width):
+    x = torch.randint(0, 100, (8, 8, width), device=DEV).to(dtype)
+    beams = torch.randint(0, 8, (8, 8), dtype=torch.int32, device=DEV)
+    print(f"[case] large reorder {dtype} {width}", flush=True)
+    (got,) = C.beam_reorder([x], beams)
+    assert torch.equal(got, x[torch.arange(8, device=DEV)[:, None], beams.long()])
 
 
 @pytest.mark.gpu

@@ -275,6 +275,28 @@ def test_copy_lists_longer_than_a_launch(n, layers):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("layout", ["thd", "htd"])
+@pytest.mark.parametrize("pages,layers,tokens", [(260, 4, 16), (600, 4, 3), (600, 8, 16)])
+def test_copy_more_than_the_caches_hold(pages, layers, tokens, layout):
+    """Calls of 68 MB, 29 MB and 315 MB read: stores, or loads too, with the streaming hint; whole pages and short runs."""
+    head = HeadConfig(8, 8, 128, DTYPE_BF16)
+    pools = pools_of(head, 2 * pages, layers, layout)
+    order = torch.from_numpy(np.random.default_rng(pages).permutation(2 * pages)).to(DEV)
+    src, dst = order[:pages], order[pages:]
+    want = [p.clone() for kv in pools for p in kv]
+    for w in want:
+        if layout == "thd":
+            w[dst, :tokens] = w[src, 16 - tokens:]
+        else:
+            w[dst, :, :tokens] = w[src, :, 16 - tokens:]
+    print(f"[case] large copy {pages} {layers} {tokens} {layout}", flush=True)
+    runs = torch.stack([src, torch.full_like(src, 16 - tokens), dst, torch.zeros_like(dst), torch.full_like(dst, tokens)], 1).cpu().numpy()
+    C.KVCache(head, 2 * pages, layout=layout, device=DEV, pools=pools).copy(runs)
+    for p, w in zip((p for kv in pools for p in kv), want):
+        assert torch.equal(p.view(torch.int16), w.view(torch.int16))
+
+
+@pytest.mark.gpu
 def test_copy_in_pools_side_by_side():
     """K and V of a page and head in one pool: the strides are the view's, the other half keeps its bits."""
     head = HeadConfig(4, 2, 64, DTYPE_BF16)
