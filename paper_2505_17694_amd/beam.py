@@ -25,9 +25,9 @@ def beam_select(logits: torch.Tensor, scores: torch.Tensor, k: int, finished: to
     """The k best continuations of every search: logits [batch, beams, vocab] (16 or 32 bits), scores [batch, beams] (32 bits),
     ``finished`` [batch, beams] (truth values) beams go on with ``eos`` alone.  Returns (scores, beams, tokens), each
     [batch, k], best first; ties go to the lowest beam, then the lowest token (see codec_beam_select)."""
-    if logits.dim() != 3 or logits.dtype not in _CODE or logits.device.type != "cuda":
+    if logits.dim() != 3 or logits.dtype not in _CODE or not logits.is_cuda:
         raise ValueError(f"logits: need [batch, beams, vocab] of 16 or 32 bits on a GPU, got {logits.dtype} {tuple(logits.shape)} on {logits.device}")
-    s = _enter(logits.device, stream)
+    s = _enter(logits.get_device(), stream)
     if s is None:
         with _on(logits.device, stream) as s:
             return _select(logits, scores, k, finished, eos, s)
@@ -62,9 +62,9 @@ def beam_reorder(states, beams: torch.Tensor, out=None, stream=None):
     (int32) names, as new tensors [batch, n, ...] or in those of ``out``.  Rows have to be contiguous.  A row whose entry is no
     beam is left as it was (in a new tensor: undefined)."""
     states = list(states)
-    if beams.dim() != 2 or beams.device.type != "cuda":
+    if beams.dim() != 2 or not beams.is_cuda:
         raise ValueError(f"beams: need [batch, n] on a GPU, got {tuple(beams.shape)} on {beams.device}")
-    s = _enter(beams.device, stream)
+    s = _enter(beams.get_device(), stream)
     if s is None:
         with _on(beams.device, stream) as s:
             return _reorder(states, beams, out, s)

@@ -16,6 +16,11 @@ _SCALINGS = {"linear": B.CODEC_ROTARY_LINEAR, "ntk": B.CODEC_ROTARY_NTK, "wavele
              "yarn": B.CODEC_ROTARY_YARN}
 
 
+_current_device = getattr(torch._C, "_cuda_getDevice", None)               # absent in a PyTorch without a GPU runtime
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_Rows = B.codec_rows
+
+
 def _device(device) -> torch.device:
     d = torch.device(device)
     if d.type == "cuda" and d.index is None:
@@ -33,11 +38,10 @@ def _on(device: torch.device, stream):
         yield _current_stream(device)
 
 
-def _enter(device: torch.device, stream):
-    """The stream's handle if the call can go ahead as things are, else None: another device or stream has to be made current."""
-    if stream is None and torch._C._cuda_getDevice() == device.index:
-        return _current_stream(device)
-    return None
+def _enter(index: int, stream):
+    """The stream's handle if a call on device `index` can go ahead as things are, else None: another device or stream has to be
+    made current."""
+    return _raw_stream(index) if stream is None and _current_device() == index else None
 
 
 def _check_reach(t: torch.Tensor, what: str, last: int, size: int) -> None:
@@ -49,23 +53,28 @@ def _check_reach(t: torch.Tensor, what: str, last: int, size: int) -> None:
 
 def _rows(t: torch.Tensor, what: str, shape, dtype: torch.dtype, index: int):
     """`t` as codec_rows: `shape` = (tokens, heads, head_dim) with contiguous channels, in storage that is there."""
-    s = t.stride()
-    if t.shape != shape or t.dtype is not dtype or t.get_device() != index or s[2] != 1:
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != index or t.stride()[2] != 1:
         raise ValueError(f"{what}: need a {dtype} tensor of shape {tuple(shape)} with contiguous channels on cuda:{index}, "
-                         f"got {t.dtype} {tuple(t.shape)} on {t.device}, strides {s}")
+                         f"got {t.dtype} {tuple(t.shape)} on {t.device}, strides {t.stride()}")
     tokens, heads, head_dim = shape
     if tokens == 0:
-        return B.codec_rows(0, 0, 0)
-    _check_reach(t, what, (tokens - 1) * s[0] + (heads - 1) * s[1] + head_dim, 2)
-    # the stride of a single token or head says nothing
-    return B.codec_rows(t.data_ptr(), s[0] if tokens > 1 else 0, s[1] if heads > 1 else 0)
+        return _Rows(0, 0, 0)
+    token_stride, head_stride, _ = t.stride()
+    if tokens == 1:                         # the stride of a single token or head says nothing
+        token_stride = 0
+    if heads == 1:
+        head_stride = 0
+    if t.untyped_storage().nbytes() < 2 * (t.storage_offset() + (tokens - 1) * token_stride + (heads - 1) * head_stride + head_dim):
+        raise ValueError(f"{what}: the tensor's storage ends before its last element")
+    return _Rows(t.data_ptr(), token_stride, head_stride)
 
 
 def _index(t: torch.Tensor, what: str, tokens: int, index: int) -> int:
-    if t.dim() != 1 or t.shape[0] != tokens or t.dtype is not torch.int64 or t.get_device() != index or not t.is_contiguous():
+    if t.shape != (tokens,) or t.dtype is not torch.int64 or t.get_device() != index or not t.is_contiguous():
         raise ValueError(f"{what}: need a contiguous int64 tensor of shape {(tokens,)} on cuda:{index}, "
                          f"got {t.dtype} {tuple(t.shape)} on {t.device}")
-    _check_reach(t, what, tokens, 8)
+    if t.untyped_storage().nbytes() < 8 * (t.storage_offset() + tokens):
+        raise ValueError(f"{what}: the tensor's storage ends before its last element")
     return t.data_ptr()
 
 
@@ -102,7 +111,7 @@ class Rotary:
         """x [tokens, heads, head_dim] turned to its positions, or back (the gradient); ``out`` may be x itself."""
         if x.dim() != 3 or x.dtype not in _CODE or self.device.type != "cuda":
             raise ValueError(f"x: need a 16-bit tensor [tokens, heads, head_dim] and a GPU, got {x.dtype} {tuple(x.shape)} on {x.device}")
-        s = _enter(self.device, stream)
+        s = _enter(self.device.index, stream)
         if s is None:
             with _on(self.device, stream) as s:
                 return self._apply(x, positions, inverse, out, s)
@@ -144,7 +153,7 @@ class KVCache:
         shape = (self.num_pages, ps, h, d) if layout == "thd" else (self.num_pages, h, ps, d)
         if pools is None:
             pools = [tuple(torch.empty(shape, dtype=self.dtype, device=self.device) for _ in "kv") for _ in range(layers)]
-        self.pools = [tuple(kv) for kv in pools]
+        self.pools = tuple(tuple(kv) for kv in pools)
         flat = [p for kv in self.pools for p in kv]
         if not flat or any(len(kv) != 2 for kv in self.pools):
             raise ValueError("pools: need a (k, v) pair for every layer")
@@ -157,6 +166,7 @@ class KVCache:
         self.page_stride, self.token_stride, self.head_stride = page, token, kv_head
         self._layout = B.codec_kv_layout(self.num_pages, page, token, kv_head)
         self._head = B.codec_head_config(head.num_q_heads, h, d, head.dtype, ps, 0.0)
+        self._index = self.device.index if self.device.type == "cuda" else None
         self._q_row, self._kv_row = (head.num_q_heads, d), (h, d)
         self._reach = (self.num_pages - 1) * page + (ps - 1) * token + (h - 1) * kv_head + d
         # per layer, what has to be there: (storage, bytes)
@@ -190,16 +200,16 @@ class KVCache:
         """The step's tokens into ``layer``: queries and keys turned to ``positions``, keys and values stored at ``slots``
         (page * page_size + token; negative: not stored).  Returns the turned queries (``q_out``, which may be q itself);
         q None: keys and values only.  Without ``rotary`` rows pass as they are and ``positions`` may be None."""
-        if self.device.type != "cuda":
+        if self._index is None:
             raise ValueError(f"append needs pools on a GPU, these are on {self.device}")
-        s = _enter(self.device, stream)
+        s = _enter(self._index, stream)
         if s is None:
             with _on(self.device, stream) as s:
                 return self._append(layer, q, k, v, positions, slots, rotary, q_out, s)
         return self._append(layer, q, k, v, positions, slots, rotary, q_out, s)
 
     def _append(self, layer, q, k, v, positions, slots, rotary, q_out, s):
-        index, dtype, tokens = self.device.index, self.dtype, k.shape[0]
+        index, dtype, tokens = self._index, self.dtype, k.shape[0]
         self._check_storage(layer)
         kv_shape = (tokens, *self._kv_row)
         k_rows = _rows(k, "k", kv_shape, dtype, index)
@@ -256,7 +266,7 @@ class KVCache:
         self._copy_on(runs, stream)
 
     def _copy_on(self, runs, stream):
-        s = _enter(self.device, stream)
+        s = _enter(self.device.index, stream)
         if s is None:
             with _on(self.device, stream) as s:
                 return self._copy(runs, s)

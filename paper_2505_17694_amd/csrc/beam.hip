@@ -168,8 +168,8 @@ __device__ __forceinline__ float max3(float a, float b, float c)
 
 // ---- the sum of exponentials -----------------------------------------------------------------------------
 //
-// Kept as sum * 2^ref, in 64 bits, with whole references; log2(e) stands for its 32-bit value throughout: what it is off by (1.3e-8 of x - m)
-// weighs on the distance from the largest logit only, because that is brought to the same scale at the end.
+// Kept as sum * 2^ref, in 64 bits, with whole references.  log2(e) stands for its 32-bit value throughout: what that is off by,
+// 1.3e-8 of itself, weighs on the distance from the largest logit only, because that is brought to the same scale at the end.
 
 constexpr float kLog2e = 1.44269502f;
 constexpr double kNoRef = -1e300;

@@ -349,10 +349,10 @@ int codec_cache_copy(const codec_head_config *head, const codec_kv_layout *layou
     if (int st = check_head(*head)) return st;
     if (pool_span(*head, *layout) < 0) return CODEC_ERR_INVALID_ARGUMENT;
     if (layout->num_pages * head->page_size > int64_t(1) << 32) return CODEC_ERR_UNSUPPORTED;      // slots are 32-bit: 512 GB a pool
-    if (num_runs == 0) return CODEC_OK;
-    if (!k_pages || !v_pages || !runs) return CODEC_ERR_INVALID_ARGUMENT;
+    if (!k_pages || !v_pages || (num_runs && !runs)) return CODEC_ERR_INVALID_ARGUMENT;
     for (int32_t l = 0; l < num_layers; ++l)
         if (!k_pages[l] || !v_pages[l] || !aligned16(k_pages[l]) || !aligned16(v_pages[l]) || !pools_apart(*head, *layout, k_pages[l], v_pages[l])) return CODEC_ERR_INVALID_ARGUMENT;
+    if (num_runs == 0) return CODEC_OK;
     const int32_t ps = head->page_size;
     for (int32_t i = 0; i < num_runs; ++i) {
         const codec_run &r = runs[i];
