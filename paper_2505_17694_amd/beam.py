@@ -41,6 +41,8 @@ def _select(logits, scores, k, finished, eos, s):
         raise ValueError(f"logits: the tokens of a beam must be contiguous, strides are {strides}")
     if batch and beams and vocab:
         _check_reach(logits, "logits", (batch - 1) * strides[0] + (beams - 1) * strides[1] + vocab, logits.element_size())
+    if (batch | beams | vocab | abs(k) | abs(eos)) >> 31:
+        raise ValueError(f"batch {batch}, beams {beams}, vocab {vocab}, k {k}, eos {eos}: one of them is out of range")
     config = B.codec_beam_config(batch, beams, vocab, k, _CODE[logits.dtype], eos)
     scores_at = _dense(scores, "scores", batch, beams, _SCORES, index)
     finished_at = None if finished is None else _dense(finished, "finished", batch, beams, _FLAGS, index)
@@ -122,6 +124,8 @@ def _reorder(states, beams, out, s):
     index = beams.get_device()
     beams_at = _dense(beams, "beams", batch, n, _BEAMS, index)
     wide = states[0].shape[1] if states and states[0].dim() >= 2 else 1
+    if (batch | wide | n) >> 31:
+        raise ValueError(f"batch {batch}, beams {wide}, n {n}: one of them is out of range")
     src = _states(states, "states", batch, wide, index)
     if out is None:
         out = _like(states, src, n, wide)

@@ -233,6 +233,11 @@ class CodecError(RuntimeError):
         super().__init__(f"{where}: {codec_status_string(status)} ({status})" + (f": {detail}" if detail else ""))
 
 
+def _is_int32(n) -> bool:
+    """Whether n passes as an int32: ctypes would take its low bits."""
+    return -0x80000000 <= n <= 0x7fffffff
+
+
 def _i32(a):
     return np.ascontiguousarray(a, dtype=np.int32)
 
@@ -405,6 +410,8 @@ def codec_stream_read_probe(buffer_ptr: int, nbytes: int, pattern: int, nontempo
 
 def codec_rotary_turns(rotary_dim: int, theta: float, scaling=None):
     """Returns (status, turns of the pairs as float64 array or None, magnitude).  ``scaling``: codec_rotary_scaling or None."""
+    if not _is_int32(rotary_dim):
+        return CODEC_ERR_INVALID_ARGUMENT, None, 0.0
     turns = np.zeros(max(1, rotary_dim // 2), np.float64)
     magnitude = c_float(0.0)
     st = _lib.codec_rotary_turns(rotary_dim, theta, byref(scaling) if scaling is not None else None, _ptr(turns, c_double),
@@ -442,7 +449,9 @@ def codec_pages_free(pages) -> int:
 
 def codec_pages_take(pages, n: int):
     """Returns (status, ids or None)."""
-    ids = np.empty(max(0, n), np.int32)
+    if not _is_int32(n):
+        return CODEC_ERR_INVALID_ARGUMENT, None
+    ids = np.empty(max(0, min(n, codec_pages_free(pages))), np.int32)           # (the call writes all of n or nothing)
     st = _lib.codec_pages_take(pages, n, ids.ctypes.data)
     return st, (ids if st == CODEC_OK else None)
 

@@ -93,6 +93,8 @@ class Rotary:
             known = {"kind", "factor", "original_length", "low", "high", "fast", "slow"}
             if scaling.get("kind") not in _SCALINGS or set(scaling) - known:
                 raise ValueError(f"scaling: kind is one of {sorted(_SCALINGS)}, beside {sorted(known - {'kind'})}; got {scaling}")
+            if not B._is_int32(scaling.get("original_length", 0)):
+                raise B.CodecError(B.CODEC_ERR_INVALID_ARGUMENT, "codec_rotary_turns")
             s = B.codec_rotary_scaling(_SCALINGS[scaling["kind"]], scaling.get("original_length", 0), scaling.get("factor", 0.0),
                                        scaling.get("low", 1.0), scaling.get("high", 4.0), scaling.get("fast", 32.0),
                                        scaling.get("slow", 1.0))
@@ -119,6 +121,8 @@ class Rotary:
 
     def _apply(self, x, positions, inverse, out, s):
         shape, index = x.shape, self.device.index
+        if (shape[0] | shape[1]) >> 31:
+            raise ValueError(f"x: {tuple(shape)} is too large for a call")
         rows = _rows(x, "x", shape, x.dtype, index)
         at = _index(positions, "positions", shape[0], index)
         if out is None:
@@ -171,6 +175,7 @@ class KVCache:
         self._reach = (self.num_pages - 1) * page + (ps - 1) * token + (h - 1) * kv_head + d
         # per layer, what has to be there: (storage, bytes)
         self._storages = [[(p.untyped_storage(), 2 * (p.storage_offset() + self._reach)) for p in kv] for kv in self.pools]
+        self._copy_status = self._enqueue(np.empty((0, 5), np.int32), 0)        # whether pages of these pools can be copied
         st, self._pages = B.codec_pages_create(self.num_pages)
         if st != B.CODEC_OK:
             raise B.CodecError(st, "codec_pages_create")
@@ -192,10 +197,6 @@ class KVCache:
             if storage.nbytes() < need:
                 raise ValueError(f"pools of layer {layer}: the storage ends before the last page")
 
-    def _check_storages(self) -> None:
-        for layer in range(len(self.pools)):
-            self._check_storage(layer)
-
     def append(self, layer, q, k, v, positions, slots, rotary: Rotary = None, q_out: torch.Tensor = None, stream=None):
         """The step's tokens into ``layer``: queries and keys turned to ``positions``, keys and values stored at ``slots``
         (page * page_size + token; negative: not stored).  Returns the turned queries (``q_out``, which may be q itself);
@@ -210,6 +211,8 @@ class KVCache:
 
     def _append(self, layer, q, k, v, positions, slots, rotary, q_out, s):
         index, dtype, tokens = self._index, self.dtype, k.shape[0]
+        if tokens >> 31:
+            raise ValueError(f"k: {tokens} tokens, at most 2^31 - 1 go into a call")
         self._check_storage(layer)
         kv_shape = (tokens, *self._kv_row)
         k_rows = _rows(k, "k", kv_shape, dtype, index)
@@ -260,10 +263,19 @@ class KVCache:
     def copy(self, runs, stream=None) -> None:
         """Copies runs of tokens, rows (source page, source token, destination page, destination token, tokens), in the
         pools of every layer.  No token may be written twice, or read and written."""
-        if self.device.type != "cuda":
-            raise ValueError(f"copy needs pools on a GPU, these are on {self.device}")
-        self._check_storages()
+        self._check_copy("copy", stream)
         self._copy_on(runs, stream)
+
+    def _check_copy(self, what: str, stream) -> None:
+        """All that can refuse a copy but its runs: looked at before pages change hands."""
+        if self._copy_status != B.CODEC_OK:
+            raise B.CodecError(self._copy_status, "codec_cache_copy")
+        if self.device.type != "cuda":
+            raise ValueError(f"{what} needs pools on a GPU, these are on {self.device}")
+        if stream is not None and stream.device != self.device:
+            raise ValueError(f"stream: on {stream.device}, the pools are on {self.device}")
+        for layer in range(len(self.pools)):
+            self._check_storage(layer)
 
     def _copy_on(self, runs, stream):
         s = _enter(self.device.index, stream)
@@ -273,19 +285,20 @@ class KVCache:
         self._copy(runs, s)
 
     def _copy(self, runs, s):
-        st = B.codec_cache_copy(self._head, self._layout, [k.data_ptr() for k, _ in self.pools],
-                                [v.data_ptr() for _, v in self.pools], runs, s)
+        st = self._enqueue(runs, s)
         if st != B.CODEC_OK:
             raise B.CodecError(st, "codec_cache_copy")
+
+    def _enqueue(self, runs, s):
+        return B.codec_cache_copy(self._head, self._layout, [k.data_ptr() for k, _ in self.pools],
+                                  [v.data_ptr() for _, v in self.pools], runs, s)
 
     def fork(self, page_off, page_ids, tokens, parents, stream=None):
         """Sequence s holds the pages page_ids[page_off[s]:page_off[s + 1]] with tokens[s] tokens.  In the place of these
         sequences others go on, sequence j from sequence parents[j]: a sequence may go on once, several times or not at
         all.  Returns the page lists (page_off, page_ids) of those that go on.  They share whole pages; what is partly
         filled is copied on `stream` for all but the first (see codec_pages_fork)."""
-        if self.device.type != "cuda":
-            raise ValueError(f"fork needs pools on a GPU, these are on {self.device}")
-        self._check_storages()
+        self._check_copy("fork", stream)
         st, off, ids, runs = B.codec_pages_fork(self._pages, self.head.page_size, page_off, page_ids, tokens, parents)
         if st != B.CODEC_OK:
             raise B.CodecError(st, "codec_pages_fork")
@@ -296,9 +309,7 @@ class KVCache:
     def compact(self, stream=None) -> np.ndarray:
         """Moves the held pages to the lowest ids, copying them on `stream`.  Returns the new id of every page: page
         lists go on as ``moved[page_ids]``."""
-        if self.device.type != "cuda":
-            raise ValueError(f"compact needs pools on a GPU, these are on {self.device}")
-        self._check_storages()
+        self._check_copy("compact", stream)
         st, runs = B.codec_pages_compact(self._pages, self.head.page_size, self.num_pages // 2)
         if st != B.CODEC_OK:
             raise B.CodecError(st, "codec_pages_compact")

@@ -367,3 +367,16 @@ def test_beam_tensor_refusals():
     with pytest.raises(C.CodecError):
         C.beam_reorder([x], beams, out=[x])             # onto itself
     assert C.beam_reorder([], beams) == []
+
+
+@pytest.mark.gpu
+def test_numbers_beyond_32_bits_are_refused():
+    x, scores, fin = torch.zeros(1, 2, 64, device=DEV), torch.zeros(1, 2, device=DEV), torch.ones(1, 2, dtype=torch.bool, device=DEV)
+    for k, eos in (((1 << 32) + 2, 0), (2, (1 << 32) + 5), (2, -(1 << 32) + 5), (-(1 << 32) + 2, 0)):
+        with pytest.raises(ValueError):
+            C.beam_select(x, scores, k, finished=fin, eos=eos)
+    wide = torch.zeros(1, 1, 1, dtype=torch.bfloat16, device=DEV).expand(1, (1 << 32) + 2, 1)
+    with pytest.raises(ValueError):
+        C.beam_reorder([wide], torch.zeros(1, 2, dtype=torch.int32, device=DEV))
+    with pytest.raises(ValueError):
+        C.beam_select(torch.zeros(1, 1, 1, device=DEV).expand(1, (1 << 32) + 2, 1), scores, 2)

@@ -1,5 +1,6 @@
 """Pages of a cache: who holds them, branches, moves (on the CPU), and the copies that belong to them (on the GPU)."""
 import ctypes
+from types import SimpleNamespace
 
 import numpy as np
 import pytest
@@ -203,6 +204,40 @@ def test_cache_without_a_gpu_refuses():
     assert cache.free_pages == 8
 
 
+def test_pools_no_copy_can_write_are_refused_before_pages_change_hands():
+    def views(d=128, side=0, offset=0, stride=None):
+        flat = torch.zeros(1 << 17, dtype=torch.bfloat16)
+        shape = (4, 2, 16, d)
+        strides = stride or (32 * d, 16 * d, d, 1)
+        return [(flat.as_strided(shape, strides, offset), flat.as_strided(shape, strides, (side or 128 * d) + offset))]
+
+    for head, pools, status in ((HeadConfig(8, 2, 96, DTYPE_BF16), views(96), C.CODEC_ERR_UNSUPPORTED),
+                                (HeadConfig(8, 2, 128, DTYPE_BF16), views(side=256), C.CODEC_ERR_INVALID_ARGUMENT),
+                                (HeadConfig(8, 2, 128, DTYPE_BF16), views(offset=4), C.CODEC_ERR_INVALID_ARGUMENT),
+                                (HeadConfig(8, 2, 128, DTYPE_BF16), views(stride=(2048, 4096, 128, 1)), C.CODEC_ERR_INVALID_ARGUMENT)):
+        cache = C.KVCache(head, 4, pools=pools, device="cpu")
+        ids = cache.take(2)
+        cache.release(ids[:1])
+        for call in (lambda: cache.copy([[1, 0, 2, 0, 1]]), lambda: cache.fork([0, 1], ids[1:], [3], [0, 0]), cache.compact):
+            with pytest.raises(C.CodecError) as e:
+                call()
+            assert e.value.status == status and cache.free_pages == 3 and cache.take(1).tolist() == [0]
+            cache.release([0])
+
+
+def test_numbers_beyond_32_bits_are_refused():
+    cache = C.KVCache(HeadConfig(8, 2, 128, DTYPE_BF16), 8, device="cpu")
+    for n in (-1, 9, (1 << 32) + 1, 1 << 31):
+        with pytest.raises(C.CodecError):
+            cache.take(n)
+    assert cache.free_pages == 8
+    for dim in (-2, 0, 258, (1 << 32) + 64):
+        with pytest.raises(C.CodecError):
+            C.Rotary(dim, device="cpu")
+    with pytest.raises(C.CodecError):
+        C.Rotary(64, device="cpu", scaling=dict(kind="yarn", factor=4.0, original_length=(1 << 32) + 4096))
+
+
 # ---- on the GPU ------------------------------------------------------------------------------------------
 
 
@@ -397,3 +432,18 @@ def test_refused_calls_change_nothing():
         with pytest.raises(ValueError):
             call()
     assert cache.free_pages == 1
+
+
+@pytest.mark.gpu
+def test_a_refused_stream_changes_nothing():
+    cache = C.KVCache(HeadConfig(8, 2, 128, DTYPE_BF16), 8, device=DEV)
+    ids = cache.take(4)
+    cache.release(ids[:2])
+    elsewhere = SimpleNamespace(device=torch.device("cuda", 1))
+    for call in (lambda s: cache.fork([0, 1], ids[2:3], [3], [0, 0], stream=s), lambda s: cache.compact(stream=s),
+                 lambda s: cache.copy([[2, 0, 1, 0, 3]], stream=s)):
+        with pytest.raises(ValueError):
+            call(elsewhere)
+    assert cache.free_pages == 6 and cache.take(2).tolist() == [0, 1]
+    cache.release([0, 1, 2, 3])
+    assert cache.free_pages == 8
