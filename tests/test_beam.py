@@ -380,3 +380,42 @@ def test_numbers_beyond_32_bits_are_refused():
         C.beam_reorder([wide], torch.zeros(1, 2, dtype=torch.int32, device=DEV))
     with pytest.raises(ValueError):
         C.beam_select(torch.zeros(1, 1, 1, device=DEV).expand(1, (1 << 32) + 2, 1), scores, 2)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("batch,beams,vocab,k", [(1 << 22, 1, 5, 3), (1 << 16, 64, 3, 64)])
+def test_select_most_beams(batch, beams, vocab, k):
+    """As many beams as a call takes.  Scores are below 16: half a step of 32 bits is 2^-21; an exponential is off by the rounding of
+    its argument (2^-20, below 16 octaves) and of itself (2^-22), the logarithm of their sum by as much."""
+    gen = torch.Generator(device=DEV).manual_seed(k)
+    x = torch.randn(batch, beams, vocab, device=DEV, generator=gen)
+    start = -torch.rand(batch, beams, device=DEV, generator=gen) * 4
+    print(f"[case] most beams {batch} {beams} {vocab} {k}", flush=True)
+    scores, b, t = C.beam_select(x, start, k)
+    at = (b.long() * vocab + t.long())
+    assert int(at.min()) >= 0 and int(b.max()) < beams and int(t.max()) < vocab
+    assert bool((at.sort(dim=1).values.diff(dim=1) > 0).all())                                     # none twice
+    all_ = (start.double()[:, :, None] + torch.log_softmax(x.double(), -1)).flatten(1)
+    best = all_.sort(dim=1, descending=True).values[:, :k]
+    assert float(all_.min()) > -16
+    assert float((all_.gather(1, at) - scores).abs().max()) < 2.0 ** -18
+    assert float((best - scores).abs().max()) < 2.0 ** -18
+
+
+@pytest.mark.gpu
+def test_reorder_most_beams_and_beyond_four_gigabytes():
+    gen = torch.Generator(device=DEV).manual_seed(9)
+    x = torch.randint(0, 1 << 30, (1 << 16, 64, 3), dtype=torch.int32, device=DEV, generator=gen)
+    beams = torch.randint(0, 64, (1 << 16, 64), dtype=torch.int32, device=DEV, generator=gen)
+    print("[case] most beams", flush=True)
+    out, = C.beam_reorder([x], beams)
+    assert torch.equal(out, x.gather(1, beams.long()[:, :, None].expand(-1, -1, 3)))
+    for shape, beams in (((1, 1, (1 << 32) + 48), [[0]]), ((2, 2, (1 << 31) + 17), [[1, 0], [0, 0]])):
+        print(f"[case] beyond four gigabytes {shape}", flush=True)
+        x = torch.randint(0, 256, shape, dtype=torch.uint8, device=DEV, generator=gen)
+        out, = C.beam_reorder([x], torch.tensor(beams, dtype=torch.int32, device=DEV))
+        for s, row in enumerate(beams):
+            for j, beam in enumerate(row):
+                assert torch.equal(out[s, j], x[s, beam])
+        del x, out
+        torch.cuda.empty_cache()
