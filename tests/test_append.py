@@ -417,3 +417,25 @@ def test_append_tensor_refusals():
                 side.append(0, None, k, k.clone(), i, torch.arange(3, device=DEV), rot)
             with pytest.raises(C.CodecError):
                 side.copy([(0, 0, 1, 0, 3)])
+
+
+@pytest.mark.gpu
+def test_append_more_tokens_than_a_launch():
+    """2^24 + 5 tokens: every row as by a call of few tokens, stored in reverse order."""
+    n = (1 << 24) + 5
+    head = HeadConfig(1, 1, 64, DTYPE_BF16, 16)
+    cache = C.KVCache(head, (n + 15) // 16, device=DEV)
+    gen = torch.Generator(device=DEV).manual_seed(11)
+    x = torch.randint(-30000, 30000, (1024, 3, 64), dtype=torch.int16, device=DEV, generator=gen) & 0xbfff       # (no NaN, no inf)
+    x = x.view(torch.bfloat16).repeat((n + 1023) // 1024, 1, 1)[:n]
+    positions = torch.arange(n, device=DEV)
+    rot = C.Rotary(64, device=DEV)
+    print("[case] more tokens than a launch", flush=True)
+    q = cache.append(0, x[:, :1], x[:, 1:2], x[:, 2:], positions, n - 1 - positions, rot)
+    k, v = (p[:, 0].reshape(-1, 64)[:n].flip(0) for p in cache.pools[0])
+    assert torch.equal(v, x[:, 2])
+    for at in (0, 12345, (1 << 23) - 100, (1 << 24) - 200, n - 300):
+        part = slice(at, at + 300)
+        assert torch.equal(q[part], rot.apply(x[part, :1], positions[part])) and torch.equal(k[part, None], rot.apply(x[part, 1:2], positions[part]))
+    del cache, k, v, q, x
+    torch.cuda.empty_cache()
