@@ -352,14 +352,15 @@ __global__ __launch_bounds__(kRowWaves * 64) void beam_rows_kernel(BeamParams P)
             const float all = wave_max(top);
             if (__builtin_fabsf(all) < 0x1p20f) ref = __builtin_ceilf(all * kLog2e);
         }
-        // 2^20: the reference is still near enough for the fraction of x log2 e - ref; false for NaN, too
+        // The chunk's terms go by the reference where 32 bits hold it (2^24; one that the other branch has set may be of any size)
+        // and none lies far above it; false for NaN, too.
         const float r = float(ref);
         const float chunk_sum = total([r](float a) { return __builtin_amdgcn_exp2f(__builtin_fmaf(a, kLog2e, -r)); });
-        if (ref != kNoRef && __all(chunk_sum < 0x1p20f)) {
+        if (__builtin_fabs(ref) <= 0x1p24 && __all(chunk_sum < 0x1p20f)) {
             sum += double(chunk_sum);
         } else {
-            // a larger reference, +inf, NaN, no token at all, or logits of a size that leaves the reference no fraction:
-            // differences from the chunk's largest
+            // no reference yet or one too large, terms far above it, +inf, NaN, no token at all: differences from the
+            // chunk's largest, whose distance to the reference is taken in 64 bits
 #pragma unroll
             for (int e = 0; e < kPieces; ++e) v[e] = v[e] != v[e] ? kMinusInf : fminf(v[e], 3.402823466e38f);
             top = largest();

@@ -223,6 +223,43 @@ def test_select_large():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+def test_select_logits_of_any_size(dtype):
+    """Three or four chunks of 2048 tokens a wave, 32 chunks apart.  Beams of one logit of any size, whose sum's logarithm is log(vocab); one
+    to three large ones in a wave's chunks; +inf beside the largest number; beams masked with -1e9 among ordinary ones.  check()'s
+    tolerance holds: differences of logits are 0, a few units, or so large that their exponential is 0."""
+    gen = torch.Generator().manual_seed(21)
+    most = torch.finfo(dtype).max
+    values = [0.0, 1e6, 1.4e6, 1.5e6, 3e6, 1.2e7, 2e7, 1e8, 1.1e8, 1e9, 1e20, 3e38, most]
+    values += [-v for v in values]
+    x = torch.empty(16, 8, 200000)
+    for i in range(64):                                 # one logit
+        x[i // 8, i % 8] = values[i % len(values)]
+    for i, v in enumerate(values + values[1:7]):        # the largest in three chunks, in two, in one
+        row = x[8 + i // 8, i % 8].fill_(-most)
+        for chunk in (3, 35, 67)[:3 - i % 3]:
+            row[2048 * chunk + 7] = v
+    x[12:] = draw(gen, 4, 8, 200000)
+    x[12, 3] = -1e9                                     # ruled out by a large negative number: all of a beam,
+    x[13, :, :2048 * 40] = -1e9                         # all that most waves read first,
+    x[13, 2, 2048 * 40:] = -1e9
+    x[14, 0, 5], x[14, 0, 2048 * 33] = math.inf, most   # what counts as the largest number, and that itself
+    x[14, 1, 5], x[14, 1, 2048 * 32 + 5] = most, math.inf
+    x[14, 2, 5], x[14, 2, 2048 * 32 + 5] = most, most
+    x[14, 3, 5], x[14, 3, 2048 * 32 + 5] = math.inf, math.inf
+    x[15, :, 2048 * 32:] += 1e8                         # far above the first chunk, and far below
+    x[15, 4:] *= -1
+    x = x.to(dtype)
+    scores = -3.0 * torch.arange(8.0)[None] - torch.rand(16, 8, generator=gen)
+    # every beam on its own, and 16 searches.  Of the rows with large ones the best only: the other tokens score -most - v,
+    # which is beyond 32 bits (and rounds to -inf) for v = most; of search 14 the best two: the oracle's 64 bits hold 3.4e38 to
+    # 2^75, so that the others are equal to it
+    for rows, k, alone in ((slice(0, 8), 64, 4), (slice(8, 12), 1, 1), (slice(12, 14), 64, 4), (slice(14, 15), 64, 2), (slice(15, 16), 64, 4)):
+        check(x[rows].reshape(-1, 1, x.shape[2]), scores[rows].reshape(-1, 1), alone)
+        check(x[rows], scores[rows], k)
+
+
+@pytest.mark.gpu
 def test_select_beyond_four_gigabytes():
     """64 beams of 2^24 logits: 4.3 GB; the best tokens are planted, the sum is known."""
     beams, vocab = 64, 1 << 24
