@@ -242,6 +242,16 @@ def _i32(a):
     return np.ascontiguousarray(a, dtype=np.int32)
 
 
+def _ids(a):
+    """A list of pages, tokens or sequences as int32; None if one of them is no whole number of 32 bits (a cast would take
+    its low bits, or another page)."""
+    a = np.asarray(a)
+    if a.dtype.kind not in "iu" and a.size:
+        return None
+    ids = _i32(a)
+    return None if a.dtype.char != "i" and np.count_nonzero(ids != a) else ids
+
+
 def _in(a):
     """Read-only argument of a short call: the array's bytes (a fifth of the time its pointer takes to get), if they are few."""
     return a.tobytes() if a.nbytes <= 1 << 16 else a.ctypes.data
@@ -434,6 +444,8 @@ def codec_append(head, rotary, q, q_out, k, v, positions_ptr: int, slots_ptr: in
 
 def codec_pages_create(num_pages: int):
     """Returns (status, handle or None)."""
+    if not _is_int32(num_pages):
+        return CODEC_ERR_INVALID_ARGUMENT, None
     handle = c_void_p()
     st = _lib.codec_pages_create(num_pages, byref(handle))
     return st, (handle if st == CODEC_OK else None)
@@ -457,18 +469,24 @@ def codec_pages_take(pages, n: int):
 
 
 def codec_pages_hold(pages, ids) -> int:
-    ids = _i32(ids)
+    ids = _ids(ids)
+    if ids is None:
+        return CODEC_ERR_INVALID_ARGUMENT
     return _lib.codec_pages_hold(pages, _in(ids), ids.size)
 
 
 def codec_pages_release(pages, ids) -> int:
-    ids = _i32(ids)
+    ids = _ids(ids)
+    if ids is None:
+        return CODEC_ERR_INVALID_ARGUMENT
     return _lib.codec_pages_release(pages, _in(ids), ids.size)
 
 
 def codec_pages_fork(pages, page_size: int, page_off, page_ids, tokens, parents):
     """Returns (status, page_off, page_ids, runs [n, 5]) of the sequences that go on, or (status, None, None, None)."""
-    off, ids, tokens, parents = _i32(page_off), _i32(page_ids), _i32(tokens), _i32(parents)
+    off, ids, tokens, parents = _ids(page_off), _ids(page_ids), _ids(tokens), _ids(parents)
+    if off is None or ids is None or tokens is None or parents is None or not _is_int32(page_size):
+        return CODEC_ERR_INVALID_ARGUMENT, None, None, None
     num_seq, num_out = tokens.size, parents.size
     if off.ndim != 1 or off.size != num_seq + 1 or off[0] != 0 or off[-1] != ids.size:      # the C call reads by these lengths
         return CODEC_ERR_INVALID_ARGUMENT, None, None, None
@@ -489,6 +507,8 @@ def codec_pages_fork(pages, page_size: int, page_off, page_ids, tokens, parents)
 
 def codec_pages_compact(pages, page_size: int, capacity: int):
     """Returns (status, runs [n, 5] or None)."""
+    if not (_is_int32(page_size) and _is_int32(capacity)):
+        return CODEC_ERR_INVALID_ARGUMENT, None
     runs, n = np.empty((max(0, capacity), 5), np.int32), c_int32(0)
     st = _lib.codec_pages_compact(pages, page_size, runs.ctypes.data, capacity, byref(n))
     return st, (runs[:n.value] if st == CODEC_OK else None)
@@ -496,8 +516,8 @@ def codec_pages_compact(pages, page_size: int, capacity: int):
 
 def codec_cache_copy(head, layout, k_ptrs, v_ptrs, runs, stream: int = 0) -> int:
     """``head``: codec_head_config; ``layout``: codec_kv_layout; ``k_ptrs``, ``v_ptrs``: the layers' pools; ``runs``: [n, 5]."""
-    runs = _i32(runs)
-    if len(k_ptrs) != len(v_ptrs) or runs.ndim != 2 or runs.shape[1] != 5:
+    runs = _ids(runs)
+    if runs is None or len(k_ptrs) != len(v_ptrs) or runs.ndim != 2 or runs.shape[1] != 5:
         return CODEC_ERR_INVALID_ARGUMENT
     pools = f"{len(k_ptrs)}P"                           # bytes as an array of pointers
     return _lib.codec_cache_copy(head, layout, len(k_ptrs), struct.pack(pools, *k_ptrs), struct.pack(pools, *v_ptrs), _in(runs), len(runs),

@@ -141,7 +141,8 @@ class KVCache:
     "thd": pools [num_pages, page_size, num_kv_heads, head_dim]; "htd": [num_pages, num_kv_heads, page_size, head_dim].
     ``pools``: the (k, v) tensors of the layers if the program has them already (views with other strides too, the same
     in every layer); otherwise they are allocated.  All pages are free at first: page lists that are in use already
-    are made known by ``hold``.
+    are made known by ``hold``.  Lists of pages, tokens, sequences and runs are arrays of any integer type; a number beyond
+    32 bits is refused, and so is a fraction.
     """
 
     _pages = None

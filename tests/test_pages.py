@@ -238,6 +238,52 @@ def test_numbers_beyond_32_bits_are_refused():
         C.Rotary(64, device="cpu", scaling=dict(kind="yarn", factor=4.0, original_length=(1 << 32) + 4096))
 
 
+BEYOND = [(1 << 32) + 3, (1 << 33) + 3, (1 << 31) + 3, -(1 << 32) + 3, -(1 << 31) - 1]
+OTHERS = [np.array([2.9]), np.array([3.0]), np.array([np.nan]), np.array([True]), np.array([(1 << 63) + 3], np.uint64), np.array([(1 << 32) + 3], np.uint64),
+          [1 << 70], torch.tensor([(1 << 32) + 3]), torch.tensor([3.5])] + [np.array([n]) for n in BEYOND] + [[n] for n in BEYOND]
+
+
+@pytest.mark.parametrize("bad", OTHERS, ids=str)
+def test_lists_of_other_than_32_bit_numbers_are_refused(bad):
+    """64-bit numbers are not cut to another page's, fractions not rounded; nothing changes hands."""
+    x = Held(8)
+    assert C.codec_pages_take(x.h, 5)[0] == C.CODEC_OK
+    for call in (C.codec_pages_hold, C.codec_pages_release):
+        assert call(x.h, bad) == C.CODEC_ERR_INVALID_ARGUMENT and C.codec_pages_free(x.h) == 3
+    fork = lambda off=(0, 1, 2), ids=(0, 3), tokens=(5, 3), parents=(1,): C.codec_pages_fork(x.h, 16, off, ids, tokens, parents)
+    n = bad[0].item() if isinstance(bad, (np.ndarray, torch.Tensor)) else bad[0]
+    same = (lambda v: v) if isinstance(bad, list) else torch.tensor if isinstance(bad, torch.Tensor) else lambda v: np.array(v, dtype=bad.dtype)
+    for kw in (dict(off=same([0, 1, n])), dict(ids=same([0, n])), dict(tokens=same([5, n])), dict(parents=same([n]))):
+        assert fork(**kw) == (C.CODEC_ERR_INVALID_ARGUMENT, None, None, None), kw
+        assert C.codec_pages_free(x.h) == 3
+    head, lay = C.codec_head_config(8, 2, 128, 1, 16, 0.0), C.codec_kv_layout(9, 4096, 128, 2048)
+    for run in ([n, 0, 4, 0, 1], [1, n, 4, 0, 1], [1, 0, n, 0, 1], [1, 0, 4, n, 1], [1, 0, 4, 0, n]):
+        assert C.codec_cache_copy(head, lay, (1 << 32,), (1 << 33,), same([run])) == C.CODEC_ERR_INVALID_ARGUMENT
+
+
+@pytest.mark.parametrize("dtype", [np.int8, np.uint8, np.int16, np.uint16, np.int32, np.uint32, np.int64, np.uint64, np.dtype(">i8"), None])
+def test_lists_of_whole_numbers_of_any_type(dtype):
+    x = Held(8)
+    make = list if dtype is None else lambda v: np.array(v, dtype)
+    assert C.codec_pages_hold(x.h, make([0, 3, 3])) == C.codec_pages_release(x.h, make([3])) == C.CODEC_OK
+    assert C.codec_pages_hold(x.h, []) == C.codec_pages_release(x.h, ()) == C.codec_pages_hold(x.h, make([])) == C.CODEC_OK
+    st, off, ids, runs = C.codec_pages_fork(x.h, 16, make([0, 1, 2]), make([0, 3]), make([5, 3]), make([1, 1]))
+    assert st == C.CODEC_OK and ids.tolist() == [3, 1] and runs.tolist() == [[3, 0, 1, 0, 3]] and C.codec_pages_free(x.h) == 6
+    st, off, ids, runs = C.codec_pages_fork(x.h, 16, off, ids, [3, 3], [])
+    assert st == C.CODEC_OK and off.tolist() == [0] and C.codec_pages_free(x.h) == 8
+
+
+def test_counts_beyond_32_bits_are_refused():
+    for n in ((1 << 32) + 5, 1 << 31, -(1 << 32) + 5):
+        assert C.codec_pages_create(n) == (C.CODEC_ERR_INVALID_ARGUMENT, None)
+    x = Held(8)
+    assert C.codec_pages_hold(x.h, [7]) == C.CODEC_OK
+    for page_size, capacity in (((1 << 32) + 16, 4), (16, (1 << 32) + 4), (16, -(1 << 32) + 4)):
+        assert C.codec_pages_compact(x.h, page_size, capacity) == (C.CODEC_ERR_INVALID_ARGUMENT, None)
+    assert C.codec_pages_fork(x.h, (1 << 32) + 16, [0, 1], [7], [3], [0])[0] == C.CODEC_ERR_INVALID_ARGUMENT
+    assert C.codec_pages_free(x.h) == 7
+
+
 # ---- on the GPU ------------------------------------------------------------------------------------------
 
 
