@@ -19,6 +19,8 @@ _SCALINGS = {"linear": B.CODEC_ROTARY_LINEAR, "ntk": B.CODEC_ROTARY_NTK, "wavele
 _current_device = getattr(torch._C, "_cuda_getDevice", None)               # absent in a PyTorch without a GPU runtime
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 _Rows = B.codec_rows
+_data_ptr, _base_ptr, _nbytes = torch.Tensor.data_ptr, torch.UntypedStorage.data_ptr, torch.UntypedStorage.nbytes
+_NO_RUNS = np.empty((0, 5), np.int32)
 
 
 def _device(device) -> torch.device:
@@ -53,13 +55,14 @@ def _check_reach(t: torch.Tensor, what: str, last: int, size: int) -> None:
 
 def _rows(t: torch.Tensor, what: str, shape, dtype: torch.dtype, index: int):
     """`t` as codec_rows: `shape` = (tokens, heads, head_dim) with contiguous channels, in storage that is there."""
-    if t.shape != shape or t.dtype is not dtype or t.get_device() != index or t.stride()[2] != 1:
+    strides = t.stride()
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != index or strides[2] != 1:
         raise ValueError(f"{what}: need a {dtype} tensor of shape {tuple(shape)} with contiguous channels on cuda:{index}, "
-                         f"got {t.dtype} {tuple(t.shape)} on {t.device}, strides {t.stride()}")
+                         f"got {t.dtype} {tuple(t.shape)} on {t.device}, strides {strides}")
     tokens, heads, head_dim = shape
     if tokens == 0:
         return _Rows(0, 0, 0)
-    token_stride, head_stride, _ = t.stride()
+    token_stride, head_stride, _ = strides
     if tokens == 1:                         # the stride of a single token or head says nothing
         token_stride = 0
     if heads == 1:
@@ -158,9 +161,9 @@ class KVCache:
         shape = (self.num_pages, ps, h, d) if layout == "thd" else (self.num_pages, h, ps, d)
         if pools is None:
             pools = [tuple(torch.empty(shape, dtype=self.dtype, device=self.device) for _ in "kv") for _ in range(layers)]
-        self.pools = tuple(tuple(kv) for kv in pools)
-        flat = [p for kv in self.pools for p in kv]
-        if not flat or any(len(kv) != 2 for kv in self.pools):
+        self._pools = tuple(tuple(kv) for kv in pools)
+        flat = [p for kv in self._pools for p in kv]
+        if not flat or any(len(kv) != 2 for kv in self._pools):
             raise ValueError("pools: need a (k, v) pair for every layer")
         strides = flat[0].stride()
         for p in flat:
@@ -173,10 +176,13 @@ class KVCache:
         self._head = B.codec_head_config(head.num_q_heads, h, d, head.dtype, ps, 0.0)
         self._index = self.device.index if self.device.type == "cuda" else None
         self._q_row, self._kv_row = (head.num_q_heads, d), (h, d)
+        # what a pool has to be when it is used
+        self._flat, self._strides, self._count = tuple(flat), strides, flat[0].numel()
         self._reach = (self.num_pages - 1) * page + (ps - 1) * token + (h - 1) * kv_head + d
-        # per layer, what has to be there: (storage, bytes)
-        self._storages = [[(p.untyped_storage(), 2 * (p.storage_offset() + self._reach)) for p in kv] for kv in self.pools]
-        self._copy_status = self._enqueue(np.empty((0, 5), np.int32), 0)        # whether pages of these pools can be copied
+        # and where the pools were when they were last looked at: address, storage with its address and bytes
+        self._places, self._storages = [p.data_ptr() for p in flat], [p.untyped_storage() for p in flat]
+        self._bases, self._sizes = [-1] * len(flat), [-1] * len(flat)
+        self._copy_status = None            # whether pages of these pools can be copied, once that was asked
         st, self._pages = B.codec_pages_create(self.num_pages)
         if st != B.CODEC_OK:
             raise B.CodecError(st, "codec_pages_create")
@@ -187,16 +193,42 @@ class KVCache:
         except Exception:
             pass
 
+    @property
+    def pools(self):
+        """The layers' (k, v) tensors."""
+        return self._pools
+
     def paged(self, node_page_off, page_ids):
         """These pools with a forest's page lists: the ``paged`` of a PlannedAttention."""
         return SimpleNamespace(node_page_off=node_page_off, page_ids=page_ids, num_pages=self.num_pages,
                                page_stride=self.page_stride, token_stride=self.token_stride, head_stride=self.head_stride)
 
+    def _check_pool(self, i: int) -> None:
+        """Looks at pool i as it is now, and keeps where it is."""
+        p = self._flat[i]
+        storage = p.untyped_storage()
+        if storage.nbytes() < 2 * (p.storage_offset() + self._reach):
+            raise ValueError(f"pools of layer {i // 2}: the storage ends before the last page")
+        if p.stride() != self._strides or p.numel() != self._count or p.dtype is not self.dtype or p.device != self.device:
+            raise ValueError(f"pools of layer {i // 2}: {self._count} elements of {self.dtype} on {self.device} with strides {self._strides} "
+                             f"were handed over, now they are {p.dtype} {tuple(p.shape)} on {p.device} with strides {p.stride()}")
+        self._places[i], self._storages[i], self._bases[i], self._sizes[i] = p.data_ptr(), storage, storage.data_ptr(), storage.nbytes()
+        self._copy_status = None
+
     def _check_storage(self, layer: int) -> None:
-        """A tensor keeps its shape when its storage is given back: the memory behind it is what counts."""
-        for storage, need in self._storages[layer]:
-            if storage.nbytes() < need:
-                raise ValueError(f"pools of layer {layer}: the storage ends before the last page")
+        """A pool is a tensor that others hold too: it may get other memory (``data``, ``set_``), or its storage may.  What has been
+        looked at is not looked at again while the tensor begins where it did and the storage, which is held, is still there."""
+        for i in (2 * layer, 2 * layer + 1):
+            storage = self._storages[i]
+            if self._flat[i].data_ptr() != self._places[i] or storage.data_ptr() != self._bases[i] or storage.nbytes() != self._sizes[i]:
+                self._check_pool(i)
+
+    def _check_storages(self) -> None:
+        """_check_storage of all layers."""
+        if (list(map(_data_ptr, self._flat)) != self._places or list(map(_base_ptr, self._storages)) != self._bases
+                or list(map(_nbytes, self._storages)) != self._sizes):
+            for i in range(len(self._flat)):
+                self._check_pool(i)
 
     def append(self, layer, q, k, v, positions, slots, rotary: Rotary = None, q_out: torch.Tensor = None, stream=None):
         """The step's tokens into ``layer``: queries and keys turned to ``positions``, keys and values stored at ``slots``
@@ -231,9 +263,9 @@ class KVCache:
             if rotary.device != self.device:
                 raise ValueError(f"rotary is on {rotary.device}, the pools are on {self.device}")
             config, at = rotary._config[0], _index(positions, "positions", tokens, index)
-        kp, vp = self.pools[layer]
+        kp, vp = self._places[2 * layer], self._places[2 * layer + 1]
         st = B.codec_append(self._head, config, q_rows, out_rows, k_rows, v_rows, at, _index(slots, "slots", tokens, index),
-                            tokens, kp.data_ptr(), vp.data_ptr(), self._layout, s)
+                            tokens, kp, vp, self._layout, s)
         if st != B.CODEC_OK:
             raise B.CodecError(st, "codec_append")
         return q_out
@@ -264,19 +296,23 @@ class KVCache:
     def copy(self, runs, stream=None) -> None:
         """Copies runs of tokens, rows (source page, source token, destination page, destination token, tokens), in the
         pools of every layer.  No token may be written twice, or read and written."""
-        self._check_copy("copy", stream)
+        self._check_pools()
+        self._check_call("copy", stream)
         self._copy_on(runs, stream)
 
-    def _check_copy(self, what: str, stream) -> None:
-        """All that can refuse a copy but its runs: looked at before pages change hands."""
+    def _check_pools(self) -> None:
+        """Whether pages of the pools can be copied."""
+        self._check_storages()
+        if self._copy_status is None:
+            self._copy_status = self._enqueue(_NO_RUNS, 0)
         if self._copy_status != B.CODEC_OK:
             raise B.CodecError(self._copy_status, "codec_cache_copy")
+
+    def _check_call(self, what: str, stream) -> None:
         if self.device.type != "cuda":
             raise ValueError(f"{what} needs pools on a GPU, these are on {self.device}")
         if stream is not None and stream.device != self.device:
             raise ValueError(f"stream: on {stream.device}, the pools are on {self.device}")
-        for layer in range(len(self.pools)):
-            self._check_storage(layer)
 
     def _copy_on(self, runs, stream):
         s = _enter(self.device.index, stream)
@@ -291,26 +327,34 @@ class KVCache:
             raise B.CodecError(st, "codec_cache_copy")
 
     def _enqueue(self, runs, s):
-        return B.codec_cache_copy(self._head, self._layout, [k.data_ptr() for k, _ in self.pools],
-                                  [v.data_ptr() for _, v in self.pools], runs, s)
+        return B.codec_cache_copy(self._head, self._layout, self._places[0::2], self._places[1::2], runs, s)
 
     def fork(self, page_off, page_ids, tokens, parents, stream=None):
         """Sequence s holds the pages page_ids[page_off[s]:page_off[s + 1]] with tokens[s] tokens.  In the place of these
         sequences others go on, sequence j from sequence parents[j]: a sequence may go on once, several times or not at
         all.  Returns the page lists (page_off, page_ids) of those that go on.  They share whole pages; what is partly
         filled is copied on `stream` for all but the first (see codec_pages_fork)."""
-        self._check_copy("fork", stream)
+        if self._copy_status != B.CODEC_OK:             # not looked at yet, or known to be refused
+            self._check_pools()
+        self._check_call("fork", stream)
         st, off, ids, runs = B.codec_pages_fork(self._pages, self.head.page_size, page_off, page_ids, tokens, parents)
         if st != B.CODEC_OK:
             raise B.CodecError(st, "codec_pages_fork")
         if len(runs):
-            self._copy_on(runs, stream)
+            try:
+                self._check_pools()
+                self._copy_on(runs, stream)
+            except Exception:                           # the pages are held by the old lists again
+                B.codec_pages_hold(self._pages, page_ids)
+                B.codec_pages_release(self._pages, ids)
+                raise
         return off, ids
 
     def compact(self, stream=None) -> np.ndarray:
         """Moves the held pages to the lowest ids, copying them on `stream`.  Returns the new id of every page: page
         lists go on as ``moved[page_ids]``."""
-        self._check_copy("compact", stream)
+        self._check_pools()
+        self._check_call("compact", stream)
         st, runs = B.codec_pages_compact(self._pages, self.head.page_size, self.num_pages // 2)
         if st != B.CODEC_OK:
             raise B.CodecError(st, "codec_pages_compact")

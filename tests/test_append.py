@@ -133,6 +133,66 @@ def test_cache_refusals():
         C.KVCache(HeadConfig(8, 2, 128, 2), 4, device="cpu")
 
 
+def other_pools(cache, device):
+    """What may become of a pool after it was handed over, that no call can use: (what, how)."""
+    like = dict(dtype=cache.dtype, device=device)
+    shape = cache.pools[0][0].shape
+    p_bytes = 2 * cache.pools[0][0].numel()
+
+    def cut(t):
+        t.untyped_storage().resize_(p_bytes)
+        return t
+
+    def data(make):
+        def change(p):
+            p.data = make()
+        return change
+    return [("smaller", data(lambda: torch.zeros(shape[0] - 1, *shape[1:], **like))),
+            ("a view that ends early", data(lambda: torch.zeros(shape, **like)[:2])),
+            ("spread", data(lambda: torch.zeros(shape[0], 2 * shape[1], *shape[2:], **like)[:, ::2])),
+            ("turned", data(lambda: torch.zeros(shape, **like).transpose(1, 2).contiguous().transpose(1, 2))),
+            ("of 32 bits", data(lambda: torch.zeros(shape, dtype=torch.float32, device=device))),
+            ("broadcast", data(lambda: torch.zeros(1, *shape[1:], **like).expand(shape))),
+            ("set, then cut", lambda p: (p.set_(torch.zeros(shape, **like)), p.untyped_storage().resize_(64))),
+            ("16 bytes too far", data(lambda: cut(torch.zeros(p_bytes // 2 + 8, **like)[8:].view(shape)))),
+            ("given back", lambda p: p.untyped_storage().resize_(0))]
+
+
+@pytest.mark.parametrize("which", range(9))
+@pytest.mark.parametrize("layout", ["thd", "htd"])
+def test_pools_are_looked_at_as_they_are_now(which, layout):
+    head = HeadConfig(8, 2, 128, DTYPE_BF16)
+    for at in (0, 1):
+        cache = C.KVCache(head, 4, layers=2, layout=layout, device="cpu")
+        cache._check_storage(0)
+        what, change = other_pools(cache, "cpu")[which]
+        change(cache.pools[1][at])
+        cache._check_storage(0)
+        with pytest.raises(ValueError):
+            cache._check_storage(1)
+    cache = C.KVCache(head, 4, layout=layout, device="cpu")
+    for p in cache.pools[0]:                            # other memory of the same kind
+        p.data = torch.zeros(8, *p.shape[1:], dtype=p.dtype)[2:6]
+    cache._check_storage(0)
+    with pytest.raises(AttributeError):
+        cache.pools = [tuple(torch.zeros_like(p) for p in cache.pools[0])]
+
+
+def test_pools_that_moved_where_no_copy_can_write_are_refused_before_pages_change_hands():
+    cache = C.KVCache(HeadConfig(8, 2, 128, DTYPE_BF16), 4, device="cpu")
+    ids = cache.take(2)
+    with pytest.raises(ValueError):                     # no GPU
+        cache.copy([(0, 0, 1, 0, 1)])
+    k, v = cache.pools[0]
+    k.data = v.data                                     # onto each other, and not aligned
+    for _ in range(2):
+        for call in (lambda: cache.copy([(0, 0, 1, 0, 1)]), cache.compact, lambda: cache.fork([0, 1], ids[:1], [3], [0, 0])):
+            with pytest.raises(C.CodecError):
+                call()
+            assert cache.free_pages == 2
+        k.data = torch.zeros(v.numel() + 8, dtype=v.dtype)[4:-4].view(v.shape)
+
+
 # ---- on the GPU ------------------------------------------------------------------------------------------
 
 
@@ -417,6 +477,80 @@ def test_append_tensor_refusals():
                 side.append(0, None, k, k.clone(), i, torch.arange(3, device=DEV), rot)
             with pytest.raises(C.CodecError):
                 side.copy([(0, 0, 1, 0, 3)])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("which", range(9))
+def test_pools_that_became_something_else_are_refused(which):
+    head = HeadConfig(8, 2, 128, DTYPE_BF16)
+    q, k = (torch.zeros(3, n, 128, dtype=torch.bfloat16, device=DEV) for n in (8, 2))
+    i = torch.arange(3, device=DEV)
+    cache = C.KVCache(head, 8, layers=2, device=DEV)
+    ids = cache.take(3)
+    cache.release(ids[:1])
+    what, change = other_pools(cache, DEV)[which]
+    print(f"[case] pool {what}", flush=True)
+    if which % 3:                                       # before or after they were looked at
+        cache.copy([(1, 0, 2, 0, 1)])
+    change(cache.pools[1][which % 2])
+    cache.append(0, q, k, k.clone(), i, i, C.Rotary(128, device=DEV))
+    for call in (lambda: cache.append(1, q, k, k.clone(), i, i, C.Rotary(128, device=DEV)), lambda: cache.copy([(1, 0, 2, 0, 1)]), cache.compact,
+                 lambda: cache.fork([0, 1], ids[1:2], [3], [0, 0])):
+        with pytest.raises(ValueError):
+            call()
+        assert cache.free_pages == 6 and cache.take(1)[0] == 0
+        cache.release([0])
+    cache.release(ids[1:])                              # they are held as they were
+    assert cache.free_pages == 8
+    torch.cuda.synchronize()
+
+
+@pytest.mark.gpu
+def test_fork_into_pools_that_moved_onto_each_other():
+    """What the fork would copy is refused when its pages are known: they go back."""
+    head = HeadConfig(8, 2, 128, DTYPE_BF16)
+    cache = C.KVCache(head, 8, device=DEV)
+    ids = cache.take(5)
+    cache.hold(ids[:2])
+    cache.copy([(0, 0, 1, 0, 1)])
+    k, v = cache.pools[0]
+    k.data = v.data
+    off = [0, 2, 3, 5, 7]                               # two sequences share a page and a half, one goes on twice, one ends
+    lists = ids[[0, 1, 2, 0, 1, 3, 4]]
+    for _ in range(2):
+        with pytest.raises(C.CodecError):
+            cache.fork(off, lists, [20, 3, 20, 32], [0, 1, 1, 2])
+        assert cache.free_pages == 3 and cache.take(3).tolist() == [5, 6, 7]
+        cache.release([7, 6, 5])
+    k.data = torch.zeros_like(v)
+    new_off, new = cache.fork(off, lists, [20, 3, 20, 32], [0, 1, 1, 2])
+    assert new_off.tolist() == [0, 2, 3, 4, 6] and new.tolist() == [0, 5, 2, 6, 0, 7] and cache.free_pages == 3      # 1, 3, 4
+    cache.release(new)
+    assert cache.free_pages == 8
+
+
+@pytest.mark.gpu
+def test_pools_that_got_other_memory():
+    """The calls write where the tensor is now; what it had before is free."""
+    head = HeadConfig(8, 2, 128, DTYPE_BF16)
+    gen = torch.Generator().manual_seed(12)
+    k, v = (torch.randn(3, 2, 128, generator=gen).to(torch.bfloat16).to(DEV) for _ in "kv")
+    cache = C.KVCache(head, 4096, device=DEV)
+    before = torch.cuda.memory_allocated()
+    big = [torch.zeros(8192, 2, 16, 128, dtype=torch.bfloat16, device=DEV) for _ in "kv"]
+    for p, b in zip(cache.pools[0], big):
+        p.data = b[100:100 + 4096]
+    slots = torch.tensor([5, 65535, 17], device=DEV)
+    cache.append(0, None, k, v, None, slots)
+    cache.copy([(1, 1, 4000, 3, 1)])
+    del slots
+    assert torch.cuda.memory_allocated() - before == 4096 * 2 * 16 * 128 * 2 * 2         # twice as much as there was, which is free
+    torch.cuda.synchronize()
+    for x, b in zip((k, v), big):
+        want = torch.zeros_like(b)
+        for row, page, token in ((0, 0, 5), (1, 4095, 15), (2, 1, 1), (2, 4000, 3)):
+            want[100 + page, :, token] = x[row]
+        assert torch.equal(b, want)
 
 
 @pytest.mark.gpu
