@@ -6,6 +6,7 @@ import torch
 from . import binding as B
 from .cache import _check_reach, _enter, _on
 
+_is_conj, _is_neg = torch.Tensor.is_conj, torch.Tensor.is_neg
 _CODE = {torch.float16: B.CODEC_DTYPE_FP16, torch.bfloat16: B.CODEC_DTYPE_BF16, torch.float32: B.CODEC_DTYPE_FP32}
 
 
@@ -37,6 +38,8 @@ def beam_select(logits: torch.Tensor, scores: torch.Tensor, k: int, finished: to
 def _select(logits, scores, k, finished, eos, s):
     batch, beams, vocab = logits.shape
     strides, index = logits.stride(), logits.get_device()
+    if logits.is_neg() or scores.is_neg():
+        raise ValueError("logits or scores: a view that is negated when it is read (see torch.Tensor.resolve_neg)")
     if vocab > 1 and strides[2] != 1:
         raise ValueError(f"logits: the tokens of a beam must be contiguous, strides are {strides}")
     if batch and beams and vocab:
@@ -97,6 +100,8 @@ def _state(t: torch.Tensor, what: str, batch: int, beams: int, index: int):
 
 def _states(tensors, what: str, batch: int, beams: int, index: int):
     """_state of each; a dense tensor like the one before it is only looked at for what may differ."""
+    if any(map(_is_conj, tensors)) or any(map(_is_neg, tensors)):
+        raise ValueError(f"{what}: a view that is conjugated or negated when it is read (bytes are moved as they are; see torch.Tensor.resolve_conj)")
     out, shape, dtype, dense, fields = [], None, None, False, None
     for i, t in enumerate(tensors):
         if dense and t.shape == shape and t.dtype is dtype and t.is_contiguous() and t.get_device() == index:

@@ -407,6 +407,33 @@ def test_beam_tensor_refusals():
 
 
 @pytest.mark.gpu
+def test_views_that_change_when_they_are_read_are_refused():
+    """Conjugated and negated views: their bytes are not their values."""
+    gen = torch.Generator().manual_seed(22)
+    z = torch.randn(2, 3, 5, dtype=torch.complex64, generator=gen).to(DEV)
+    x = torch.randn(2, 3, 50, generator=gen).to(DEV)
+    beams = torch.tensor([[2, 0, 0], [1, 1, 2]], dtype=torch.int32, device=DEV)
+    rows = torch.arange(2, device=DEV)[:, None], beams.long()
+    one = torch.randn(1, 1, dtype=torch.complex64, generator=gen).to(DEV).conj().imag
+    lazy = [z.conj(), z.conj()[:, :, 1:4], z[..., 0].conj().imag, z[..., 0].conj()]
+    for t in lazy:
+        assert t.is_conj() or t.is_neg()
+        for states, out in (([t], None), ([x, t], None), ([t.resolve_conj().resolve_neg(), t], None), ([t.resolve_conj().resolve_neg()], [t])):
+            with pytest.raises(ValueError):
+                C.beam_reorder(states, beams, out=out)
+    for t in lazy + [z, z[..., 0].imag]:
+        t = t.resolve_conj().resolve_neg()
+        assert torch.equal(C.beam_reorder([t, t], beams)[1], t[rows])
+    row = torch.randn(1, 1, 4, generator=gen).to(DEV)
+    assert one.is_neg() and one.is_contiguous()
+    with pytest.raises(ValueError):
+        C.beam_select(row, one, 2)
+    with pytest.raises(ValueError):
+        C.beam_select(one[:, :, None], torch.zeros(1, 1, device=DEV), 1)
+    assert torch.equal(C.beam_select(row, one.resolve_neg(), 2)[2][0].cpu(), row[0, 0].topk(2).indices.int().cpu())
+
+
+@pytest.mark.gpu
 def test_numbers_beyond_32_bits_are_refused():
     x, scores, fin = torch.zeros(1, 2, 64, device=DEV), torch.zeros(1, 2, device=DEV), torch.ones(1, 2, dtype=torch.bool, device=DEV)
     for k, eos in (((1 << 32) + 2, 0), (2, (1 << 32) + 5), (2, -(1 << 32) + 5), (-(1 << 32) + 2, 0)):
