@@ -124,7 +124,7 @@ class Rotary:
 
     def _apply(self, x, positions, inverse, out, s):
         shape, index = x.shape, self.device.index
-        if (shape[0] | shape[1]) >> 31:
+        if (shape[0] | shape[1] | shape[2]) >> 31:
             raise ValueError(f"x: {tuple(shape)} is too large for a call")
         rows = _rows(x, "x", shape, x.dtype, index)
         at = _index(positions, "positions", shape[0], index)

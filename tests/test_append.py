@@ -554,6 +554,16 @@ def test_pools_that_got_other_memory():
 
 
 @pytest.mark.gpu
+def test_rows_beyond_32_bits_are_refused():
+    """2^32 + 64 channels are not 64."""
+    x = torch.empty(1, 1, (1 << 32) + 64, dtype=torch.bfloat16, device=DEV)
+    with pytest.raises(ValueError):
+        C.Rotary(64, device=DEV).apply(x, torch.zeros(1, dtype=torch.int64, device=DEV))
+    del x
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.gpu
 def test_append_more_tokens_than_a_launch():
     """2^24 + 5 tokens: every row as by a call of few tokens, stored in reverse order."""
     n = (1 << 24) + 5
