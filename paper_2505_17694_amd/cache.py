@@ -107,10 +107,15 @@ class Rotary:
         self.device = _device(device)
         self.rotary_dim = rotary_dim
         self.magnitude = factor if magnitude is None else magnitude
-        self.turns = torch.from_numpy(turns).to(self.device)        # turns a position, 64 bits
+        self._turns = torch.from_numpy(turns).to(self.device)
         layout = B.CODEC_ROTARY_INTERLEAVED if interleaved else B.CODEC_ROTARY_HALF
-        self._config = [B.codec_rotary_config(rotary_dim, layout, inverse, self.magnitude, self.turns.data_ptr())
+        self._config = [B.codec_rotary_config(rotary_dim, layout, inverse, self.magnitude, self._turns.data_ptr())
                         for inverse in (0, 1)]
+
+    @property
+    def turns(self) -> torch.Tensor:
+        """Turns of a pair from one position to the next, 64 bits (a copy: the table itself is what the calls read)."""
+        return self._turns.clone()
 
     def apply(self, x: torch.Tensor, positions: torch.Tensor, inverse=False, out: torch.Tensor = None, stream=None) -> torch.Tensor:
         """x [tokens, heads, head_dim] turned to its positions, or back (the gradient); ``out`` may be x itself."""

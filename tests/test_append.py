@@ -193,6 +193,18 @@ def test_pools_that_moved_where_no_copy_can_write_are_refused_before_pages_chang
         k.data = torch.zeros(v.numel() + 8, dtype=v.dtype)[4:-4].view(v.shape)
 
 
+def test_the_table_of_turns_is_the_calls_own():
+    """What is done to the tensor that a program gets leaves the memory the kernels read as it is."""
+    rot = C.Rotary(64, device="cpu")
+    want, at = rot.turns, rot._config[0].turns
+    rot.turns.untyped_storage().resize_(0)
+    rot.turns.data = torch.zeros(3)
+    rot.turns.mul_(2)
+    with pytest.raises(AttributeError):
+        rot.turns = want * 2
+    assert torch.equal(rot.turns, want) and rot._config[0].turns == rot._config[1].turns == at != want.data_ptr()
+
+
 # ---- on the GPU ------------------------------------------------------------------------------------------
 
 
