@@ -118,7 +118,8 @@ class Rotary:
         return self._turns.clone()
 
     def apply(self, x: torch.Tensor, positions: torch.Tensor, inverse=False, out: torch.Tensor = None, stream=None) -> torch.Tensor:
-        """x [tokens, heads, head_dim] turned to its positions, or back (the gradient); ``out`` may be x itself."""
+        """x [tokens, heads, head_dim] turned to its positions, or back (the gradient); ``out`` may be x itself.  Gradients pass
+        from the result to x, unless ``out`` is given: then x must not want any."""
         if x.dim() != 3 or x.dtype not in _CODE or self.device.type != "cuda":
             raise ValueError(f"x: need a 16-bit tensor [tokens, heads, head_dim] and a GPU, got {x.dtype} {tuple(x.shape)} on {x.device}")
         s = _enter(self.device.index, stream)
@@ -128,6 +129,13 @@ class Rotary:
         return self._apply(x, positions, inverse, out, s)
 
     def _apply(self, x, positions, inverse, out, s):
+        if x.requires_grad and torch.is_grad_enabled():
+            if out is not None:
+                raise ValueError("out: x wants a gradient, which does not pass through out")
+            return _Turn.apply(x, positions, self, inverse, s)
+        return self._turn(x, positions, inverse, out, s)
+
+    def _turn(self, x, positions, inverse, out, s):
         shape, index = x.shape, self.device.index
         if (shape[0] | shape[1] | shape[2]) >> 31:
             raise ValueError(f"x: {tuple(shape)} is too large for a call")
@@ -140,6 +148,23 @@ class Rotary:
         if st != B.CODEC_OK:
             raise B.CodecError(st, "codec_rotary")
         return out
+
+
+class _Turn(torch.autograd.Function):
+    """The turn is linear in x; its transpose is the turn the other way."""
+
+    @staticmethod
+    def forward(ctx, x, positions, rotary, inverse, s):
+        ctx.rotary, ctx.inverse = rotary, inverse
+        ctx.save_for_backward(positions)
+        return rotary._turn(x, positions, inverse, None, s)
+
+    @staticmethod
+    def backward(ctx, g):
+        positions, = ctx.saved_tensors
+        if not g.is_contiguous() or g.data_ptr() % 16:
+            g = g.clone(memory_format=torch.contiguous_format)
+        return ctx.rotary.apply(g, positions, not ctx.inverse), None, None, None, None
 
 
 class KVCache:
@@ -238,7 +263,8 @@ class KVCache:
     def append(self, layer, q, k, v, positions, slots, rotary: Rotary = None, q_out: torch.Tensor = None, stream=None):
         """The step's tokens into ``layer``: queries and keys turned to ``positions``, keys and values stored at ``slots``
         (page * page_size + token; negative: not stored).  Returns the turned queries (``q_out``, which may be q itself);
-        q None: keys and values only.  Without ``rotary`` rows pass as they are and ``positions`` may be None."""
+        q None: keys and values only.  Without ``rotary`` rows pass as they are and ``positions`` may be None.  A cache takes part
+        in no gradient: the queries come back without one (Rotary.apply passes it)."""
         if self._index is None:
             raise ValueError(f"append needs pools on a GPU, these are on {self.device}")
         s = _enter(self._index, stream)

@@ -414,6 +414,93 @@ def test_rotary_back(tokens, heads, d, r, interleaved):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("inverse", [False, True])
+@pytest.mark.parametrize("tokens,heads,d,r,dtype", [(1, 1, 64, 64, DTYPE_BF16), (37, 3, 128, 128, DTYPE_FP16), (200, 5, 256, 64, DTYPE_BF16), (9, 2, 64, 30, DTYPE_FP16)])
+def test_rotary_gradient(tokens, heads, d, r, dtype, interleaved, inverse):
+    """Against the formula (the transpose) and against differences; gradients of any strides, broadcast ones too; twice."""
+    print(f"[case] gradient {tokens} {heads} {d} {r} {interleaved} {inverse}", flush=True)
+    gen = torch.Generator().manual_seed(tokens)
+    scaling = dict(kind="yarn", factor=4.0, original_length=4096)
+    rot = C.Rotary(r, interleaved=interleaved, scaling=scaling, device=DEV)
+    turns, magnitude = rot.turns.cpu().numpy(), rot.magnitude
+    positions = np.random.default_rng(tokens).integers(0, 1 << 17, tokens)
+    at = torch.from_numpy(positions).to(DEV)
+    x, w, u = (torch.randn(tokens, heads, d, generator=gen).to(TORCH[dtype]) for _ in range(3))
+    leaf = x.to(DEV).requires_grad_()
+    y = rot.apply(leaf, at, inverse=inverse)
+    with torch.no_grad():
+        plain = rot.apply(leaf, at, inverse=inverse)
+    assert y.requires_grad and not plain.requires_grad and torch.equal(y, plain)
+    back, size = O.rotary(w.double().numpy(), positions, turns, magnitude, interleaved, inverse=not inverse)
+    odd = torch.zeros(tokens, heads, d + 3, dtype=TORCH[dtype], device=DEV)[:, :, 3:]     # no multiple of 16 bytes
+    wide = torch.zeros(tokens * heads * d + 3, dtype=TORCH[dtype], device=DEV)[3:].view(tokens, heads, d)
+    turned = torch.zeros(d, heads, tokens, dtype=TORCH[dtype], device=DEV).permute(2, 1, 0)
+    for g in (w.to(DEV), odd.copy_(w), wide.copy_(w), turned.copy_(w)):
+        (got,) = torch.autograd.grad(y, leaf, g, retain_graph=True)
+        close(got, back, size, dtype)
+    (got,) = torch.autograd.grad(y.sum(), leaf, retain_graph=True)                        # a broadcast gradient
+    ones, ones_size = O.rotary(np.ones((tokens, heads, d)), positions, turns, magnitude, interleaved, inverse=not inverse)
+    close(got, ones, ones_size, dtype)
+    # the turn is linear, so the difference along u is the turn of u; each side is rounded by half a step, of |w| |turned u| and |u| |back|
+    step = torch.finfo(TORCH[dtype]).eps / 2
+    u_turned = rot.apply(u.to(DEV), at, inverse=inverse).double().cpu().numpy()
+    (g,) = torch.autograd.grad(y, leaf, w.to(DEV), retain_graph=True)
+    g, w64, u64 = g.double().cpu().numpy(), w.double().numpy(), u.double().numpy()
+    assert abs(np.sum(w64 * u_turned) - np.sum(u64 * g)) <= 1.01 * step * (np.sum(np.abs(w64 * u_turned)) + np.sum(np.abs(u64 * g)))
+    # the gradient of the gradient by what it was taken of: the turn itself
+    v = w.to(DEV).requires_grad_()
+    (g,) = torch.autograd.grad(y, leaf, v, create_graph=True)
+    (gg,) = torch.autograd.grad(g, v, u.to(DEV))
+    assert torch.equal(gg, rot.apply(u.to(DEV), at, inverse=inverse))
+
+
+@pytest.mark.gpu
+def test_rotary_gradient_in_a_program():
+    """Through a projection, on another stream, of a part of a projection's output; what does not pass a gradient says so."""
+    gen = torch.Generator().manual_seed(31)
+    rot = C.Rotary(64, device=DEV)
+    at = torch.arange(6, device=DEV)
+    weight = torch.randn(3 * 64 * 4, 32, generator=gen).to(torch.bfloat16).to(DEV).requires_grad_()
+    x = torch.randn(6, 32, generator=gen).to(torch.bfloat16).to(DEV)
+    w = torch.randn(6, 4, 64, generator=gen).to(torch.bfloat16).to(DEV)
+    grads = []
+    side = torch.cuda.Stream()
+    for stream in (None, side):
+        q = (x @ weight.t()).view(6, 12, 64)[:, 4:8]
+        if stream is not None:
+            stream.wait_stream(torch.cuda.current_stream())
+        y = rot.apply(q, at, stream=stream)
+        if stream is not None:
+            torch.cuda.current_stream().wait_stream(stream)
+        y.backward(w)
+        torch.cuda.synchronize()
+        grads.append(weight.grad.clone())
+        weight.grad = None
+    back = rot.apply(w, at, inverse=True)
+    want = torch.zeros(6, 12, 64, dtype=torch.bfloat16, device=DEV)
+    want[:, 4:8] = back
+    want = want.view(6, -1).float().t() @ x.float()
+    size = want.new_zeros(6, 12, 64)
+    size[:, 4:8] = back.float().abs()
+    size = size.view(6, -1).t() @ x.float().abs()
+    # half a step of the sum, and 32-bit sums of six
+    for g in grads:
+        assert bool(((g.float() - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -20 * size).all())
+    leaf = w.clone().requires_grad_()
+    for out in (torch.empty_like(w), leaf):
+        with pytest.raises(ValueError):
+            rot.apply(leaf, at, out=out)
+    with torch.no_grad():
+        assert torch.equal(rot.apply(leaf, at, out=torch.empty_like(w)), rot.apply(w, at))
+    y = rot.apply(leaf, at)
+    at.add_(1)                                          # other positions than those of the call
+    with pytest.raises(RuntimeError):
+        y.backward(w)
+    assert not rot.apply(w, at).requires_grad
+
+
+@pytest.mark.gpu
 def test_append_on_another_stream_and_captured():
     """The call's stream is the one it is given; a captured call replays on what its tensors then hold."""
     head = HeadConfig(8, 2, 128, DTYPE_BF16)
