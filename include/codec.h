@@ -602,6 +602,7 @@ size_t codec_beam_workspace_bytes(const codec_beam_config *config);
  *   finished    device [batch][beams], bytes, nonzero = finished; NULL: none is
  *   out_scores, out_beams, out_tokens   device [batch][k], best first
  *   workspace   device scratch, >= codec_beam_workspace_bytes, 256-byte aligned; calls that share one must not overlap
+ * Outputs and scratch must not overlap one another or an input; out_scores may be scores itself where k == beams.
  * Equal scores go by the lowest beam, then the lowest token: in one beam equal logits, between beams scores that
  * agree to 2^-40 of themselves (they are 64-bit sums of 32-bit exponentials).  A logit of -inf is a token that is ruled out; NaN counts
  * as -inf, +inf as the largest 32-bit number; a score of NaN or +inf counts as -inf.  Candidates that score

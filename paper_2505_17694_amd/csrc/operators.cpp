@@ -415,6 +415,20 @@ int codec_beam_select(const codec_beam_config *config, const void *logits, int64
     if (finished && (c.eos < 0 || c.eos >= c.vocab)) return CODEC_ERR_INVALID_ARGUMENT;
     const BeamScratch s = beam_scratch(c);
     if (workspace_bytes < s.total) return CODEC_ERR_WORKSPACE_TOO_SMALL;
+    {
+        // what is written is neither read nor written twice; scores may go back to where they came from, search by search
+        const int64_t rows = int64_t(c.batch) * c.beams, span = (c.batch - 1) * batch_stride + (c.beams - 1) * beam_stride + c.vocab;
+        auto range = [](const void *p, int64_t bytes) { return Range{static_cast<const char *>(p), static_cast<const char *>(p) + bytes}; };
+        const Range out[] = {range(out_scores, 4 * int64_t(c.batch) * c.k), range(out_beams, 4 * int64_t(c.batch) * c.k),
+                             range(out_tokens, 4 * int64_t(c.batch) * c.k), range(workspace, int64_t(s.total))};
+        const Range in[] = {range(logits, size * span), range(scores, 4 * rows), range(finished, finished ? rows : 0)};
+        for (int i = 0; i < 4; ++i) {
+            for (int j = i + 1; j < 4; ++j)
+                if (overlap(out[i], out[j])) return CODEC_ERR_INVALID_ARGUMENT;
+            for (int j = 0; j < 3; ++j)
+                if (overlap(out[i], in[j]) && !(i == 0 && j == 1 && out_scores == scores && c.k == c.beams)) return CODEC_ERR_INVALID_ARGUMENT;
+        }
+    }
 
     char *ws = static_cast<char *>(workspace);
     codec::BeamParams p{};

@@ -56,6 +56,28 @@ def test_select_refusals():
         C.beam_select(torch.zeros(1, 2, 5), torch.zeros(1, 2), 2)
 
 
+def test_select_refuses_outputs_that_overlap():
+    """Every pair of them, and with every input; the scores of k == beams continuations may go back to their place."""
+    beams, vocab, k = 4, 1000, 4
+    at = dict(logits=1 << 30, scores=2 << 30, finished=3 << 30, out_scores=4 << 30, out_beams=5 << 30, out_tokens=6 << 30, workspace=7 << 30)
+    need = C.codec_beam_workspace_bytes(C.codec_beam_config(2, beams, vocab, k, 1, 2))
+    size = dict(logits=(1 * 6000 + 3 * 1200 + vocab) * 2, scores=32, finished=8, out_scores=32, out_beams=32, out_tokens=32, workspace=need)
+
+    def status(k=k, **kw):
+        a = dict(at, **kw)
+        return C.codec_beam_select(C.codec_beam_config(2, beams, vocab, k, 1, 2), a["logits"], 6000, 1200, a["scores"], a["finished"], a["out_scores"], a["out_beams"],
+                                   a["out_tokens"], a["workspace"], 1 << 20)
+    written = ["out_scores", "out_beams", "out_tokens", "workspace"]
+    for x in written:
+        for y in at:
+            if x != y:
+                for where in (at[y], at[y] + size[y] - 1, at[y] - size[x] + 1):
+                    if x != "workspace" and not (x == "out_scores" and y == "scores" and where == at[y]):
+                        assert status(**{x: where}) == C.CODEC_ERR_INVALID_ARGUMENT, (x, y, where)
+    assert status(logits=at["workspace"] + need - 2) == status(scores=at["workspace"] - 28) == C.CODEC_ERR_INVALID_ARGUMENT
+    assert status(k=3, out_scores=at["scores"]) == status(k=5, out_scores=at["scores"]) == C.CODEC_ERR_INVALID_ARGUMENT
+
+
 def test_reorder_refusals():
     a, b = 1 << 20, 1 << 21
 
@@ -257,6 +279,20 @@ def test_select_logits_of_any_size(dtype):
     for rows, k, alone in ((slice(0, 8), 64, 4), (slice(8, 12), 1, 1), (slice(12, 14), 64, 4), (slice(14, 15), 64, 2), (slice(15, 16), 64, 4)):
         check(x[rows].reshape(-1, 1, x.shape[2]), scores[rows].reshape(-1, 1), alone)
         check(x[rows], scores[rows], k)
+
+
+@pytest.mark.gpu
+def test_select_scores_back_to_their_place():
+    gen = torch.Generator().manual_seed(23)
+    for batch, beams in ((300, 7), (2, 64), (1, 1)):
+        x, c = draw(gen, batch, beams, 901, dtype=BF16).to(DEV), (-torch.rand(batch, beams, generator=gen)).to(DEV)
+        want = C.beam_select(x, c, beams)
+        cfg = C.codec_beam_config(batch, beams, 901, beams, 1, 0)
+        ws = torch.empty(C.codec_beam_workspace_bytes(cfg), dtype=torch.uint8, device=DEV)
+        got = torch.empty(2, batch, beams, dtype=torch.int32, device=DEV)
+        st = C.codec_beam_select(cfg, x.data_ptr(), beams * 901, 901, c.data_ptr(), None, c.data_ptr(), got[0].data_ptr(), got[1].data_ptr(), ws.data_ptr(),
+                                 ws.numel(), torch.cuda.current_stream().cuda_stream)
+        assert st == C.CODEC_OK and torch.equal(c, want[0]) and torch.equal(got[0], want[1]) and torch.equal(got[1], want[2])
 
 
 @pytest.mark.gpu
