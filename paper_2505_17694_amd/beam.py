@@ -25,7 +25,8 @@ _SCORES, _FLAGS, _BEAMS = (torch.float32,), (torch.bool, torch.uint8), (torch.in
 def beam_select(logits: torch.Tensor, scores: torch.Tensor, k: int, finished: torch.Tensor = None, eos: int = 0, stream=None):
     """The k best continuations of every search: logits [batch, beams, vocab] (16 or 32 bits), scores [batch, beams] (32 bits),
     ``finished`` [batch, beams] (truth values) beams go on with ``eos`` alone.  Returns (scores, beams, tokens), each
-    [batch, k], best first; ties go to the lowest beam, then the lowest token (see codec_beam_select)."""
+    [batch, k], best first; ties go to the lowest beam, then the lowest token (see codec_beam_select).  The three share one
+    allocation (to keep one of them for long, clone it) and have no gradient."""
     if logits.dim() != 3 or logits.dtype not in _CODE or not logits.is_cuda:
         raise ValueError(f"logits: need [batch, beams, vocab] of 16 or 32 bits on a GPU, got {logits.dtype} {tuple(logits.shape)} on {logits.device}")
     s = _enter(logits.get_device(), stream)
@@ -65,7 +66,9 @@ def _select(logits, scores, k, finished, eos, s):
 def beam_reorder(states, beams: torch.Tensor, out=None, stream=None):
     """The states of the beams that go on: of every tensor [batch, beams, ...] in ``states`` the rows ``beams`` [batch, n]
     (int32) names, as new tensors [batch, n, ...] or in those of ``out``.  Rows have to be contiguous.  A row whose entry is no
-    beam is left as it was (in a new tensor: undefined)."""
+    beam is left as it was (in a new tensor: undefined).  New tensors of neighbouring states of one shape and type share an
+    allocation, which lives as long as one of them: to keep one for long, or to save it alone, clone it.  Bytes are moved: the new
+    tensors have no gradient."""
     states = list(states)
     if beams.dim() != 2 or not beams.is_cuda:
         raise ValueError(f"beams: need [batch, n] on a GPU, got {tuple(beams.shape)} on {beams.device}")
@@ -76,11 +79,11 @@ def beam_reorder(states, beams: torch.Tensor, out=None, stream=None):
     return _reorder(states, beams, out, s)
 
 
-def _state(t: torch.Tensor, what: str, batch: int, beams: int, index: int):
+def _state(t: torch.Tensor, what: str, i: int, batch: int, beams: int, index: int):
     """Checks [batch, beams, ...] with contiguous rows in storage that is there; (bytes of a row, strides in bytes)."""
     shape, size = t.shape, t.element_size()
     if len(shape) < 2 or shape[0] != batch or shape[1] != beams or t.get_device() != index:
-        raise ValueError(f"{what}: need [{batch}, {beams}, ...] on cuda:{index}, got {tuple(shape)} on {t.device}")
+        raise ValueError(f"{what}[{i}]: need [{batch}, {beams}, ...] on cuda:{index}, got {tuple(shape)} on {t.device}")
     if t.is_contiguous():
         count = t.numel()
         if count == 0:
@@ -91,7 +94,7 @@ def _state(t: torch.Tensor, what: str, batch: int, beams: int, index: int):
     row, strides = 1, t.stride()
     for n, stride in zip(shape[:1:-1], strides[:1:-1]):
         if n != 1 and stride != row:
-            raise ValueError(f"{what}: the row of a beam must be contiguous, strides are {strides}")
+            raise ValueError(f"{what}[{i}]: the row of a beam must be contiguous, strides are {strides}")
         row *= n
     if row:
         _check_reach(t, what, (batch - 1) * strides[0] + (beams - 1) * strides[1] + row, size)
@@ -106,10 +109,12 @@ def _states(tensors, what: str, batch: int, beams: int, index: int):
     for i, t in enumerate(tensors):
         if dense and t.shape == shape and t.dtype is dtype and t.is_contiguous() and t.get_device() == index:
             if fields[0]:
+                if not count:
+                    count, size = t.numel(), t.element_size()
                 _check_reach(t, what, count, size)
         else:
-            fields = _state(t, f"{what}[{i}]", batch, beams, index)
-            shape, dtype, dense, count, size = t.shape, t.dtype, t.is_contiguous(), t.numel(), t.element_size()
+            fields = _state(t, what, i, batch, beams, index)
+            shape, dtype, dense, count = t.shape, t.dtype, t.is_contiguous(), 0
         out.append(fields)
     return out
 
