@@ -423,7 +423,7 @@ enum {
     CODEC_ROTARY_YARN = 4           /* YaRN (arXiv 2309.00071): f_i up to the pair that turns `fast` times
                                        over the original context (rounded down), f_i / factor from the one
                                        that turns `slow` times (rounded up), in between blended in i; the
-                                       turned channels grow by 0.1 ln(factor) + 1                          */
+                                       turned channels grow by 0.1 ln(factor) + 1 for factor > 1           */
 };
 
 typedef struct {

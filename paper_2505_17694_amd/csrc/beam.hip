@@ -298,9 +298,10 @@ struct Collector {
 // `kept`-th largest of the groups' largest is a bar that at least `kept` tokens reach, all of them in lanes whose largest does.
 // Groups are as wide as leaves two for every token wanted: with 32 groups and 16 wanted half of the groups reach the bar, which
 // 22 tokens then do.  Only the chunks of a lane whose largest reaches it are read again: 134 MB of logits make 139 MB fetched
-// (all chunks of such a lane: 170 MB, and 28 us for the largest of the times below).
+// (all chunks of such a lane: 170 MB, and 2 us more).  A mask that leaves tokens in fewer groups than are wanted leaves no bar: every
+// logit is looked at again, and a selection of 64 x 8 x 131072 takes 165 us in the place of 34.
 // Bound by the loads: a token takes seven lane operations, four of them the exponential.  64 x 8 beams of 131072 bf16 logits
-// (134 MB) take 26 us, of which the search for the tokens is 3 to 4; the read alone would be 20 at 6.9 TB/s.  The waves of a
+// (134 MB) take 27 us, of which the search for the tokens is 3 to 4; the read alone would be 20 at 6.9 TB/s.  The waves of a
 // workgroup take turns along the vocabulary: without that search, and with the kernel that follows, 34.0 us where each has a
 // stretch of its own, 31.6 in turn, 28.7 with the streaming hint too (ONCE); 4 x 32768 fp32 logits, which stay in the caches, 6.4
 // in turn and 7.6 with the hint.
@@ -551,8 +552,10 @@ __global__ __launch_bounds__(kMergeBeams * 64) void beam_merge_kernel(BeamParams
 }
 
 // A workgroup copies PIECES * 256 units of one row of one state, PIECES of a lane in flight.  Bound by HBM: 33 states of 16 KB a
-// beam of 512 beams (553 MB read and written, beams that several follow read once) take 64 us.  PIECES 2, 4 and 8: 64, 66 and 66
-// us there, 46, 29 and 21 us for 8 states of 16386 bytes, in units of two.  LARGE: with the streaming hint; 89 us without.
+// beam of 512 beams (277 MB written, 181 MB of rows that a beam follows) take 79 us, whether the same buffers are moved again or
+// others.  PIECES 2, 4 and 8: 79, 81 and 81 us there; 8 states of 16386 bytes, in units of two, 57, 37 and 29 us out of HBM, 46, 31
+// and 25 out of the last-level cache.  LARGE: with the streaming hint; 86 us without.  One state of single bytes beside 32 of 16 KB
+// makes bytes the unit of all: 108 us in the place of 77.  (All with random contents: zeros move up to a fifth faster.)
 template <class Unit, int PIECES, bool LARGE>
 __global__ __launch_bounds__(256) void reorder_kernel(ReorderParams P)
 {
@@ -583,7 +586,9 @@ __global__ __launch_bounds__(256) void reorder_kernel(ReorderParams P)
 
 }  // namespace
 
-// Waves that share a beam: enough for 16 on every CU, each with a chunk at least.
+// Waves that share a beam: enough for 16 on every CU, each with a chunk at least.  From 1366 rows on a workgroup has fewer than four
+// waves, and a CU's LDS holds four workgroups: 1024 rows of 131072 bf16 logits (16 waves a CU) are read at 5.0 TB/s, 4096 rows
+// (four) at 3.8, 285 us.
 BeamSplit beam_split(int64_t rows, int vocab)
 {
     const int64_t chunks = (int64_t(vocab) + kChunk - 1) / kChunk;

@@ -17,10 +17,11 @@ typedef uint32_t __attribute__((ext_vector_type(4))) Piece;
 // consecutive memory, `row_pieces` long: with tokens side by side a head's, with heads side by side a token's, else a token's in
 // one head (a plane each).  A lane finds its first piece by a division and the others by steps of 256.
 // Bound by HBM: 1000 pages of 8 x 128 channels in 8 layers (1.05 GB read and written) take 198 us, 5.3 TB/s; a plain copy of 1 GiB
-// reaches 5.15.  STORES_ONCE, LOADS_ONCE: with the streaming hint; without either 222 us, with that on the stores 206.  What
-// may lie in the last-level cache is loaded without: the last pages of 192 sequences in 16 layers take 27 us where they are there and
-// 47 with the hint, out of HBM 51 and 50.  PIECES 8 and 2: those pages 27 and 33 us; runs of one to five tokens of 8 x 64
-// channels 18.7 and 13.0, four pages of one layer 3.05 and 2.75.
+// reaches 5.15.  STORES_ONCE, LOADS_ONCE: with the streaming hint; without either 222 us, with that on the stores 207.  What
+// may lie in the last-level cache is loaded without: the last pages of 192 sequences in 16 layers (207 MB) take 32 us where the cache
+// has them and 45 with the hint, out of HBM 51 (4.1 TB/s) and 49.  PIECES 8 and 2: those pages 32 and 38 us, out of HBM 51 and 49;
+// 96 pages out of runs of one to five tokens of 8 x 64 channels in 8 layers (two launches) 18.6 and 13.7 out of HBM, 14.4 and 9.6
+// out of the cache; four pages of one layer 3.05 and 2.85.  (All with random contents: zeros move up to a fifth faster.)
 template <bool TOKENS_INSIDE, int PIECES, bool STORES_ONCE, bool LOADS_ONCE>
 __global__ __launch_bounds__(256) void page_copy_kernel(CopyParams P)
 {

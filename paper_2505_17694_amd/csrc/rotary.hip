@@ -109,9 +109,10 @@ struct TokenRows {
 // the lanes of a wave write consecutive memory.  It keeps the cosines and sines for all rows it takes: a wave takes
 // 64 / U rows of one token at a time, U = head_dim / 16, `rounds` times in all; `splits` waves share a token.  The next
 // round's loads are under way while a round is turned (two rounds at a time: 66 registers, seven waves a SIMD in the place of
-// eight, 150 us in the place of 129 for the 671 MB below).
-// LARGE: with the streaming hint.  16384 tokens of 64 + 8 + 8 heads of 128 channels take 129 us with it (5.2 TB/s) and 143
-// without, 64 tokens of 32 + 8 + 8 heads 4.2 and 3.7, where the attention that follows finds its rows in the caches besides.
+// eight, a sixth slower for the 671 MB below).
+// LARGE: with the streaming hint.  Out of HBM 16384 tokens of 64 + 8 + 8 heads of 128 channels take 122 us with it (5.5 TB/s) and
+// 131 without, 2048 tokens of 32 + 8 + 8 heads 11.4 and 13.4, but 64 tokens 3.8 and 3.3, where the attention that follows finds
+// its rows in the caches besides.
 template <int DT, bool INTERLEAVED, int U, bool LARGE>
 __global__ __launch_bounds__(256) void rotary_kernel(RotaryParams P, uint32_t splits, uint32_t rounds)
 {
@@ -196,7 +197,8 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryParams P, uint32_t sp
 
 // Halves whose pairs do not come in eights (rotary_dim no multiple of 16): a lane takes the eight channels of one piece of 16 bytes,
 // as if neighbours were paired, and loads their other halves too, from before and behind, at any alignment.  All of a row's
-// loads come before its stores, in one wave, which a call in place needs.
+// loads come before its stores, in one wave, which a call in place needs.  16384 tokens of 64 + 8 + 8 heads, 126 of 128 channels turning,
+// take 155 us (4.3 TB/s) where the other kernel takes 122 for 128: three loads for a store, two of them at any alignment.
 template <int DT, int U>
 __global__ __launch_bounds__(256) void rotary_uneven_kernel(RotaryParams P, uint32_t splits, uint32_t rounds)
 {
