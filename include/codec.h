@@ -628,7 +628,8 @@ typedef struct {
  *               call moves them in the largest unit that divides them all).  From its first row to its last, no dst
  *               may overlap a src; no two rows of the dsts may
  *               overlap
- *   beams       device [batch][beams_out], at most 2^22 in all; a row whose entry is not in 0..beams_in - 1 is left as it was
+ *   beams       device [batch][beams_out], at most 2^22 in all; a row whose entry is not in 0..beams_in - 1 is left as it was.
+ *               No dst may overlap it
  * Enqueued on `stream` without synchronising.
  */
 int codec_beam_reorder(const codec_state *states, int32_t num_states, const int32_t *beams, int32_t batch,

@@ -65,7 +65,8 @@ def _select(logits, scores, k, finished, eos, s):
 
 def beam_reorder(states, beams: torch.Tensor, out=None, stream=None):
     """The states of the beams that go on: of every tensor [batch, beams, ...] in ``states`` the rows ``beams`` [batch, n]
-    (int32) names, as new tensors [batch, n, ...] or in those of ``out``.  Rows have to be contiguous.  A row whose entry is no
+    (int32) names, as new tensors [batch, n, ...] or in those of ``out`` (memory apart from the states, from ``beams`` and from
+    one another).  Rows have to be contiguous.  A row whose entry is no
     beam is left as it was (in a new tensor: undefined).  New tensors of neighbouring states of one shape and type share an
     allocation, which lives as long as one of them: to keep one for long, or to save it alone, clone it.  Bytes are moved: the new
     tensors have no gradient."""

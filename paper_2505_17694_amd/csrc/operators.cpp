@@ -462,10 +462,11 @@ int codec_beam_reorder(const codec_state *states, int32_t num_states, const int3
     struct Touched { Range range; bool written; };
     std::vector<Touched> touched;
     try {
-        touched.reserve(2 * size_t(num_states));
+        touched.reserve(2 * size_t(num_states) + 1);
     } catch (const std::bad_alloc &) {
         return CODEC_ERR_OUT_OF_MEMORY;
     }
+    touched.push_back({{reinterpret_cast<const char *>(beams), reinterpret_cast<const char *>(beams + int64_t(batch) * beams_out)}, false});
     uint64_t bits = 0;                      // of every address, stride and size: their common factor of two
     for (int32_t i = 0; i < num_states; ++i) {
         const codec_state &s = states[i];

@@ -95,6 +95,18 @@ def test_reorder_refusals():
         C.beam_reorder([torch.zeros(1, 2)], torch.zeros(1, 2, dtype=torch.int32))
 
 
+def test_reorder_onto_its_own_list_is_refused():
+    """Rows that are written while other rows' beams are still read there."""
+    a, beams = 1 << 20, 1 << 21                         # [2, 4] beams: 32 bytes
+
+    def status(dst, row=4, batch_stride=16, beam_stride=4):
+        return C.codec_beam_reorder([a, dst, row, 16, 4, batch_stride, beam_stride], beams, 2, 4, 4)
+    for dst in (beams, beams + 28, beams - 28):
+        assert status(dst) == C.CODEC_ERR_INVALID_ARGUMENT
+    assert status(beams - 4096, 4, 8192, 4) == C.CODEC_ERR_INVALID_ARGUMENT       # between the searches of a dst
+    assert C.codec_beam_reorder([beams, a, 4, 16, 4, 16, 4, a + 4096, beams, 4, 16, 4, 16, 4], beams, 2, 4, 4) == C.CODEC_ERR_INVALID_ARGUMENT
+
+
 # ---- on the GPU ------------------------------------------------------------------------------------------
 
 
