@@ -497,6 +497,32 @@ int codec_append(const codec_head_config *head, const codec_rotary_config *rotar
                  void *k_pages, void *v_pages, const codec_kv_layout *layout, void *stream);
 
 /*
+ * Positions of several axes: tokens of images and video have a time, a row and a column, and each pair of channels turns by
+ * one of them.  Pairs may also be counted in blocks of a head that turn like a head each, as the two maps of
+ * codec_differential_attention need.
+ */
+typedef struct {
+    codec_rotary_config rotary;     /* as for codec_rotary; turns[i] belongs to pair i, of all blocks one after the other  */
+    int32_t block_dim;              /* channels of a block, a divisor of rotary_dim; 0 = rotary_dim.  Of block b pair j is, with
+                                       HALF, channels b * block_dim + j and + j + block_dim / 2 (several blocks: multiples
+                                       of 16), with INTERLEAVED b * block_dim + 2j and + 2j + 1; its number is b * block_dim / 2 + j */
+    int32_t num_axes;               /* 1..4                                                     */
+    const uint8_t *axes;            /* device [rotary_dim / 2]: the axis whose position turns pair i; an axis that does not
+                                       exist counts as axis 0                                   */
+    int64_t axis_stride;            /* the position of token t on axis a is positions[a * axis_stride + t]; 0: one position
+                                       for all axes, as tokens of text have                     */
+} codec_rotary_axes;
+
+/* codec_rotary and codec_append with several axes (rotary is not NULL in either); everything else as there. */
+int codec_rotary_by_axes(const codec_rotary_axes *rotary, int32_t num_heads, int32_t head_dim, int32_t dtype,
+                         const codec_rows *x, const codec_rows *out, const int64_t *positions,
+                         int32_t num_tokens, void *stream);
+int codec_append_by_axes(const codec_head_config *head, const codec_rotary_axes *rotary,
+                         const codec_rows *q, const codec_rows *q_out, const codec_rows *k, const codec_rows *v,
+                         const int64_t *positions, const int64_t *slots, int32_t num_tokens,
+                         void *k_pages, void *v_pages, const codec_kv_layout *layout, void *stream);
+
+/*
  * Pages of a cache: who holds them, branches, moves
  * -------------------------------------------------
  *

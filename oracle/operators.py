@@ -49,6 +49,41 @@ def rotary(x, positions, turns, magnitude, interleaved, inverse=False):
     return out, size
 
 
+def axes_frequencies(axes, theta, alternating=False, restart=False, blocks=1, **scaling):
+    """Pair by pair of all blocks: angle from one position to the next and axis; and the factor on turned channels."""
+    order, left, magnitude = [], list(axes), 1.0
+    while sum(left):
+        for a, n in enumerate(axes):
+            take = (left[a] > 0) if alternating else left[a]
+            order += [(a, n - left[a] + j) for j in range(take)]
+            left[a] -= take
+    out = []
+    for i, (a, nth) in enumerate(order):
+        r, place = (2 * axes[a], nth) if restart else (2 * sum(axes), i)
+        f, magnitude = rotary_frequencies(r, theta, **scaling)
+        out.append((f[place], a))
+    return np.array([f for f, _ in out] * blocks), np.array([a for _, a in out] * blocks), magnitude
+
+
+def rotary_by_axes(x, positions, turns, axis, magnitude, interleaved, blocks=1, inverse=False):
+    """rotary() with positions [axes][tokens] and the axis of every pair, block of channels by block of channels."""
+    x = np.asarray(x, np.float64)
+    n = len(turns) // blocks
+    out, size = x.copy(), np.zeros_like(x)
+    for b in range(blocks):
+        for j in range(n):
+            i = b * n + j
+            lo = 2 * n * b + (2 * j if interleaved else j)
+            hi = lo + (1 if interleaved else n)
+            angle = np.array([math.fmod(float(p) * turns[i], 1.0) * 2 * math.pi for p in positions[axis[i]]])[:, None]
+            c, s = magnitude * np.cos(angle), magnitude * np.sin(-angle if inverse else angle)
+            with np.errstate(invalid="ignore"):
+                out[..., lo] = x[..., lo] * c - x[..., hi] * s
+                out[..., hi] = x[..., hi] * c + x[..., lo] * s
+                size[..., lo] = size[..., hi] = np.abs(x[..., lo]) + np.abs(x[..., hi])
+    return out, size
+
+
 class Pages:
     """Who holds which page: lists of holders, nothing clever."""
 

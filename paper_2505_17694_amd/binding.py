@@ -50,6 +50,7 @@ EXPORTED_SYMBOLS = [
     "codec_pages_create", "codec_pages_destroy", "codec_pages_free", "codec_pages_take", "codec_pages_hold",
     "codec_pages_release", "codec_pages_fork", "codec_pages_compact", "codec_cache_copy",
     "codec_beam_workspace_bytes", "codec_beam_select", "codec_beam_reorder",
+    "codec_rotary_by_axes", "codec_append_by_axes",
 ]
 
 _i32p = POINTER(c_int32)
@@ -115,6 +116,11 @@ class codec_rotary_scaling(Structure):
 class codec_rotary_config(Structure):
     _fields_ = [("rotary_dim", c_int32), ("layout", c_int32), ("inverse", c_int32), ("magnitude", c_float),
                 ("turns", c_void_p)]
+
+
+class codec_rotary_axes(Structure):
+    _fields_ = [("rotary", codec_rotary_config), ("block_dim", c_int32), ("num_axes", c_int32), ("axes", c_void_p),
+                ("axis_stride", c_int64)]
 
 
 class codec_rows(Structure):
@@ -193,6 +199,10 @@ _lib.codec_rotary.argtypes = [POINTER(codec_rotary_config), c_int32, c_int32, c_
 _lib.codec_append.restype = c_int
 _lib.codec_append.argtypes = [POINTER(codec_head_config), POINTER(codec_rotary_config)] + [POINTER(codec_rows)] * 4 + [
     c_void_p, c_void_p, c_int32, c_void_p, c_void_p, POINTER(codec_kv_layout), c_void_p]
+_lib.codec_rotary_by_axes.restype = c_int
+_lib.codec_rotary_by_axes.argtypes = [POINTER(codec_rotary_axes)] + _lib.codec_rotary.argtypes[1:]
+_lib.codec_append_by_axes.restype = c_int
+_lib.codec_append_by_axes.argtypes = [POINTER(codec_head_config), POINTER(codec_rotary_axes)] + _lib.codec_append.argtypes[2:]
 _lib.codec_pages_create.restype = c_int
 _lib.codec_pages_create.argtypes = [c_int32, POINTER(c_void_p)]
 _lib.codec_pages_destroy.restype = c_int
@@ -440,6 +450,18 @@ def codec_append(head, rotary, q, q_out, k, v, positions_ptr: int, slots_ptr: in
     """``head``: codec_head_config; ``rotary``: codec_rotary_config or None; ``q``, ``q_out``: codec_rows or None; ``k``,
     ``v``: codec_rows; ``layout``: codec_kv_layout."""
     return _lib.codec_append(head, rotary, q, q_out, k, v, positions_ptr, slots_ptr, num_tokens, k_ptr, v_ptr, layout, stream)
+
+
+def codec_rotary_by_axes(rotary, num_heads: int, head_dim: int, dtype: int, x, out, positions_ptr: int, num_tokens: int,
+                         stream: int = 0) -> int:
+    """``rotary``: codec_rotary_axes; ``x`` and ``out``: codec_rows."""
+    return _lib.codec_rotary_by_axes(rotary, num_heads, head_dim, dtype, x, out, positions_ptr, num_tokens, stream)
+
+
+def codec_append_by_axes(head, rotary, q, q_out, k, v, positions_ptr: int, slots_ptr: int, num_tokens: int, k_ptr: int, v_ptr: int,
+                         layout, stream: int = 0) -> int:
+    """codec_append with a codec_rotary_axes."""
+    return _lib.codec_append_by_axes(head, rotary, q, q_out, k, v, positions_ptr, slots_ptr, num_tokens, k_ptr, v_ptr, layout, stream)
 
 
 def codec_pages_create(num_pages: int):

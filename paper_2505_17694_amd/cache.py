@@ -81,6 +81,53 @@ def _index(t: torch.Tensor, what: str, tokens: int, index: int) -> int:
     return t.data_ptr()
 
 
+def _axis_index(t: torch.Tensor, tokens: int, axes: int, index: int):
+    """Positions of a rotary with axes: [axes, tokens] whose tokens are contiguous, or [tokens], the same on every axis.
+    (address, elements from one axis to the next)"""
+    if t.dim() != 2:
+        return _index(t, "positions", tokens, index), 0
+    stride, one = t.stride()
+    if t.shape != (axes, tokens) or t.dtype is not torch.int64 or t.get_device() != index or (tokens > 1 and one != 1):
+        raise ValueError(f"positions: need an int64 tensor of shape {(axes, tokens)}, tokens contiguous, or of shape {(tokens,)} on "
+                         f"cuda:{index}, got {t.dtype} {tuple(t.shape)} on {t.device}, strides {t.stride()}")
+    if tokens:
+        _check_reach(t, "positions", (axes - 1) * stride + tokens, 8)
+    return t.data_ptr(), stride
+
+
+def _turns(rotary_dim, theta, scaling):
+    st, turns, magnitude = B.codec_rotary_turns(rotary_dim, theta, scaling)
+    if st != B.CODEC_OK:
+        raise B.CodecError(st, "codec_rotary_turns")
+    return turns, magnitude
+
+
+def _axes(rotary_dim, axes, blocks):
+    """Pairs of each axis in one of the blocks."""
+    if not 1 <= blocks <= 128:
+        raise ValueError(f"blocks: {blocks}")
+    axes = [rotary_dim // (2 * blocks)] if axes is None else [int(n) for n in axes]
+    if not 1 <= len(axes) <= 4 or min(axes) < 0 or 2 * blocks * sum(axes) != rotary_dim:
+        raise ValueError(f"axes: up to four counts of pairs that make rotary_dim = {rotary_dim} channels in {blocks} blocks, got {axes}")
+    return axes
+
+
+def _turns_by_axes(axes, theta, scaling, alternating, restart, blocks):
+    """Turns and axis of every pair of all blocks, and the factor on turned channels."""
+    pairs = sum(axes)
+    if alternating:
+        axis = [a for i in range(max(axes)) for a, n in enumerate(axes) if i < n]
+    else:
+        axis = [a for a, n in enumerate(axes) for _ in range(n)]
+    axis = np.array(axis, np.uint8)
+    turns, magnitude = _turns(2 * pairs, theta, scaling)
+    if restart:
+        for a, n in enumerate(axes):
+            if n:
+                turns[axis == a], _ = _turns(2 * n, theta, scaling)
+    return np.tile(turns, blocks), magnitude, np.tile(axis, blocks)
+
+
 class Rotary:
     """Rotary positions: which channels turn and how fast (codec_rotary_config), with the device table behind them.
 
@@ -88,9 +135,16 @@ class Rotary:
     ``scaling``: None or a dict with ``kind`` ("linear", "ntk", "wavelength", "yarn"), ``factor`` and, for the last two,
     ``original_length`` and ``low``, ``high`` (wavelength; 1 and 4 unless given) or ``fast``, ``slow`` (yarn; 32 and 1).
     ``magnitude`` overrides the factor on turned channels that belongs to the scaling.
+
+    ``axes``: how many pairs turn by each of up to four positions of a token (time, row and column of images and video;
+    codec_rotary_axes), first those of the first axis and so on, or, with ``alternating``, the axes in turn while they have
+    pairs left.  Frequencies go by a pair's place among all, or, with ``restart``, among those of its axis.  ``blocks``: so
+    many equal parts of the rotary_dim channels turn like a head each (``axes`` then counts the pairs of one of
+    them).  Positions are then [axes, tokens], or [tokens]: the same on every axis.
     """
 
-    def __init__(self, rotary_dim, theta=10000.0, interleaved=False, scaling=None, device="cuda:0", magnitude=None):
+    def __init__(self, rotary_dim, theta=10000.0, interleaved=False, scaling=None, device="cuda:0", magnitude=None, axes=None,
+                 alternating=False, restart=False, blocks=1):
         s = None
         if scaling is not None:
             known = {"kind", "factor", "original_length", "low", "high", "fast", "slow"}
@@ -101,9 +155,12 @@ class Rotary:
             s = B.codec_rotary_scaling(_SCALINGS[scaling["kind"]], scaling.get("original_length", 0), scaling.get("factor", 0.0),
                                        scaling.get("low", 1.0), scaling.get("high", 4.0), scaling.get("fast", 32.0),
                                        scaling.get("slow", 1.0))
-        st, turns, factor = B.codec_rotary_turns(rotary_dim, theta, s)
-        if st != B.CODEC_OK:
-            raise B.CodecError(st, "codec_rotary_turns")
+        axis = None
+        if axes is None and blocks == 1 and not alternating and not restart:
+            turns, factor = _turns(rotary_dim, theta, s)
+        else:
+            axes = _axes(rotary_dim, axes, blocks)
+            turns, factor, axis = _turns_by_axes(axes, theta, s, alternating, restart, blocks)
         self.device = _device(device)
         self.rotary_dim = rotary_dim
         self.magnitude = factor if magnitude is None else magnitude
@@ -111,6 +168,13 @@ class Rotary:
         layout = B.CODEC_ROTARY_INTERLEAVED if interleaved else B.CODEC_ROTARY_HALF
         self._config = [B.codec_rotary_config(rotary_dim, layout, inverse, self.magnitude, self._turns.data_ptr())
                         for inverse in (0, 1)]
+        self._axes = None if axis is None else torch.from_numpy(axis).to(self.device)
+        self._num_axes, self._block = (0, 0) if axis is None else (len(axes), rotary_dim // blocks)
+
+    def _by_axes(self, inverse, positions, tokens, index):
+        """The codec_rotary_axes of a call, and its positions' address."""
+        at, stride = _axis_index(positions, tokens, self._num_axes, index)
+        return B.codec_rotary_axes(self._config[inverse], self._block, self._num_axes, self._axes.data_ptr(), stride), at
 
     @property
     def turns(self) -> torch.Tensor:
@@ -140,13 +204,18 @@ class Rotary:
         if (shape[0] | shape[1] | shape[2]) >> 31:
             raise ValueError(f"x: {tuple(shape)} is too large for a call")
         rows = _rows(x, "x", shape, x.dtype, index)
-        at = _index(positions, "positions", shape[0], index)
+        call, name, config = B.codec_rotary, "codec_rotary", self._config[bool(inverse)]
+        if self._axes is None:
+            at = _index(positions, "positions", shape[0], index)
+        else:
+            call, name = B.codec_rotary_by_axes, "codec_rotary_by_axes"
+            config, at = self._by_axes(bool(inverse), positions, shape[0], index)
         if out is None:
             out = torch.empty_like(x, memory_format=torch.contiguous_format)
         into = _rows(out, "out", shape, x.dtype, index)
-        st = B.codec_rotary(self._config[bool(inverse)], shape[1], shape[2], _CODE[x.dtype], rows, into, at, shape[0], s)
+        st = call(config, shape[1], shape[2], _CODE[x.dtype], rows, into, at, shape[0], s)
         if st != B.CODEC_OK:
-            raise B.CodecError(st, "codec_rotary")
+            raise B.CodecError(st, name)
         return out
 
 
@@ -282,6 +351,7 @@ class KVCache:
         k_rows = _rows(k, "k", kv_shape, dtype, index)
         v_rows = _rows(v, "v", kv_shape, dtype, index)
         q_rows = out_rows = config = at = None
+        call, name = B.codec_append, "codec_append"
         if q is not None:
             q_shape = (tokens, *self._q_row)
             q_rows = _rows(q, "q", q_shape, dtype, index)
@@ -293,12 +363,16 @@ class KVCache:
         if rotary is not None:
             if rotary.device != self.device:
                 raise ValueError(f"rotary is on {rotary.device}, the pools are on {self.device}")
-            config, at = rotary._config[0], _index(positions, "positions", tokens, index)
+            if rotary._axes is None:
+                config, at = rotary._config[0], _index(positions, "positions", tokens, index)
+            else:
+                call, name = B.codec_append_by_axes, "codec_append_by_axes"
+                config, at = rotary._by_axes(0, positions, tokens, index)
         kp, vp = self._places[2 * layer], self._places[2 * layer + 1]
-        st = B.codec_append(self._head, config, q_rows, out_rows, k_rows, v_rows, at, _index(slots, "slots", tokens, index),
-                            tokens, kp, vp, self._layout, s)
+        st = call(self._head, config, q_rows, out_rows, k_rows, v_rows, at, _index(slots, "slots", tokens, index),
+                  tokens, kp, vp, self._layout, s)
         if st != B.CODEC_OK:
-            raise B.CodecError(st, "codec_append")
+            raise B.CodecError(st, name)
         return q_out
 
     @property

@@ -121,6 +121,16 @@ int check_rotary(const codec_rotary_config &r, int32_t head_dim, const int64_t *
     return CODEC_OK;
 }
 
+int check_axes(const codec_rotary_axes &a, int32_t head_dim, const int64_t *positions)
+{
+    if (int st = check_rotary(a.rotary, head_dim, positions)) return st;
+    if (a.num_axes < 1 || a.num_axes > codec::kMaxAxes || !a.axes || a.axis_stride < 0 || a.axis_stride > kMaxSpan) return CODEC_ERR_INVALID_ARGUMENT;
+    if (a.block_dim < 0 || (a.block_dim && a.rotary.rotary_dim % a.block_dim)) return CODEC_ERR_INVALID_ARGUMENT;
+    const bool blocks = a.block_dim && a.block_dim != a.rotary.rotary_dim;
+    if (blocks && (a.block_dim % 2 || (a.rotary.layout == CODEC_ROTARY_HALF && a.block_dim % 16))) return CODEC_ERR_UNSUPPORTED;
+    return CODEC_OK;
+}
+
 // Tokens of the pages that a list of copies writes, as bits: an open-addressing table of pages.
 class WrittenTokens {
 public:
@@ -230,6 +240,95 @@ void set_rotary(codec::RotaryParams &p, const codec_rotary_config &r, const int6
     p.sign = r.inverse ? -1.f : 1.f;
 }
 
+// The launch of either form: by one position a token, or by several axes.
+int launch(const codec::RotaryParams &p, int dtype, const codec_rotary_config *rotary, const codec_rotary_axes *axes, const char *what, void *stream)
+{
+    const bool interleaved = rotary && rotary->layout == CODEC_ROTARY_INTERLEAVED;
+    int e;
+    if (axes) {
+        codec::AxesParams by{};
+        static_cast<codec::RotaryParams &>(by) = p;
+        by.axes = axes->axes;
+        by.axis_stride = axes->axis_stride;
+        by.num_axes = axes->num_axes;
+        by.block_pairs = (axes->block_dim ? axes->block_dim : rotary->rotary_dim) / 2;
+        e = codec::launch_rotary_axes(by, dtype, interleaved, stream);
+    } else {
+        e = codec::launch_rotary(p, dtype, interleaved, stream);
+    }
+    return e ? hip_failure(what, e) : CODEC_OK;
+}
+
+// codec_rotary, and codec_rotary_by_axes where `axes` is not NULL (`rotary` is then its first member).
+int rotate_rows(const codec_rotary_config *rotary, const codec_rotary_axes *axes, int32_t num_heads, int32_t head_dim, int32_t dtype,
+                const codec_rows *x, const codec_rows *out, const int64_t *positions, int32_t num_tokens, void *stream)
+{
+    if (!rotary || num_heads < 1 || num_heads > (1 << 16) || num_tokens < 0) return CODEC_ERR_INVALID_ARGUMENT;
+    if (int st = check_rows_of(head_dim, dtype)) return st;
+    if (num_tokens == 0) return CODEC_OK;
+    if (int st = axes ? check_axes(*axes, head_dim, positions) : check_rotary(*rotary, head_dim, positions)) return st;
+    if (!rows_ok(x, num_tokens, num_heads) || !rows_ok(out, num_tokens, num_heads) || !separate(*out, num_tokens, num_heads, head_dim)) return CODEC_ERR_INVALID_ARGUMENT;
+    if (!same_rows(*x, *out, num_tokens, num_heads) && !apart(*x, num_heads, *out, num_heads, num_tokens, head_dim)) return CODEC_ERR_INVALID_ARGUMENT;
+
+    codec::RotaryParams p{};
+    p.q = view_of(*x);
+    p.q_out = view_of(*out);
+    p.q_heads = num_heads;
+    p.head_dim = head_dim;
+    p.num_tokens = num_tokens;
+    set_rotary(p, *rotary, positions);
+    return launch(p, dtype, rotary, axes, "rotary launch", stream);
+}
+
+// codec_append and codec_append_by_axes, alike.
+int append_rows(const codec_head_config *head, const codec_rotary_config *rotary, const codec_rotary_axes *axes, const codec_rows *q,
+                const codec_rows *q_out, const codec_rows *k, const codec_rows *v, const int64_t *positions, const int64_t *slots,
+                int32_t num_tokens, void *k_pages, void *v_pages, const codec_kv_layout *layout, void *stream)
+{
+    if (!head || !layout || num_tokens < 0 || !q != !q_out) return CODEC_ERR_INVALID_ARGUMENT;
+    if (int st = check_head(*head)) return st;
+    const int64_t pool = pool_span(*head, *layout);
+    if (pool < 0) return CODEC_ERR_INVALID_ARGUMENT;
+    if (num_tokens == 0) return CODEC_OK;
+    if (rotary)
+        if (int st = axes ? check_axes(*axes, head->head_dim, positions) : check_rotary(*rotary, head->head_dim, positions)) return st;
+    if (!slots || !k_pages || !v_pages || !aligned16(k_pages) || !aligned16(v_pages) || !pools_apart(*head, *layout, k_pages, v_pages)) return CODEC_ERR_INVALID_ARGUMENT;
+    const int64_t t = num_tokens, d = head->head_dim, hq = head->num_q_heads, h = head->num_kv_heads;
+    if (!rows_ok(k, t, h) || !rows_ok(v, t, h) || (q && (!rows_ok(q, t, hq) || !rows_ok(q_out, t, hq)))) return CODEC_ERR_INVALID_ARGUMENT;
+    for (const void *pages : {k_pages, v_pages}) {
+        const Range r{static_cast<const char *>(pages), static_cast<const char *>(pages) + 2 * pool};
+        if (overlap(r, range_of(*k, t, h, d)) || overlap(r, range_of(*v, t, h, d))) return CODEC_ERR_INVALID_ARGUMENT;
+        if (q && (overlap(r, range_of(*q, t, hq, d)) || overlap(r, range_of(*q_out, t, hq, d)))) return CODEC_ERR_INVALID_ARGUMENT;
+    }
+    if (q) {
+        if (!separate(*q_out, t, hq, d)) return CODEC_ERR_INVALID_ARGUMENT;
+        if (!same_rows(*q, *q_out, t, hq) && !apart(*q, hq, *q_out, hq, t, d)) return CODEC_ERR_INVALID_ARGUMENT;
+        if (!apart(*q_out, hq, *k, h, t, d) || !apart(*q_out, hq, *v, h, t, d)) return CODEC_ERR_INVALID_ARGUMENT;
+    }
+
+    codec::RotaryParams p{};
+    if (q) {
+        p.q = view_of(*q);
+        p.q_out = view_of(*q_out);
+        p.q_heads = head->num_q_heads;
+    }
+    p.k = view_of(*k);
+    p.v = view_of(*v);
+    p.kv_heads = head->num_kv_heads;
+    p.k_pages = static_cast<char *>(k_pages);
+    p.v_pages = static_cast<char *>(v_pages);
+    p.page_stride = 2 * layout->page_stride;
+    p.slot_stride = 2 * layout->token_stride;
+    p.head_stride = 2 * layout->head_stride;
+    p.slots = slots;
+    p.num_slots = layout->num_pages * head->page_size;
+    while ((1 << p.page_shift) < head->page_size) ++p.page_shift;
+    p.head_dim = head->head_dim;
+    p.num_tokens = num_tokens;
+    if (rotary) set_rotary(p, *rotary, positions);
+    return launch(p, head->dtype, rotary, axes, "append launch", stream);
+}
+
 }  // namespace
 
 extern "C" {
@@ -275,71 +374,28 @@ int codec_rotary_turns(int32_t rotary_dim, double theta, const codec_rotary_scal
 int codec_rotary(const codec_rotary_config *rotary, int32_t num_heads, int32_t head_dim, int32_t dtype, const codec_rows *x,
                  const codec_rows *out, const int64_t *positions, int32_t num_tokens, void *stream)
 {
-    if (!rotary || num_heads < 1 || num_heads > (1 << 16) || num_tokens < 0) return CODEC_ERR_INVALID_ARGUMENT;
-    if (int st = check_rows_of(head_dim, dtype)) return st;
-    if (num_tokens == 0) return CODEC_OK;
-    if (int st = check_rotary(*rotary, head_dim, positions)) return st;
-    if (!rows_ok(x, num_tokens, num_heads) || !rows_ok(out, num_tokens, num_heads) || !separate(*out, num_tokens, num_heads, head_dim)) return CODEC_ERR_INVALID_ARGUMENT;
-    if (!same_rows(*x, *out, num_tokens, num_heads) && !apart(*x, num_heads, *out, num_heads, num_tokens, head_dim)) return CODEC_ERR_INVALID_ARGUMENT;
+    return rotate_rows(rotary, nullptr, num_heads, head_dim, dtype, x, out, positions, num_tokens, stream);
+}
 
-    codec::RotaryParams p{};
-    p.q = view_of(*x);
-    p.q_out = view_of(*out);
-    p.q_heads = num_heads;
-    p.head_dim = head_dim;
-    p.num_tokens = num_tokens;
-    set_rotary(p, *rotary, positions);
-    if (int e = codec::launch_rotary(p, dtype, rotary->layout == CODEC_ROTARY_INTERLEAVED, stream)) return hip_failure("rotary launch", e);
-    return CODEC_OK;
+int codec_rotary_by_axes(const codec_rotary_axes *rotary, int32_t num_heads, int32_t head_dim, int32_t dtype, const codec_rows *x,
+                         const codec_rows *out, const int64_t *positions, int32_t num_tokens, void *stream)
+{
+    return rotate_rows(rotary ? &rotary->rotary : nullptr, rotary, num_heads, head_dim, dtype, x, out, positions, num_tokens, stream);
 }
 
 int codec_append(const codec_head_config *head, const codec_rotary_config *rotary, const codec_rows *q, const codec_rows *q_out,
                  const codec_rows *k, const codec_rows *v, const int64_t *positions, const int64_t *slots, int32_t num_tokens,
                  void *k_pages, void *v_pages, const codec_kv_layout *layout, void *stream)
 {
-    if (!head || !layout || num_tokens < 0 || !q != !q_out) return CODEC_ERR_INVALID_ARGUMENT;
-    if (int st = check_head(*head)) return st;
-    const int64_t pool = pool_span(*head, *layout);
-    if (pool < 0) return CODEC_ERR_INVALID_ARGUMENT;
-    if (num_tokens == 0) return CODEC_OK;
-    if (rotary)
-        if (int st = check_rotary(*rotary, head->head_dim, positions)) return st;
-    if (!slots || !k_pages || !v_pages || !aligned16(k_pages) || !aligned16(v_pages) || !pools_apart(*head, *layout, k_pages, v_pages)) return CODEC_ERR_INVALID_ARGUMENT;
-    const int64_t t = num_tokens, d = head->head_dim, hq = head->num_q_heads, h = head->num_kv_heads;
-    if (!rows_ok(k, t, h) || !rows_ok(v, t, h) || (q && (!rows_ok(q, t, hq) || !rows_ok(q_out, t, hq)))) return CODEC_ERR_INVALID_ARGUMENT;
-    for (const void *pages : {k_pages, v_pages}) {
-        const Range r{static_cast<const char *>(pages), static_cast<const char *>(pages) + 2 * pool};
-        if (overlap(r, range_of(*k, t, h, d)) || overlap(r, range_of(*v, t, h, d))) return CODEC_ERR_INVALID_ARGUMENT;
-        if (q && (overlap(r, range_of(*q, t, hq, d)) || overlap(r, range_of(*q_out, t, hq, d)))) return CODEC_ERR_INVALID_ARGUMENT;
-    }
-    if (q) {
-        if (!separate(*q_out, t, hq, d)) return CODEC_ERR_INVALID_ARGUMENT;
-        if (!same_rows(*q, *q_out, t, hq) && !apart(*q, hq, *q_out, hq, t, d)) return CODEC_ERR_INVALID_ARGUMENT;
-        if (!apart(*q_out, hq, *k, h, t, d) || !apart(*q_out, hq, *v, h, t, d)) return CODEC_ERR_INVALID_ARGUMENT;
-    }
+    return append_rows(head, rotary, nullptr, q, q_out, k, v, positions, slots, num_tokens, k_pages, v_pages, layout, stream);
+}
 
-    codec::RotaryParams p{};
-    if (q) {
-        p.q = view_of(*q);
-        p.q_out = view_of(*q_out);
-        p.q_heads = head->num_q_heads;
-    }
-    p.k = view_of(*k);
-    p.v = view_of(*v);
-    p.kv_heads = head->num_kv_heads;
-    p.k_pages = static_cast<char *>(k_pages);
-    p.v_pages = static_cast<char *>(v_pages);
-    p.page_stride = 2 * layout->page_stride;
-    p.slot_stride = 2 * layout->token_stride;
-    p.head_stride = 2 * layout->head_stride;
-    p.slots = slots;
-    p.num_slots = layout->num_pages * head->page_size;
-    while ((1 << p.page_shift) < head->page_size) ++p.page_shift;
-    p.head_dim = head->head_dim;
-    p.num_tokens = num_tokens;
-    if (rotary) set_rotary(p, *rotary, positions);
-    if (int e = codec::launch_rotary(p, head->dtype, rotary && rotary->layout == CODEC_ROTARY_INTERLEAVED, stream)) return hip_failure("append launch", e);
-    return CODEC_OK;
+int codec_append_by_axes(const codec_head_config *head, const codec_rotary_axes *rotary, const codec_rows *q, const codec_rows *q_out,
+                         const codec_rows *k, const codec_rows *v, const int64_t *positions, const int64_t *slots, int32_t num_tokens,
+                         void *k_pages, void *v_pages, const codec_kv_layout *layout, void *stream)
+{
+    if (!rotary) return CODEC_ERR_INVALID_ARGUMENT;
+    return append_rows(head, &rotary->rotary, rotary, q, q_out, k, v, positions, slots, num_tokens, k_pages, v_pages, layout, stream);
 }
 
 int codec_cache_copy(const codec_head_config *head, const codec_kv_layout *layout, int32_t num_layers, void *const *k_pages,

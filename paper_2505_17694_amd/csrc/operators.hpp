@@ -32,6 +32,14 @@ struct RotaryParams {
     float magnitude, sign;          // factors on the turned channels and on the sine
 };
 
+constexpr int kMaxAxes = 4;
+
+struct AxesParams : RotaryParams {
+    const uint8_t *axes;            // [rotary_dim / 2]: the axis whose positions turn a pair
+    int64_t axis_stride;            // positions of an axis, from one axis to the next
+    int32_t num_axes, block_pairs;  // pairs of a block of halves
+};
+
 // A launch's worth of codec_cache_copy: pools and runs travel in the kernel's arguments, which hold 4 KB.
 constexpr int kCopyPools = 64;
 constexpr int kCopyRuns = 288;
@@ -91,6 +99,7 @@ static_assert(sizeof(ReorderParams) <= 4096, "kernel arguments");
 
 // All return a hipError_t value (0 = success) without synchronising.
 int launch_rotary(const RotaryParams &p, int dtype, bool interleaved, void *stream);
+int launch_rotary_axes(const AxesParams &p, int dtype, bool interleaved, void *stream);
 int launch_copy(CopyParams &p, void *stream);
 int launch_beam_select(const BeamParams &p, int dtype, void *stream);
 // `unit`: bytes moved at a time, 1, 2, 4, 8 or 16

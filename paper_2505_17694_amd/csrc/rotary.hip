@@ -104,6 +104,38 @@ struct TokenRows {
     }
 };
 
+// The position that turns a pair: the token's, or the token's on the pair's axis.
+template <class Params>
+struct PositionOf {
+    double position;
+    __device__ __forceinline__ PositionOf(const Params &P, int64_t token) : position(double(P.positions[token])) {}
+    __device__ __forceinline__ double of(const Params &, int) const { return position; }
+};
+
+// All positions of a token are read at once, beside the axes of the lane's pairs: no read waits for another.
+template <>
+struct PositionOf<AxesParams> {
+    double position[kMaxAxes];
+    __device__ __forceinline__ PositionOf(const AxesParams &P, int64_t token)
+    {
+#pragma unroll
+        for (int a = 0; a < kMaxAxes; ++a) position[a] = double(P.positions[(a < P.num_axes ? a : 0) * P.axis_stride + token]);
+    }
+    // (an axis that does not exist counts as the first)
+    __device__ __forceinline__ double of(const AxesParams &P, int pair) const
+    {
+        const int axis = P.axes[pair];
+        const double low = axis == 1 ? position[1] : position[0], high = axis == 2 ? position[2] : position[3];
+        return axis >= 2 && axis < kMaxAxes ? high : low;
+    }
+};
+
+// Halves: channels from a pair's number to its first channel, and from there to its second.  Blocks turn like a head each.
+__device__ __forceinline__ int before_block(const RotaryParams &, int) { return 0; }
+__device__ __forceinline__ int before_block(const AxesParams &P, int pair) { return pair / P.block_pairs * P.block_pairs; }
+__device__ __forceinline__ int half_block(const RotaryParams &, int turning) { return turning; }
+__device__ __forceinline__ int half_block(const AxesParams &P, int) { return P.block_pairs; }
+
 // A copy with some arithmetic on the way, bound by HBM.  A lane takes 16 bytes of a row and 16 others that the same cosines and
 // sines serve: the other halves of its eight pairs, or, with neighbouring pairs, the same four pairs of another row, so that
 // the lanes of a wave write consecutive memory.  It keeps the cosines and sines for all rows it takes: a wave takes
@@ -113,8 +145,8 @@ struct TokenRows {
 // LARGE: with the streaming hint.  Out of HBM 16384 tokens of 64 + 8 + 8 heads of 128 channels take 122 us with it (5.5 TB/s) and
 // 131 without, 2048 tokens of 32 + 8 + 8 heads 11.4 and 13.4, but 64 tokens 3.8 and 3.3, where the attention that follows finds
 // its rows in the caches besides.
-template <int DT, bool INTERLEAVED, int U, bool LARGE>
-__global__ __launch_bounds__(256) void rotary_kernel(RotaryParams P, uint32_t splits, uint32_t rounds)
+template <int DT, bool INTERLEAVED, int U, bool LARGE, class Params>
+__device__ __forceinline__ void turn_rows(const Params &P, uint32_t splits, uint32_t rounds)
 {
     constexpr int kRows = 64 / U;
     constexpr int kLanes = INTERLEAVED ? 2 * U : U;     // of a row
@@ -128,8 +160,8 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryParams P, uint32_t sp
     const int turning = P.rotary_dim / 2;               // pairs
     const int pair = unit * kPairs;                     // the lane's first
     const bool turns = pair < turning;
-    const int first = INTERLEAVED || turns ? unit * 8 : unit * 16;                                  // channels
-    const int second = INTERLEAVED ? first : turns ? first + turning : first + 8;
+    const int first = INTERLEAVED ? unit * 8 : turns ? pair + before_block(P, pair) : unit * 16;     // channels
+    const int second = INTERLEAVED ? first : turns ? first + half_block(P, turning) : first + 8;
 
     const TokenRows places(P, token);
     if (places.stored == 0) return;
@@ -149,10 +181,11 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryParams P, uint32_t sp
 
     float c[kPairs], s[kPairs];
     if (turning) {
-        const double position = double(P.positions[token]);
+        const PositionOf<Params> position(P, token);
 #pragma unroll
         for (int i = 0; i < kPairs; ++i) {
-            const Turn t = turn_of(position * P.turns[INTERLEAVED ? (pair + i < turning ? pair + i : 0) : (turns ? pair : 0) + i]);
+            const int at = INTERLEAVED ? (pair + i < turning ? pair + i : 0) : (turns ? pair : 0) + i;
+            const Turn t = turn_of(position.of(P, at) * P.turns[at]);
             c[i] = t.cos * P.magnitude;
             s[i] = t.sin * (P.magnitude * P.sign);
         }
@@ -199,8 +232,8 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryParams P, uint32_t sp
 // as if neighbours were paired, and loads their other halves too, from before and behind, at any alignment.  All of a row's
 // loads come before its stores, in one wave, which a call in place needs.  16384 tokens of 64 + 8 + 8 heads, 126 of 128 channels turning,
 // take 155 us (4.3 TB/s) where the other kernel takes 122 for 128: three loads for a store, two of them at any alignment.
-template <int DT, int U>
-__global__ __launch_bounds__(256) void rotary_uneven_kernel(RotaryParams P, uint32_t splits, uint32_t rounds)
+template <int DT, int U, class Params>
+__device__ __forceinline__ void turn_uneven_rows(const Params &P, uint32_t splits, uint32_t rounds)
 {
     constexpr int kLanes = 2 * U, kRows = 64 / U, kOther = kRows / 2;
     const int lane = threadIdx.x & 63, channel = lane % kLanes * 8, sub = lane / kLanes;
@@ -218,11 +251,11 @@ __global__ __launch_bounds__(256) void rotary_uneven_kernel(RotaryParams P, uint
     const int behind = low ? (channel + half < d - 8 ? channel + half : d - 8) : 0, behind_by = low ? channel + half - behind : 0;
     const int before = high && channel > half ? channel - half : 0, before_by = high && channel < half ? half - channel : 0;
     float c[8], s[8];
-    const double position = double(P.positions[token]);
+    const PositionOf<Params> position(P, token);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        const int x = channel + e;
-        const Turn t = turn_of(position * P.turns[x < half ? x : x < P.rotary_dim ? x - half : 0]);
+        const int x = channel + e, at = x < half ? x : x < P.rotary_dim ? x - half : 0;
+        const Turn t = turn_of(position.of(P, at) * P.turns[at]);
         c[e] = t.cos * P.magnitude;
         s[e] = t.sin * (x < half ? -P.magnitude * P.sign : P.magnitude * P.sign);
     }
@@ -262,11 +295,32 @@ __global__ __launch_bounds__(256) void rotary_uneven_kernel(RotaryParams P, uint
     }
 }
 
-}  // namespace
+template <int DT, bool INTERLEAVED, int U, bool LARGE>
+__global__ __launch_bounds__(256) void rotary_kernel(RotaryParams P, uint32_t splits, uint32_t rounds)
+{
+    turn_rows<DT, INTERLEAVED, U, LARGE>(P, splits, rounds);
+}
 
-namespace {
+template <int DT, int U>
+__global__ __launch_bounds__(256) void rotary_uneven_kernel(RotaryParams P, uint32_t splits, uint32_t rounds)
+{
+    turn_uneven_rows<DT, U>(P, splits, rounds);
+}
 
-int launch_slice(const RotaryParams &p, int dtype, bool interleaved, hipStream_t s)
+template <int DT, bool INTERLEAVED, int U, bool LARGE>
+__global__ __launch_bounds__(256) void rotary_axes_kernel(AxesParams P, uint32_t splits, uint32_t rounds)
+{
+    turn_rows<DT, INTERLEAVED, U, LARGE>(P, splits, rounds);
+}
+
+template <int DT, int U>
+__global__ __launch_bounds__(256) void rotary_axes_uneven_kernel(AxesParams P, uint32_t splits, uint32_t rounds)
+{
+    turn_uneven_rows<DT, U>(P, splits, rounds);
+}
+
+template <class Params>
+int launch_slice(const Params &p, int dtype, bool interleaved, hipStream_t s)
 {
     const int64_t rows = p.q_heads + 2 * p.kv_heads;
     // a wave for every token, or as many as it takes to have 32 on every CU
@@ -277,13 +331,23 @@ int launch_slice(const RotaryParams &p, int dtype, bool interleaved, hipStream_t
     const bool large = 4.0 * double(p.num_tokens) * double(rows) * p.head_dim > kLargeBytes;
     const bool uneven = !interleaved && p.rotary_dim % 16;
     const uint32_t n = uint32_t(splits), r = uint32_t(rounds);
+    constexpr bool kAxes = std::is_same_v<Params, AxesParams>;
+    auto launch_even = [&](auto dt, auto u, auto neighbours, auto hint) {
+        constexpr int DT = decltype(dt)::value, U = decltype(u)::value;
+        constexpr bool INTERLEAVED = decltype(neighbours)::value, LARGE = decltype(hint)::value;
+        if constexpr (kAxes) hipLaunchKernelGGL((rotary_axes_kernel<DT, INTERLEAVED, U, LARGE>), grid, dim3(256), 0, s, p, n, r);
+        else                 hipLaunchKernelGGL((rotary_kernel<DT, INTERLEAVED, U, LARGE>), grid, dim3(256), 0, s, p, n, r);
+    };
     auto launch_dim = [&](auto dt, auto u) {
         constexpr int DT = decltype(dt)::value, U = decltype(u)::value;
-        if (uneven)                    hipLaunchKernelGGL((rotary_uneven_kernel<DT, U>), grid, dim3(256), 0, s, p, n, r);
-        else if (interleaved && large) hipLaunchKernelGGL((rotary_kernel<DT, true, U, true>), grid, dim3(256), 0, s, p, n, r);
-        else if (interleaved)          hipLaunchKernelGGL((rotary_kernel<DT, true, U, false>), grid, dim3(256), 0, s, p, n, r);
-        else if (large)                hipLaunchKernelGGL((rotary_kernel<DT, false, U, true>), grid, dim3(256), 0, s, p, n, r);
-        else                           hipLaunchKernelGGL((rotary_kernel<DT, false, U, false>), grid, dim3(256), 0, s, p, n, r);
+        if (uneven) {
+            if constexpr (kAxes) hipLaunchKernelGGL((rotary_axes_uneven_kernel<DT, U>), grid, dim3(256), 0, s, p, n, r);
+            else                 hipLaunchKernelGGL((rotary_uneven_kernel<DT, U>), grid, dim3(256), 0, s, p, n, r);
+        }
+        else if (interleaved && large) launch_even(dt, u, std::true_type{}, std::true_type{});
+        else if (interleaved)          launch_even(dt, u, std::true_type{}, std::false_type{});
+        else if (large)                launch_even(dt, u, std::false_type{}, std::true_type{});
+        else                           launch_even(dt, u, std::false_type{}, std::false_type{});
     };
     auto launch = [&](auto dt) {
         if (p.head_dim == 64)       launch_dim(dt, std::integral_constant<int, 4>{});
@@ -295,14 +359,13 @@ int launch_slice(const RotaryParams &p, int dtype, bool interleaved, hipStream_t
     return int(hipGetLastError());
 }
 
-}  // namespace
-
 // A launch takes 2^24 tokens: its threads are counted in 32 bits.
-int launch_rotary(const RotaryParams &p, int dtype, bool interleaved, void *stream)
+template <class Params>
+int launch_slices(const Params &p, int dtype, bool interleaved, void *stream)
 {
     constexpr int64_t kSlice = int64_t(1) << 24;
     for (int64_t at = 0; at < p.num_tokens; at += kSlice) {
-        RotaryParams part = p;
+        Params part = p;
         part.num_tokens = p.num_tokens - at < kSlice ? p.num_tokens - at : kSlice;
         for (RowsView *r : {&part.q, &part.q_out, &part.k, &part.v})
             if (r->data) r->data += at * r->token_stride;
@@ -312,5 +375,11 @@ int launch_rotary(const RotaryParams &p, int dtype, bool interleaved, void *stre
     }
     return 0;
 }
+
+}  // namespace
+
+int launch_rotary(const RotaryParams &p, int dtype, bool interleaved, void *stream) { return launch_slices(p, dtype, interleaved, stream); }
+
+int launch_rotary_axes(const AxesParams &p, int dtype, bool interleaved, void *stream) { return launch_slices(p, dtype, interleaved, stream); }
 
 }  // namespace codec
