@@ -602,6 +602,61 @@ int codec_cache_copy(const codec_head_config *head, const codec_kv_layout *layou
                      void *const *k_pages, void *const *v_pages, const codec_run *runs, int32_t num_runs, void *stream);
 
 /*
+ * Block tables and slots of new tokens, from lengths on the GPU
+ * -------------------------------------------------------------
+ *
+ * codec_append wants a position and a slot for every token.  They follow from how many tokens the sequences hold and get, and from
+ * their pages; these calls make them where the lengths are, so that a step needs no list from the host and no wait for
+ * one (lengths that a verification has just cut, captured steps).  Lengths below zero count as zero.
+ */
+
+/*
+ * Page lists as a dense table: entry i of row s is page_ids[page_off[s] + i] for i < min(ceil(tokens[s] / page_size), page_off[s + 1] -
+ * page_off[s]), else -1.
+ *   page_off, page_ids, tokens   device [num_seq + 1], [num_ids], [num_seq]: as codec_pages_fork leaves them (entries that
+ *               do not lie in page_ids count as not there)
+ *   table       device [num_seq] rows of `width` entries, table_stride (>= width) apart; must not overlap what is read
+ * num_seq is 0..2^22.  Enqueued on `stream` without synchronising.
+ */
+int codec_block_table(int32_t page_size, int32_t num_seq, const int32_t *page_off, const int32_t *page_ids, int32_t num_ids,
+                      const int32_t *tokens, int32_t *table, int64_t table_stride, int32_t width, void *stream);
+
+typedef struct {
+    int32_t num_seq;            /* 0..2^22                                                      */
+    int32_t page_size;          /* as for codec_append                                          */
+    int32_t width;              /* entries of a table's row, >= 0                               */
+    int32_t num_tokens;         /* entries of positions, slots and sequences, >= 0              */
+    int32_t num_spare;          /* pages in spare, >= 0                                         */
+    int64_t num_pages;          /* pages of the pools: another id is no page                    */
+    int64_t table_stride;       /* entries from one row to the next, >= width                   */
+} codec_slot_config;
+
+/* Bytes of scratch codec_slot_map needs; 0: none (up to 4096 sequences). */
+size_t codec_slot_workspace_bytes(const codec_slot_config *config);
+
+/*
+ * Sequence s holds tokens[s] tokens in the pages of row s of `table` and gets new_tokens[s] more; the new tokens of all sequences
+ * follow one another.  Token t, the j-th new one of sequence s, is at position before[s] + tokens[s] + j, and in slot
+ * page * page_size + (tokens[s] + j) % page_size of the page that the row names for it.
+ *   spare       device [num_spare]: pages that the sequences' new pages are taken from, in order, and entered in the table;
+ *               NULL: the table names the new tokens' pages already, and is only read
+ *   before      device [num_seq]: what positions count from (tokens of the nodes above; of images, the distance of
+ *               positions from places); NULL: zero
+ *   positions, slots, sequences   device [num_tokens]; sequences, the s of every token, may be NULL.  Slot -1: a token for which
+ *               there is no page (the row ends, spare does, the entry is none of num_pages), which codec_append does not store.
+ *               Behind the last token: position 0, slot -1, sequence -1
+ *   offsets     device [num_seq + 1]: the first token of every sequence, and their number
+ *   tokens_out  device [num_seq]: tokens with the new ones (2^31 - 1 at most)
+ *   taken       device [1]: spare pages that the new tokens take; beyond num_spare there were too few
+ *   workspace   device scratch, >= codec_slot_workspace_bytes, 256-byte aligned; calls that share one must not overlap
+ * New tokens beyond num_tokens are left out, from the last sequences, in offsets, tokens_out, taken and the table as well.
+ * Outputs and scratch must not overlap one another or what is read.  Enqueued on `stream` without synchronising.
+ */
+int codec_slot_map(const codec_slot_config *config, int32_t *table, const int32_t *tokens, const int32_t *new_tokens,
+                   const int64_t *before, const int32_t *spare, int64_t *positions, int64_t *slots, int32_t *sequences,
+                   int32_t *offsets, int32_t *tokens_out, int32_t *taken, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * Beam search: which continuations go on, and their states
  * --------------------------------------------------------
  */

@@ -84,6 +84,47 @@ def rotary_by_axes(x, positions, turns, axis, magnitude, interleaved, blocks=1, 
     return out, size
 
 
+def block_table(page_size, page_off, page_ids, tokens, width):
+    """Row by row: the pages that hold the tokens, -1 behind them."""
+    rows = []
+    for s, n in enumerate(tokens):
+        begin, end = int(page_off[s]), int(page_off[s + 1])
+        pages = []
+        for i in range(min(-(-max(int(n), 0) // page_size), width)):
+            if 0 <= begin and begin + i < min(end, len(page_ids)):
+                pages.append(int(page_ids[begin + i]))
+        rows.append(pages + [-1] * (width - len(pages)))
+    return np.array(rows, np.int64).reshape(len(tokens), width)
+
+
+def slot_map(page_size, num_pages, table, tokens, new, num_tokens, before=None, spare=None):
+    """Token by token.  (positions, slots, sequences, offsets, tokens, taken, table)"""
+    table = np.array(table, np.int64)
+    width = table.shape[1]
+    positions, slots, sequences, offsets, now, taken = [], [], [], [0], [], 0
+    for s in range(len(tokens)):
+        n = held = max(int(tokens[s]), 0)
+        held = min(-(-held // page_size), width)        # pages that the table has
+        for _ in range(max(int(new[s]), 0)):
+            if len(slots) == num_tokens:
+                break
+            page = n // page_size
+            if spare is not None and held <= page < width:
+                i = int(spare[taken]) if taken < len(spare) else -1
+                table[s, page] = i if 0 <= i < num_pages else -1
+                held, taken = held + 1, taken + 1
+            entry = int(table[s, page]) if page < width else -1
+            slots.append(entry * page_size + n % page_size if 0 <= entry < num_pages else -1)
+            positions.append(n + (0 if before is None else int(before[s])))
+            sequences.append(s)
+            n += 1
+        offsets.append(len(slots))
+        now.append(min(n, 2 ** 31 - 1))
+    behind = num_tokens - len(slots)
+    return (np.array(positions + [0] * behind, np.int64), np.array(slots + [-1] * behind, np.int64), np.array(sequences + [-1] * behind, np.int64),
+            np.array(offsets), np.array(now, np.int64), np.array([taken]), table)
+
+
 class Pages:
     """Who holds which page: lists of holders, nothing clever."""
 

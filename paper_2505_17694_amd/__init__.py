@@ -10,8 +10,8 @@ import fails.
 from .binding import *          # noqa: F401,F403
 from .binding import EXPORTED_SYMBOLS, LIB_PATH, CodecError
 from .beam import beam_reorder, beam_select
-from .cache import KVCache, Rotary
+from .cache import KVCache, Rotary, StepTokens
 from .runtime import PlannedAttention
 
-__all__ = ["EXPORTED_SYMBOLS", "LIB_PATH", "CodecError", "KVCache", "PlannedAttention", "Rotary",
+__all__ = ["EXPORTED_SYMBOLS", "LIB_PATH", "CodecError", "KVCache", "PlannedAttention", "Rotary", "StepTokens",
            "beam_reorder", "beam_select"]

@@ -51,6 +51,7 @@ EXPORTED_SYMBOLS = [
     "codec_pages_release", "codec_pages_fork", "codec_pages_compact", "codec_cache_copy",
     "codec_beam_workspace_bytes", "codec_beam_select", "codec_beam_reorder",
     "codec_rotary_by_axes", "codec_append_by_axes",
+    "codec_block_table", "codec_slot_workspace_bytes", "codec_slot_map",
 ]
 
 _i32p = POINTER(c_int32)
@@ -130,6 +131,11 @@ class codec_rows(Structure):
 class codec_run(Structure):
     _fields_ = [("src_page", c_int32), ("src_token", c_int32), ("dst_page", c_int32), ("dst_token", c_int32),
                 ("tokens", c_int32)]
+
+
+class codec_slot_config(Structure):
+    _fields_ = [("num_seq", c_int32), ("page_size", c_int32), ("width", c_int32), ("num_tokens", c_int32), ("num_spare", c_int32),
+                ("num_pages", c_int64), ("table_stride", c_int64)]
 
 
 class codec_beam_config(Structure):
@@ -223,6 +229,12 @@ _lib.codec_pages_compact.argtypes = [c_void_p, c_int32, c_void_p, c_int32, _i32p
 _lib.codec_cache_copy.restype = c_int
 _lib.codec_cache_copy.argtypes = [POINTER(codec_head_config), POINTER(codec_kv_layout), c_int32, c_void_p, c_void_p, c_void_p, c_int32,
                                   c_void_p]
+_lib.codec_block_table.restype = c_int
+_lib.codec_block_table.argtypes = [c_int32, c_int32, c_void_p, c_void_p, c_int32, c_void_p, c_void_p, c_int64, c_int32, c_void_p]
+_lib.codec_slot_workspace_bytes.restype = c_size_t
+_lib.codec_slot_workspace_bytes.argtypes = [POINTER(codec_slot_config)]
+_lib.codec_slot_map.restype = c_int
+_lib.codec_slot_map.argtypes = [POINTER(codec_slot_config)] + [c_void_p] * 12 + [c_size_t, c_void_p]
 _lib.codec_beam_workspace_bytes.restype = c_size_t
 _lib.codec_beam_workspace_bytes.argtypes = [POINTER(codec_beam_config)]
 _lib.codec_beam_select.restype = c_int
@@ -544,6 +556,23 @@ def codec_cache_copy(head, layout, k_ptrs, v_ptrs, runs, stream: int = 0) -> int
     pools = f"{len(k_ptrs)}P"                           # bytes as an array of pointers
     return _lib.codec_cache_copy(head, layout, len(k_ptrs), struct.pack(pools, *k_ptrs), struct.pack(pools, *v_ptrs), _in(runs), len(runs),
                                  stream)
+
+
+def codec_block_table(page_size: int, num_seq: int, page_off_ptr: int, page_ids_ptr: int, num_ids: int, tokens_ptr: int, table_ptr: int,
+                      table_stride: int, width: int, stream: int = 0) -> int:
+    return _lib.codec_block_table(page_size, num_seq, page_off_ptr, page_ids_ptr, num_ids, tokens_ptr, table_ptr, table_stride, width, stream)
+
+
+def codec_slot_workspace_bytes(config) -> int:
+    return int(_lib.codec_slot_workspace_bytes(config))
+
+
+def codec_slot_map(config, table_ptr: int, tokens_ptr: int, new_tokens_ptr: int, before_ptr: int, spare_ptr: int, positions_ptr: int,
+                   slots_ptr: int, sequences_ptr: int, offsets_ptr: int, tokens_out_ptr: int, taken_ptr: int, workspace_ptr: int = 0,
+                   workspace_bytes: int = 0, stream: int = 0) -> int:
+    """``config``: codec_slot_config."""
+    return _lib.codec_slot_map(config, table_ptr, tokens_ptr, new_tokens_ptr, before_ptr, spare_ptr, positions_ptr, slots_ptr, sequences_ptr,
+                               offsets_ptr, tokens_out_ptr, taken_ptr, workspace_ptr, workspace_bytes, stream)
 
 
 def codec_beam_workspace_bytes(config) -> int:

@@ -3,6 +3,7 @@ from __future__ import annotations
 
 import contextlib
 from types import SimpleNamespace
+from typing import NamedTuple
 
 import numpy as np
 import torch
@@ -236,6 +237,35 @@ class _Turn(torch.autograd.Function):
         return ctx.rotary.apply(g, positions, not ctx.inverse), None, None, None, None
 
 
+def _list(t: torch.Tensor, what: str, n: int, index: int, dtype=torch.int32) -> int:
+    """A contiguous list of n numbers on the GPU; its address."""
+    if t.shape != (n,) or t.dtype is not dtype or t.get_device() != index or not t.is_contiguous():
+        raise ValueError(f"{what}: need a contiguous {dtype} tensor of shape {(n,)} on cuda:{index}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    _check_reach(t, what, n, t.element_size())
+    return t.data_ptr()
+
+
+def _table_rows(t: torch.Tensor, what: str, n: int, width: int, index: int):
+    """A block table [n, width] whose rows are contiguous; (address, entries from one row to the next)."""
+    if t.shape != (n, width) or t.dtype is not torch.int32 or t.get_device() != index or (width > 1 and t.stride(1) != 1):
+        raise ValueError(f"{what}: need an int32 tensor of shape {(n, width)}, rows contiguous, on cuda:{index}, got {t.dtype} {tuple(t.shape)} on "
+                         f"{t.device}, strides {t.stride()}")
+    stride = t.stride(0) if n > 1 else width
+    if n and width:
+        _check_reach(t, what, (n - 1) * stride + width, 4)
+    return t.data_ptr(), stride
+
+
+class StepTokens(NamedTuple):
+    """The new tokens of a step (KVCache.slots)."""
+    positions: torch.Tensor         # [num_tokens] int64
+    slots: torch.Tensor             # [num_tokens] int64; -1: no token, or one for which there is no page
+    sequences: torch.Tensor         # [num_tokens] int32; -1: no token
+    offsets: torch.Tensor           # [sequences + 1] int32: the first token of every sequence, and their number
+    tokens: torch.Tensor            # [sequences] int32: what the sequences hold now
+    taken: torch.Tensor             # [1] int32: pages taken from spare; more than it holds: there were too few
+
+
 class KVCache:
     """The page pools of a cache, one K and one V pool per layer, with the operations that fill them, and who holds which page.
 
@@ -374,6 +404,79 @@ class KVCache:
         if st != B.CODEC_OK:
             raise B.CodecError(st, name)
         return q_out
+
+    def table(self, page_off, page_ids, tokens, width, out: torch.Tensor = None, stream=None) -> torch.Tensor:
+        """Page lists as a dense table [sequences, width] on the GPU (int32): the pages that hold sequence s's tokens[s] tokens,
+        page_ids[page_off[s]:], -1 behind them; into ``out`` if that is given (codec_block_table).  page_off, page_ids and tokens
+        are int32 tensors on the GPU, or lists on the host as fork returns them, which are copied there first (that waits)."""
+        self._check_call("table", stream)
+        s = _enter(self._index, stream)
+        if s is None:
+            with _on(self.device, stream) as s:
+                return self._table(page_off, page_ids, tokens, width, out, s)
+        return self._table(page_off, page_ids, tokens, width, out, s)
+
+    def _to_device(self, a, what: str) -> torch.Tensor:
+        if isinstance(a, torch.Tensor):
+            return a
+        a = B._ids(a)
+        if a is None or a.ndim != 1:
+            raise ValueError(f"{what}: need a list of whole numbers of 32 bits")
+        return torch.from_numpy(a).to(self.device)
+
+    def _table(self, page_off, page_ids, tokens, width, out, s):
+        off, ids, tokens = (self._to_device(a, w) for a, w in ((page_off, "page_off"), (page_ids, "page_ids"), (tokens, "tokens")))
+        if tokens.dim() != 1 or ids.dim() != 1 or not 0 <= width < 1 << 31 or (tokens.shape[0] | ids.shape[0]) >> 31:
+            raise ValueError(f"tokens {tuple(tokens.shape)}, page_ids {tuple(ids.shape)}, width {width}: need lists, and a width of 32 bits")
+        n, count, index = tokens.shape[0], ids.shape[0], self._index
+        if out is None:
+            out = torch.empty((n, width), dtype=torch.int32, device=self.device)
+        at, stride = _table_rows(out, "out", n, width, index)
+        st = B.codec_block_table(self.head.page_size, n, _list(off, "page_off", n + 1, index), _list(ids, "page_ids", count, index), count,
+                                 _list(tokens, "tokens", n, index), at, stride, width, s)
+        if st != B.CODEC_OK:
+            raise B.CodecError(st, "codec_block_table")
+        return out
+
+    def slots(self, table: torch.Tensor, tokens: torch.Tensor, new: torch.Tensor, num_tokens: int, before: torch.Tensor = None,
+              spare: torch.Tensor = None, stream=None) -> StepTokens:
+        """Positions and slots of a step's new tokens, from lengths on the GPU (codec_slot_map): sequence s holds tokens[s] tokens in
+        the pages of table[s] and gets new[s] more (int32).  Positions count from before[s] (int64; zero without).  With ``spare``
+        (int32, pages that ``take`` gave) new pages are taken from it in order and entered in the table, in place; without, the
+        table names them already.  num_tokens: the length of the map, behind whose last token there is padding that ``append``
+        does not store; new tokens beyond it are left out.  The result's tensors share two allocations."""
+        self._check_call("slots", stream)
+        s = _enter(self._index, stream)
+        if s is None:
+            with _on(self.device, stream) as s:
+                return self._slots(table, tokens, new, num_tokens, before, spare, s)
+        return self._slots(table, tokens, new, num_tokens, before, spare, s)
+
+    def _slots(self, table, tokens, new, num_tokens, before, spare, s):
+        if table.dim() != 2 or not 0 <= num_tokens < 1 << 31 or (table.shape[0] | table.shape[1]) >> 31 or (spare is not None and spare.dim() != 1):
+            raise ValueError(f"table {tuple(table.shape)}, num_tokens {num_tokens}: need a table of two dimensions, spare of one, and a "
+                             "number of tokens of 32 bits")
+        (n, width), index = table.shape, self._index
+        at, stride = _table_rows(table, "table", n, width, index)
+        pages = 0 if spare is None else spare.shape[0]
+        if pages >> 31:
+            raise ValueError(f"spare: {pages} pages are too many for a call")
+        config = B.codec_slot_config(n, self.head.page_size, width, num_tokens, pages, self.num_pages, stride)
+        tokens_at, new_at = _list(tokens, "tokens", n, index), _list(new, "new", n, index)
+        before_at = None if before is None else _list(before, "before", n, index, torch.int64)
+        # spare without a page is not the same as none: the new pages are wanted from it
+        spare_at = None if spare is None else _list(spare, "spare", pages, index) or at
+        need = B.codec_slot_workspace_bytes(config)
+        wide = torch.empty((2, num_tokens), dtype=torch.int64, device=self.device)
+        lists = torch.empty((num_tokens + 2 * n + 2,), dtype=torch.int32, device=self.device)
+        workspace = torch.empty((need,), dtype=torch.uint8, device=self.device) if need else None
+        first, second = wide.data_ptr(), lists.data_ptr()
+        offsets = second + 4 * num_tokens
+        st = B.codec_slot_map(config, at, tokens_at, new_at, before_at, spare_at, first, first + 8 * num_tokens, second, offsets,
+                              offsets + 4 * (n + 1), offsets + 4 * (2 * n + 1), workspace.data_ptr() if need else None, need, s)
+        if st != B.CODEC_OK:
+            raise B.CodecError(st, "codec_slot_map")
+        return StepTokens(*wide.unbind(0), *lists.split([num_tokens, n + 1, n, 1]))
 
     @property
     def free_pages(self) -> int:

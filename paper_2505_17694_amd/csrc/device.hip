@@ -3,3 +3,4 @@
 #include "beam.hip"
 #include "pagecopy.hip"
 #include "rotary.hip"
+#include "slots.hip"

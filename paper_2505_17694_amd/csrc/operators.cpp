@@ -15,6 +15,7 @@ using codec::hip_failure;
 
 constexpr double kTwoPi = 6.283185307179586476925;
 constexpr int64_t kMaxSpan = int64_t(1) << 58;          // elements: byte offsets, and sums of a few, stay in 64 bits
+constexpr int32_t kMaxSequences = 1 << 22;
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
@@ -26,12 +27,13 @@ int check_rows_of(int32_t head_dim, int32_t dtype)
     return CODEC_OK;
 }
 
+bool page_size_ok(int32_t n) { return n >= 16 && n <= 4096 && (n & (n - 1)) == 0; }
+
 int check_head(const codec_head_config &h)
 {
     if (h.num_kv_heads < 1 || h.num_q_heads < 1 || h.num_kv_heads > (1 << 12) || h.num_q_heads > (1 << 16)) return CODEC_ERR_INVALID_ARGUMENT;
     if (int st = check_rows_of(h.head_dim, h.dtype)) return st;
-    if (h.page_size < 16 || h.page_size > 4096 || (h.page_size & (h.page_size - 1)) != 0) return CODEC_ERR_UNSUPPORTED;
-    return CODEC_OK;
+    return page_size_ok(h.page_size) ? CODEC_OK : CODEC_ERR_UNSUPPORTED;
 }
 
 struct Extent { int64_t count, stride; };
@@ -71,6 +73,7 @@ bool pools_apart(const codec_head_config &h, const codec_kv_layout &l, const voi
 
 struct Range { const char *begin, *end; };
 bool overlap(const Range &a, const Range &b) { return a.begin < b.end && b.begin < a.end; }
+Range bytes_at(const void *p, int64_t n) { return {static_cast<const char *>(p), static_cast<const char *>(p) + n}; }
 
 bool rows_ok(const codec_rows *r, int64_t tokens, int64_t heads)
 {
@@ -450,6 +453,99 @@ int codec_cache_copy(const codec_head_config *head, const codec_kv_layout *layou
     return CODEC_OK;
 }
 
+int codec_block_table(int32_t page_size, int32_t num_seq, const int32_t *page_off, const int32_t *page_ids, int32_t num_ids,
+                      const int32_t *tokens, int32_t *table, int64_t table_stride, int32_t width, void *stream)
+{
+    if (num_seq < 0 || num_seq > kMaxSequences || num_ids < 0 || width < 0 || table_stride < width || table_stride > kMaxSpan / kMaxSequences) return CODEC_ERR_INVALID_ARGUMENT;
+    if (!page_size_ok(page_size)) return CODEC_ERR_UNSUPPORTED;
+    if (num_seq == 0 || width == 0) return CODEC_OK;
+    if (!page_off || (num_ids && !page_ids) || !tokens || !table) return CODEC_ERR_INVALID_ARGUMENT;
+    for (const void *p : {static_cast<const void *>(page_off), static_cast<const void *>(page_ids), static_cast<const void *>(tokens), static_cast<const void *>(table)})
+        if (reinterpret_cast<uintptr_t>(p) % 4) return CODEC_ERR_INVALID_ARGUMENT;
+    const Range written = bytes_at(table, 4 * ((num_seq - 1) * table_stride + width));
+    if (overlap(written, bytes_at(page_off, 4 * (int64_t(num_seq) + 1))) || overlap(written, bytes_at(page_ids, 4 * int64_t(num_ids))) ||
+        overlap(written, bytes_at(tokens, 4 * int64_t(num_seq))))
+        return CODEC_ERR_INVALID_ARGUMENT;
+    codec::TableParams p{};
+    p.page_off = page_off;
+    p.page_ids = page_ids;
+    p.tokens = tokens;
+    p.table = table;
+    p.table_stride = table_stride;
+    p.num_ids = num_ids;
+    p.num_seq = num_seq;
+    p.width = width;
+    while ((1 << p.page_shift) < page_size) ++p.page_shift;
+    if (int e = codec::launch_block_table(p, stream)) return hip_failure("block table launch", e);
+    return CODEC_OK;
+}
+
+size_t codec_slot_workspace_bytes(const codec_slot_config *config)
+{
+    return config && config->num_seq > codec::kSlotsAtOnce && config->num_seq <= kMaxSequences ? align_up(8 * size_t(config->num_seq) + 4) : 0;
+}
+
+int codec_slot_map(const codec_slot_config *config, int32_t *table, const int32_t *tokens, const int32_t *new_tokens, const int64_t *before,
+                   const int32_t *spare, int64_t *positions, int64_t *slots, int32_t *sequences, int32_t *offsets, int32_t *tokens_out,
+                   int32_t *taken, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!config) return CODEC_ERR_INVALID_ARGUMENT;
+    const codec_slot_config &c = *config;
+    if (c.num_seq < 0 || c.num_seq > kMaxSequences || c.width < 0 || c.num_tokens < 0 || c.num_spare < 0 || c.num_pages < 0 ||
+        c.num_pages > (int64_t(1) << 31) || c.table_stride < c.width || c.table_stride > kMaxSpan / kMaxSequences)
+        return CODEC_ERR_INVALID_ARGUMENT;
+    if (!page_size_ok(c.page_size)) return CODEC_ERR_UNSUPPORTED;
+    const size_t need = codec_slot_workspace_bytes(config);
+    if (workspace_bytes < need) return CODEC_ERR_WORKSPACE_TOO_SMALL;
+    if (need && !workspace) return CODEC_ERR_INVALID_ARGUMENT;
+    if (!offsets || !taken || (c.num_seq && (!tokens || !new_tokens || !tokens_out)) || (c.num_seq && c.width && !table) ||
+        (c.num_tokens && (!positions || !slots)))
+        return CODEC_ERR_INVALID_ARGUMENT;
+    if (reinterpret_cast<uintptr_t>(need ? workspace : nullptr) % 256) return CODEC_ERR_INVALID_ARGUMENT;
+    for (const void *p : {static_cast<const void *>(table), static_cast<const void *>(tokens), static_cast<const void *>(new_tokens),
+                          static_cast<const void *>(spare), static_cast<const void *>(sequences), static_cast<const void *>(offsets),
+                          static_cast<const void *>(tokens_out), static_cast<const void *>(taken)})
+        if (reinterpret_cast<uintptr_t>(p) % 4) return CODEC_ERR_INVALID_ARGUMENT;
+    for (const void *p : {static_cast<const void *>(before), static_cast<const void *>(positions), static_cast<const void *>(slots)})
+        if (reinterpret_cast<uintptr_t>(p) % 8) return CODEC_ERR_INVALID_ARGUMENT;
+    {
+        // what is written is neither read elsewhere nor written twice; the table is written only where pages are taken for it
+        const int64_t n = c.num_seq, t = c.num_tokens, rows = n && c.width ? (n - 1) * c.table_stride + c.width : 0;
+        const Range out[] = {bytes_at(positions, 8 * t), bytes_at(slots, 8 * t), bytes_at(sequences, sequences ? 4 * t : 0), bytes_at(offsets, 4 * (n + 1)),
+                             bytes_at(tokens_out, 4 * n), bytes_at(taken, 4), bytes_at(workspace, int64_t(need)), bytes_at(table, 4 * rows)};
+        const Range in[] = {bytes_at(tokens, 4 * n), bytes_at(new_tokens, 4 * n), bytes_at(before, before ? 8 * n : 0), bytes_at(spare, spare ? 4 * int64_t(c.num_spare) : 0)};
+        auto meet = [](const Range &a, const Range &b) { return a.begin < a.end && b.begin < b.end && overlap(a, b); };
+        for (int i = 0; i < 8; ++i) {
+            for (int j = i + 1; j < 8; ++j)
+                if (meet(out[i], out[j])) return CODEC_ERR_INVALID_ARGUMENT;
+            for (const Range &r : in)
+                if (meet(out[i], r) && (i < 7 || spare)) return CODEC_ERR_INVALID_ARGUMENT;
+        }
+    }
+    codec::SlotParams p{};
+    p.table = table;
+    p.table_stride = c.table_stride;
+    p.num_pages = c.num_pages;
+    p.tokens = tokens;
+    p.new_tokens = new_tokens;
+    p.before = before;
+    p.spare = spare;
+    p.positions = positions;
+    p.slots = slots;
+    p.sequences = sequences;
+    p.offsets = offsets;
+    p.tokens_out = tokens_out;
+    p.taken = taken;
+    p.sums = static_cast<uint32_t *>(workspace);
+    p.num_seq = c.num_seq;
+    p.width = c.width;
+    p.num_tokens = c.num_tokens;
+    p.num_spare = c.num_spare;
+    while ((1 << p.page_shift) < c.page_size) ++p.page_shift;
+    if (int e = codec::launch_slot_map(p, stream)) return hip_failure("slot map launch", e);
+    return CODEC_OK;
+}
+
 size_t codec_beam_workspace_bytes(const codec_beam_config *config)
 {
     if (!config || check_beams(*config)) return 0;
@@ -474,10 +570,9 @@ int codec_beam_select(const codec_beam_config *config, const void *logits, int64
     {
         // what is written is neither read nor written twice; scores may go back to where they came from, search by search
         const int64_t rows = int64_t(c.batch) * c.beams, span = (c.batch - 1) * batch_stride + (c.beams - 1) * beam_stride + c.vocab;
-        auto range = [](const void *p, int64_t bytes) { return Range{static_cast<const char *>(p), static_cast<const char *>(p) + bytes}; };
-        const Range out[] = {range(out_scores, 4 * int64_t(c.batch) * c.k), range(out_beams, 4 * int64_t(c.batch) * c.k),
-                             range(out_tokens, 4 * int64_t(c.batch) * c.k), range(workspace, int64_t(s.total))};
-        const Range in[] = {range(logits, size * span), range(scores, 4 * rows), range(finished, finished ? rows : 0)};
+        const Range out[] = {bytes_at(out_scores, 4 * int64_t(c.batch) * c.k), bytes_at(out_beams, 4 * int64_t(c.batch) * c.k),
+                             bytes_at(out_tokens, 4 * int64_t(c.batch) * c.k), bytes_at(workspace, int64_t(s.total))};
+        const Range in[] = {bytes_at(logits, size * span), bytes_at(scores, 4 * rows), bytes_at(finished, finished ? rows : 0)};
         for (int i = 0; i < 4; ++i) {
             for (int j = i + 1; j < 4; ++j)
                 if (overlap(out[i], out[j])) return CODEC_ERR_INVALID_ARGUMENT;

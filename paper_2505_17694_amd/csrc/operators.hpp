@@ -59,6 +59,31 @@ struct CopyParams {
 };
 static_assert(sizeof(CopyParams) <= 4096, "kernel arguments");
 
+struct TableParams {
+    const int32_t *page_off, *page_ids, *tokens;        // [num_seq + 1], [num_ids], [num_seq]
+    int32_t *table;
+    int64_t table_stride, num_ids;
+    int32_t num_seq, width, page_shift;
+    uint32_t row_units;                                 // set by launch_block_table
+    uint64_t units;
+};
+
+// Most sequences whose sums every workgroup makes for itself, in LDS.
+constexpr int kSlotsAtOnce = 4096;
+
+struct SlotParams {
+    int32_t *table;
+    int64_t table_stride, num_pages;
+    const int32_t *tokens, *new_tokens;     // [num_seq]
+    const int64_t *before;                  // [num_seq] or nullptr
+    const int32_t *spare;                   // [num_spare] or nullptr: the table holds the new tokens' pages
+    int64_t *positions, *slots;             // [num_tokens]
+    int32_t *sequences;                     // [num_tokens] or nullptr
+    int32_t *offsets, *tokens_out, *taken;  // [num_seq + 1], [num_seq], [1]
+    uint32_t *sums;                         // [2 * num_seq + 1], more than kSlotsAtOnce sequences: new tokens, new pages before each
+    int32_t num_seq, width, num_tokens, num_spare, page_shift;
+};
+
 // A sum of exponentials: sum * 2^ref
 struct PartialSum { double ref, sum; };
 
@@ -101,6 +126,8 @@ static_assert(sizeof(ReorderParams) <= 4096, "kernel arguments");
 int launch_rotary(const RotaryParams &p, int dtype, bool interleaved, void *stream);
 int launch_rotary_axes(const AxesParams &p, int dtype, bool interleaved, void *stream);
 int launch_copy(CopyParams &p, void *stream);
+int launch_block_table(TableParams p, void *stream);
+int launch_slot_map(const SlotParams &p, void *stream);
 int launch_beam_select(const BeamParams &p, int dtype, void *stream);
 // `unit`: bytes moved at a time, 1, 2, 4, 8 or 16
 int launch_reorder(const ReorderParams &p, int unit, void *stream);
