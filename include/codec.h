@@ -385,6 +385,40 @@ int codec_decode_attention_static(const codec_plan_t *plan, const void *q,
 size_t codec_static_scratch_bytes(void);       /* CODEC_STATIC_SCRATCH_BYTES of the built library */
 
 /*
+ * Differential attention: the difference of two softmax maps over the same values, out = gain * norm(o_1 - lambda o_2) with
+ * o_m = softmax(scale * q_m . K_m^T) V and, if wanted, norm(x) = weight * x / sqrt(mean(x^2) + eps) over the channels of a head.
+ *
+ * The maps have d channels, the values and the result 2d: a KV head of the pools holds [K_1 | K_2] and V, 2d channels each.
+ * A plan for it has head_dim = 2d, num_kv_heads KV heads, num_q_heads = 2 H query heads for H heads of the result, and the scale of
+ * the maps (1 / sqrt(d)); head h uses KV head h / (H / num_kv_heads).  Everything a plan can do holds: shared nodes are read
+ * once for all requests and both maps, visibility masks (values of hidden tokens are multiplied by zero: they have to be
+ * finite, as for codec_decode_attention), refreshed lengths, the run-time queue (fused is without effect).
+ */
+typedef struct {
+    const float *lambda;            /* device: of request r and head h at r * lambda_request_stride + h * lambda_head_stride   */
+    int64_t lambda_request_stride, lambda_head_stride;      /* elements, 0 (one for all) .. 2^36                        */
+    int32_t norm;                   /* 1: normalised over the channels of a head; 0: not (eps and weight are not used)  */
+    int32_t weight_dtype;           /* CODEC_DTYPE_FP32 or the plan's                                                   */
+    const void *weight;             /* device [2d], aligned as its type; NULL: no weights (ones)                        */
+    float eps;                      /* >= 0                                                                             */
+    float gain;                     /* factor on the result                                                             */
+} codec_differential;
+
+/* Bytes of scratch codec_differential_attention needs (more than codec_plan_workspace_bytes). */
+size_t codec_differential_workspace_bytes(const codec_plan_t *plan);
+
+/*
+ * One step, enqueued on `stream` without synchronising.
+ *   q        device [num_requests][H][2][d], dtype of the plan, 16-byte aligned: both maps' queries of a head side by side
+ *   out      device [num_requests][H][2d], same dtype, 16-byte aligned; must not overlap q, lambda, weight or workspace
+ *   plan, k_pages, v_pages, layout, workspace   as for codec_decode_attention; workspace of codec_differential_workspace_bytes
+ * CODEC_ERR_UNSUPPORTED for a plan with an odd number of query heads per KV head.
+ */
+int codec_differential_attention(const codec_plan_t *plan, const codec_differential *differential, const void *q,
+                                 const void *k_pages, const void *v_pages, const codec_kv_layout *layout, void *out,
+                                 void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * Measurement support (no part of the method): a read-only streaming kernel that gives the HBM read
  * rate this machine reaches, for pricing the attention kernel against something measured beside the
  * vendor's 8 TB/s.  Reads `bytes` (a power of two, >= 4096) of device memory at `buffer` (16-byte

@@ -84,6 +84,42 @@ def rotary_by_axes(x, positions, turns, axis, magnitude, interleaved, blocks=1, 
     return out, size
 
 
+def differential(q, k, v, scale, lam, norm=None, gain=1.0, half_step=0.0, least=0.0):
+    """One request: q [H, 2, d], k and v [n, G, 2 d] (a head's keys are [K_1 | K_2]), lam [H]; norm: None or (eps, weight [2 d]).  All
+    64 bits.  Returns out [H, 2 d] and how far a result may be off whose exponentials were rounded by half_step of themselves, or
+    by `least` where they are smaller than that goes, whose products and sums ran in 32 bits, and which was rounded by half_step."""
+    heads, _, d = q.shape
+    n, group, u = len(k), heads // k.shape[1], 2.0 ** -24
+    out, off = np.zeros((heads, 2 * d)), np.zeros((heads, 2 * d))
+    for h in range(heads):
+        o, e = [], []
+        for m in range(2):
+            keys, values = k[:, h // group, m * d:(m + 1) * d], v[:, h // group]
+            x = scale * (keys @ q[h, m])
+            p = np.exp(x - x.max())
+            total = p.sum()
+            p = p / total
+            o.append(p @ values)
+            away = np.abs(values - o[-1])
+            # a weight is off by: its rounding, which the sum of weights shares; its score, d products summed in 32 bits, times
+            # the scale and log2(e), less a reference; the exponential, 2 ulp; the rescalings of partial sums, a few more
+            score = (d + 3) * u * scale * (np.abs(keys) @ np.abs(q[h, m])) + 4 * u * np.abs(x).max() + 16 * u
+            weight = p * (half_step + score) + least / total
+            # the sums of weights and of products run over n tokens in 32 bits
+            e.append((weight @ away) / (1 - half_step - score.max()) + (2 * n + 32) * u * (p @ np.abs(values)))
+        x = o[0] - lam[h] * o[1]
+        dx = e[0] + abs(lam[h]) * e[1] + 2 * u * (np.abs(o[0]) + np.abs(lam[h] * o[1]))
+        if norm is not None:
+            eps, w = norm
+            rho, drho = np.sqrt(np.mean(x * x) + eps), np.sqrt(np.mean(dx * dx))
+            y = x / rho * w
+            dx = np.abs(w) * (dx + np.abs(x) * drho / rho) / max(rho - drho, np.sqrt(eps)) + (2 * d + 8) * u * np.abs(y)
+            x = y
+        out[h], dx = gain * x, abs(gain) * dx
+        off[h] = dx + half_step * (np.abs(out[h]) + dx) + 2 * u * np.abs(out[h]) + least
+    return out, off
+
+
 def block_table(page_size, page_off, page_ids, tokens, width):
     """Row by row: the pages that hold the tokens, -1 behind them."""
     rows = []

@@ -52,6 +52,7 @@ EXPORTED_SYMBOLS = [
     "codec_beam_workspace_bytes", "codec_beam_select", "codec_beam_reorder",
     "codec_rotary_by_axes", "codec_append_by_axes",
     "codec_block_table", "codec_slot_workspace_bytes", "codec_slot_map",
+    "codec_differential_workspace_bytes", "codec_differential_attention",
 ]
 
 _i32p = POINTER(c_int32)
@@ -107,6 +108,11 @@ class codec_plan_view(Structure):
 class codec_kv_layout(Structure):
     _fields_ = [("num_pages", c_int64), ("page_stride", c_int64), ("token_stride", c_int64),
                 ("head_stride", c_int64)]
+
+
+class codec_differential(Structure):
+    _fields_ = [("lambda_", c_void_p), ("lambda_request_stride", c_int64), ("lambda_head_stride", c_int64), ("norm", c_int32),
+                ("weight_dtype", c_int32), ("weight", c_void_p), ("eps", c_float), ("gain", c_float)]
 
 
 class codec_rotary_scaling(Structure):
@@ -195,6 +201,11 @@ _lib.codec_decode_attention_static.argtypes = [c_void_p, c_void_p, c_void_p, c_v
                                                POINTER(codec_kv_layout), c_void_p, c_void_p]
 _lib.codec_static_scratch_bytes.restype = c_size_t
 _lib.codec_static_scratch_bytes.argtypes = []
+_lib.codec_differential_workspace_bytes.restype = c_size_t
+_lib.codec_differential_workspace_bytes.argtypes = [c_void_p]
+_lib.codec_differential_attention.restype = c_int
+_lib.codec_differential_attention.argtypes = [c_void_p, POINTER(codec_differential), c_void_p, c_void_p, c_void_p,
+                                              POINTER(codec_kv_layout), c_void_p, c_void_p, c_size_t, c_void_p]
 _lib.codec_stream_read_probe.restype = c_int
 _lib.codec_stream_read_probe.argtypes = [c_void_p, c_size_t, c_int32, c_int32, c_int32, c_void_p, c_void_p]
 _lib.codec_rotary_turns.restype = c_int
@@ -428,6 +439,16 @@ def codec_decode_attention_static(plan, q_ptr: int, k_ptr: int, v_ptr: int, num_
     lay = codec_kv_layout(num_pages, page_stride, token_stride, head_stride)
     return _lib.codec_decode_attention_static(plan, c_void_p(q_ptr), c_void_p(k_ptr), c_void_p(v_ptr),
                                               byref(lay), c_void_p(out_ptr), c_void_p(stream))
+
+
+def codec_differential_workspace_bytes(plan) -> int:
+    return int(_lib.codec_differential_workspace_bytes(plan))
+
+
+def codec_differential_attention(plan, differential, q_ptr: int, k_ptr: int, v_ptr: int, layout, out_ptr: int, workspace_ptr: int,
+                                 workspace_bytes: int, stream: int = 0) -> int:
+    """``differential``: codec_differential; ``layout``: codec_kv_layout."""
+    return _lib.codec_differential_attention(plan, differential, q_ptr, k_ptr, v_ptr, layout, out_ptr, workspace_ptr, workspace_bytes, stream)
 
 
 def codec_static_scratch_bytes() -> int:

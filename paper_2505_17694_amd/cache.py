@@ -1,7 +1,6 @@
 """Page pools of a K/V cache with what fills them, and rotary positions (marshalling only)."""
 from __future__ import annotations
 
-import contextlib
 from types import SimpleNamespace
 from typing import NamedTuple
 
@@ -9,16 +8,13 @@ import numpy as np
 import torch
 
 from . import binding as B
-from .runtime import _current_stream
+from .runtime import _enter, _on
 
 _TORCH_DTYPE = {B.CODEC_DTYPE_FP16: torch.float16, B.CODEC_DTYPE_BF16: torch.bfloat16}
 _CODE = {t: c for c, t in _TORCH_DTYPE.items()}
 _SCALINGS = {"linear": B.CODEC_ROTARY_LINEAR, "ntk": B.CODEC_ROTARY_NTK, "wavelength": B.CODEC_ROTARY_WAVELENGTH,
              "yarn": B.CODEC_ROTARY_YARN}
 
-
-_current_device = getattr(torch._C, "_cuda_getDevice", None)               # absent in a PyTorch without a GPU runtime
-_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 _Rows = B.codec_rows
 _data_ptr, _base_ptr, _nbytes = torch.Tensor.data_ptr, torch.UntypedStorage.data_ptr, torch.UntypedStorage.nbytes
 _NO_RUNS = np.empty((0, 5), np.int32)
@@ -29,22 +25,6 @@ def _device(device) -> torch.device:
     if d.type == "cuda" and d.index is None:
         d = torch.device("cuda", torch.cuda.current_device())
     return d
-
-
-@contextlib.contextmanager
-def _on(device: torch.device, stream):
-    """Makes `device` and `stream` the current ones; the handle of the stream.  What is allocated meanwhile belongs to the
-    stream that uses it."""
-    if stream is not None and stream.device != device:
-        raise ValueError(f"stream: on {stream.device}, the tensors are on {device}")
-    with torch.cuda.device(device), torch.cuda.stream(stream):
-        yield _current_stream(device)
-
-
-def _enter(index: int, stream):
-    """The stream's handle if a call on device `index` can go ahead as things are, else None: another device or stream has to be
-    made current."""
-    return _raw_stream(index) if stream is None and _current_device() == index else None
 
 
 def _check_reach(t: torch.Tensor, what: str, last: int, size: int) -> None:

@@ -49,6 +49,9 @@ size_t part_ml_bytes(const codec::PlanData &d)
     return align_up(size_t(d.head.num_kv_heads) * size_t(d.part_rows) * 2 * sizeof(float), 256);
 }
 
+// Query rows of a step, as the kernels read them
+size_t query_bytes(const codec::PlanData &d) { return size_t(d.num_requests) * size_t(d.head.num_q_heads) * size_t(d.head.head_dim) * 2; }
+
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 }  // namespace
@@ -225,15 +228,11 @@ codec::MergeParams merge_params(const codec_plan_t *plan, const void *workspace,
     return mp;
 }
 
-// Partial attention over the plan's tasks; with `fused_out` the launch also reduces (single-launch mode), or
-// has nothing to reduce (single_parts).
-int partial_attention(const codec_plan_t *plan, const void *q, const void *k_pages,
-                      const void *v_pages, const codec_kv_layout *layout,
-                      void *workspace, size_t workspace_bytes, void *fused_out, void *stream)
+// What a launch over the plan's tasks wants of its arguments (a plan with requests).
+int check_partial_attention(const codec_plan_t *plan, const void *q, const void *k_pages, const void *v_pages, const codec_kv_layout *layout,
+                            const void *workspace, size_t workspace_bytes)
 {
-    if (!plan || !layout) return CODEC_ERR_INVALID_ARGUMENT;
     const codec::PlanData &d = plan->d;
-    if (d.num_requests == 0) return CODEC_OK;               // nothing to compute
     if (!q || !k_pages || !v_pages || !workspace) return CODEC_ERR_INVALID_ARGUMENT;
     if (!plan->device_meta) return CODEC_ERR_NOT_UPLOADED;
     if (workspace_bytes < codec_plan_workspace_bytes(plan)) return CODEC_ERR_WORKSPACE_TOO_SMALL;
@@ -247,6 +246,19 @@ int partial_attention(const codec_plan_t *plan, const void *q, const void *k_pag
     if (layout->page_stride > (int64_t(1) << 30) || layout->token_stride > (int64_t(1) << 30) ||
         int64_t(d.head.page_size) * layout->token_stride * 2 >= (int64_t(1) << 32))
         return CODEC_ERR_INVALID_ARGUMENT;
+    return CODEC_OK;
+}
+
+// Partial attention over the plan's tasks; with `fused_out` the launch also reduces (single-launch mode), or
+// has nothing to reduce (single_parts).
+int partial_attention(const codec_plan_t *plan, const void *q, const void *k_pages,
+                      const void *v_pages, const codec_kv_layout *layout,
+                      void *workspace, size_t workspace_bytes, void *fused_out, void *stream)
+{
+    if (!plan || !layout) return CODEC_ERR_INVALID_ARGUMENT;
+    const codec::PlanData &d = plan->d;
+    if (d.num_requests == 0) return CODEC_OK;               // nothing to compute
+    if (int st = check_partial_attention(plan, q, k_pages, v_pages, layout, workspace, workspace_bytes)) return st;
 
     const char *meta = static_cast<const char *>(plan->device_meta);
     const codec::DevLayout &L = d.layout;
@@ -352,6 +364,63 @@ int codec_decode_attention_static(const codec_plan_t *plan, const void *q, const
     void *ws = nullptr;
     if (int e = codec::static_scratch_address(&ws)) return hip_failure("hipGetSymbolAddress(scratch)", e);
     return codec_decode_attention(plan, q, k_pages, v_pages, layout, out, ws, codec::kStaticScratchBytes, stream);
+}
+
+size_t codec_differential_workspace_bytes(const codec_plan_t *plan)
+{
+    return plan ? align_up(codec_plan_workspace_bytes(plan), 256) + align_up(query_bytes(plan->d), 256) : 0;
+}
+
+int codec_differential_attention(const codec_plan_t *plan, const codec_differential *differential, const void *q, const void *k_pages,
+                                 const void *v_pages, const codec_kv_layout *layout, void *out, void *workspace,
+                                 size_t workspace_bytes, void *stream)
+{
+    if (!plan || !differential || !layout) return CODEC_ERR_INVALID_ARGUMENT;
+    const codec::PlanData &d = plan->d;
+    const codec_differential &c = *differential;
+    if (d.group % 2) return CODEC_ERR_UNSUPPORTED;
+    if (c.lambda_request_stride < 0 || c.lambda_head_stride < 0 || c.lambda_request_stride > (int64_t(1) << 36) || c.lambda_head_stride > (int64_t(1) << 36))
+        return CODEC_ERR_INVALID_ARGUMENT;
+    if ((c.norm != 0 && c.norm != 1) || !std::isfinite(c.gain) || (c.norm && (!(c.eps >= 0.f) || !std::isfinite(c.eps)))) return CODEC_ERR_INVALID_ARGUMENT;
+    if (c.weight && !c.norm) return CODEC_ERR_INVALID_ARGUMENT;
+    if (c.weight && c.weight_dtype != CODEC_DTYPE_FP32 && c.weight_dtype != d.head.dtype) return CODEC_ERR_UNSUPPORTED;
+    if (d.num_requests == 0) return CODEC_OK;
+    if (!c.lambda || reinterpret_cast<uintptr_t>(c.lambda) % 4) return CODEC_ERR_INVALID_ARGUMENT;
+    if (c.weight && reinterpret_cast<uintptr_t>(c.weight) % (c.weight_dtype == CODEC_DTYPE_FP32 ? 4 : 2)) return CODEC_ERR_INVALID_ARGUMENT;
+    if (!q || !aligned16(q) || !out || !aligned16(out) || !workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return CODEC_ERR_INVALID_ARGUMENT;
+    if (workspace_bytes < codec_differential_workspace_bytes(plan)) return CODEC_ERR_WORKSPACE_TOO_SMALL;
+    {
+        // what is written, and what is read beside it
+        struct Range { const char *begin, *end; };
+        auto bytes_at = [](const void *p, size_t n) { return Range{static_cast<const char *>(p), static_cast<const char *>(p) + (p ? n : 0)}; };
+        const size_t rows = query_bytes(d) / 2, lambdas = 4 * (size_t(d.num_requests - 1) * size_t(c.lambda_request_stride) +
+                                                              size_t(d.head.num_q_heads / 2 - 1) * size_t(c.lambda_head_stride) + 1);
+        const Range all[] = {bytes_at(out, rows), bytes_at(workspace, codec_differential_workspace_bytes(plan)), bytes_at(q, rows),
+                             bytes_at(c.lambda, lambdas), bytes_at(c.weight, size_t(d.head.head_dim) * (c.weight_dtype == CODEC_DTYPE_FP32 ? 4 : 2))};
+        for (int i = 0; i < 2; ++i)
+            for (int j = i + 1; j < 5; ++j)
+                if (all[i].begin < all[j].end && all[j].begin < all[i].end) return CODEC_ERR_INVALID_ARGUMENT;
+    }
+    const size_t partials = align_up(codec_plan_workspace_bytes(plan), 256);
+    void *rows = static_cast<char *>(workspace) + partials;
+    // everything that codec_partial_attention refuses is refused before the first launch
+    if (int st = check_partial_attention(plan, rows, k_pages, v_pages, layout, workspace, partials)) return st;
+    if (int e = codec::launch_spread_queries(q, rows, int64_t(d.num_requests) * d.head.num_q_heads, d.head.head_dim, stream))
+        return hip_failure("query rows launch", e);
+    if (int st = codec_partial_attention(plan, rows, k_pages, v_pages, layout, workspace, partials, stream)) return st;
+
+    codec::DifferentialParams p{};
+    p.merge = merge_params(plan, workspace, out);
+    p.lambda = c.lambda;
+    p.lambda_request_stride = c.lambda_request_stride;
+    p.lambda_head_stride = c.lambda_head_stride;
+    p.weight = c.weight;
+    p.weight_dtype = c.weight_dtype;
+    p.norm = c.norm;
+    p.eps = c.eps;
+    p.gain = c.gain;
+    if (int e = codec::launch_differential(p, d.head.dtype, d.head.head_dim, stream)) return hip_failure("differential reduction launch", e);
+    return CODEC_OK;
 }
 
 size_t codec_static_scratch_bytes(void) { return codec::kStaticScratchBytes; }

@@ -1,14 +1,35 @@
 """Thin holder of a plan and the PyTorch tensors that back it (marshalling only)."""
 from __future__ import annotations
 
+import contextlib
+
 import torch
 
 from . import binding as B
+
+_current_device = getattr(torch._C, "_cuda_getDevice", None)               # absent in a PyTorch without a GPU runtime
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
 def _current_stream(device: torch.device) -> int:
     """Handle of PyTorch's current stream on `device`, without the Stream object around it."""
     return torch._C._cuda_getCurrentRawStream(device.index)
+
+
+@contextlib.contextmanager
+def _on(device: torch.device, stream):
+    """Makes `device` and `stream` the current ones; the handle of the stream.  What is allocated meanwhile belongs to the
+    stream that uses it."""
+    if stream is not None and stream.device != device:
+        raise ValueError(f"stream: on {stream.device}, the tensors are on {device}")
+    with torch.cuda.device(device), torch.cuda.stream(stream):
+        yield _current_stream(device)
+
+
+def _enter(index: int, stream):
+    """The stream's handle if a call on device `index` can go ahead as things are, else None: another device or stream has to be
+    made current."""
+    return _raw_stream(index) if stream is None and _current_device() == index else None
 
 
 class PlannedAttention:
@@ -40,6 +61,7 @@ class PlannedAttention:
         self.num_requests = len(forest.req_node)
         self.meta = None
         self.workspace = None
+        self._rows = None
         if self.device.type == "cuda":
             self.meta = torch.empty(B.codec_plan_device_bytes(plan), dtype=torch.uint8, device=self.device)
             stream = torch.cuda.current_stream(self.device).cuda_stream
@@ -83,11 +105,18 @@ class PlannedAttention:
             raise ValueError(f"{what}: {have} elements from the tensor's first one on {pool.device}, "
                              f"the page table and strides reach {last} on {self.device}")
 
+    def _check_end(self, t: torch.Tensor, what: str, last: int) -> None:
+        """The storage behind t holds its first `last` elements (it may have been given back)."""
+        if t.untyped_storage().nbytes() < (t.storage_offset() + last) * t.element_size():
+            raise ValueError(f"{what}: the tensor's storage ends before its last element")
+
     def _check_rows(self, t: torch.Tensor, what: str) -> None:
         """q and out are dense [num_requests][num_q_heads][head_dim] tensors of the plan's dtype on its device."""
         h = self.head
-        want = (self.num_requests, h.num_q_heads, h.head_dim)
-        dtype = torch.float16 if h.dtype == B.CODEC_DTYPE_FP16 else torch.bfloat16
+        self._check_dense(t, what, (self.num_requests, h.num_q_heads, h.head_dim))
+
+    def _check_dense(self, t: torch.Tensor, what: str, want) -> None:
+        dtype = torch.float16 if self.head.dtype == B.CODEC_DTYPE_FP16 else torch.bfloat16
         if t.shape != want or t.dtype != dtype or t.device != self.device or not t.is_contiguous():
             raise ValueError(f"{what}: need a contiguous {dtype} tensor of shape {want} on {self.device}, "
                              f"got {t.dtype} {tuple(t.shape)} on {t.device}, contiguous={t.is_contiguous()}")
@@ -109,6 +138,56 @@ class PlannedAttention:
                                       self.workspace.numel(), s)
         if st != B.CODEC_OK:
             raise B.CodecError(st, "codec_decode_attention")
+        return out
+
+    def decode_differential(self, q: torch.Tensor, k_pool: torch.Tensor, v_pool: torch.Tensor, lam: torch.Tensor,
+                            weight: torch.Tensor = None, eps: float = None, gain: float = 1.0, out: torch.Tensor = None,
+                            stream=None) -> torch.Tensor:
+        """Differential attention (codec_differential_attention), out = gain * norm(o_1 - lam * o_2).  The plan's heads: num_q_heads =
+        2 H for H heads of the result, head_dim = 2 d for maps of d channels, scale of the maps; a KV head of the pools holds
+        [K_1 | K_2] and V.  q [requests, 2 H, d], the two maps of a head side by side; returns [requests, H, 2 d].  ``lam``: one
+        number (no dimension), [H] or [requests, H], 32 bits, any strides.  No gradient.  ``eps``: normalised over the channels of a head,
+        times ``weight`` [2 d] (32 bits or the plan's type) if given; None: no norm."""
+        if self.device.type != "cuda":
+            raise ValueError(f"decode_differential needs a GPU, the plan is on {self.device}")
+        s = _enter(self.device.index, stream)
+        if s is None:
+            with _on(self.device, stream) as s:
+                return self._decode_differential(q, k_pool, v_pool, lam, weight, eps, gain, out, s)
+        return self._decode_differential(q, k_pool, v_pool, lam, weight, eps, gain, out, s)
+
+    def _decode_differential(self, q, k_pool, v_pool, lam, weight, eps, gain, out, s):
+        h = self.head
+        requests, heads, d = self.num_requests, h.num_q_heads // 2, h.head_dim // 2
+        self._check_pool(k_pool, "k_pool")
+        self._check_pool(v_pool, "v_pool")
+        self._check_dense(q, "q", (requests, h.num_q_heads, d))
+        if out is None:
+            out = torch.empty((requests, heads, 2 * d), dtype=q.dtype, device=self.device)
+        else:
+            self._check_dense(out, "out", (requests, heads, 2 * d))
+        if lam.shape not in ((), (heads,), (requests, heads)) or lam.dtype is not torch.float32 or lam.device != q.device:
+            raise ValueError(f"lam: need a float32 tensor of shape (), {(heads,)} or {(requests, heads)} on {q.device}, "
+                             f"got {lam.dtype} {tuple(lam.shape)} on {lam.device}")
+        of_request, of_head = (0, 0, *lam.stride())[-2:]
+        if lam.numel():
+            self._check_end(lam, "lam", sum((n - 1) * step for n, step in zip(lam.shape, lam.stride())) + 1)
+        if weight is not None:
+            if weight.shape != (2 * d,) or weight.dtype not in (torch.float32, q.dtype) or weight.device != q.device or not weight.is_contiguous():
+                raise ValueError(f"weight: need a contiguous float32 or {q.dtype} tensor of shape {(2 * d,)} on {q.device}, "
+                                 f"got {weight.dtype} {tuple(weight.shape)} on {weight.device}")
+            self._check_end(weight, "weight", 2 * d)
+        p = self.paged
+        config = B.codec_differential(lam.data_ptr(), of_request, of_head, eps is not None,
+                                      B.CODEC_DTYPE_FP32 if weight is None or weight.dtype is torch.float32 else h.dtype,
+                                      None if weight is None else weight.data_ptr(), 0.0 if eps is None else eps, gain)
+        if self._rows is None:                  # kept: never given back while a launch on some stream may use it
+            self._rows = torch.empty(B.codec_differential_workspace_bytes(self.plan), dtype=torch.uint8, device=self.device)
+        st = B.codec_differential_attention(self.plan, config, q.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(),
+                                            B.codec_kv_layout(p.num_pages, p.page_stride, p.token_stride, p.head_stride), out.data_ptr(),
+                                            self._rows.data_ptr(), self._rows.numel(), s)
+        if st != B.CODEC_OK:
+            raise B.CodecError(st, "codec_differential_attention")
         return out
 
     def partial_attention(self, q, k_pool, v_pool, stream=None) -> None:
