@@ -250,10 +250,11 @@ int check_partial_attention(const codec_plan_t *plan, const void *q, const void 
 }
 
 // Partial attention over the plan's tasks; with `fused_out` the launch also reduces (single-launch mode), or
-// has nothing to reduce (single_parts).
+// has nothing to reduce (single_parts).  With `pairs` differential attention's, whose rows go to pairs->merge.out if there is nothing
+// to reduce.
 int partial_attention(const codec_plan_t *plan, const void *q, const void *k_pages,
-                      const void *v_pages, const codec_kv_layout *layout,
-                      void *workspace, size_t workspace_bytes, void *fused_out, void *stream)
+                      const void *v_pages, const codec_kv_layout *layout, void *workspace, size_t workspace_bytes,
+                      void *fused_out, void *stream, const codec::DifferentialParams *pairs = nullptr)
 {
     if (!plan || !layout) return CODEC_ERR_INVALID_ARGUMENT;
     const codec::PlanData &d = plan->d;
@@ -294,6 +295,15 @@ int partial_attention(const codec_plan_t *plan, const void *q, const void *k_pag
     if (!d.req_mask_off.empty()) {
         pp.nodeq_mask = reinterpret_cast<const int32_t *>(meta + L.nodeq_mask);
         pp.mask_words = reinterpret_cast<const uint32_t *>(meta + L.mask_words);
+    }
+    if (pairs) {
+        codec::PairParams by{};
+        static_cast<codec::PacParams &>(by) = pp;
+        by.finish = *pairs;
+        if (plan->single_parts) by.part_o = nullptr;
+        if (int e = codec::launch_pairs(by, d.head.dtype, d.head.head_dim, L.num_slots, plan->max_task_rows, !d.packs.empty(), stream))
+            return hip_failure("partial attention launch", e);
+        return CODEC_OK;
     }
     if (fused_out) {
         pp.merge = merge_params(plan, workspace, fused_out);
@@ -366,10 +376,7 @@ int codec_decode_attention_static(const codec_plan_t *plan, const void *q, const
     return codec_decode_attention(plan, q, k_pages, v_pages, layout, out, ws, codec::kStaticScratchBytes, stream);
 }
 
-size_t codec_differential_workspace_bytes(const codec_plan_t *plan)
-{
-    return plan ? align_up(codec_plan_workspace_bytes(plan), 256) + align_up(query_bytes(plan->d), 256) : 0;
-}
+size_t codec_differential_workspace_bytes(const codec_plan_t *plan) { return codec_plan_workspace_bytes(plan); }
 
 int codec_differential_attention(const codec_plan_t *plan, const codec_differential *differential, const void *q, const void *k_pages,
                                  const void *v_pages, const codec_kv_layout *layout, void *out, void *workspace,
@@ -401,14 +408,6 @@ int codec_differential_attention(const codec_plan_t *plan, const codec_different
             for (int j = i + 1; j < 5; ++j)
                 if (all[i].begin < all[j].end && all[j].begin < all[i].end) return CODEC_ERR_INVALID_ARGUMENT;
     }
-    const size_t partials = align_up(codec_plan_workspace_bytes(plan), 256);
-    void *rows = static_cast<char *>(workspace) + partials;
-    // everything that codec_partial_attention refuses is refused before the first launch
-    if (int st = check_partial_attention(plan, rows, k_pages, v_pages, layout, workspace, partials)) return st;
-    if (int e = codec::launch_spread_queries(q, rows, int64_t(d.num_requests) * d.head.num_q_heads, d.head.head_dim, stream))
-        return hip_failure("query rows launch", e);
-    if (int st = codec_partial_attention(plan, rows, k_pages, v_pages, layout, workspace, partials, stream)) return st;
-
     codec::DifferentialParams p{};
     p.merge = merge_params(plan, workspace, out);
     p.lambda = c.lambda;
@@ -419,6 +418,8 @@ int codec_differential_attention(const codec_plan_t *plan, const codec_different
     p.norm = c.norm;
     p.eps = c.eps;
     p.gain = c.gain;
+    if (int st = partial_attention(plan, q, k_pages, v_pages, layout, workspace, workspace_bytes, nullptr, stream, &p)) return st;
+    if (plan->single_parts) return CODEC_OK;
     if (int e = codec::launch_differential(p, d.head.dtype, d.head.head_dim, stream)) return hip_failure("differential reduction launch", e);
     return CODEC_OK;
 }

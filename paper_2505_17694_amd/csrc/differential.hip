@@ -2,23 +2,395 @@
 //
 // A KV head of the pools is [K_1 | K_2], two maps' keys of d channels each, beside V of 2d.  With the query of map m in its half of
 // a row of 2d channels and zeros in the other, scale q_m K_m^T is an ordinary score of that head, exactly: what the zeros
-// multiply adds nothing.  So the attention kernels run as they are, on a plan with two query heads for every head of the result,
-// and K_1, K_2 and V are read once for both maps.  The products with zeros cost nothing where a tile holds at most sixteen rows
-// (its rows are of both maps, and the tile is as wide as it is); dense tasks do a third more matrix work than they have to.
+// multiply adds nothing.  So plans, their tasks and partial rows are the ordinary ones, with two query heads for every head of the
+// result, and K_1, K_2 and V are read once for both maps.
+//  * Tasks of at most sixteen rows run in the stream path, whose rows are gathered into their halves (gather_q).  A tile there is
+//    sixteen rows wide whatever it holds, so the zeros cost nothing.
+//  * Larger tasks run in the path below, where a wave's rows are all of one map and only that map's half of the keys is multiplied.
+//  * A reduction folds both rows of a head, subtracts and normalises; where every request has a single partial result the attention
+//    kernel does that itself (store_finished_pairs).
 #include "kernels.hpp"
 
 namespace codec {
 namespace {
 
-// Query rows [request][head][map][d] to rows of 2d channels, 16 bytes a thread.
-__global__ __launch_bounds__(256) void spread_queries_kernel(const u32x4 *q, u32x4 *rows, int64_t units, int half)
+// ---- tasks of more than sixteen rows ---------------------------------------------------------------------
+//
+// A wave owns 32 rows of one map, pairs 32 g .. 32 g + 31 of the task (pair p is the task's rows 2p and 2p + 1), and runs 32 x 32 x 16
+// tiles: d / 16 k-steps of scores S^T = K_m Q_m^T and 2 * D / 32 matrix instructions of O^T += V^T P^T in a block of 32 tokens, where
+// rows padded with zeros take 2 * d / 16 k-steps.  Blocks travel HBM -> LDS as in the tile path (TilePath, whose ring, copies and
+// swizzle of K this shares), K is read by 16 bytes a lane and V by transposing reads.
+template <int DT, int D, int GROUPS, int SHARE>
+__device__ __forceinline__ void run_pairs_of(const PairParams &P, const DevTask &t, int head, char *lds, RowStore how)
 {
-    const int64_t unit = int64_t(blockIdx.x) * 256 + threadIdx.x;
-    if (unit >= units) return;
-    const int64_t row = unit / (2 * half);
-    const int at = int(unit - row * (2 * half)), map = int(row & 1), channel = at - map * half;
-    rows[unit] = channel >= 0 && channel < half ? q[row * half + channel] : u32x4{0u, 0u, 0u, 0u};
+    using T = TilePath<D>;
+    constexpr int RB = T::kRowBytes, KS = D / 32, CT = D / 32, NB = T::kBlocks, R = T::kIntervals;
+    static_assert(2 * GROUPS * SHARE <= T::kWaves && NB % SHARE == 0 && (SHARE & (SHARE - 1)) == 0, "waves for all row groups and shares");
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = opaque_lane();
+    const int l32 = lane & 31, kg = lane >> 5, l16 = lane & 15, grp = lane >> 4;
+    const int pairs = t.n_req * P.group / 2;
+    const int unit = wave % (2 * GROUPS), phase = wave / (2 * GROUPS);
+    const int map = unit & 1, pair0 = (unit >> 1) * 32;
+    const bool live = pair0 < pairs && phase < SHARE;       // else: the wave only helps moving blocks
+    const SliceCtx c = make_ctx(P, t, head);
+    const int nblk = (t.kv_len + 31) >> 5;
+    const int nint = (nblk + NB - 1) / NB;
+
+    // Copies: see run_tile_of.  A K row keeps its 16-byte column g in slot g ^ fk(token) and a V row in slot g ^ fv(token): eight lanes of
+    // a K read, on eight tokens, then meet eight different columns of the 256 bytes of banks, and the four tokens of 64 bytes that 32
+    // lanes of a transposing V read take lie in its four quarters (64 channels: a row is half of the banks).
+    constexpr int LPR = RB / 16, TPC = 64 / LPR, MINE = T::kMine, STEP = T::kWaves / 4;
+    auto fk = [](int token) { return D == 64 ? (token >> 1) & 7 : token & 15; };
+    auto fv = [](int token) { return D == 64 ? ((token >> 1) & 1) << 2 : (token & 3) << 2; };
+    const int my_block = wave >> 2, my_token = (wave & 3) * 8;
+    const uint32_t lds_base = uint32_t(uintptr_t(lds));
+    uint32_t voff_k[T::kPieces], voff_v[T::kPieces];
+#pragma unroll
+    for (int i = 0; i < T::kPieces; ++i) {
+        const int in_copy = lane / LPR, token = my_token + i * TPC + in_copy;
+        voff_k[i] = uint32_t(i * TPC + in_copy) * c.token_bytes + uint32_t(((lane % LPR) ^ fk(token)) << 4);
+        voff_v[i] = uint32_t(i * TPC + in_copy) * c.token_bytes + uint32_t(((lane % LPR) ^ fv(token)) << 4);
+    }
+    auto first_token = [&](int i, int u) {                  // tokens past the slice's end: its first ones (masked later)
+        const int tok0 = (NB * i + my_block + u * STEP) * 32 + my_token;
+        return tok0 >= c.kv_len ? 0 : tok0;
+    };
+    auto page_issue = [&](int i, int u) { return uniform_load(c.pages, first_token(i, u) >> c.page_shift); };
+    const uint32_t my_slot = lds_base + uint32_t(my_block) * T::kBlock + uint32_t(my_token) * RB;
+    auto request = [&](int i, const int (&pg)[MINE]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < MINE; ++u) {
+            const uint32_t at = my_slot + uint32_t(i % R) * T::kInterval + uint32_t(u * STEP) * T::kBlock;
+            const int64_t off = page_offset(c, pg[u], first_token(i, u) & c.page_mask);
+#pragma unroll
+            for (int n = 0; n < T::kPieces; ++n) dma16(at + n * 1024, voff_k[n], c.k_head + off, c.read_once);
+#pragma unroll
+            for (int n = 0; n < T::kPieces; ++n) dma16(at + T::kHalf + n * 1024, voff_v[n], c.v_head + off, c.read_once);
+        }
+    };
+
+    // Operand reads, as in the dense path.  K, k-step ks: lane (l32, kg) reads 16-byte column map * D / 16 + 2 * ks + kg of token l32.  V,
+    // channel tile ct, k-step tt, h: lane (k, q) of lane group (kg, ch) addresses token 16 * tt + 8 * h + 4 * kg + k, channels
+    // 32 * ct + 16 * ch + 4 * q .. +3, and receives channel 32 * ct + l32 of tokens 16 * tt + 8 * h + 4 * kg .. +3.
+    const uint32_t k_lane = uint32_t(l32 * RB + ((kg ^ fk(l32)) << 4));
+    const int vtok = 4 * kg + (l16 >> 2), vq = l16 & 3;
+    const uint32_t v_lane = uint32_t(T::kHalf + vtok * RB + (((2 * (grp & 1) + (vq >> 1)) ^ fv(vtok)) << 4) + 8 * (vq & 1));
+    typedef const u32x4 __attribute__((address_space(3))) *lds_u32x4_ptr;
+    typedef __attribute__((ext_vector_type(4))) short s16x4;
+    typedef s16x4 __attribute__((address_space(3))) *lds_s16x4_ptr;
+
+    u32x4 qb[KS];           // row l32 (of pair pair0 + l32), channels 16 * ks + 8 * kg .. +7 of the map
+    f32x16 o[CT];           // O^T: row l32, channel 32 * ct + 8 * (r / 4) + 4 * kg + r % 4
+    float m = kNoReference, l = 0.f;
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[ct][r] = 0.f;
+
+    auto compute = [&](int b, uint32_t kb) __attribute__((always_inline)) {
+        u32x4 kr[KS], vr[CT][2];
+        const uint32_t keys = kb + (k_lane ^ uint32_t(map * (D / 16) << 4));
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) kr[ks] = *reinterpret_cast<lds_u32x4_ptr>(uintptr_t(keys ^ uint32_t(ks << 5)));
+        // V travels during the scores and their exponentials
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const uint32_t at = ((kb + v_lane) ^ uint32_t(ct << 6)) + (16 * tt + 8 * h) * RB;
+                    const uint2 w = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_s16x4_ptr>(uintptr_t(at))));
+                    vr[ct][tt][2 * h] = w.x;
+                    vr[ct][tt][2 * h + 1] = w.y;
+                }
+        __builtin_amdgcn_sched_barrier(0);
+        f32x16 s;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) s = mfma32<DT>(kr[ks], qb[ks], s);
+        const int valid = c.kv_len - b * 32;
+        if (valid < 32) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] = 8 * (r >> 2) + 4 * kg + (r & 3) >= valid ? -INFINITY : s[r];
+        }
+        float lm = s[0];
+#pragma unroll
+        for (int r = 1; r < 16; ++r) lm = fmaxf(lm, s[r]);
+        lm *= P.scale_log2e;
+        if (__any(lm > m + kLag)) {                         // see raise_reference
+            const float m_new = fmaxf(m, fmaxf(lm, __shfl_xor(lm, 32))), alpha = fast_exp2(m - m_new);
+            l *= alpha;
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o[ct][r] *= alpha;
+            m = m_new;
+        }
+        u32x4 p[2];
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt) {
+            float e[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) e[i] = fast_exp2(__builtin_fmaf(s[8 * tt + i], P.scale_log2e, -m));
+#pragma unroll
+            for (int d = 0; d < 4; ++d) {
+                p[tt][d] = pack2<DT>(e[2 * d], e[2 * d + 1]);
+                l = add_pair<DT>(p[tt][d], l);
+            }
+        }
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) o[ct] = mfma32<DT>(vr[ct][tt], p[tt], o[ct]);
+    };
+
+    // V rows of the last block past the end of the slice count as zero: each wave clears the ones that it copied
+    auto clear_tail = [&]() __attribute__((always_inline)) {
+        const int valid = c.kv_len - (nblk - 1) * 32, last = (nblk - 1) % NB;
+        if (last % STEP != my_block) return;
+        const uint32_t at = lds_base + uint32_t((nint - 1) % R) * T::kInterval + uint32_t(last) * T::kBlock + T::kHalf
+                            + uint32_t(my_token) * RB + uint32_t(lane) * 16;
+#pragma unroll
+        for (int n = 0; n < T::kPieces; ++n)
+            if (my_token + n * TPC + lane / LPR >= valid)
+                *reinterpret_cast<u32x4 __attribute__((address_space(3))) *>(uintptr_t(at + n * 1024)) = u32x4{0u, 0u, 0u, 0u};
+    };
+
+    // Start: see run_tile_of
+    int pg[R][MINE];
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+#pragma unroll
+        for (int u = 0; u < MINE; ++u) pg[i][u] = page_issue(i, u);
+    const bool row_live = pair0 + l32 < pairs;
+    {
+        const int row = row_live ? 2 * (pair0 + l32) + map : map, qi = row / P.group, hj = row - qi * P.group;
+        int req = t.single_req >= 0 ? t.single_req : P.node_q[t.q_off + qi];
+        pin(req);
+        const char *qp = static_cast<const char *>(P.q) + (int64_t(req) * P.h_q + int64_t(head) * P.group + hj) * D + kg * 16;
+        request(0, pg[0]);
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            qb[ks] = ld16(qp + ks * 32);
+            if (!row_live) qb[ks] = u32x4{0u, 0u, 0u, 0u};
+        }
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) pin(qb[ks]);
+    }
+#pragma unroll
+    for (int i = 1; i + 1 < R; ++i)
+        if (i < nint) request(i, pg[i]);
+    int pg_next[MINE];
+#pragma unroll
+    for (int u = 0; u < MINE; ++u) pg_next[u] = pg[R - 1][u];
+    auto enter_interval = [&](int i) __attribute__((always_inline)) {
+        // interval i has landed once at most the copies of the intervals requested after it are outstanding
+        if (i + R - 2 < nint) __builtin_amdgcn_s_waitcnt(vmcnt_imm((R - 2) * T::kCopies));
+        else                  __builtin_amdgcn_s_waitcnt(0x0F70);
+        if (i == nint - 1 && (c.kv_len & 31)) clear_tail();
+        __syncthreads();                    // everyone's part has landed; interval i - 1 has been read by all
+        if (i + R - 1 < nint) {
+            request(i + R - 1, pg_next);
+#pragma unroll
+            for (int u = 0; u < MINE; ++u) pg_next[u] = page_issue(i + R, u);
+        }
+    };
+    if (live) {
+#pragma unroll 1
+        for (int i = 0; i < nint; ++i) {
+            enter_interval(i);
+            const uint32_t kb = lds_base + uint32_t(i % R) * T::kInterval;
+            if constexpr (NB == 1) {
+                compute(i, kb);
+            } else {
+                const int end = nblk - NB * i < NB ? nblk - NB * i : NB;
+#pragma unroll 1
+                for (int u = phase; u < end; u += SHARE) compute(NB * i + u, kb + uint32_t(u) * T::kBlock);
+            }
+        }
+    } else {
+#pragma unroll 1
+        for (int i = 0; i < nint; ++i) enter_interval(i);
+    }
+    l += __shfl_xor(l, 32);
+    __syncthreads();                        // every block has been read: the ring is free
+
+    // the waves of a row group hand their states over pairwise: phases [h, 2h) to phases [0, h)
+    constexpr int kState = (16 * CT + 2) * 64;              // floats
+    static_assert(GROUPS * SHARE * kState * 4 <= wide_lds_bytes<D>() || SHARE == 1, "hand-over areas fit");
+    if constexpr (SHARE > 1) {
+#pragma unroll 1
+        for (int h = SHARE / 2; h >= 1; h >>= 1) {
+            float *x = reinterpret_cast<float *>(lds) + (phase % h * 2 * GROUPS + unit) * kState + lane;
+            if (phase >= h && phase < 2 * h) {
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) x[(ct * 16 + r) * 64] = o[ct][r];
+                x[16 * CT * 64] = m;
+                x[(16 * CT + 1) * 64] = l;
+            }
+            __syncthreads();
+            if (phase < h) {
+                const float m2 = x[16 * CT * 64], mm = fmaxf(m, m2), a = weight(m, mm), b = weight(m2, mm);
+                l = l * a + x[(16 * CT + 1) * 64] * b;
+                m = mm;
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) o[ct][r] = o[ct][r] * a + x[(ct * 16 + r) * 64] * b;
+            }
+            __syncthreads();
+        }
+    }
+
+    // Partial rows go out through LDS, up to 128 channels of the wave's rows at a time, so that a store instruction covers
+    // consecutive memory of a few rows (see dense32_wave).
+    if (live && phase == 0) {
+        const bool tiled = (t.flags & kTaskTiles) != 0;
+        const int tile_rows = (t.flags >> kTaskTileShift) & 255, stride = ~t.single_req;
+        const int last_tile = tiled ? (2 * pairs - 1) / tile_rows : 0, last_back = t.flags >> kTaskLastShift;
+        auto place = [&](int row) {                         // of a row of the task among the partial rows
+            if (!tiled) return int64_t(row);
+            const int tile = row / tile_rows;
+            return int64_t(tile) * stride + (row - tile * tile_rows) - (tile == last_tile ? last_back : 0);
+        };
+        float *po = P.part_o + (int64_t(head) * P.part_rows + t.part_row_base) * D;
+        float *pml = P.part_ml + (int64_t(head) * P.part_rows + t.part_row_base) * 2;
+        if (tiled && how == kRowsThrough && int64_t(last_tile + 1) * stride * (D * 4) >= int64_t(1) << 31) how = kRowsPlain;   // see run_tile_of
+        constexpr int kWidth = D < 128 ? D : 128, kPitch = kWidth * 4 + 16, kLanes = kWidth / 4, kRows = 64 / kLanes;
+        static_assert(2 * GROUPS * 32 * kPitch <= wide_lds_bytes<D>(), "staging areas fit");
+        typedef f32x4 __attribute__((address_space(3))) *lds_f32x4_ptr;
+        const uint32_t area = lds_base + uint32_t(unit) * 32 * kPitch, put = area + uint32_t(l32) * kPitch + uint32_t(kg) * 16;
+        const uint32_t get = area + uint32_t(lane / kLanes) * kPitch + uint32_t(lane % kLanes) * 16;
+        auto store = [&](auto h) __attribute__((always_inline)) {
+            constexpr RowStore HOW = decltype(h)::value;
+            if (row_live && kg == 0) st8_partial<HOW>(pml + place(2 * (pair0 + l32) + map) * 2, m, l);
+#pragma unroll
+            for (int u = 0; u < D / kWidth; ++u) {
+#pragma unroll
+                for (int ct = 0; ct < kWidth / 32; ++ct)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const f32x16 &x = o[u * (kWidth / 32) + ct];
+                        *reinterpret_cast<lds_f32x4_ptr>(uintptr_t(put + ct * 128 + q * 32)) = f32x4{x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]};
+                    }
+                __builtin_amdgcn_wave_barrier();            // LDS serves a wave's accesses in order: no wait needed
+#pragma unroll
+                for (int j = 0; j < 32 / kRows; ++j) {
+                    const int pair = pair0 + j * kRows + lane / kLanes;
+                    const f32x4 x = *reinterpret_cast<lds_f32x4_ptr>(uintptr_t(get + j * kRows * kPitch));
+                    if (pair < pairs) {
+                        const int64_t off = place(2 * pair + map) * D + u * kWidth + (lane % kLanes) * 4;
+                        if constexpr (HOW == kRowsThrough) st16_rows<HOW>(rows_at(po, -1), int(off) * 4, x);
+                        else                               st16_partial<HOW>(po + off, x);
+                    }
+                }
+                __builtin_amdgcn_wave_barrier();
+            }
+        };
+        if (how == kRowsThrough) store(std::integral_constant<RowStore, kRowsThrough>{});
+        else                     store(std::integral_constant<RowStore, kRowsPlain>{});
+    }
+    __syncthreads();                        // the staging areas are free for the next task
 }
+
+// Row groups of 32 pairs: one, two or four, times two maps, over the waves; what is left over shares blocks of an interval.
+template <int DT, int D>
+__device__ __forceinline__ void run_pairs(const PairParams &P, const DevTask &t, int head, char *lds, RowStore how)
+{
+    const int pairs = t.n_req * P.group / 2;
+    if constexpr (D == 256) {               // four waves, a block an interval
+        if (pairs <= 32) run_pairs_of<DT, D, 1, 1>(P, t, head, lds, how);
+        else             run_pairs_of<DT, D, 2, 1>(P, t, head, lds, how);
+    } else {
+        if (pairs <= 32)      run_pairs_of<DT, D, 1, D == 64 ? 4 : 2>(P, t, head, lds, how);
+        else if (pairs <= 64) run_pairs_of<DT, D, 2, 2>(P, t, head, lds, how);
+        else                  run_pairs_of<DT, D, 4, 1>(P, t, head, lds, how);
+    }
+}
+
+// The kernel of differential attention: pac_kernel's task loop (there is more about it), for two launches or finished rows.
+template <int DT, int FORM, int D>
+__global__ void __launch_bounds__(kernel_waves(FORM, D) * 64, D > 128 ? 1 : 2) pair_kernel(const PairParams P)
+{
+    constexpr bool WIDE = FORM == kFormWide, FINISH = FORM == kFormFinish;
+    constexpr int W = kernel_waves(FORM, D), kMerge = merge_bytes(W, stream_tiles(D), D);
+    char *lds;
+    if constexpr (WIDE) {
+        static_assert(kMerge + W * solo_stage_bytes(D) <= wide_lds_bytes<D>(), "staging areas fit the ring");
+        lds = dyn_lds;
+    } else {
+        __shared__ __attribute__((aligned(16))) char static_lds[kMerge + W * solo_stage_bytes(D)];
+        lds = static_lds;
+    }
+    const int head = blockIdx.x % P.h_kv, slot = blockIdx.x / P.h_kv;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    char *stage = lds + kMerge + wave * solo_stage_bytes(D);
+    const RowStore early = int64_t(P.part_rows) * P.h_kv * (D * 4) > kEarlyThroughBytes ? kRowsThrough : kRowsPlain;
+    const RowStore late = last_rows_through(P.h_kv) ? kRowsThrough : kRowsPlain;
+    auto run_tasks = [&](const DevTask *recs, int i, int end, bool marked, bool more) __attribute__((always_inline)) {
+#pragma unroll 1
+        while (i < end) {
+            const DevTask t = recs[i];
+            const int n = marked ? t.solo_run : end - i;
+            if (n >= 2) {                       // short tasks, a wave each
+                int *next = reinterpret_cast<int *>(lds);
+                if (threadIdx.x == 0) *next = W;
+                __syncthreads();
+                int k = wave;
+#pragma unroll 1
+                while (k < n) {
+                    const DevTask mine = recs[i + k];
+                    if (mine.flags & kTaskReadOnce) run_stream<DT, true, 1, 1, D, FINISH>(P, mine, head, lds, 0, stage);
+                    else                            run_stream<DT, false, 1, 1, D, FINISH>(P, mine, head, lds, 0, stage);
+                    k = 0;
+                    if ((threadIdx.x & 63) == 0) k = atomicAdd(next, 1);
+                    k = __builtin_amdgcn_readfirstlane(k);
+                }
+                __syncthreads();
+                i += n;
+                continue;
+            }
+            const int rows = t.n_req * P.group;
+            if (rows <= 16) {
+                if (t.flags & kTaskReadOnce) run_stream<DT, true, 1, W, D, FINISH>(P, t, head, lds, wave);
+                else                         run_stream<DT, false, 1, W, D, FINISH>(P, t, head, lds, wave);
+            } else if constexpr (WIDE) {
+                run_pairs<DT, D>(P, t, head, lds, i + 1 < end || more ? early : late);
+            } else if constexpr (stream_tiles(D) == 2 && !FINISH) {
+                if (t.flags & kTaskReadOnce) run_stream<DT, true, 2, W, D>(P, t, head, lds, wave);
+                else                         run_stream<DT, false, 2, W, D>(P, t, head, lds, wave);
+            }
+            ++i;
+        }
+    };
+    const bool queued = P.queue_off != nullptr, fetching = queued && P.num_entries > P.num_slots;
+    const DevTask *recs = queued ? P.queue_recs : P.slot_recs;
+    const int32_t *off = queued ? P.queue_off : P.slot_off;
+    const int limit = queued ? P.num_entries : slot + 1;
+    int32_t *taken = P.counters + 2 * head, *finished = taken + 1;
+    int *word = reinterpret_cast<int *>(lds);
+    int e = slot;
+#pragma unroll 1
+    while (e < limit) {
+        run_tasks(recs, off[e], off[e + 1], !queued, fetching);
+        if (!fetching) break;
+        if (threadIdx.x == 0) *word = P.num_slots + atomicAdd(taken, 1);
+        __syncthreads();
+        e = __builtin_amdgcn_readfirstlane(*word);
+        __syncthreads();
+    }
+    if (fetching && threadIdx.x == 0 && atomicAdd(finished, 1) == P.num_slots - 1) {
+        atomicExch(taken, 0);
+        atomicExch(finished, 0);
+    }
+}
+
+// ---- both rows of a head ----------------------------------------------------------------------------------
 
 // The two rows of a head in a wave: row `row` (the map) in 32 lanes, whose channels are 128 * (c / 4) + 4 * lane + c % 4 (64
 // channels: 2 * lane + c).
@@ -60,6 +432,53 @@ __device__ __forceinline__ float norm_weight(const DifferentialParams &P, int ch
     if (P.weight_dtype == CODEC_DTYPE_FP32) return static_cast<const float *>(P.weight)[channel];
     const uint16_t bits = static_cast<const uint16_t *>(P.weight)[channel];
     return P.weight_dtype == CODEC_DTYPE_FP16 ? float(__builtin_bit_cast(_Float16, bits)) : __uint_as_float(uint32_t(bits) << 16);
+}
+
+// The finished rows of a stream task: the rows of a head are neighbouring lanes.  Each stores half of the channels.
+template <int DT, int D>
+__device__ __forceinline__ void store_finished_pairs(const PairParams &P, const DevTask &t, int head, int rows, int l16, int grp,
+                                                     const RowState<1, D> &st)
+{
+    const DifferentialParams &F = P.finish;
+    const bool live = l16 < rows;
+    const int qi = live ? l16 / P.group : 0, hj = live ? l16 - qi * P.group : l16 & 1;
+    const int r = t.single_req >= 0 ? t.single_req : P.node_q[t.q_off + qi], h = (head * P.group + hj) >> 1;
+    const float inv = 1.f / st.l[0], lambda = F.lambda[r * F.lambda_request_stride + h * F.lambda_head_stride];
+    const bool second = hj & 1, whole = D >= 128 || grp * 32 < D;       // whole: channels that the head has
+    float x[channel_tiles(D)][4], squares = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < channel_tiles(D); ++dt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float mine = st.o[0][dt][e] * inv, other = __shfl_xor(mine, 1);
+            x[dt][e] = __builtin_fmaf(-lambda, second ? mine : other, second ? other : mine);
+            squares = __builtin_fmaf(x[dt][e], x[dt][e], squares);
+        }
+    float factor = F.gain;
+    if (F.norm) {
+        squares = whole ? squares : 0.f;
+        squares += __shfl_xor(squares, 16);
+        squares += __shfl_xor(squares, 32);
+        factor = F.gain / __builtin_sqrtf(squares * (1.f / D) + F.eps);
+    }
+    if (!live || !whole) return;
+    char *out = static_cast<char *>(F.merge.out) + ((int64_t(r) * (P.h_q / 2) + h) * D + grp * 32) * 2;
+#pragma unroll
+    for (int u = 0; u < BlockRegs<D>::VU; ++u)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            u32x4 y;
+            float w[8];
+#pragma unroll
+            for (int c = 0; c < 8; ++c) w[c] = x[8 * u + c][e] * factor;
+            if (F.weight) {
+#pragma unroll
+                for (int c = 0; c < 8; ++c) w[c] *= norm_weight(F, 128 * u + 32 * grp + 8 * e + c);
+            }
+#pragma unroll
+            for (int c = 0; c < 4; ++c) y[c] = pack2<DT>(w[2 * c], w[2 * c + 1]);
+            if (second == (e >= 2)) *reinterpret_cast<u32x4 *>(out + u * 256 + e * 16) = y;
+        }
 }
 
 // Both rows of a head, unnormalised, to its result.
@@ -173,12 +592,46 @@ int launch_differential_of(const DifferentialParams &p, hipStream_t s)
 
 }  // namespace
 
-int launch_spread_queries(const void *q, void *rows, int64_t num_rows, int head_dim, void *stream)
+// See prepare_kernels
+int prepare_pair_kernels()
 {
-    const int half = head_dim / 16;                     // 16-byte pieces of a map's row
-    const int64_t units = num_rows * 2 * half;
-    hipLaunchKernelGGL(spread_queries_kernel, dim3(unsigned((units + 255) / 256)), dim3(256), 0, static_cast<hipStream_t>(stream),
-                       static_cast<const u32x4 *>(q), static_cast<u32x4 *>(rows), units, half);
+    auto wide = [](auto dt, auto d) {
+        constexpr int D = decltype(d)::value;
+        return int(hipFuncSetAttribute(reinterpret_cast<const void *>(pair_kernel<decltype(dt)::value, kFormWide, D>),
+                                       hipFuncAttributeMaxDynamicSharedMemorySize, wide_lds_bytes<D>()));
+    };
+    int e = 0;
+    auto all = [&](auto dt) {
+        for (int one : {wide(dt, std::integral_constant<int, 64>{}), wide(dt, std::integral_constant<int, 128>{}), wide(dt, std::integral_constant<int, 256>{})})
+            e = e ? e : one;
+    };
+    all(std::integral_constant<int, CODEC_DTYPE_FP16>{});
+    all(std::integral_constant<int, CODEC_DTYPE_BF16>{});
+    return e;
+}
+
+int launch_pairs(const PairParams &p, int dtype, int head_dim, int num_slots, int max_rows_in_plan, bool tiles, void *stream)
+{
+    if (head_dim != 64 && head_dim != 128 && head_dim != 256) return int(hipErrorInvalidValue);
+    const bool wide = head_dim == kHeadDim ? max_rows_in_plan > 16 : tiles;         // see launch_pac
+    if (!wide && max_rows_in_plan > 16 * stream_tiles(head_dim)) return int(hipErrorInvalidValue);
+    if (!p.part_o && (wide || max_rows_in_plan > 16)) return int(hipErrorInvalidValue);
+    const dim3 grid(unsigned(num_slots) * unsigned(p.h_kv));
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    auto launch = [&](auto dt, auto d) {
+        constexpr int DT = decltype(dt)::value, D = decltype(d)::value;
+        const dim3 block((wide ? kernel_waves(kFormWide, D) : kNarrowWaves) * 64);
+        if (!p.part_o) hipLaunchKernelGGL((pair_kernel<DT, kFormFinish, D>), grid, block, 0, s, p);
+        else if (wide) hipLaunchKernelGGL((pair_kernel<DT, kFormWide, D>), grid, block, wide_lds_bytes<D>(), s, p);
+        else           hipLaunchKernelGGL((pair_kernel<DT, kFormNarrow, D>), grid, block, 0, s, p);
+    };
+    auto launch_dim = [&](auto dt) {
+        if (head_dim == 64)       launch(dt, std::integral_constant<int, 64>{});
+        else if (head_dim == 128) launch(dt, std::integral_constant<int, 128>{});
+        else                      launch(dt, std::integral_constant<int, 256>{});
+    };
+    if (dtype == CODEC_DTYPE_FP16) launch_dim(std::integral_constant<int, CODEC_DTYPE_FP16>{});
+    else                           launch_dim(std::integral_constant<int, CODEC_DTYPE_BF16>{});
     return int(hipGetLastError());
 }
 

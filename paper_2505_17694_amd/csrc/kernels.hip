@@ -493,8 +493,12 @@ __device__ __forceinline__ void accumulate(const u32x4 (&v)[8][BlockRegs<D>::VU]
 }
 
 // Gather the wave's query rows (task rows row0 .. row0 + 16*NT) into B-operand registers.
-template <int NT, int D>
-__device__ __forceinline__ void gather_q(const PacParams &P, const DevTask &t, int head, int row0, int rows,
+// Of differential attention (PairParams) a row is one map's query, of half the channels, in its half of the row: see differential.hip.
+template <class Params>
+constexpr bool kPairs = std::is_same_v<Params, PairParams>;
+
+template <int NT, int D, class Params>
+__device__ __forceinline__ void gather_q(const Params &P, const DevTask &t, int head, int row0, int rows,
                                          int l16, int grp, u32x4 (&qb)[NT][D / 32])
 {
 #pragma unroll
@@ -504,10 +508,18 @@ __device__ __forceinline__ void gather_q(const PacParams &P, const DevTask &t, i
         const int qi = live ? row / P.group : 0;
         const int hj = live ? row - qi * P.group : 0;
         const int req = t.single_req >= 0 ? t.single_req : P.node_q[t.q_off + qi];
+        constexpr int kRow = kPairs<Params> ? D : D * 2;        // bytes
         const char *qp = static_cast<const char *>(P.q)
-                         + (int64_t(req) * P.h_q + int64_t(head) * P.group + hj) * (D * 2) + grp * 16;
+                         + (int64_t(req) * P.h_q + int64_t(head) * P.group + hj) * kRow + grp * 16;
 #pragma unroll
-        for (int ks = 0; ks < D / 32; ++ks) qb[nt][ks] = live ? ld16(qp + ks * 64) : u32x4{0u, 0u, 0u, 0u};
+        for (int ks = 0; ks < D / 32; ++ks) {
+            if constexpr (kPairs<Params>) {
+                constexpr int kHalf = D / 64;                   // k-steps of a map
+                qb[nt][ks] = live && ks / kHalf == (hj & 1) ? ld16(qp + (ks % kHalf) * 64) : u32x4{0u, 0u, 0u, 0u};
+            } else {
+                qb[nt][ks] = live ? ld16(qp + ks * 64) : u32x4{0u, 0u, 0u, 0u};
+            }
+        }
     }
 }
 
@@ -602,6 +614,11 @@ __device__ __forceinline__ void store_finished(const PacParams &P, const DevTask
         }
 }
 
+// The same of differential attention (differential.hip).
+template <int DT, int D>
+__device__ __forceinline__ void store_finished_pairs(const PairParams &P, const DevTask &t, int head, int rows, int l16, int grp,
+                                                     const RowState<1, D> &st);
+
 __device__ __forceinline__ SliceCtx make_ctx(const PacParams &P, const DevTask &t, int head)
 {
     SliceCtx c;
@@ -625,8 +642,8 @@ __device__ __forceinline__ float weight(float a, float m) { return a == m ? 1.f 
 // `wave` is the wave's index in its team.  A team of one wave (W = 1) uses no LDS and no barrier, so
 // several such waves may work on different tasks at the same time.
 // FINISH: the task's rows go out finished (store_finished).
-template <int DT, bool ONCE, int NT, int W, int D, bool FINISH = false>
-__device__ __forceinline__ void run_stream(const PacParams &P, const DevTask &t, int head, char *lds_raw, int wave,
+template <int DT, bool ONCE, int NT, int W, int D, bool FINISH = false, class Params>
+__device__ __forceinline__ void run_stream(const Params &P, const DevTask &t, int head, char *lds_raw, int wave,
                                            char *stage = nullptr)   // W = 1, up to 128 channels: the wave's staging area
 {
     constexpr int KS = D / 32, CT = channel_tiles(D);
@@ -733,7 +750,9 @@ __device__ __forceinline__ void run_stream(const PacParams &P, const DevTask &t,
         }
         __syncthreads();
     }
-    if constexpr (FINISH) {
+    if constexpr (FINISH && kPairs<Params>) {
+        if (wave == 0) store_finished_pairs<DT, D>(P, t, head, rows, l16, grp, st);
+    } else if constexpr (FINISH) {
         if (wave == 0) store_finished<DT, D>(P, t, head, rows, l16, grp, st);
     } else if constexpr (W == 1 && NT == 1 && D <= 128) {
         if (P.arrive) store_partial_staged<kRowsCoherent, D>(P, t, head, rows, lane, st, stage);
@@ -1345,7 +1364,7 @@ struct TilePath {
     static constexpr int kRowBytes = D * 2;
     static constexpr int kHalf = 32 * kRowBytes;            // K (or V) of a block
     static constexpr int kBlock = 2 * kHalf;
-    static constexpr int kBlocks = D == 64 ? 4 : 1;         // blocks of an interval
+    static constexpr int kBlocks = 256 / D;                 // blocks of an interval (128 channels: differential attention only)
     static constexpr int kInterval = kBlocks * kBlock;
     static constexpr int kMine = kBlocks * 4 / kWaves;      // blocks of an interval of which a wave copies eight tokens
     static constexpr int kIntervals = 131072 / kInterval;   // slots of the ring
@@ -2360,6 +2379,7 @@ int prepare_kernels()
     };
     for (const auto &k : kernels)
         if (hipError_t e = hipFuncSetAttribute(k.kernel, hipFuncAttributeMaxDynamicSharedMemorySize, k.bytes)) return int(e);
+    if (int e = prepare_pair_kernels()) return e;
     done[dev] = true;
     return 0;
 }

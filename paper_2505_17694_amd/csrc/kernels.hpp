@@ -20,16 +20,6 @@ struct MergeParams {
     int32_t split_waves;            // 4 or 8 waves share a list; less: one wave folds it, and there is no req_line (split_waves())
 };
 
-// The reduction of differential attention: merge.h_q query heads are two rows for each head of the result.
-struct DifferentialParams {
-    MergeParams merge;
-    const float *lambda;            // of request r and head h at r * lambda_request_stride + h * lambda_head_stride
-    int64_t lambda_request_stride, lambda_head_stride;
-    const void *weight;             // [head_dim] or nullptr
-    int32_t weight_dtype, norm;
-    float eps, gain;
-};
-
 struct PacParams {
     const void *q;                  // [B][h_q][head_dim], 16-bit
     const void *k_pages;
@@ -65,6 +55,20 @@ struct PacParams {
     const uint32_t *mask_words;
 };
 
+// The reduction of differential attention: merge.h_q query heads are two rows for each head of the result.
+struct DifferentialParams {
+    MergeParams merge;
+    const float *lambda;            // of request r and head h at r * lambda_request_stride + h * lambda_head_stride
+    int64_t lambda_request_stride, lambda_head_stride;
+    const void *weight;             // [head_dim] or nullptr
+    int32_t weight_dtype, norm;
+    float eps, gain;
+};
+
+// Partial attention of differential attention: q is [B][h_q][head_dim / 2].
+struct PairParams : PacParams {
+    DifferentialParams finish;      // what becomes of finished rows (part_o == nullptr)
+};
 
 // Size of the library's own scratch array (one per GPU) behind codec_decode_attention_static.
 constexpr size_t kStaticScratchBytes = size_t(64) << 20;
@@ -87,8 +91,9 @@ int launch_stream_read(const void *buf, uint64_t chunks, uint64_t mult, int once
 // round the KV heads (heads_in_turn; two launches only).
 int launch_pac(const PacParams &p, int dtype, int head_dim, int num_slots, int max_rows_in_plan, bool tiles, bool turns, void *stream);
 int launch_merge(const MergeParams &p, int dtype, int head_dim, void *stream);
-// Query rows of head_dim / 2 channels, of two maps in turn, into their halves of rows of head_dim channels.
-int launch_spread_queries(const void *q, void *rows, int64_t num_rows, int head_dim, void *stream);
+// The same for differential attention; finished rows (part_o == nullptr) go to p.finish.merge.out.
+int launch_pairs(const PairParams &p, int dtype, int head_dim, int num_slots, int max_rows_in_plan, bool tiles, void *stream);
+int prepare_pair_kernels();         // called by prepare_kernels
 int launch_differential(const DifferentialParams &p, int dtype, int head_dim, void *stream);
 
 }  // namespace codec
