@@ -18,29 +18,49 @@ namespace {
 //
 // A wave owns 32 rows of one map, pairs 32 g .. 32 g + 31 of the task (pair p is the task's rows 2p and 2p + 1), and runs 32 x 32 x 16
 // tiles: d / 16 k-steps of scores S^T = K_m Q_m^T and 2 * D / 32 matrix instructions of O^T += V^T P^T in a block of 32 tokens, where
-// rows padded with zeros take 2 * d / 16 k-steps.  Blocks travel HBM -> LDS as in the tile path (TilePath, whose ring, copies and
-// swizzle of K this shares), K is read by 16 bytes a lane and V by transposing reads.
-template <int DT, int D, int GROUPS, int SHARE>
+// rows padded with zeros take 2 * d / 16 k-steps.  Blocks are copied HBM -> LDS asynchronously into a ring of all of the CU's LDS, K is
+// read by 16 bytes a lane and V by transposing reads (swizzles below).
+//
+// A step is NB blocks between two barriers, the row groups' waves taking turns with them (SHARE); S slots hold blocks, so that
+// S - NB of them are on their way when a step starts.  With 256 channels a SIMD has one wave: in a block its reads of K travel beside
+// the accumulation of the block before, its reads of V beside the exponentials.
+template <int D, int GROUPS>
+struct PairPath {
+    static constexpr int kWaves = kernel_waves(kFormWide, D), kUnits = 2 * GROUPS;
+    static constexpr int kRowBytes = D * 2, kHalf = 32 * kRowBytes, kBlock = 2 * kHalf;      // K (or V) of a block; both
+    static constexpr int kLds = 163840, kSlots = kLds / kBlock;                                 // 20, 10, 5
+    // 256 channels: 32 pairs are two units for four waves; more are four
+    static constexpr int kBlocks = D == 256 ? (GROUPS == 1 ? 2 : 1) : 256 / D;
+    static constexpr int kShare = kWaves / kUnits < kBlocks ? kWaves / kUnits : kBlocks;
+    static constexpr int kMine = kBlocks * 4 / kWaves;      // blocks of a step of which a wave copies eight tokens
+    static constexpr int kStride = kWaves / 4;              // from one of them to the next
+    static constexpr int kPieces = 8 * kRowBytes / 1024;    // 1 KB copies of eight tokens of one pool
+    static constexpr int kCopies = kMine * 2 * kPieces;     // copies of a wave in a step
+    static constexpr int kAhead = kSlots - kBlocks;         // blocks requested when a step starts
+    static constexpr int kOutstanding = (kSlots - 2 * kBlocks) * kCopies / kBlocks;         // copies that a step need not wait for
+    static_assert(kUnits * kShare <= kWaves && kBlocks % kShare == 0 && kOutstanding < 64, "waves for all row groups and shares");
+    static_assert(kAhead % kBlocks == 0 || kStride == 1, "a step's copies are requested together");
+};
+
+template <int DT, int D, int GROUPS>
 __device__ __forceinline__ void run_pairs_of(const PairParams &P, const DevTask &t, int head, char *lds, RowStore how)
 {
-    using T = TilePath<D>;
-    constexpr int RB = T::kRowBytes, KS = D / 32, CT = D / 32, NB = T::kBlocks, R = T::kIntervals;
-    static_assert(2 * GROUPS * SHARE <= T::kWaves && NB % SHARE == 0 && (SHARE & (SHARE - 1)) == 0, "waves for all row groups and shares");
+    using T = PairPath<D, GROUPS>;
+    constexpr int RB = T::kRowBytes, KS = D / 32, CT = D / 32, NB = T::kBlocks, S = T::kSlots, SHARE = T::kShare;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lane = opaque_lane();
     const int l32 = lane & 31, kg = lane >> 5, l16 = lane & 15, grp = lane >> 4;
     const int pairs = t.n_req * P.group / 2;
-    const int unit = wave % (2 * GROUPS), phase = wave / (2 * GROUPS);
+    const int unit = wave % T::kUnits, phase = wave / T::kUnits;
     const int map = unit & 1, pair0 = (unit >> 1) * 32;
     const bool live = pair0 < pairs && phase < SHARE;       // else: the wave only helps moving blocks
     const SliceCtx c = make_ctx(P, t, head);
-    const int nblk = (t.kv_len + 31) >> 5;
-    const int nint = (nblk + NB - 1) / NB;
+    const int nblk = (t.kv_len + 31) >> 5, nstep = (nblk + NB - 1) / NB;
 
-    // Copies: see run_tile_of.  A K row keeps its 16-byte column g in slot g ^ fk(token) and a V row in slot g ^ fv(token): eight lanes of
+    // Copies, TPC tokens each.  A K row keeps its 16-byte column g in slot g ^ fk(token) and a V row in slot g ^ fv(token): eight lanes of
     // a K read, on eight tokens, then meet eight different columns of the 256 bytes of banks, and the four tokens of 64 bytes that 32
     // lanes of a transposing V read take lie in its four quarters (64 channels: a row is half of the banks).
-    constexpr int LPR = RB / 16, TPC = 64 / LPR, MINE = T::kMine, STEP = T::kWaves / 4;
+    constexpr int LPR = RB / 16, TPC = 64 / LPR, MINE = T::kMine;
     auto fk = [](int token) { return D == 64 ? (token >> 1) & 7 : token & 15; };
     auto fv = [](int token) { return D == 64 ? ((token >> 1) & 1) << 2 : (token & 3) << 2; };
     const int my_block = wave >> 2, my_token = (wave & 3) * 8;
@@ -52,28 +72,28 @@ __device__ __forceinline__ void run_pairs_of(const PairParams &P, const DevTask 
         voff_k[i] = uint32_t(i * TPC + in_copy) * c.token_bytes + uint32_t(((lane % LPR) ^ fk(token)) << 4);
         voff_v[i] = uint32_t(i * TPC + in_copy) * c.token_bytes + uint32_t(((lane % LPR) ^ fv(token)) << 4);
     }
-    auto first_token = [&](int i, int u) {                  // tokens past the slice's end: its first ones (masked later)
-        const int tok0 = (NB * i + my_block + u * STEP) * 32 + my_token;
+    // eight tokens past the end of the slice are redirected to its first ones (masked later): no address leaves the slice's
+    // pages, and every step has the same number of copies
+    auto first_token = [&](int block) {
+        const int tok0 = block * 32 + my_token;
         return tok0 >= c.kv_len ? 0 : tok0;
     };
-    auto page_issue = [&](int i, int u) { return uniform_load(c.pages, first_token(i, u) >> c.page_shift); };
-    const uint32_t my_slot = lds_base + uint32_t(my_block) * T::kBlock + uint32_t(my_token) * RB;
-    auto request = [&](int i, const int (&pg)[MINE]) __attribute__((always_inline)) {
+    auto block_of = [&](int first, int u) { return first + my_block + u * T::kStride; };     // that the wave copies, of NB from `first` on
+    auto page_issue = [&](int block) { return uniform_load(c.pages, first_token(block) >> c.page_shift); };
+    auto slot_of = [&](int block) { return lds_base + uint32_t(block % S) * T::kBlock; };
+    auto request = [&](int block, int pg) __attribute__((always_inline)) {          // pg: page_issue(block)
+        const uint32_t at = slot_of(block) + uint32_t(my_token) * RB;
+        const int64_t off = page_offset(c, pg, first_token(block) & c.page_mask);
 #pragma unroll
-        for (int u = 0; u < MINE; ++u) {
-            const uint32_t at = my_slot + uint32_t(i % R) * T::kInterval + uint32_t(u * STEP) * T::kBlock;
-            const int64_t off = page_offset(c, pg[u], first_token(i, u) & c.page_mask);
+        for (int n = 0; n < T::kPieces; ++n) dma16(at + n * 1024, voff_k[n], c.k_head + off, c.read_once);
 #pragma unroll
-            for (int n = 0; n < T::kPieces; ++n) dma16(at + n * 1024, voff_k[n], c.k_head + off, c.read_once);
-#pragma unroll
-            for (int n = 0; n < T::kPieces; ++n) dma16(at + T::kHalf + n * 1024, voff_v[n], c.v_head + off, c.read_once);
-        }
+        for (int n = 0; n < T::kPieces; ++n) dma16(at + T::kHalf + n * 1024, voff_v[n], c.v_head + off, c.read_once);
     };
 
     // Operand reads, as in the dense path.  K, k-step ks: lane (l32, kg) reads 16-byte column map * D / 16 + 2 * ks + kg of token l32.  V,
     // channel tile ct, k-step tt, h: lane (k, q) of lane group (kg, ch) addresses token 16 * tt + 8 * h + 4 * kg + k, channels
     // 32 * ct + 16 * ch + 4 * q .. +3, and receives channel 32 * ct + l32 of tokens 16 * tt + 8 * h + 4 * kg .. +3.
-    const uint32_t k_lane = uint32_t(l32 * RB + ((kg ^ fk(l32)) << 4));
+    const uint32_t k_lane = uint32_t(l32 * RB + ((kg ^ fk(l32)) << 4)) ^ uint32_t(map * (D / 16) << 4);
     const int vtok = 4 * kg + (l16 >> 2), vq = l16 & 3;
     const uint32_t v_lane = uint32_t(T::kHalf + vtok * RB + (((2 * (grp & 1) + (vq >> 1)) ^ fv(vtok)) << 4) + 8 * (vq & 1));
     typedef const u32x4 __attribute__((address_space(3))) *lds_u32x4_ptr;
@@ -82,36 +102,46 @@ __device__ __forceinline__ void run_pairs_of(const PairParams &P, const DevTask 
 
     u32x4 qb[KS];           // row l32 (of pair pair0 + l32), channels 16 * ks + 8 * kg .. +7 of the map
     f32x16 o[CT];           // O^T: row l32, channel 32 * ct + 8 * (r / 4) + 4 * kg + r % 4
+    u32x4 kr[KS], vr[CT][2], p[2];
     float m = kNoReference, l = 0.f;
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[ct][r] = 0.f;
 
-    auto compute = [&](int b, uint32_t kb) __attribute__((always_inline)) {
-        u32x4 kr[KS], vr[CT][2];
-        const uint32_t keys = kb + (k_lane ^ uint32_t(map * (D / 16) << 4));
+    auto accumulate = [&]() __attribute__((always_inline)) {        // the block whose V and P are in registers
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) kr[ks] = *reinterpret_cast<lds_u32x4_ptr>(uintptr_t(keys ^ uint32_t(ks << 5)));
-        // V travels during the scores and their exponentials
+        for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) o[ct] = mfma32<DT>(vr[ct][tt], p[tt], o[ct]);
+    };
+    bool begun = false;
+    auto compute = [&](int block) __attribute__((always_inline)) {
+        const uint32_t at = slot_of(block);
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) kr[ks] = *reinterpret_cast<lds_u32x4_ptr>(uintptr_t((at + k_lane) ^ uint32_t(ks << 5)));
+        __builtin_amdgcn_sched_barrier(0);
+        if (begun) accumulate();
+        begun = true;
+        f32x16 s;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) s = mfma32<DT>(kr[ks], qb[ks], s);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const uint32_t at = ((kb + v_lane) ^ uint32_t(ct << 6)) + (16 * tt + 8 * h) * RB;
-                    const uint2 w = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_s16x4_ptr>(uintptr_t(at))));
+                    const uint32_t from = ((at + v_lane) ^ uint32_t(ct << 6)) + (16 * tt + 8 * h) * RB;
+                    const uint2 w = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_s16x4_ptr>(uintptr_t(from))));
                     vr[ct][tt][2 * h] = w.x;
                     vr[ct][tt][2 * h + 1] = w.y;
                 }
         __builtin_amdgcn_sched_barrier(0);
-        f32x16 s;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] = 0.f;
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) s = mfma32<DT>(kr[ks], qb[ks], s);
-        const int valid = c.kv_len - b * 32;
+        const int valid = c.kv_len - block * 32;
         if (valid < 32) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[r] = 8 * (r >> 2) + 4 * kg + (r & 3) >= valid ? -INFINITY : s[r];
@@ -129,7 +159,6 @@ __device__ __forceinline__ void run_pairs_of(const PairParams &P, const DevTask 
                 for (int r = 0; r < 16; ++r) o[ct][r] *= alpha;
             m = m_new;
         }
-        u32x4 p[2];
 #pragma unroll
         for (int tt = 0; tt < 2; ++tt) {
             float e[8];
@@ -141,37 +170,37 @@ __device__ __forceinline__ void run_pairs_of(const PairParams &P, const DevTask 
                 l = add_pair<DT>(p[tt][d], l);
             }
         }
-#pragma unroll
-        for (int tt = 0; tt < 2; ++tt)
-#pragma unroll
-            for (int ct = 0; ct < CT; ++ct) o[ct] = mfma32<DT>(vr[ct][tt], p[tt], o[ct]);
     };
 
     // V rows of the last block past the end of the slice count as zero: each wave clears the ones that it copied
     auto clear_tail = [&]() __attribute__((always_inline)) {
-        const int valid = c.kv_len - (nblk - 1) * 32, last = (nblk - 1) % NB;
-        if (last % STEP != my_block) return;
-        const uint32_t at = lds_base + uint32_t((nint - 1) % R) * T::kInterval + uint32_t(last) * T::kBlock + T::kHalf
-                            + uint32_t(my_token) * RB + uint32_t(lane) * 16;
+        const int valid = c.kv_len - (nblk - 1) * 32;
+        if ((nblk - 1) % T::kStride != my_block) return;
+        const uint32_t at = slot_of(nblk - 1) + T::kHalf + uint32_t(my_token) * RB + uint32_t(lane) * 16;
 #pragma unroll
         for (int n = 0; n < T::kPieces; ++n)
             if (my_token + n * TPC + lane / LPR >= valid)
                 *reinterpret_cast<u32x4 __attribute__((address_space(3))) *>(uintptr_t(at + n * 1024)) = u32x4{0u, 0u, 0u, 0u};
     };
 
-    // Start: see run_tile_of
-    int pg[R][MINE];
+    // Start: the rows' requests and the page ids, read together; then the first step's copies and the query rows.  Waiting for the
+    // rows (the compiler waits for every load in flight) waits for that step too, so the others are requested behind it.
+    constexpr int kRounds = (T::kAhead + NB - 1) / NB;      // of requests ahead of the first step
+    int pg[kRounds + 1][MINE];
 #pragma unroll
-    for (int i = 0; i < R; ++i)
+    for (int i = 0; i < kRounds; ++i)
 #pragma unroll
-        for (int u = 0; u < MINE; ++u) pg[i][u] = page_issue(i, u);
+        for (int u = 0; u < MINE; ++u) pg[i][u] = page_issue(block_of(i * NB, u));
+#pragma unroll
+    for (int u = 0; u < MINE; ++u) pg[kRounds][u] = page_issue(block_of(T::kAhead, u));
     const bool row_live = pair0 + l32 < pairs;
     {
         const int row = row_live ? 2 * (pair0 + l32) + map : map, qi = row / P.group, hj = row - qi * P.group;
         int req = t.single_req >= 0 ? t.single_req : P.node_q[t.q_off + qi];
         pin(req);
         const char *qp = static_cast<const char *>(P.q) + (int64_t(req) * P.h_q + int64_t(head) * P.group + hj) * D + kg * 16;
-        request(0, pg[0]);
+#pragma unroll
+        for (int u = 0; u < MINE; ++u) request(block_of(0, u), pg[0][u]);
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
             qb[ks] = ld16(qp + ks * 32);
@@ -181,46 +210,53 @@ __device__ __forceinline__ void run_pairs_of(const PairParams &P, const DevTask 
         for (int ks = 0; ks < KS; ++ks) pin(qb[ks]);
     }
 #pragma unroll
-    for (int i = 1; i + 1 < R; ++i)
-        if (i < nint) request(i, pg[i]);
+    for (int i = 1; i < kRounds; ++i)
+        if (i * NB < nblk) {
+#pragma unroll
+            for (int u = 0; u < MINE; ++u)
+                if (i * NB + u * T::kStride < T::kAhead) request(block_of(i * NB, u), pg[i][u]);
+        }
     int pg_next[MINE];
 #pragma unroll
-    for (int u = 0; u < MINE; ++u) pg_next[u] = pg[R - 1][u];
-    auto enter_interval = [&](int i) __attribute__((always_inline)) {
-        // interval i has landed once at most the copies of the intervals requested after it are outstanding
-        if (i + R - 2 < nint) __builtin_amdgcn_s_waitcnt(vmcnt_imm((R - 2) * T::kCopies));
-        else                  __builtin_amdgcn_s_waitcnt(0x0F70);
-        if (i == nint - 1 && (c.kv_len & 31)) clear_tail();
-        __syncthreads();                    // everyone's part has landed; interval i - 1 has been read by all
-        if (i + R - 1 < nint) {
-            request(i + R - 1, pg_next);
+    for (int u = 0; u < MINE; ++u) pg_next[u] = pg[kRounds][u];
+    auto enter_step = [&](int j) __attribute__((always_inline)) {
+        // the blocks of step j have landed once at most the copies requested after them are outstanding
+        if (NB * j + T::kAhead <= nblk) __builtin_amdgcn_s_waitcnt(vmcnt_imm(T::kOutstanding));
+        else                            __builtin_amdgcn_s_waitcnt(0x0F70);
+        if (j == nstep - 1 && (c.kv_len & 31)) clear_tail();
+        __builtin_amdgcn_s_waitcnt(0xC07F);     // V of the step before is in registers
+        __syncthreads();                        // everyone's part has landed; step j - 1 has been read by all
+        const int next = NB * j + T::kAhead;
+        if (next < nblk) {
 #pragma unroll
-            for (int u = 0; u < MINE; ++u) pg_next[u] = page_issue(i + R, u);
+            for (int u = 0; u < MINE; ++u) request(block_of(next, u), pg_next[u]);
+#pragma unroll
+            for (int u = 0; u < MINE; ++u) pg_next[u] = page_issue(block_of(next + NB, u));
         }
     };
     if (live) {
 #pragma unroll 1
-        for (int i = 0; i < nint; ++i) {
-            enter_interval(i);
-            const uint32_t kb = lds_base + uint32_t(i % R) * T::kInterval;
-            if constexpr (NB == 1) {
-                compute(i, kb);
+        for (int j = 0; j < nstep; ++j) {
+            enter_step(j);
+            if constexpr (NB == SHARE) {
+                if (NB * j + phase < nblk) compute(NB * j + phase);
             } else {
-                const int end = nblk - NB * i < NB ? nblk - NB * i : NB;
+                const int end = nblk - NB * j < NB ? nblk - NB * j : NB;
 #pragma unroll 1
-                for (int u = phase; u < end; u += SHARE) compute(NB * i + u, kb + uint32_t(u) * T::kBlock);
+                for (int u = phase; u < end; u += SHARE) compute(NB * j + u);
             }
         }
+        if (begun) accumulate();
     } else {
 #pragma unroll 1
-        for (int i = 0; i < nint; ++i) enter_interval(i);
+        for (int j = 0; j < nstep; ++j) enter_step(j);
     }
     l += __shfl_xor(l, 32);
     __syncthreads();                        // every block has been read: the ring is free
 
     // the waves of a row group hand their states over pairwise: phases [h, 2h) to phases [0, h)
     constexpr int kState = (16 * CT + 2) * 64;              // floats
-    static_assert(GROUPS * SHARE * kState * 4 <= wide_lds_bytes<D>() || SHARE == 1, "hand-over areas fit");
+    static_assert(GROUPS * SHARE * kState * 4 <= T::kLds || SHARE == 1, "hand-over areas fit");
     if constexpr (SHARE > 1) {
 #pragma unroll 1
         for (int h = SHARE / 2; h >= 1; h >>= 1) {
@@ -262,7 +298,7 @@ __device__ __forceinline__ void run_pairs_of(const PairParams &P, const DevTask 
         float *pml = P.part_ml + (int64_t(head) * P.part_rows + t.part_row_base) * 2;
         if (tiled && how == kRowsThrough && int64_t(last_tile + 1) * stride * (D * 4) >= int64_t(1) << 31) how = kRowsPlain;   // see run_tile_of
         constexpr int kWidth = D < 128 ? D : 128, kPitch = kWidth * 4 + 16, kLanes = kWidth / 4, kRows = 64 / kLanes;
-        static_assert(2 * GROUPS * 32 * kPitch <= wide_lds_bytes<D>(), "staging areas fit");
+        static_assert(2 * GROUPS * 32 * kPitch <= T::kLds, "staging areas fit");
         typedef f32x4 __attribute__((address_space(3))) *lds_f32x4_ptr;
         const uint32_t area = lds_base + uint32_t(unit) * 32 * kPitch, put = area + uint32_t(l32) * kPitch + uint32_t(kg) * 16;
         const uint32_t get = area + uint32_t(lane / kLanes) * kPitch + uint32_t(lane % kLanes) * 16;
@@ -298,19 +334,14 @@ __device__ __forceinline__ void run_pairs_of(const PairParams &P, const DevTask 
     __syncthreads();                        // the staging areas are free for the next task
 }
 
-// Row groups of 32 pairs: one, two or four, times two maps, over the waves; what is left over shares blocks of an interval.
+// Row groups of 32 pairs: one, two or four, times two maps, over the waves.
 template <int DT, int D>
 __device__ __forceinline__ void run_pairs(const PairParams &P, const DevTask &t, int head, char *lds, RowStore how)
 {
     const int pairs = t.n_req * P.group / 2;
-    if constexpr (D == 256) {               // four waves, a block an interval
-        if (pairs <= 32) run_pairs_of<DT, D, 1, 1>(P, t, head, lds, how);
-        else             run_pairs_of<DT, D, 2, 1>(P, t, head, lds, how);
-    } else {
-        if (pairs <= 32)      run_pairs_of<DT, D, 1, D == 64 ? 4 : 2>(P, t, head, lds, how);
-        else if (pairs <= 64) run_pairs_of<DT, D, 2, 2>(P, t, head, lds, how);
-        else                  run_pairs_of<DT, D, 4, 1>(P, t, head, lds, how);
-    }
+    if (pairs <= 32)                    run_pairs_of<DT, D, 1>(P, t, head, lds, how);
+    else if (D == 256 || pairs <= 64)   run_pairs_of<DT, D, 2>(P, t, head, lds, how);
+    else if constexpr (D != 256)        run_pairs_of<DT, D, 4>(P, t, head, lds, how);
 }
 
 // The kernel of differential attention: pac_kernel's task loop (there is more about it), for two launches or finished rows.
@@ -321,7 +352,7 @@ __global__ void __launch_bounds__(kernel_waves(FORM, D) * 64, D > 128 ? 1 : 2) p
     constexpr int W = kernel_waves(FORM, D), kMerge = merge_bytes(W, stream_tiles(D), D);
     char *lds;
     if constexpr (WIDE) {
-        static_assert(kMerge + W * solo_stage_bytes(D) <= wide_lds_bytes<D>(), "staging areas fit the ring");
+        static_assert(kMerge + W * solo_stage_bytes(D) <= PairPath<D, 1>::kLds, "staging areas fit the ring");
         lds = dyn_lds;
     } else {
         __shared__ __attribute__((aligned(16))) char static_lds[kMerge + W * solo_stage_bytes(D)];
@@ -598,7 +629,7 @@ int prepare_pair_kernels()
     auto wide = [](auto dt, auto d) {
         constexpr int D = decltype(d)::value;
         return int(hipFuncSetAttribute(reinterpret_cast<const void *>(pair_kernel<decltype(dt)::value, kFormWide, D>),
-                                       hipFuncAttributeMaxDynamicSharedMemorySize, wide_lds_bytes<D>()));
+                                       hipFuncAttributeMaxDynamicSharedMemorySize, PairPath<D, 1>::kLds));
     };
     int e = 0;
     auto all = [&](auto dt) {
@@ -622,7 +653,7 @@ int launch_pairs(const PairParams &p, int dtype, int head_dim, int num_slots, in
         constexpr int DT = decltype(dt)::value, D = decltype(d)::value;
         const dim3 block((wide ? kernel_waves(kFormWide, D) : kNarrowWaves) * 64);
         if (!p.part_o) hipLaunchKernelGGL((pair_kernel<DT, kFormFinish, D>), grid, block, 0, s, p);
-        else if (wide) hipLaunchKernelGGL((pair_kernel<DT, kFormWide, D>), grid, block, wide_lds_bytes<D>(), s, p);
+        else if (wide) hipLaunchKernelGGL((pair_kernel<DT, kFormWide, D>), grid, block, (PairPath<D, 1>::kLds), s, p);
         else           hipLaunchKernelGGL((pair_kernel<DT, kFormNarrow, D>), grid, block, 0, s, p);
     };
     auto launch_dim = [&](auto dt) {

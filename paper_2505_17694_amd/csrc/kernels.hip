@@ -1364,7 +1364,7 @@ struct TilePath {
     static constexpr int kRowBytes = D * 2;
     static constexpr int kHalf = 32 * kRowBytes;            // K (or V) of a block
     static constexpr int kBlock = 2 * kHalf;
-    static constexpr int kBlocks = 256 / D;                 // blocks of an interval (128 channels: differential attention only)
+    static constexpr int kBlocks = D == 64 ? 4 : 1;         // blocks of an interval
     static constexpr int kInterval = kBlocks * kBlock;
     static constexpr int kMine = kBlocks * 4 / kWaves;      // blocks of an interval of which a wave copies eight tokens
     static constexpr int kIntervals = 131072 / kInterval;   // slots of the ring
