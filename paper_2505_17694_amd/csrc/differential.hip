@@ -22,8 +22,11 @@ namespace {
 // read by 16 bytes a lane and V by transposing reads (swizzles below).
 //
 // A step is NB blocks between two barriers, the row groups' waves taking turns with them (SHARE); S slots hold blocks, so that
-// S - NB of them are on their way when a step starts.  With 256 channels a SIMD has one wave: in a block its reads of K travel beside
-// the accumulation of the block before, its reads of V beside the exponentials.
+// S - NB of them are on their way when a step starts.  In a wave the scores of a block and the accumulation of its block before are one
+// stream of matrix instructions, between which stand the exponentials of the block before, the reads of V and the copies.  ns a
+// block, K and V out of L2, all CUs busy (with the accumulation, the scores, the reads and the exponentials one after the other):
+// 256 channels, 32 pairs 514 (763), 64 pairs 830 (1125); 128 channels 32, 64, 128 pairs 286 (379), 443 (518), 771 (973); 64 channels
+// 170 (229), 284 (372), 512 (619).  Out of HBM tasks of up to 64 pairs run at what HBM gives, 6.5 to 6.8 TB/s.
 template <int D, int GROUPS>
 struct PairPath {
     static constexpr int kWaves = kernel_waves(kFormWide, D), kUnits = 2 * GROUPS;
@@ -42,7 +45,28 @@ struct PairPath {
     static_assert(kAhead % kBlocks == 0 || kStride == 1, "a step's copies are requested together");
 };
 
-template <int DT, int D, int GROUPS>
+// A wave-uniform address, in scalar registers also where the compiler has lost track of that.
+__device__ __forceinline__ const char *uniform_pointer(const char *p)
+{
+    const uint64_t x = uint64_t(uintptr_t(p));
+    return reinterpret_cast<const char *>(uintptr_t(uint64_t(uint32_t(__builtin_amdgcn_readfirstlane(uint32_t(x >> 32)))) << 32 |
+                                                     uint32_t(__builtin_amdgcn_readfirstlane(uint32_t(x)))));
+}
+
+// dma16 (kernels.hip) from a base that is in scalar registers already.
+template <bool ONCE>
+__device__ __forceinline__ void copy_1k(uint32_t lds_addr, uint32_t voff, const char *base)
+{
+    uint32_t m0_saved;
+    if constexpr (ONCE)
+        asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3 nt\n\ts_mov_b32 m0, %0"
+                     : "=&s"(m0_saved) : "s"(lds_addr), "v"(voff), "s"(base) : "memory");
+    else
+        asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3\n\ts_mov_b32 m0, %0"
+                     : "=&s"(m0_saved) : "s"(lds_addr), "v"(voff), "s"(base) : "memory");
+}
+
+template <int DT, int D, int GROUPS, bool ONCE>
 __device__ __forceinline__ void run_pairs_of(const PairParams &P, const DevTask &t, int head, char *lds, RowStore how)
 {
     using T = PairPath<D, GROUPS>;
@@ -81,13 +105,37 @@ __device__ __forceinline__ void run_pairs_of(const PairParams &P, const DevTask 
     auto block_of = [&](int first, int u) { return first + my_block + u * T::kStride; };     // that the wave copies, of NB from `first` on
     auto page_issue = [&](int block) { return uniform_load(c.pages, first_token(block) >> c.page_shift); };
     auto slot_of = [&](int block) { return lds_base + uint32_t(block % S) * T::kBlock; };
-    auto request = [&](int block, int pg) __attribute__((always_inline)) {          // pg: page_issue(block)
-        const uint32_t at = slot_of(block) + uint32_t(my_token) * RB;
-        const int64_t off = page_offset(c, pg, first_token(block) & c.page_mask);
+    // copies of the wave's blocks of a step, each K first
+    const char *k_head = uniform_pointer(c.k_head), *v_head = uniform_pointer(c.v_head);
+    struct Copies {
+        uint32_t at[MINE];
+        const char *k[MINE], *v[MINE];
+    };
+    auto copies_of = [&](int first, const int (&pg)[MINE]) __attribute__((always_inline)) {        // pg: their page_issue
+        Copies x;
 #pragma unroll
-        for (int n = 0; n < T::kPieces; ++n) dma16(at + n * 1024, voff_k[n], c.k_head + off, c.read_once);
+        for (int u = 0; u < MINE; ++u) {
+            const int block = block_of(first, u);
+            const int64_t off = page_offset(c, pg[u], first_token(block) & c.page_mask);
+            x.at[u] = slot_of(block) + uint32_t(my_token) * RB;
+            x.k[u] = k_head + off;
+            x.v[u] = v_head + off;
+        }
+        return x;
+    };
+    auto copy = [&](const Copies &x, int n) __attribute__((always_inline)) {
+        const int u = n / (2 * T::kPieces), i = n % (2 * T::kPieces), piece = i % T::kPieces;
+        if (i < T::kPieces) copy_1k<ONCE>(x.at[u] + piece * 1024, voff_k[piece], x.k[u]);
+        else                copy_1k<ONCE>(x.at[u] + T::kHalf + piece * 1024, voff_v[piece], x.v[u]);
+    };
+    auto request_block = [&](const Copies &x, int u) __attribute__((always_inline)) {
 #pragma unroll
-        for (int n = 0; n < T::kPieces; ++n) dma16(at + T::kHalf + n * 1024, voff_v[n], c.v_head + off, c.read_once);
+        for (int n = 0; n < 2 * T::kPieces; ++n) copy(x, u * 2 * T::kPieces + n);
+    };
+    auto request = [&](int first, const int (&pg)[MINE]) __attribute__((always_inline)) {
+        const Copies x = copies_of(first, pg);
+#pragma unroll
+        for (int u = 0; u < MINE; ++u) request_block(x, u);
     };
 
     // Operand reads, as in the dense path.  K, k-step ks: lane (l32, kg) reads 16-byte column map * D / 16 + 2 * ks + kg of token l32.  V,
@@ -102,74 +150,120 @@ __device__ __forceinline__ void run_pairs_of(const PairParams &P, const DevTask 
 
     u32x4 qb[KS];           // row l32 (of pair pair0 + l32), channels 16 * ks + 8 * kg .. +7 of the map
     f32x16 o[CT];           // O^T: row l32, channel 32 * ct + 8 * (r / 4) + 4 * kg + r % 4
-    u32x4 kr[KS], vr[CT][2], p[2];
-    float m = kNoReference, l = 0.f;
+    u32x4 kr[KS], p[2];
+    u32x4 vr[CT][2];
+    f32x16 sc[2];           // scores of the wave's even and odd blocks: row l32, token 8 * (r / 4) + 4 * kg + r % 4
+    float m = kNoReference, l2[2] = {0.f, 0.f};
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[ct][r] = 0.f;
 
-    auto accumulate = [&]() __attribute__((always_inline)) {        // the block whose V and P are in registers
-#pragma unroll
-        for (int tt = 0; tt < 2; ++tt)
-#pragma unroll
-            for (int ct = 0; ct < CT; ++ct) o[ct] = mfma32<DT>(vr[ct][tt], p[tt], o[ct]);
-    };
-    bool begun = false;
-    auto compute = [&](int block) __attribute__((always_inline)) {
-        const uint32_t at = slot_of(block);
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) kr[ks] = *reinterpret_cast<lds_u32x4_ptr>(uintptr_t((at + k_lane) ^ uint32_t(ks << 5)));
-        __builtin_amdgcn_sched_barrier(0);
-        if (begun) accumulate();
-        begun = true;
-        f32x16 s;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] = 0.f;
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) s = mfma32<DT>(kr[ks], qb[ks], s);
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int tt = 0; tt < 2; ++tt)
-#pragma unroll
-            for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const uint32_t from = ((at + v_lane) ^ uint32_t(ct << 6)) + (16 * tt + 8 * h) * RB;
-                    const uint2 w = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_s16x4_ptr>(uintptr_t(from))));
-                    vr[ct][tt][2 * h] = w.x;
-                    vr[ct][tt][2 * h + 1] = w.y;
-                }
-        __builtin_amdgcn_sched_barrier(0);
-        const int valid = c.kv_len - block * 32;
-        if (valid < 32) {
-#pragma unroll
-            for (int r = 0; r < 16; ++r) s[r] = 8 * (r >> 2) + 4 * kg + (r & 3) >= valid ? -INFINITY : s[r];
-        }
+    auto reference = [&](const f32x16 &s) __attribute__((always_inline)) {
         float lm = s[0];
 #pragma unroll
         for (int r = 1; r < 16; ++r) lm = fmaxf(lm, s[r]);
         lm *= P.scale_log2e;
         if (__any(lm > m + kLag)) {                         // see raise_reference
             const float m_new = fmaxf(m, fmaxf(lm, __shfl_xor(lm, 32))), alpha = fast_exp2(m - m_new);
-            l *= alpha;
+            l2[0] *= alpha;
+            l2[1] *= alpha;
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) o[ct][r] *= alpha;
             m = m_new;
         }
+    };
+    auto exponential_pair = [&](const f32x16 &s, int tt, int d) __attribute__((always_inline)) {
+        p[tt][d] = pack2<DT>(fast_exp2(__builtin_fmaf(s[8 * tt + 2 * d], P.scale_log2e, -m)),
+                             fast_exp2(__builtin_fmaf(s[8 * tt + 2 * d + 1], P.scale_log2e, -m)));
+        l2[tt] = add_pair<DT>(p[tt][d], l2[tt]);
+    };
+    // n of `of` steps through four pairs of exponentials
+    auto exponentials = [&](const f32x16 &s, int tt, int n, int of) __attribute__((always_inline)) {
 #pragma unroll
-        for (int tt = 0; tt < 2; ++tt) {
-            float e[8];
+        for (int d = n * 4 / of; d < (n + 1) * 4 / of; ++d) exponential_pair(s, tt, d);
+    };
+    auto load_value = [&](uint32_t at, int ct, int tt) __attribute__((always_inline)) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) e[i] = fast_exp2(__builtin_fmaf(s[8 * tt + i], P.scale_log2e, -m));
-#pragma unroll
-            for (int d = 0; d < 4; ++d) {
-                p[tt][d] = pack2<DT>(e[2 * d], e[2 * d + 1]);
-                l = add_pair<DT>(p[tt][d], l);
-            }
+        for (int h = 0; h < 2; ++h) {
+            const uint32_t from = ((at + v_lane) ^ uint32_t(ct << 6)) + (16 * tt + 8 * h) * RB;
+            const uint2 w = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_s16x4_ptr>(uintptr_t(from))));
+            vr[ct][tt][2 * h] = w.x;
+            vr[ct][tt][2 * h + 1] = w.y;
         }
+    };
+    // The wave's next block, whose scores go to set X; the other set's are those of the block before, whose V is in registers (FIRST:
+    // there is none).  COPY: the copies x of a step are issued, too, one by one between the matrix instructions: all at once they keep the wave,
+    // and those of the other SIMDs, until the last of them has been taken (a CU takes 64 bytes a cycle).
+    auto compute = [&](int block, auto set, auto first, auto copying, const Copies &x) __attribute__((always_inline)) {
+        constexpr int X = decltype(set)::value, kAll = KS + 2 * CT;
+        constexpr bool COPY = decltype(copying)::value;
+        const uint32_t at = slot_of(block);
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) kr[ks] = *reinterpret_cast<lds_u32x4_ptr>(uintptr_t((at + k_lane) ^ uint32_t(ks << 5)));
+        __builtin_amdgcn_sched_barrier(0);
+        f32x16 &acc = sc[X];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[r] = 0.f;
+        if constexpr (decltype(first)::value) {
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) acc = mfma32<DT>(kr[ks], qb[ks], acc);
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) {
+                load_value(at, ct, 0);
+                load_value(at, ct, 1);
+            }
+        } else {
+            auto behind = [&](int i) __attribute__((always_inline)) {      // matrix instruction i of kAll
+                if constexpr (COPY) {
+#pragma unroll
+                    for (int n = i * T::kCopies / kAll; n < (i + 1) * T::kCopies / kAll; ++n) copy(x, n);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            };
+            const f32x16 &s = sc[1 - X];
+            reference(s);
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                acc = mfma32<DT>(kr[ks], qb[ks], acc);
+                exponentials(s, 0, ks, KS);
+                behind(ks);
+            }
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) {
+                o[ct] = mfma32<DT>(vr[ct][0], p[0], o[ct]);
+                exponentials(s, 1, ct, CT);
+                behind(KS + ct);
+            }
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) {
+                o[ct] = mfma32<DT>(vr[ct][1], p[1], o[ct]);
+                load_value(at, ct, 0);
+                if (ct > 0) load_value(at, ct - 1, 1);
+                behind(KS + CT + ct);
+            }
+            load_value(at, CT - 1, 1);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    // the last of the wave's blocks, in set X
+    auto complete = [&](int block, auto x) __attribute__((always_inline)) {
+        constexpr int X = decltype(x)::value;
+        f32x16 &s = sc[X];
+        const int valid = c.kv_len - block * 32;
+        if (valid < 32) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] = 8 * (r >> 2) + 4 * kg + (r & 3) >= valid ? -INFINITY : s[r];
+        }
+        reference(s);
+        exponentials(s, 0, 0, 1);
+        exponentials(s, 1, 0, 1);
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) o[ct] = mfma32<DT>(vr[ct][tt], p[tt], o[ct]);
     };
 
     // V rows of the last block past the end of the slice count as zero: each wave clears the ones that it copied
@@ -186,21 +280,20 @@ __device__ __forceinline__ void run_pairs_of(const PairParams &P, const DevTask 
     // Start: the rows' requests and the page ids, read together; then the first step's copies and the query rows.  Waiting for the
     // rows (the compiler waits for every load in flight) waits for that step too, so the others are requested behind it.
     constexpr int kRounds = (T::kAhead + NB - 1) / NB;      // of requests ahead of the first step
-    int pg[kRounds + 1][MINE];
+    int pg[kRounds][MINE], pg_next[MINE];
 #pragma unroll
     for (int i = 0; i < kRounds; ++i)
 #pragma unroll
         for (int u = 0; u < MINE; ++u) pg[i][u] = page_issue(block_of(i * NB, u));
 #pragma unroll
-    for (int u = 0; u < MINE; ++u) pg[kRounds][u] = page_issue(block_of(T::kAhead, u));
+    for (int u = 0; u < MINE; ++u) pg_next[u] = page_issue(block_of(T::kAhead, u));
     const bool row_live = pair0 + l32 < pairs;
     {
         const int row = row_live ? 2 * (pair0 + l32) + map : map, qi = row / P.group, hj = row - qi * P.group;
         int req = t.single_req >= 0 ? t.single_req : P.node_q[t.q_off + qi];
         pin(req);
         const char *qp = static_cast<const char *>(P.q) + (int64_t(req) * P.h_q + int64_t(head) * P.group + hj) * D + kg * 16;
-#pragma unroll
-        for (int u = 0; u < MINE; ++u) request(block_of(0, u), pg[0][u]);
+        request(0, pg[0]);
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
             qb[ks] = ld16(qp + ks * 32);
@@ -212,45 +305,96 @@ __device__ __forceinline__ void run_pairs_of(const PairParams &P, const DevTask 
 #pragma unroll
     for (int i = 1; i < kRounds; ++i)
         if (i * NB < nblk) {
+            const Copies x = copies_of(i * NB, pg[i]);
 #pragma unroll
             for (int u = 0; u < MINE; ++u)
-                if (i * NB + u * T::kStride < T::kAhead) request(block_of(i * NB, u), pg[i][u]);
+                if (i * NB + u * T::kStride < T::kAhead) request_block(x, u);
         }
-    int pg_next[MINE];
-#pragma unroll
-    for (int u = 0; u < MINE; ++u) pg_next[u] = pg[kRounds][u];
+    auto meet = [&]() __attribute__((always_inline)) {
+        __builtin_amdgcn_s_waitcnt(0xC07F);     // V of the step before is in registers
+        __syncthreads();                        // everyone's part has landed; step j - 1 has been read by all
+    };
+    // the blocks of step j have landed once at most the copies requested after them are outstanding
     auto enter_step = [&](int j) __attribute__((always_inline)) {
-        // the blocks of step j have landed once at most the copies requested after them are outstanding
         if (NB * j + T::kAhead <= nblk) __builtin_amdgcn_s_waitcnt(vmcnt_imm(T::kOutstanding));
         else                            __builtin_amdgcn_s_waitcnt(0x0F70);
         if (j == nstep - 1 && (c.kv_len & 31)) clear_tail();
-        __builtin_amdgcn_s_waitcnt(0xC07F);     // V of the step before is in registers
-        __syncthreads();                        // everyone's part has landed; step j - 1 has been read by all
-        const int next = NB * j + T::kAhead;
-        if (next < nblk) {
+        meet();
+    };
+    auto pages_of = [&](int first) __attribute__((always_inline)) {
 #pragma unroll
-            for (int u = 0; u < MINE; ++u) request(block_of(next, u), pg_next[u]);
-#pragma unroll
-            for (int u = 0; u < MINE; ++u) pg_next[u] = page_issue(block_of(next + NB, u));
-        }
+        for (int u = 0; u < MINE; ++u) pg_next[u] = page_issue(block_of(first, u));
     };
     if (live) {
+        int last = -1;                          // the wave's last block so far
+        using yes = std::true_type;
+        using no = std::false_type;
+        // FULL: all blocks of step j and of the copies behind it exist
+        auto step = [&](int j, auto set, auto first, auto full) __attribute__((always_inline)) {
+            constexpr int X = decltype(set)::value;
+            constexpr bool FIRST = decltype(first)::value, FULL = decltype(full)::value;
+            const int next = NB * j + T::kAhead;
+            Copies x{};
+            if constexpr (FULL) {
+                __builtin_amdgcn_s_waitcnt(vmcnt_imm(T::kOutstanding));
+                x = copies_of(next, pg_next);
+                meet();
+                pages_of(next + NB);
+            } else {
+                enter_step(j);
+                if (next < nblk) {
+                    request(next, pg_next);
+                    pages_of(next + NB);
+                }
+            }
+            auto own = [&](auto n) __attribute__((always_inline)) {
+                constexpr int U = decltype(n)::value;
+                if constexpr (U < NB / SHARE) {
+                    const int block = NB * j + phase + U * SHARE;
+                    if (!FULL && block >= nblk) return;
+                    compute(block, std::integral_constant<int, (X + U) % 2>{}, std::integral_constant<bool, FIRST && U == 0>{},
+                            std::integral_constant<bool, FULL && U == 0>{}, x);
+                    last = block;
+                }
+            };
+            static_assert(NB / SHARE <= 4, "blocks of a step");
+            own(std::integral_constant<int, 0>{});
+            own(std::integral_constant<int, 1>{});
+            own(std::integral_constant<int, 2>{});
+            own(std::integral_constant<int, 3>{});
+        };
+        constexpr bool kEven = NB / SHARE % 2 == 0;             // a step leaves the sets as they were
+        using zero = std::integral_constant<int, 0>;
+        using other = std::integral_constant<int, kEven ? 0 : 1>;
+        step(0, zero{}, yes{}, no{});
+        int j = 1;
+#pragma unroll 1
+        for (; NB * (j + 1) + T::kAhead < nblk; j += 2) {
+            step(j, other{}, no{}, yes{});
+            step(j + 1, zero{}, no{}, yes{});
+        }
+#pragma unroll 1
+        for (; j < nstep; j += 2) {
+            step(j, other{}, no{}, no{});
+            if (j + 1 < nstep) step(j + 1, zero{}, no{}, no{});
+        }
+        if (last >= 0) {
+            const bool odd = (kEven ? (last % NB) / SHARE : last / NB) & 1;
+            if (odd) complete(last, std::integral_constant<int, 1>{});
+            else     complete(last, std::integral_constant<int, 0>{});
+        }
+    } else {
 #pragma unroll 1
         for (int j = 0; j < nstep; ++j) {
             enter_step(j);
-            if constexpr (NB == SHARE) {
-                if (NB * j + phase < nblk) compute(NB * j + phase);
-            } else {
-                const int end = nblk - NB * j < NB ? nblk - NB * j : NB;
-#pragma unroll 1
-                for (int u = phase; u < end; u += SHARE) compute(NB * j + u);
+            const int next = NB * j + T::kAhead;
+            if (next < nblk) {
+                request(next, pg_next);
+                pages_of(next + NB);
             }
         }
-        if (begun) accumulate();
-    } else {
-#pragma unroll 1
-        for (int j = 0; j < nstep; ++j) enter_step(j);
     }
+    float l = l2[0] + l2[1];
     l += __shfl_xor(l, 32);
     __syncthreads();                        // every block has been read: the ring is free
 
@@ -298,7 +442,7 @@ __device__ __forceinline__ void run_pairs_of(const PairParams &P, const DevTask 
         float *pml = P.part_ml + (int64_t(head) * P.part_rows + t.part_row_base) * 2;
         if (tiled && how == kRowsThrough && int64_t(last_tile + 1) * stride * (D * 4) >= int64_t(1) << 31) how = kRowsPlain;   // see run_tile_of
         constexpr int kWidth = D < 128 ? D : 128, kPitch = kWidth * 4 + 16, kLanes = kWidth / 4, kRows = 64 / kLanes;
-        static_assert(2 * GROUPS * 32 * kPitch <= T::kLds, "staging areas fit");
+        static_assert(T::kUnits * 32 * kPitch <= T::kLds, "staging areas fit");
         typedef f32x4 __attribute__((address_space(3))) *lds_f32x4_ptr;
         const uint32_t area = lds_base + uint32_t(unit) * 32 * kPitch, put = area + uint32_t(l32) * kPitch + uint32_t(kg) * 16;
         const uint32_t get = area + uint32_t(lane / kLanes) * kPitch + uint32_t(lane % kLanes) * 16;
@@ -334,14 +478,21 @@ __device__ __forceinline__ void run_pairs_of(const PairParams &P, const DevTask 
     __syncthreads();                        // the staging areas are free for the next task
 }
 
-// Row groups of 32 pairs: one, two or four, times two maps, over the waves.
+// Row groups of 32 pairs: one, two or four, times two maps, over the waves.  Slices that one task alone reads are read with the
+// streaming hint, but not under more than 64 pairs.  32 nodes of 4096 tokens and eight KV heads, us with / without it: 256 channels
+// 173 / 195 (16 pairs), 179 / 202 (32), 187 / 214 (64); 128 channels 89 / 101, 91 / 104, 98 / 113, but 198 / 147 (128 pairs).
 template <int DT, int D>
 __device__ __forceinline__ void run_pairs(const PairParams &P, const DevTask &t, int head, char *lds, RowStore how)
 {
     const int pairs = t.n_req * P.group / 2;
-    if (pairs <= 32)                    run_pairs_of<DT, D, 1>(P, t, head, lds, how);
-    else if (D == 256 || pairs <= 64)   run_pairs_of<DT, D, 2>(P, t, head, lds, how);
-    else if constexpr (D != 256)        run_pairs_of<DT, D, 4>(P, t, head, lds, how);
+    auto run = [&](auto groups) __attribute__((always_inline)) {
+        constexpr int GROUPS = decltype(groups)::value;
+        if (t.flags & kTaskReadOnce) run_pairs_of<DT, D, GROUPS, true>(P, t, head, lds, how);
+        else                         run_pairs_of<DT, D, GROUPS, false>(P, t, head, lds, how);
+    };
+    if (pairs <= 32)                    run(std::integral_constant<int, 1>{});
+    else if (D == 256 || pairs <= 64)   run(std::integral_constant<int, 2>{});
+    else if constexpr (D != 256)        run_pairs_of<DT, D, 4, false>(P, t, head, lds, how);
 }
 
 // The kernel of differential attention: pac_kernel's task loop (there is more about it), for two launches or finished rows.
