@@ -404,14 +404,11 @@ typedef struct {
     float gain;                     /* factor on the result                                                             */
 } codec_differential;
 
-/* Bytes of scratch codec_differential_attention needs (more than codec_plan_workspace_bytes). */
-size_t codec_differential_workspace_bytes(const codec_plan_t *plan);
-
 /*
  * One step, enqueued on `stream` without synchronising.
  *   q        device [num_requests][H][2][d], dtype of the plan, 16-byte aligned: both maps' queries of a head side by side
  *   out      device [num_requests][H][2d], same dtype, 16-byte aligned; must not overlap q, lambda, weight or workspace
- *   plan, k_pages, v_pages, layout, workspace   as for codec_decode_attention; workspace of codec_differential_workspace_bytes
+ *   plan, k_pages, v_pages, layout, workspace   as for codec_decode_attention (codec_plan_workspace_bytes)
  * CODEC_ERR_UNSUPPORTED for a plan with an odd number of query heads per KV head.
  */
 int codec_differential_attention(const codec_plan_t *plan, const codec_differential *differential, const void *q,

@@ -52,7 +52,7 @@ EXPORTED_SYMBOLS = [
     "codec_beam_workspace_bytes", "codec_beam_select", "codec_beam_reorder",
     "codec_rotary_by_axes", "codec_append_by_axes",
     "codec_block_table", "codec_slot_workspace_bytes", "codec_slot_map",
-    "codec_differential_workspace_bytes", "codec_differential_attention",
+    "codec_differential_attention",
 ]
 
 _i32p = POINTER(c_int32)
@@ -201,11 +201,8 @@ _lib.codec_decode_attention_static.argtypes = [c_void_p, c_void_p, c_void_p, c_v
                                                POINTER(codec_kv_layout), c_void_p, c_void_p]
 _lib.codec_static_scratch_bytes.restype = c_size_t
 _lib.codec_static_scratch_bytes.argtypes = []
-_lib.codec_differential_workspace_bytes.restype = c_size_t
-_lib.codec_differential_workspace_bytes.argtypes = [c_void_p]
 _lib.codec_differential_attention.restype = c_int
-_lib.codec_differential_attention.argtypes = [c_void_p, POINTER(codec_differential), c_void_p, c_void_p, c_void_p,
-                                              POINTER(codec_kv_layout), c_void_p, c_void_p, c_size_t, c_void_p]
+_lib.codec_differential_attention.argtypes = [c_void_p] * 8 + [c_size_t, c_void_p]
 _lib.codec_stream_read_probe.restype = c_int
 _lib.codec_stream_read_probe.argtypes = [c_void_p, c_size_t, c_int32, c_int32, c_int32, c_void_p, c_void_p]
 _lib.codec_rotary_turns.restype = c_int
@@ -217,9 +214,9 @@ _lib.codec_append.restype = c_int
 _lib.codec_append.argtypes = [POINTER(codec_head_config), POINTER(codec_rotary_config)] + [POINTER(codec_rows)] * 4 + [
     c_void_p, c_void_p, c_int32, c_void_p, c_void_p, POINTER(codec_kv_layout), c_void_p]
 _lib.codec_rotary_by_axes.restype = c_int
-_lib.codec_rotary_by_axes.argtypes = [POINTER(codec_rotary_axes)] + _lib.codec_rotary.argtypes[1:]
+_lib.codec_rotary_by_axes.argtypes = [c_void_p] + _lib.codec_rotary.argtypes[1:]
 _lib.codec_append_by_axes.restype = c_int
-_lib.codec_append_by_axes.argtypes = [POINTER(codec_head_config), POINTER(codec_rotary_axes)] + _lib.codec_append.argtypes[2:]
+_lib.codec_append_by_axes.argtypes = [POINTER(codec_head_config), c_void_p] + _lib.codec_append.argtypes[2:]
 _lib.codec_pages_create.restype = c_int
 _lib.codec_pages_create.argtypes = [c_int32, POINTER(c_void_p)]
 _lib.codec_pages_destroy.restype = c_int
@@ -243,9 +240,9 @@ _lib.codec_cache_copy.argtypes = [POINTER(codec_head_config), POINTER(codec_kv_l
 _lib.codec_block_table.restype = c_int
 _lib.codec_block_table.argtypes = [c_int32, c_int32, c_void_p, c_void_p, c_int32, c_void_p, c_void_p, c_int64, c_int32, c_void_p]
 _lib.codec_slot_workspace_bytes.restype = c_size_t
-_lib.codec_slot_workspace_bytes.argtypes = [POINTER(codec_slot_config)]
+_lib.codec_slot_workspace_bytes.argtypes = [c_void_p]
 _lib.codec_slot_map.restype = c_int
-_lib.codec_slot_map.argtypes = [POINTER(codec_slot_config)] + [c_void_p] * 12 + [c_size_t, c_void_p]
+_lib.codec_slot_map.argtypes = [c_void_p] * 13 + [c_size_t, c_void_p]
 _lib.codec_beam_workspace_bytes.restype = c_size_t
 _lib.codec_beam_workspace_bytes.argtypes = [POINTER(codec_beam_config)]
 _lib.codec_beam_select.restype = c_int
@@ -288,6 +285,20 @@ def _ids(a):
 def _in(a):
     """Read-only argument of a short call: the array's bytes (a fifth of the time its pointer takes to get), if they are few."""
     return a.tobytes() if a.nbytes <= 1 << 16 else a.ctypes.data
+
+
+# Structures of short calls as bytes, in a third of the time that their classes take.
+pack_slot_config = struct.Struct("5i4x2q").pack             # fields of codec_slot_config
+pack_differential = struct.Struct("P2q2iP2f").pack          # codec_differential
+pack_kv_layout = struct.Struct("4q").pack                   # codec_kv_layout
+pack_rotary_axes = struct.Struct("3ifP2iPq").pack           # codec_rotary_axes
+assert [len(p(*[0] * n)) for p, n in ((pack_slot_config, 7), (pack_differential, 8), (pack_kv_layout, 4), (pack_rotary_axes, 9))] == [
+    ctypes.sizeof(c) for c in (codec_slot_config, codec_differential, codec_kv_layout, codec_rotary_axes)]
+
+
+def _struct(s):
+    """Argument of a structure: as it is where it came as bytes (or None)."""
+    return byref(s) if isinstance(s, Structure) else s
 
 
 def _ptr(a, ct=c_int32):
@@ -441,14 +452,10 @@ def codec_decode_attention_static(plan, q_ptr: int, k_ptr: int, v_ptr: int, num_
                                               byref(lay), c_void_p(out_ptr), c_void_p(stream))
 
 
-def codec_differential_workspace_bytes(plan) -> int:
-    return int(_lib.codec_differential_workspace_bytes(plan))
-
-
 def codec_differential_attention(plan, differential, q_ptr: int, k_ptr: int, v_ptr: int, layout, out_ptr: int, workspace_ptr: int,
                                  workspace_bytes: int, stream: int = 0) -> int:
-    """``differential``: codec_differential; ``layout``: codec_kv_layout."""
-    return _lib.codec_differential_attention(plan, differential, q_ptr, k_ptr, v_ptr, layout, out_ptr, workspace_ptr, workspace_bytes, stream)
+    """``differential``: codec_differential; ``layout``: codec_kv_layout; or their bytes."""
+    return _lib.codec_differential_attention(plan, _struct(differential), q_ptr, k_ptr, v_ptr, _struct(layout), out_ptr, workspace_ptr, workspace_bytes, stream)
 
 
 def codec_static_scratch_bytes() -> int:
@@ -487,14 +494,14 @@ def codec_append(head, rotary, q, q_out, k, v, positions_ptr: int, slots_ptr: in
 
 def codec_rotary_by_axes(rotary, num_heads: int, head_dim: int, dtype: int, x, out, positions_ptr: int, num_tokens: int,
                          stream: int = 0) -> int:
-    """``rotary``: codec_rotary_axes; ``x`` and ``out``: codec_rows."""
-    return _lib.codec_rotary_by_axes(rotary, num_heads, head_dim, dtype, x, out, positions_ptr, num_tokens, stream)
+    """``rotary``: codec_rotary_axes, or its bytes; ``x`` and ``out``: codec_rows."""
+    return _lib.codec_rotary_by_axes(_struct(rotary), num_heads, head_dim, dtype, x, out, positions_ptr, num_tokens, stream)
 
 
 def codec_append_by_axes(head, rotary, q, q_out, k, v, positions_ptr: int, slots_ptr: int, num_tokens: int, k_ptr: int, v_ptr: int,
                          layout, stream: int = 0) -> int:
-    """codec_append with a codec_rotary_axes."""
-    return _lib.codec_append_by_axes(head, rotary, q, q_out, k, v, positions_ptr, slots_ptr, num_tokens, k_ptr, v_ptr, layout, stream)
+    """codec_append with a codec_rotary_axes, or its bytes."""
+    return _lib.codec_append_by_axes(head, _struct(rotary), q, q_out, k, v, positions_ptr, slots_ptr, num_tokens, k_ptr, v_ptr, layout, stream)
 
 
 def codec_pages_create(num_pages: int):
@@ -585,14 +592,15 @@ def codec_block_table(page_size: int, num_seq: int, page_off_ptr: int, page_ids_
 
 
 def codec_slot_workspace_bytes(config) -> int:
-    return int(_lib.codec_slot_workspace_bytes(config))
+    """``config``: codec_slot_config, or its bytes."""
+    return _lib.codec_slot_workspace_bytes(_struct(config))
 
 
 def codec_slot_map(config, table_ptr: int, tokens_ptr: int, new_tokens_ptr: int, before_ptr: int, spare_ptr: int, positions_ptr: int,
                    slots_ptr: int, sequences_ptr: int, offsets_ptr: int, tokens_out_ptr: int, taken_ptr: int, workspace_ptr: int = 0,
                    workspace_bytes: int = 0, stream: int = 0) -> int:
-    """``config``: codec_slot_config."""
-    return _lib.codec_slot_map(config, table_ptr, tokens_ptr, new_tokens_ptr, before_ptr, spare_ptr, positions_ptr, slots_ptr, sequences_ptr,
+    """``config``: codec_slot_config, or its bytes."""
+    return _lib.codec_slot_map(_struct(config), table_ptr, tokens_ptr, new_tokens_ptr, before_ptr, spare_ptr, positions_ptr, slots_ptr, sequences_ptr,
                                offsets_ptr, tokens_out_ptr, taken_ptr, workspace_ptr, workspace_bytes, stream)
 
 

@@ -150,12 +150,16 @@ class Rotary:
         self._config = [B.codec_rotary_config(rotary_dim, layout, inverse, self.magnitude, self._turns.data_ptr())
                         for inverse in (0, 1)]
         self._axes = None if axis is None else torch.from_numpy(axis).to(self.device)
-        self._num_axes, self._block = (0, 0) if axis is None else (len(axes), rotary_dim // blocks)
+        if axis is not None:
+            self._num_axes = len(axes)
+            # of codec_rotary_axes, all but the stride, which is a call's
+            self._fields = [(rotary_dim, layout, inverse, self.magnitude, self._turns.data_ptr(), rotary_dim // blocks, len(axes), self._axes.data_ptr())
+                            for inverse in (0, 1)]
 
     def _by_axes(self, inverse, positions, tokens, index):
         """The codec_rotary_axes of a call, and its positions' address."""
         at, stride = _axis_index(positions, tokens, self._num_axes, index)
-        return B.codec_rotary_axes(self._config[inverse], self._block, self._num_axes, self._axes.data_ptr(), stride), at
+        return B.pack_rotary_axes(*self._fields[inverse], stride), at
 
     @property
     def turns(self) -> torch.Tensor:
@@ -221,7 +225,8 @@ def _list(t: torch.Tensor, what: str, n: int, index: int, dtype=torch.int32) -> 
     """A contiguous list of n numbers on the GPU; its address."""
     if t.shape != (n,) or t.dtype is not dtype or t.get_device() != index or not t.is_contiguous():
         raise ValueError(f"{what}: need a contiguous {dtype} tensor of shape {(n,)} on cuda:{index}, got {t.dtype} {tuple(t.shape)} on {t.device}")
-    _check_reach(t, what, n, t.element_size())
+    if t.untyped_storage().nbytes() < (t.storage_offset() + n) * t.element_size():
+        raise ValueError(f"{what}: the tensor's storage ends before its last element")
     return t.data_ptr()
 
 
@@ -389,7 +394,8 @@ class KVCache:
         """Page lists as a dense table [sequences, width] on the GPU (int32): the pages that hold sequence s's tokens[s] tokens,
         page_ids[page_off[s]:], -1 behind them; into ``out`` if that is given (codec_block_table).  page_off, page_ids and tokens
         are int32 tensors on the GPU, or lists on the host as fork returns them, which are copied there first (that waits)."""
-        self._check_call("table", stream)
+        if self._index is None:
+            self._check_call("table", stream)
         s = _enter(self._index, stream)
         if s is None:
             with _on(self.device, stream) as s:
@@ -397,23 +403,26 @@ class KVCache:
         return self._table(page_off, page_ids, tokens, width, out, s)
 
     def _to_device(self, a, what: str) -> torch.Tensor:
-        if isinstance(a, torch.Tensor):
-            return a
         a = B._ids(a)
         if a is None or a.ndim != 1:
             raise ValueError(f"{what}: need a list of whole numbers of 32 bits")
         return torch.from_numpy(a).to(self.device)
 
     def _table(self, page_off, page_ids, tokens, width, out, s):
-        off, ids, tokens = (self._to_device(a, w) for a, w in ((page_off, "page_off"), (page_ids, "page_ids"), (tokens, "tokens")))
+        tensor = torch.Tensor
+        off = page_off if isinstance(page_off, tensor) else self._to_device(page_off, "page_off")
+        ids = page_ids if isinstance(page_ids, tensor) else self._to_device(page_ids, "page_ids")
+        tokens = tokens if isinstance(tokens, tensor) else self._to_device(tokens, "tokens")
         if tokens.dim() != 1 or ids.dim() != 1 or not 0 <= width < 1 << 31 or (tokens.shape[0] | ids.shape[0]) >> 31:
             raise ValueError(f"tokens {tuple(tokens.shape)}, page_ids {tuple(ids.shape)}, width {width}: need lists, and a width of 32 bits")
         n, count, index = tokens.shape[0], ids.shape[0], self._index
+        off_at, ids_at, tokens_at = _list(off, "page_off", n + 1, index), _list(ids, "page_ids", count, index), _list(tokens, "tokens", n, index)
         if out is None:
-            out = torch.empty((n, width), dtype=torch.int32, device=self.device)
-        at, stride = _table_rows(out, "out", n, width, index)
-        st = B.codec_block_table(self.head.page_size, n, _list(off, "page_off", n + 1, index), _list(ids, "page_ids", count, index), count,
-                                 _list(tokens, "tokens", n, index), at, stride, width, s)
+            out = tokens.new_empty((n, width))
+            at, stride = out.data_ptr(), width
+        else:
+            at, stride = _table_rows(out, "out", n, width, index)
+        st = B.codec_block_table(self._head.page_size, n, off_at, ids_at, count, tokens_at, at, stride, width, s)
         if st != B.CODEC_OK:
             raise B.CodecError(st, "codec_block_table")
         return out
@@ -425,7 +434,8 @@ class KVCache:
         (int32, pages that ``take`` gave) new pages are taken from it in order and entered in the table, in place; without, the
         table names them already.  num_tokens: the length of the map, behind whose last token there is padding that ``append``
         does not store; new tokens beyond it are left out.  The result's tensors share two allocations."""
-        self._check_call("slots", stream)
+        if self._index is None:
+            self._check_call("slots", stream)
         s = _enter(self._index, stream)
         if s is None:
             with _on(self.device, stream) as s:
@@ -441,15 +451,15 @@ class KVCache:
         pages = 0 if spare is None else spare.shape[0]
         if pages >> 31:
             raise ValueError(f"spare: {pages} pages are too many for a call")
-        config = B.codec_slot_config(n, self.head.page_size, width, num_tokens, pages, self.num_pages, stride)
+        config = B.pack_slot_config(n, self._head.page_size, width, num_tokens, pages, self.num_pages, stride)
         tokens_at, new_at = _list(tokens, "tokens", n, index), _list(new, "new", n, index)
         before_at = None if before is None else _list(before, "before", n, index, torch.int64)
         # spare without a page is not the same as none: the new pages are wanted from it
         spare_at = None if spare is None else _list(spare, "spare", pages, index) or at
         need = B.codec_slot_workspace_bytes(config)
-        wide = torch.empty((2, num_tokens), dtype=torch.int64, device=self.device)
-        lists = torch.empty((num_tokens + 2 * n + 2,), dtype=torch.int32, device=self.device)
-        workspace = torch.empty((need,), dtype=torch.uint8, device=self.device) if need else None
+        wide = table.new_empty((2, num_tokens), dtype=torch.int64)
+        lists = table.new_empty((num_tokens + 2 * n + 2,))
+        workspace = table.new_empty((need,), dtype=torch.uint8) if need else None
         first, second = wide.data_ptr(), lists.data_ptr()
         offsets = second + 4 * num_tokens
         st = B.codec_slot_map(config, at, tokens_at, new_at, before_at, spare_at, first, first + 8 * num_tokens, second, offsets,

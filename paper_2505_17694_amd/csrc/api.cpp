@@ -376,8 +376,6 @@ int codec_decode_attention_static(const codec_plan_t *plan, const void *q, const
     return codec_decode_attention(plan, q, k_pages, v_pages, layout, out, ws, codec::kStaticScratchBytes, stream);
 }
 
-size_t codec_differential_workspace_bytes(const codec_plan_t *plan) { return codec_plan_workspace_bytes(plan); }
-
 int codec_differential_attention(const codec_plan_t *plan, const codec_differential *differential, const void *q, const void *k_pages,
                                  const void *v_pages, const codec_kv_layout *layout, void *out, void *workspace,
                                  size_t workspace_bytes, void *stream)
@@ -395,14 +393,14 @@ int codec_differential_attention(const codec_plan_t *plan, const codec_different
     if (!c.lambda || reinterpret_cast<uintptr_t>(c.lambda) % 4) return CODEC_ERR_INVALID_ARGUMENT;
     if (c.weight && reinterpret_cast<uintptr_t>(c.weight) % (c.weight_dtype == CODEC_DTYPE_FP32 ? 4 : 2)) return CODEC_ERR_INVALID_ARGUMENT;
     if (!q || !aligned16(q) || !out || !aligned16(out) || !workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return CODEC_ERR_INVALID_ARGUMENT;
-    if (workspace_bytes < codec_differential_workspace_bytes(plan)) return CODEC_ERR_WORKSPACE_TOO_SMALL;
+    if (workspace_bytes < codec_plan_workspace_bytes(plan)) return CODEC_ERR_WORKSPACE_TOO_SMALL;
     {
         // what is written, and what is read beside it
         struct Range { const char *begin, *end; };
         auto bytes_at = [](const void *p, size_t n) { return Range{static_cast<const char *>(p), static_cast<const char *>(p) + (p ? n : 0)}; };
         const size_t rows = query_bytes(d) / 2, lambdas = 4 * (size_t(d.num_requests - 1) * size_t(c.lambda_request_stride) +
                                                               size_t(d.head.num_q_heads / 2 - 1) * size_t(c.lambda_head_stride) + 1);
-        const Range all[] = {bytes_at(out, rows), bytes_at(workspace, codec_differential_workspace_bytes(plan)), bytes_at(q, rows),
+        const Range all[] = {bytes_at(out, rows), bytes_at(workspace, codec_plan_workspace_bytes(plan)), bytes_at(q, rows),
                              bytes_at(c.lambda, lambdas), bytes_at(c.weight, size_t(d.head.head_dim) * (c.weight_dtype == CODEC_DTYPE_FP32 ? 4 : 2))};
         for (int i = 0; i < 2; ++i)
             for (int j = i + 1; j < 5; ++j)

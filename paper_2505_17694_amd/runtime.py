@@ -61,7 +61,6 @@ class PlannedAttention:
         self.num_requests = len(forest.req_node)
         self.meta = None
         self.workspace = None
-        self._rows = None
         if self.device.type == "cuda":
             self.meta = torch.empty(B.codec_plan_device_bytes(plan), dtype=torch.uint8, device=self.device)
             stream = torch.cuda.current_stream(self.device).cuda_stream
@@ -157,35 +156,41 @@ class PlannedAttention:
         return self._decode_differential(q, k_pool, v_pool, lam, weight, eps, gain, out, s)
 
     def _decode_differential(self, q, k_pool, v_pool, lam, weight, eps, gain, out, s):
-        h = self.head
-        requests, heads, d = self.num_requests, h.num_q_heads // 2, h.head_dim // 2
-        self._check_pool(k_pool, "k_pool")
-        self._check_pool(v_pool, "v_pool")
+        h, p, device = self.head, self.paged, self.device
+        requests, heads, d, dtype = self.num_requests, h.num_q_heads // 2, h.head_dim // 2, q.dtype
+        # as _check_pool
+        last = 2 * ((p.num_pages - 1) * p.page_stride + (h.page_size - 1) * p.token_stride + (h.num_kv_heads - 1) * p.head_stride + h.head_dim)
+        for pool, what in ((k_pool, "k_pool"), (v_pool, "v_pool")):
+            if pool.untyped_storage().nbytes() < 2 * pool.storage_offset() + last or pool.dtype is not dtype or pool.device != device:
+                self._check_pool(pool, what)
+                raise ValueError(f"{what}: need {dtype} like q, got {pool.dtype}")
         self._check_dense(q, "q", (requests, h.num_q_heads, d))
         if out is None:
-            out = torch.empty((requests, heads, 2 * d), dtype=q.dtype, device=self.device)
+            out = q.new_empty((requests, heads, 2 * d))
         else:
             self._check_dense(out, "out", (requests, heads, 2 * d))
-        if lam.shape not in ((), (heads,), (requests, heads)) or lam.dtype is not torch.float32 or lam.device != q.device:
-            raise ValueError(f"lam: need a float32 tensor of shape (), {(heads,)} or {(requests, heads)} on {q.device}, "
-                             f"got {lam.dtype} {tuple(lam.shape)} on {lam.device}")
-        of_request, of_head = (0, 0, *lam.stride())[-2:]
-        if lam.numel():
-            self._check_end(lam, "lam", sum((n - 1) * step for n, step in zip(lam.shape, lam.stride())) + 1)
+        shape, strides = lam.shape, lam.stride()
+        if shape not in ((), (heads,), (requests, heads)) or lam.dtype is not torch.float32 or lam.device != device:
+            raise ValueError(f"lam: need a float32 tensor of shape (), {(heads,)} or {(requests, heads)} on {device}, "
+                             f"got {lam.dtype} {tuple(shape)} on {lam.device}")
+        of_request, of_head = (0, 0, *strides)[-2:]
+        self._check_end(lam, "lam", (requests - 1) * of_request + (heads - 1) * of_head + 1 if requests else 0)
+        weight_dtype, weight_at = B.CODEC_DTYPE_FP32, 0
         if weight is not None:
-            if weight.shape != (2 * d,) or weight.dtype not in (torch.float32, q.dtype) or weight.device != q.device or not weight.is_contiguous():
-                raise ValueError(f"weight: need a contiguous float32 or {q.dtype} tensor of shape {(2 * d,)} on {q.device}, "
+            if weight.shape != (2 * d,) or weight.dtype not in (torch.float32, dtype) or weight.device != device or not weight.is_contiguous():
+                raise ValueError(f"weight: need a contiguous float32 or {dtype} tensor of shape {(2 * d,)} on {device}, "
                                  f"got {weight.dtype} {tuple(weight.shape)} on {weight.device}")
             self._check_end(weight, "weight", 2 * d)
-        p = self.paged
-        config = B.codec_differential(lam.data_ptr(), of_request, of_head, eps is not None,
-                                      B.CODEC_DTYPE_FP32 if weight is None or weight.dtype is torch.float32 else h.dtype,
-                                      None if weight is None else weight.data_ptr(), 0.0 if eps is None else eps, gain)
-        if self._rows is None:                  # kept: never given back while a launch on some stream may use it
-            self._rows = torch.empty(B.codec_differential_workspace_bytes(self.plan), dtype=torch.uint8, device=self.device)
-        st = B.codec_differential_attention(self.plan, config, q.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(),
-                                            B.codec_kv_layout(p.num_pages, p.page_stride, p.token_stride, p.head_stride), out.data_ptr(),
-                                            self._rows.data_ptr(), self._rows.numel(), s)
+            weight_dtype, weight_at = B.CODEC_DTYPE_FP32 if weight.dtype is torch.float32 else h.dtype, weight.data_ptr()
+        if eps is None:
+            norm, eps = 0, 0.0
+        else:
+            norm = 1
+        rows = self.workspace
+        st = B.codec_differential_attention(self.plan, B.pack_differential(lam.data_ptr(), of_request, of_head, norm, weight_dtype, weight_at, eps, gain),
+                                            q.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(),
+                                            B.pack_kv_layout(p.num_pages, p.page_stride, p.token_stride, p.head_stride), out.data_ptr(),
+                                            rows.data_ptr(), rows.numel(), s)
         if st != B.CODEC_OK:
             raise B.CodecError(st, "codec_differential_attention")
         return out

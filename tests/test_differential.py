@@ -33,8 +33,7 @@ def plan_of(f=None, head=None):
 def test_refusals():
     """Argument errors that are caught before any HIP call; a plan that was never uploaded refuses what is left."""
     plan = plan_of()
-    need = C.codec_differential_workspace_bytes(plan)
-    assert need >= C.codec_plan_workspace_bytes(plan) + 2 * 2 * 8 * 128 and need % 256 == 0 and C.codec_differential_workspace_bytes(None) == 0
+    need = C.codec_plan_workspace_bytes(plan)
     layout = C.codec_kv_layout(1000, 16 * 2 * 128, 2 * 128, 128)
     at = dict(q=1 << 20, k=1 << 24, v=1 << 26, out=1 << 21, ws=1 << 22, lam=4096, weight=8192)
 
