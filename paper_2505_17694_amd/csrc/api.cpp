@@ -296,10 +296,13 @@ int partial_attention(const codec_plan_t *plan, const void *q, const void *k_pag
         pp.nodeq_mask = reinterpret_cast<const int32_t *>(meta + L.nodeq_mask);
         pp.mask_words = reinterpret_cast<const uint32_t *>(meta + L.mask_words);
     }
+    const bool turns = !fused_out && layout->head_stride < layout->token_stride &&
+                       codec::heads_in_turn(int64_t(d.tasks.size()), d.head.num_kv_heads, d.makespan, L.turning_tokens, L.tokens_read);
     if (pairs) {
         codec::PairParams by{};
         static_cast<codec::PacParams &>(by) = pp;
         by.finish = *pairs;
+        by.turns = turns && d.head.head_dim <= 128;
         if (plan->single_parts) by.part_o = nullptr;
         if (int e = codec::launch_pairs(by, d.head.dtype, d.head.head_dim, L.num_slots, plan->max_task_rows, !d.packs.empty(), stream))
             return hip_failure("partial attention launch", e);
@@ -310,8 +313,6 @@ int partial_attention(const codec_plan_t *plan, const void *q, const void *k_pag
         if (plan->single_parts) pp.part_o = nullptr;
         else pp.arrive = reinterpret_cast<int32_t *>(const_cast<char *>(meta) + L.arrive);
     }
-    const bool turns = !fused_out && layout->head_stride < layout->token_stride &&
-                       codec::heads_in_turn(int64_t(d.tasks.size()), d.head.num_kv_heads, d.makespan, L.turning_tokens, L.tokens_read);
     if (int e = codec::launch_pac(pp, d.head.dtype, d.head.head_dim, L.num_slots, plan->max_task_rows, !d.packs.empty(), turns, stream))
         return hip_failure("partial attention launch", e);
     return CODEC_OK;

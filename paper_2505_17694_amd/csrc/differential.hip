@@ -496,7 +496,7 @@ __device__ __forceinline__ void run_pairs(const PairParams &P, const DevTask &t,
 }
 
 // The kernel of differential attention: pac_kernel's task loop (there is more about it), for two launches or finished rows.
-template <int DT, int FORM, int D>
+template <int DT, int FORM, int D, bool TURNS>
 __global__ void __launch_bounds__(kernel_waves(FORM, D) * 64, D > 128 ? 1 : 2) pair_kernel(const PairParams P)
 {
     constexpr bool WIDE = FORM == kFormWide, FINISH = FORM == kFormFinish;
@@ -514,6 +514,15 @@ __global__ void __launch_bounds__(kernel_waves(FORM, D) * 64, D > 128 ? 1 : 2) p
     char *stage = lds + kMerge + wave * solo_stage_bytes(D);
     const RowStore early = int64_t(P.part_rows) * P.h_kv * (D * 4) > kEarlyThroughBytes ? kRowsThrough : kRowsPlain;
     const RowStore late = last_rows_through(P.h_kv) ? kRowsThrough : kRowsPlain;
+    // Stream tasks that alone read their slice go round the KV heads where pac_kernel's do ([token][head] pools): 300 contexts of up to
+    // 2000 tokens, eight heads of 64 channels 143 -> 113 us, 200 of up to 4000 of 128 channels 306 -> 285.  A choice at run
+    // time in the form for all task shapes: a kernel for each takes long to build.
+    auto head_of = [&](const DevTask &t, int i) __attribute__((always_inline)) {
+        if constexpr (FINISH || TURNS || WIDE) {
+            if ((t.flags & kTaskReadOnce) && (!WIDE || P.turns)) return int(uint32_t(head + i) % uint32_t(P.h_kv));
+        }
+        return head;
+    };
     auto run_tasks = [&](const DevTask *recs, int i, int end, bool marked, bool more) __attribute__((always_inline)) {
 #pragma unroll 1
         while (i < end) {
@@ -527,8 +536,9 @@ __global__ void __launch_bounds__(kernel_waves(FORM, D) * 64, D > 128 ? 1 : 2) p
 #pragma unroll 1
                 while (k < n) {
                     const DevTask mine = recs[i + k];
-                    if (mine.flags & kTaskReadOnce) run_stream<DT, true, 1, 1, D, FINISH>(P, mine, head, lds, 0, stage);
-                    else                            run_stream<DT, false, 1, 1, D, FINISH>(P, mine, head, lds, 0, stage);
+                    const int own = head_of(mine, i + k);
+                    if (mine.flags & kTaskReadOnce) run_stream<DT, true, 1, 1, D, FINISH>(P, mine, own, lds, 0, stage);
+                    else                            run_stream<DT, false, 1, 1, D, FINISH>(P, mine, own, lds, 0, stage);
                     k = 0;
                     if ((threadIdx.x & 63) == 0) k = atomicAdd(next, 1);
                     k = __builtin_amdgcn_readfirstlane(k);
@@ -539,13 +549,15 @@ __global__ void __launch_bounds__(kernel_waves(FORM, D) * 64, D > 128 ? 1 : 2) p
             }
             const int rows = t.n_req * P.group;
             if (rows <= 16) {
-                if (t.flags & kTaskReadOnce) run_stream<DT, true, 1, W, D, FINISH>(P, t, head, lds, wave);
-                else                         run_stream<DT, false, 1, W, D, FINISH>(P, t, head, lds, wave);
+                const int own = head_of(t, i);
+                if (t.flags & kTaskReadOnce) run_stream<DT, true, 1, W, D, FINISH>(P, t, own, lds, wave);
+                else                         run_stream<DT, false, 1, W, D, FINISH>(P, t, own, lds, wave);
             } else if constexpr (WIDE) {
                 run_pairs<DT, D>(P, t, head, lds, i + 1 < end || more ? early : late);
             } else if constexpr (stream_tiles(D) == 2 && !FINISH) {
-                if (t.flags & kTaskReadOnce) run_stream<DT, true, 2, W, D>(P, t, head, lds, wave);
-                else                         run_stream<DT, false, 2, W, D>(P, t, head, lds, wave);
+                const int own = head_of(t, i);
+                if (t.flags & kTaskReadOnce) run_stream<DT, true, 2, W, D>(P, t, own, lds, wave);
+                else                         run_stream<DT, false, 2, W, D>(P, t, own, lds, wave);
             }
             ++i;
         }
@@ -778,8 +790,8 @@ int launch_differential_of(const DifferentialParams &p, hipStream_t s)
 int prepare_pair_kernels()
 {
     auto wide = [](auto dt, auto d) {
-        constexpr int D = decltype(d)::value;
-        return int(hipFuncSetAttribute(reinterpret_cast<const void *>(pair_kernel<decltype(dt)::value, kFormWide, D>),
+        constexpr int DT = decltype(dt)::value, D = decltype(d)::value;
+        return int(hipFuncSetAttribute(reinterpret_cast<const void *>(pair_kernel<DT, kFormWide, D, false>),
                                        hipFuncAttributeMaxDynamicSharedMemorySize, PairPath<D, 1>::kLds));
     };
     int e = 0;
@@ -803,9 +815,12 @@ int launch_pairs(const PairParams &p, int dtype, int head_dim, int num_slots, in
     auto launch = [&](auto dt, auto d) {
         constexpr int DT = decltype(dt)::value, D = decltype(d)::value;
         const dim3 block((wide ? kernel_waves(kFormWide, D) : kNarrowWaves) * 64);
-        if (!p.part_o) hipLaunchKernelGGL((pair_kernel<DT, kFormFinish, D>), grid, block, 0, s, p);
-        else if (wide) hipLaunchKernelGGL((pair_kernel<DT, kFormWide, D>), grid, block, (PairPath<D, 1>::kLds), s, p);
-        else           hipLaunchKernelGGL((pair_kernel<DT, kFormNarrow, D>), grid, block, 0, s, p);
+        constexpr bool kTurns = D <= 128;                   // see pac_kernel
+        constexpr size_t kLds = PairPath<D, 1>::kLds;
+        if (!p.part_o)          hipLaunchKernelGGL((pair_kernel<DT, kFormFinish, D, false>), grid, block, 0, s, p);
+        else if (wide)          hipLaunchKernelGGL((pair_kernel<DT, kFormWide, D, false>), grid, block, kLds, s, p);
+        else if (p.turns)       hipLaunchKernelGGL((pair_kernel<DT, kFormNarrow, D, kTurns>), grid, block, 0, s, p);
+        else                    hipLaunchKernelGGL((pair_kernel<DT, kFormNarrow, D, false>), grid, block, 0, s, p);
     };
     auto launch_dim = [&](auto dt) {
         if (head_dim == 64)       launch(dt, std::integral_constant<int, 64>{});

@@ -68,6 +68,7 @@ struct DifferentialParams {
 // Partial attention of differential attention: q is [B][h_q][head_dim / 2].
 struct PairParams : PacParams {
     DifferentialParams finish;      // what becomes of finished rows (part_o == nullptr)
+    int32_t turns;                  // heads_in_turn
 };
 
 // Size of the library's own scratch array (one per GPU) behind codec_decode_attention_static.
