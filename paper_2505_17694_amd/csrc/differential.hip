@@ -496,7 +496,7 @@ __device__ __forceinline__ void run_pairs(const PairParams &P, const DevTask &t,
 }
 
 // The kernel of differential attention: pac_kernel's task loop (there is more about it), for two launches or finished rows.
-template <int DT, int FORM, int D, bool TURNS>
+template <int DT, int FORM, int D>
 __global__ void __launch_bounds__(kernel_waves(FORM, D) * 64, D > 128 ? 1 : 2) pair_kernel(const PairParams P)
 {
     constexpr bool WIDE = FORM == kFormWide, FINISH = FORM == kFormFinish;
@@ -516,10 +516,10 @@ __global__ void __launch_bounds__(kernel_waves(FORM, D) * 64, D > 128 ? 1 : 2) p
     const RowStore late = last_rows_through(P.h_kv) ? kRowsThrough : kRowsPlain;
     // Stream tasks that alone read their slice go round the KV heads where pac_kernel's do ([token][head] pools): 300 contexts of up to
     // 2000 tokens, eight heads of 64 channels 143 -> 113 us, 200 of up to 4000 of 128 channels 306 -> 285.  A choice at run
-    // time in the form for all task shapes: a kernel for each takes long to build.
+    // time: a kernel for each takes long to build.
     auto head_of = [&](const DevTask &t, int i) __attribute__((always_inline)) {
-        if constexpr (FINISH || TURNS || WIDE) {
-            if ((t.flags & kTaskReadOnce) && (!WIDE || P.turns)) return int(uint32_t(head + i) % uint32_t(P.h_kv));
+        if constexpr (FINISH || D <= 128) {
+            if ((t.flags & kTaskReadOnce) && (FINISH || P.turns)) return int(uint32_t(head + i) % uint32_t(P.h_kv));
         }
         return head;
     };
@@ -791,7 +791,7 @@ int prepare_pair_kernels()
 {
     auto wide = [](auto dt, auto d) {
         constexpr int DT = decltype(dt)::value, D = decltype(d)::value;
-        return int(hipFuncSetAttribute(reinterpret_cast<const void *>(pair_kernel<DT, kFormWide, D, false>),
+        return int(hipFuncSetAttribute(reinterpret_cast<const void *>(pair_kernel<DT, kFormWide, D>),
                                        hipFuncAttributeMaxDynamicSharedMemorySize, PairPath<D, 1>::kLds));
     };
     int e = 0;
@@ -815,12 +815,10 @@ int launch_pairs(const PairParams &p, int dtype, int head_dim, int num_slots, in
     auto launch = [&](auto dt, auto d) {
         constexpr int DT = decltype(dt)::value, D = decltype(d)::value;
         const dim3 block((wide ? kernel_waves(kFormWide, D) : kNarrowWaves) * 64);
-        constexpr bool kTurns = D <= 128;                   // see pac_kernel
         constexpr size_t kLds = PairPath<D, 1>::kLds;
-        if (!p.part_o)          hipLaunchKernelGGL((pair_kernel<DT, kFormFinish, D, false>), grid, block, 0, s, p);
-        else if (wide)          hipLaunchKernelGGL((pair_kernel<DT, kFormWide, D, false>), grid, block, kLds, s, p);
-        else if (p.turns)       hipLaunchKernelGGL((pair_kernel<DT, kFormNarrow, D, kTurns>), grid, block, 0, s, p);
-        else                    hipLaunchKernelGGL((pair_kernel<DT, kFormNarrow, D, false>), grid, block, 0, s, p);
+        if (!p.part_o) hipLaunchKernelGGL((pair_kernel<DT, kFormFinish, D>), grid, block, 0, s, p);
+        else if (wide) hipLaunchKernelGGL((pair_kernel<DT, kFormWide, D>), grid, block, kLds, s, p);
+        else           hipLaunchKernelGGL((pair_kernel<DT, kFormNarrow, D>), grid, block, 0, s, p);
     };
     auto launch_dim = [&](auto dt) {
         if (head_dim == 64)       launch(dt, std::integral_constant<int, 64>{});
