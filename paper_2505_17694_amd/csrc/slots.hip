@@ -25,10 +25,10 @@ __global__ __launch_bounds__(256) void block_table_kernel(TableParams P)
         const int64_t begin = P.page_off[row], end = P.page_off[row + 1];
         int64_t pages = (at_least_0(P.tokens[row]) + (int64_t(1) << P.page_shift) - 1) >> P.page_shift;
         if (pages > end - begin) pages = end - begin;
-        if (begin < 0) pages = 0;
         if (pages > P.num_ids - begin) pages = P.num_ids - begin;
         if (pages > P.width) pages = P.width;
-        const int held = int(pages) - first;            // of these four
+        if (pages < 0 || begin < 0) pages = 0;          // (end - begin may be beyond 32 bits)
+        const int held = int(pages) - first, room = P.width - first;        // of these four
         int32_t *at = P.table + int64_t(row) * P.table_stride + first;
         Four x = {-1, -1, -1, -1};
         const int32_t *from = P.page_ids + begin + first;
@@ -39,12 +39,12 @@ __global__ __launch_bounds__(256) void block_table_kernel(TableParams P)
             for (int i = 0; i < 3; ++i)
                 if (i < held) x[i] = from[i];
         }
-        if (ALIGNED && first + 4 <= P.width) {
+        if (ALIGNED && room >= 4) {
             *reinterpret_cast<Four *>(at) = x;
         } else {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                if (first + i < P.width) at[i] = x[i];
+                if (i < room) at[i] = x[i];
         }
     }
 }

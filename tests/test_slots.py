@@ -116,6 +116,9 @@ def test_tables_of_lists_that_are_none():
     ids = np.arange(10) + 100
     want = O.block_table(16, off, ids, tokens, 6)
     assert np.array_equal(cache_of(1).table(gpu(off), gpu(ids), gpu(tokens), 6).cpu().numpy(), want)
+    # ends so far before begins that their difference passes 32 bits
+    off = [2 ** 31 - 1, -2 ** 31, 2 ** 31 - 1, -2 ** 31 + 5, 9, 2 ** 31 - 1]
+    assert np.array_equal(cache_of(1).table(gpu(off), gpu(ids), gpu([100] * 5), 6).cpu().numpy(), O.block_table(16, off, ids, [100] * 5, 6))
     cache = cache_of(1)
     assert cache.table([0], [], [], 6).shape == (0, 6) and cache.table([0, 0], [], [5], 0).shape == (1, 0)
     assert cache.table([0, 0], [], [5], 3).tolist() == [[-1] * 3]
