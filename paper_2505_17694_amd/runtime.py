@@ -170,6 +170,8 @@ class PlannedAttention:
         else:
             self._check_dense(out, "out", (requests, heads, 2 * d))
         shape, strides = lam.shape, lam.stride()
+        if lam.is_neg() or (weight is not None and weight.is_neg()):
+            raise ValueError("lam or weight: a view that is negated when it is read (see torch.Tensor.resolve_neg)")
         if shape not in ((), (heads,), (requests, heads)) or lam.dtype is not torch.float32 or lam.device != device:
             raise ValueError(f"lam: need a float32 tensor of shape (), {(heads,)} or {(requests, heads)} on {device}, "
                              f"got {lam.dtype} {tuple(shape)} on {lam.device}")

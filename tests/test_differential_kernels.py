@@ -3,11 +3,13 @@ import re
 
 import numpy as np
 import pytest
+import torch
 
+import paper_2505_17694_amd as C
 from differential_choice import pair_launches
 from helpers import GOING_ROUND, GOING_ROUND_OPTS, ROTATING, ROTATING_OPTS, going_round_forest, rotating_forest
 from kernel_choice import case
-from test_differential import head_of, run
+from test_differential import DEV, head_of, make, run
 from test_kernel_resources import resources, waves_per_simd
 from workloads import Forest, build_paged_kv, concat_forests, two_level_forest, unshared_forest, DTYPE_BF16, DTYPE_FP16
 
@@ -103,3 +105,18 @@ def test_many_heads_beside_contexts_of_one_token(d):
     f = concat_forests(concat_forests(two_level_forest(257, [1 + i % 3 for i in range(70)]), unshared_forest([1, 2, 1])),
                        Forest(np.array([-1]), np.array([65]), np.zeros(5, np.int64)))
     run(f, 6, 3, d, kind="token", norm=True, only=range(0, f.num_requests, 5))
+
+
+@pytest.mark.gpu
+def test_numbers_that_are_negated_when_they_are_read():
+    """Views that carry their sign beside them are refused: the kernels read memory as it is."""
+    w = make(two_level_forest(40, [20, 3]), 4, 2, 64).to(DEV)
+    pa = C.PlannedAttention(w.forest, w.paged, w.head, device=DEV)
+    lam = torch.view_as_complex(torch.rand(4, 2, device=DEV)).conj().imag
+    weight = torch._neg_view(torch.rand(128, device=DEV))
+    good = dict(lam=lam.resolve_neg(), weight=weight.resolve_neg(), eps=1e-5)
+    pa.decode_differential(w.q, w.k_pool, w.v_pool, **good)
+    for bad in (dict(lam=lam), dict(weight=weight)):
+        with pytest.raises(ValueError):
+            pa.decode_differential(w.q, w.k_pool, w.v_pool, **dict(good, **bad))
+    pa.close()
