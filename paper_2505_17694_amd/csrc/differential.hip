@@ -45,6 +45,8 @@ struct PairPath {
     static_assert(kAhead % kBlocks == 0 || kStride == 1, "a step's copies are requested together");
 };
 
+constexpr int kTurnMinLen = 2048;       // tokens of a slice; see token_block
+
 // A wave-uniform address, in scalar registers also where the compiler has lost track of that.
 __device__ __forceinline__ const char *uniform_pointer(const char *p)
 {
@@ -96,10 +98,24 @@ __device__ __forceinline__ void run_pairs_of(const PairParams &P, const DevTask 
         voff_k[i] = uint32_t(i * TPC + in_copy) * c.token_bytes + uint32_t(((lane % LPR) ^ fk(token)) << 4);
         voff_v[i] = uint32_t(i * TPC + in_copy) * c.token_bytes + uint32_t(((lane % LPR) ^ fv(token)) << 4);
     }
+    // Tasks that read a slice beside one another (the packs of a node's rows) would ask L2 for the same lines at the same time.  With 256
+    // channels, where a block has only up to 64 pairs of work, each takes every eight blocks from another one on: 564 -> 440 ns a block for a
+    // root alone.  32/8 heads of two maps of 128 channels, requests on a root of 32768 tokens, us: 16 requests 100 -> 91, 32 174 -> 149,
+    // 64 318 -> 245, 128 601 -> 459; a forest whose other tasks set the time 449 -> 459.  Slices of 1024 tokens lose 5 %, and up to
+    // 128 channels there is nothing to gain (0.97 to 1.05).
+    constexpr bool TURN = D == 256 && !ONCE;
+    int turn = 0;
+    if constexpr (TURN) {
+        const uint32_t nth = uint32_t(t.q_off) / uint32_t(t.n_req);     // of the packs, for all but the last
+        if (!(t.flags & kTaskReadOnce) && t.kv_len >= kTurnMinLen) turn = int((nth & 1) << 2 | (nth & 2) | (nth >> 2 & 1));
+    }
+    auto token_block = [&](int block) {                     // eight whole blocks, none of them the last
+        return TURN && (block | 7) < nblk - 1 ? (block & ~7) | ((block + turn) & 7) : block;
+    };
     // eight tokens past the end of the slice are redirected to its first ones (masked later): no address leaves the slice's
     // pages, and every step has the same number of copies
     auto first_token = [&](int block) {
-        const int tok0 = block * 32 + my_token;
+        const int tok0 = token_block(block) * 32 + my_token;
         return tok0 >= c.kv_len ? 0 : tok0;
     };
     auto block_of = [&](int first, int u) { return first + my_block + u * T::kStride; };     // that the wave copies, of NB from `first` on

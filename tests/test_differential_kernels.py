@@ -108,6 +108,15 @@ def test_many_heads_beside_contexts_of_one_token(d):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("length", [2047, 2048, 2049, 2079, 2304, 2305, 2337, 4100])
+@pytest.mark.parametrize("requests,dtype", [(24, DTYPE_BF16), (75, DTYPE_FP16)])
+def test_tasks_that_share_a_long_slice(length, requests, dtype):
+    """Packs of a node's rows with 256 channels, which take their blocks in orders of their own, in slices that end inside one."""
+    f = two_level_forest(length, [1 + i % 40 for i in range(requests)])
+    run(f, 8, 2, 128, kind="token", norm=True, dtype=dtype, only=range(0, requests, 7), opts=dict(fixed_slices=1, num_slots=8))
+
+
+@pytest.mark.gpu
 def test_numbers_that_are_negated_when_they_are_read():
     """Views that carry their sign beside them are refused: the kernels read memory as it is."""
     w = make(two_level_forest(40, [20, 3]), 4, 2, 64).to(DEV)
