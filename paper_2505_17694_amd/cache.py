@@ -197,7 +197,9 @@ class Rotary:
             config, at = self._by_axes(bool(inverse), positions, shape[0], index)
         if out is None:
             out = torch.empty_like(x, memory_format=torch.contiguous_format)
-        into = _rows(out, "out", shape, x.dtype, index)
+            into = _Rows(out.data_ptr(), shape[1] * shape[2], shape[2])
+        else:
+            into = _rows(out, "out", shape, x.dtype, index)
         st = call(config, shape[1], shape[2], _CODE[x.dtype], rows, into, at, shape[0], s)
         if st != B.CODEC_OK:
             raise B.CodecError(st, name)
@@ -218,7 +220,13 @@ class _Turn(torch.autograd.Function):
         positions, = ctx.saved_tensors
         if not g.is_contiguous() or g.data_ptr() % 16:
             g = g.clone(memory_format=torch.contiguous_format)
-        return ctx.rotary.apply(g, positions, not ctx.inverse), None, None, None, None
+        rotary = ctx.rotary
+        # The engine's thread finds little of this in its caches, so a call that passes no gradient on goes the short way, on the
+        # stream that the engine has made current (that of the forward pass).
+        s = None if torch.is_grad_enabled() else _enter(rotary.device.index, None)
+        if s is None:
+            return rotary.apply(g, positions, not ctx.inverse), None, None, None, None
+        return rotary._turn(g, positions, not ctx.inverse, None, s), None, None, None, None
 
 
 def _list(t: torch.Tensor, what: str, n: int, index: int, dtype=torch.int32) -> int:
