@@ -37,10 +37,11 @@ def _check_reach(t: torch.Tensor, what: str, last: int, size: int) -> None:
 def _rows(t: torch.Tensor, what: str, shape, dtype: torch.dtype, index: int):
     """`t` as codec_rows: `shape` = (tokens, heads, head_dim) with contiguous channels, in storage that is there."""
     strides = t.stride()
-    if t.shape != shape or t.dtype is not dtype or t.get_device() != index or strides[2] != 1:
+    tokens, heads, head_dim = shape
+    # (strides without a token say nothing: those of a sum's gradient are all zero)
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != index or (tokens and strides[2] != 1):
         raise ValueError(f"{what}: need a {dtype} tensor of shape {tuple(shape)} with contiguous channels on cuda:{index}, "
                          f"got {t.dtype} {tuple(t.shape)} on {t.device}, strides {strides}")
-    tokens, heads, head_dim = shape
     if tokens == 0:
         return _Rows(0, 0, 0)
     token_stride, head_stride, _ = strides
