@@ -1,6 +1,7 @@
 """Page pools of a K/V cache with what fills them, and rotary positions (marshalling only)."""
 from __future__ import annotations
 
+import operator
 from types import SimpleNamespace
 from typing import NamedTuple
 
@@ -85,13 +86,19 @@ def _turns(rotary_dim, theta, scaling):
 
 
 def _axes(rotary_dim, axes, blocks):
-    """Pairs of each axis in one of the blocks."""
+    """Blocks, and pairs of each axis in one of them."""
+    try:
+        blocks = operator.index(blocks)
+        axes = None if axes is None else [operator.index(n) for n in axes]
+    except TypeError:
+        raise ValueError(f"axes, blocks: need whole numbers, got {axes} and {blocks}") from None
     if not 1 <= blocks <= 128:
         raise ValueError(f"blocks: {blocks}")
-    axes = [rotary_dim // (2 * blocks)] if axes is None else [int(n) for n in axes]
+    if axes is None:
+        axes = [rotary_dim // (2 * blocks)]
     if not 1 <= len(axes) <= 4 or min(axes) < 0 or 2 * blocks * sum(axes) != rotary_dim:
         raise ValueError(f"axes: up to four counts of pairs that make rotary_dim = {rotary_dim} channels in {blocks} blocks, got {axes}")
-    return axes
+    return blocks, axes
 
 
 def _turns_by_axes(axes, theta, scaling, alternating, restart, blocks):
@@ -141,7 +148,7 @@ class Rotary:
         if axes is None and blocks == 1 and not alternating and not restart:
             turns, factor = _turns(rotary_dim, theta, s)
         else:
-            axes = _axes(rotary_dim, axes, blocks)
+            blocks, axes = _axes(rotary_dim, axes, blocks)
             turns, factor, axis = _turns_by_axes(axes, theta, s, alternating, restart, blocks)
         self.device = _device(device)
         self.rotary_dim = rotary_dim
