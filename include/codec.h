@@ -392,7 +392,8 @@ size_t codec_static_scratch_bytes(void);       /* CODEC_STATIC_SCRATCH_BYTES of 
  * A plan for it has head_dim = 2d, num_kv_heads KV heads, num_q_heads = 2 H query heads for H heads of the result, and the scale of
  * the maps (1 / sqrt(d)); head h uses KV head h / (H / num_kv_heads).  Everything a plan can do holds: shared nodes are read
  * once for all requests and both maps, visibility masks (values of hidden tokens are multiplied by zero: they have to be
- * finite, as for codec_decode_attention), refreshed lengths, the run-time queue (fused is without effect).
+ * finite, as for codec_decode_attention), refreshed lengths, the run-time queue (fused is without effect).  Keys of one map never
+ * meet the other: one whose score is -inf has weight zero in its own map and says nothing in the other.
  */
 typedef struct {
     const float *lambda;            /* device: of request r and head h at r * lambda_request_stride + h * lambda_head_stride   */

@@ -1,11 +1,12 @@
 // Differential attention: out = norm(o_1 - lambda o_2), o_m = softmax(scale q_m K_m^T) V.
 //
 // A KV head of the pools is [K_1 | K_2], two maps' keys of d channels each, beside V of 2d.  With the query of map m in its half of
-// a row of 2d channels and zeros in the other, scale q_m K_m^T is an ordinary score of that head, exactly: what the zeros
-// multiply adds nothing.  So plans, their tasks and partial rows are the ordinary ones, with two query heads for every head of the
-// result, and K_1, K_2 and V are read once for both maps.
-//  * Tasks of at most sixteen rows run in the stream path, whose rows are gathered into their halves (gather_q).  A tile there is
-//    sixteen rows wide whatever it holds, so the zeros cost nothing.
+// a row of 2d channels and zeros in the other, scale q_m K_m^T is an ordinary score of that head.  So plans, their tasks and partial
+// rows are the ordinary ones, with two query heads for every head of the result, and K_1, K_2 and V are read once for both
+// maps.  The zeros themselves are nowhere: times an infinite key of the other map they would be NaN.
+//  * The stream path runs tasks of at most sixteen rows, and with 64 channels those of up to 32 in plans without packs.  A tile's
+//    sixteen rows, of either map in turn, are multiplied with both halves of the keys, a product each, and a row takes that of its
+//    own map.  It takes the matrix instructions of an ordinary row (twice what two tiles of 64 channels, a map each, would need).
 //  * Larger tasks run in the path below, where a wave's rows are all of one map and only that map's half of the keys is multiplied.
 //  * A reduction folds both rows of a head, subtracts and normalises; where every request has a single partial result the attention
 //    kernel does that itself (store_finished_pairs).
@@ -18,7 +19,7 @@ namespace {
 //
 // A wave owns 32 rows of one map, pairs 32 g .. 32 g + 31 of the task (pair p is the task's rows 2p and 2p + 1), and runs 32 x 32 x 16
 // tiles: d / 16 k-steps of scores S^T = K_m Q_m^T and 2 * D / 32 matrix instructions of O^T += V^T P^T in a block of 32 tokens, where
-// rows padded with zeros take 2 * d / 16 k-steps.  Blocks are copied HBM -> LDS asynchronously into a ring of all of the CU's LDS, K is
+// rows of either map in turn would take 2 * d / 16 k-steps.  Blocks are copied HBM -> LDS asynchronously into a ring of all of the CU's LDS, K is
 // read by 16 bytes a lane and V by transposing reads (swizzles below).
 //
 // A step is NB blocks between two barriers, the row groups' waves taking turns with them (SHARE); S slots hold blocks, so that

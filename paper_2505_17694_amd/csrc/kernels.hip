@@ -492,14 +492,14 @@ __device__ __forceinline__ void accumulate(const u32x4 (&v)[8][BlockRegs<D>::VU]
     static_assert(BlockRegs<D>::VU <= 2, "head dimensions up to 256");
 }
 
-// Gather the wave's query rows (task rows row0 .. row0 + 16*NT) into B-operand registers.
-// Of differential attention (PairParams) a row is one map's query, of half the channels, in its half of the row: see differential.hip.
+// Of differential attention (PairParams) a row is one map's query, of half the channels (see differential.hip).
 template <class Params>
 constexpr bool kPairs = std::is_same_v<Params, PairParams>;
 
-template <int NT, int D, class Params>
+// Gather the wave's query rows (task rows row0 .. row0 + 16*NT) into B-operand registers.
+template <int NT, int STEPS, class Params>
 __device__ __forceinline__ void gather_q(const Params &P, const DevTask &t, int head, int row0, int rows,
-                                         int l16, int grp, u32x4 (&qb)[NT][D / 32])
+                                         int l16, int grp, u32x4 (&qb)[NT][STEPS])
 {
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
@@ -508,18 +508,10 @@ __device__ __forceinline__ void gather_q(const Params &P, const DevTask &t, int 
         const int qi = live ? row / P.group : 0;
         const int hj = live ? row - qi * P.group : 0;
         const int req = t.single_req >= 0 ? t.single_req : P.node_q[t.q_off + qi];
-        constexpr int kRow = kPairs<Params> ? D : D * 2;        // bytes
         const char *qp = static_cast<const char *>(P.q)
-                         + (int64_t(req) * P.h_q + int64_t(head) * P.group + hj) * kRow + grp * 16;
+                         + (int64_t(req) * P.h_q + int64_t(head) * P.group + hj) * (STEPS * 64) + grp * 16;
 #pragma unroll
-        for (int ks = 0; ks < D / 32; ++ks) {
-            if constexpr (kPairs<Params>) {
-                constexpr int kHalf = D / 64;                   // k-steps of a map
-                qb[nt][ks] = live && ks / kHalf == (hj & 1) ? ld16(qp + (ks % kHalf) * 64) : u32x4{0u, 0u, 0u, 0u};
-            } else {
-                qb[nt][ks] = live ? ld16(qp + ks * 64) : u32x4{0u, 0u, 0u, 0u};
-            }
-        }
+        for (int ks = 0; ks < STEPS; ++ks) qb[nt][ks] = live ? ld16(qp + ks * 64) : u32x4{0u, 0u, 0u, 0u};
     }
 }
 
@@ -651,8 +643,9 @@ __device__ __forceinline__ void run_stream(const Params &P, const DevTask &t, in
     const int l16 = lane & 15, grp = lane >> 4;
     const int rows = t.n_req * P.group;
 
-    u32x4 qb[NT][KS];
-    gather_q<NT, D>(P, t, head, 0, rows, l16, grp, qb);
+    constexpr int QS = kPairs<Params> ? KS / 2 : KS;        // k-steps of a query
+    u32x4 qb[NT][QS];
+    gather_q(P, t, head, 0, rows, l16, grp, qb);
     const SliceCtx c = make_ctx(P, t, head);
     const uint32_t koff = uint32_t(l16) * c.token_bytes + grp * 16;
     const uint32_t voff = uint32_t(grp * 4) * c.token_bytes + (D < 128 ? (l16 & (D / 8 - 1)) : l16) * 16;
@@ -677,8 +670,15 @@ __device__ __forceinline__ void run_stream(const Params &P, const DevTask &t, in
             for (int nt = 0; nt < NT; ++nt) {
                 f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks) acc = mfma16<DT>(r.k[j][ks], qb[nt][ks], acc);
+                for (int ks = 0; ks < QS; ++ks) acc = mfma16<DT>(r.k[j][ks], qb[nt][ks], acc);
                 s[j][nt] = acc;
+                if constexpr (kPairs<Params>) {     // rows are of either map in turn: the second takes the other half's scores
+                    acc = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int ks = 0; ks < QS; ++ks) acc = mfma16<DT>(r.k[j][QS + ks], qb[nt][ks], acc);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[j][nt][e] = l16 & 1 ? acc[e] : s[j][nt][e];
+                }
             }
         const int valid = c.kv_len - tb * 32;
         if (valid < 32) {
