@@ -419,10 +419,10 @@ class KVCache:
         return self._table(page_off, page_ids, tokens, width, out, s)
 
     def _to_device(self, a, what: str) -> torch.Tensor:
-        a = B._ids(a)
-        if a is None or a.ndim != 1:
+        ids = B._ids(a) if np.ndim(a) == 1 else None
+        if ids is None:
             raise ValueError(f"{what}: need a list of whole numbers of 32 bits")
-        return torch.from_numpy(a).to(self.device)
+        return torch.from_numpy(ids).to(self.device)
 
     def _table(self, page_off, page_ids, tokens, width, out, s):
         tensor = torch.Tensor
