@@ -447,8 +447,9 @@ class KVCache:
               spare: torch.Tensor = None, stream=None) -> StepTokens:
         """Positions and slots of a step's new tokens, from lengths on the GPU (codec_slot_map): sequence s holds tokens[s] tokens in
         the pages of table[s] and gets new[s] more (int32).  Positions count from before[s] (int64; zero without).  With ``spare``
-        (int32, pages that ``take`` gave) new pages are taken from it in order and entered in the table, in place; without, the
-        table names them already.  num_tokens: the length of the map, behind whose last token there is padding that ``append``
+        (int32, pages that are held for this) new pages are taken from it in order and entered in the table, in place; without, the
+        table names them already.  tokens, new and spare may be lists on the host, as ``take`` returns them, which are copied to the
+        GPU first (that waits).  num_tokens: the length of the map, behind whose last token there is padding that ``append``
         does not store; new tokens beyond it are left out.  The result's tensors share two allocations."""
         if self._index is None:
             self._check_call("slots", stream)
@@ -459,6 +460,15 @@ class KVCache:
         return self._slots(table, tokens, new, num_tokens, before, spare, s)
 
     def _slots(self, table, tokens, new, num_tokens, before, spare, s):
+        tensor = torch.Tensor
+        if not isinstance(table, tensor) or not (before is None or isinstance(before, tensor)):
+            raise ValueError(f"table, before: need tensors, got {type(table).__name__} and {type(before).__name__}")
+        if not isinstance(tokens, tensor):
+            tokens = self._to_device(tokens, "tokens")
+        if not isinstance(new, tensor):
+            new = self._to_device(new, "new")
+        if not (spare is None or isinstance(spare, tensor)):
+            spare = self._to_device(spare, "spare")
         if table.dim() != 2 or not 0 <= num_tokens < 1 << 31 or (table.shape[0] | table.shape[1]) >> 31 or (spare is not None and spare.dim() != 1):
             raise ValueError(f"table {tuple(table.shape)}, num_tokens {num_tokens}: need a table of two dimensions, spare of one, and a "
                              "number of tokens of 32 bits")
