@@ -394,6 +394,10 @@ size_t codec_static_scratch_bytes(void);       /* CODEC_STATIC_SCRATCH_BYTES of 
  * once for all requests and both maps, visibility masks (values of hidden tokens are multiplied by zero: they have to be
  * finite, as for codec_decode_attention), refreshed lengths, the run-time queue (fused is without effect).  Keys of one map never
  * meet the other: one whose score is -inf has weight zero in its own map and says nothing in the other.
+ *
+ * Softmax weights are rounded to the plan's type before they multiply V, as in codec_decode_attention (by up to 2^-11 of a weight with
+ * fp16, 2^-8 with bf16; the sum that divides them is that of the rounded ones).  Sums, both results, their difference and the norm
+ * are held in 32 bits and rounded once, at the end.  Where the maps nearly cancel, the weights' roundings are what is left.
  */
 typedef struct {
     const float *lambda;            /* device: of request r and head h at r * lambda_request_stride + h * lambda_head_stride   */
@@ -638,8 +642,10 @@ int codec_cache_copy(const codec_head_config *head, const codec_kv_layout *layou
  * -------------------------------------------------------------
  *
  * codec_append wants a position and a slot for every token.  They follow from how many tokens the sequences hold and get, and from
- * their pages; these calls make them where the lengths are, so that a step needs no list from the host and no wait for
- * one (lengths that a verification has just cut, captured steps).  Lengths below zero count as zero.
+ * their pages; these calls make them where the lengths are, so that appending needs no list from the host and no wait for
+ * one (lengths that a verification has just cut, captured steps).  Lengths below zero count as zero.  The way ends there: attention over
+ * the tokens just appended takes their lengths and pages from a plan, which is made, or refreshed, of lists on the host and uploaded
+ * (codec_plan_refresh_lengths, codec_plan_upload); a captured step keeps the lengths of its plan.
  */
 
 /*

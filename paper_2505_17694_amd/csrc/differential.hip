@@ -192,6 +192,9 @@ __device__ __forceinline__ void run_pairs_of(const PairParams &P, const DevTask 
             m = m_new;
         }
     };
+    // Weights are rounded to 16 bits, which the matrix instructions take (fp16 by 2^-11 of themselves, bf16 by 2^-8), as in every path of ordinary
+    // attention.  The row sum adds the rounded ones: a result is off by the roundings' share of the values' distances from it, not of
+    // the values.  What is subtracted later are two such results, in 32 bits.
     auto exponential_pair = [&](const f32x16 &s, int tt, int d) __attribute__((always_inline)) {
         p[tt][d] = pack2<DT>(fast_exp2(__builtin_fmaf(s[8 * tt + 2 * d], P.scale_log2e, -m)),
                              fast_exp2(__builtin_fmaf(s[8 * tt + 2 * d + 1], P.scale_log2e, -m)));

@@ -12,8 +12,8 @@ namespace {
 
 __device__ __forceinline__ int64_t at_least_0(int32_t n) { return n > 0 ? n : 0; }
 
-// A table's row in units of four entries.  Bound by HBM; what is read is a quarter of it at least (4096 sequences of up to 64k
-// tokens: 100 MB, 16.2 us, 6.2 TB/s; 33 sequences 2.1).
+// A table's row in units of four entries.  Bound by HBM, mostly by the writes: entries behind a sequence's pages are -1 without a
+// read (4096 sequences of up to 64k tokens: 67 MB written, 33 MB read, 17.4 us, 5.8 TB/s; 33 sequences 2.3).
 template <bool ALIGNED>
 __global__ __launch_bounds__(256) void block_table_kernel(TableParams P)
 {
@@ -172,7 +172,7 @@ __device__ __forceinline__ void map_tokens(const SlotParams &P, const uint32_t *
 }
 
 // Up to kSlotsAtOnce sequences: every workgroup sums them up for itself, in LDS.  Bound by dependent reads: 48 sequences with a token
-// each 3.3 us, 65k tokens of 300 sequences 5.0; a launch for the sums would be 2 more, and 3 on the host.
+// each 3.3 us, 65k tokens of 300 sequences 5.1; a launch for the sums would be 2 more (see kSlotsAtOnce), and 3 on the host.
 __global__ __launch_bounds__(256) void slot_map_kernel(SlotParams P)
 {
     extern __shared__ uint32_t sums[];                  // [n + 1], [n]
@@ -183,7 +183,8 @@ __global__ __launch_bounds__(256) void slot_map_kernel(SlotParams P)
     map_tokens(P, sums, page_first);
 }
 
-// More: one workgroup sums them up, all others' search goes through L2.
+// More: one workgroup sums them up, all others' search goes through L2.  A thread reads neighbouring sequences, its wave's lanes so many
+// entries apart: 20000 sequences take 69 us, 100000 take 387.
 __global__ __launch_bounds__(1024) void slot_sums_kernel(SlotParams P)
 {
     sum_sequences<16, true>(P, P.sums, P.sums + P.num_seq + 1);
